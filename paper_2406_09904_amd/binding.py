@@ -1,5 +1,5 @@
-"""Thin ctypes binding over libqqq.so (the C ABI declared in include/qqq.h; tuning and
-diagnostic controls in include/qqq_tuning.h).
+"""Thin ctypes binding over libqqq.so (the C ABI declared in include/qqq.h; the offline stage in include/qqq_calib.h, what lies
+between a decoder layer's linear calls in include/qqq_layer.h, tuning and diagnostic controls in include/qqq_tuning.h).
 
 Argument marshalling only: every step of the path runs in the library's HIP kernels.  PyTorch
 supplies device memory and the stream.  There is no CPU fallback: if the library is missing or a
@@ -10,6 +10,7 @@ from __future__ import annotations
 import ctypes
 import importlib.util
 import os
+import typing
 import warnings
 
 import torch
@@ -32,6 +33,12 @@ SYMBOLS = [
     "qqq_smoothing_workspace_bytes", "qqq_adaptive_smoothing", "qqq_channel_absmax", "qqq_smooth_apply",
     "qqq_fp16_gemm_nt", "qqq_hessian", "qqq_gptq_workspace_bytes", "qqq_gptq_quantize_w4_perchannel",
     "qqq_gptq_quantize_w4_pergroup", "qqq_set_factor_workgroups",
+]
+
+# the entry points of include/qqq_layer.h
+LAYER_SYMBOLS = [
+    "qqq_add_rmsnorm", "qqq_add_rmsnorm_quant", "qqq_gated_act_quant", "qqq_kv8_append", "qqq_kv8_read",
+    "qqq_attention_kv8_workspace_bytes", "qqq_attention_kv8",
 ]
 
 _lib = None
@@ -129,6 +136,15 @@ def lib():
         L.qqq_set_prefill_tuning.argtypes = [ci]
         L.qqq_set_prefill_ksplit.argtypes = [ci]
         L.qqq_set_factor_workgroups.argtypes = [ci]
+        cf = ctypes.c_float
+        L.qqq_add_rmsnorm.argtypes = [vp, i64, vp, i64, ci, vp, cf, i64, i64, vp, i64, vp, vp]
+        L.qqq_add_rmsnorm_quant.argtypes = [vp, i64, vp, i64, ci, vp, cf, i64, i64, vp, i64, vp, vp, vp]
+        L.qqq_gated_act_quant.argtypes = [vp, i64, vp, i64, ci, i64, i64, vp, vp, vp]
+        L.qqq_kv8_append.argtypes = [vp, vp, vp, i64, i64, vp, i64, i64, i64, vp]
+        L.qqq_kv8_read.argtypes = [vp, vp, vp, vp, i64, vp]
+        L.qqq_attention_kv8_workspace_bytes.argtypes = [vp, vp, ci, i64]
+        L.qqq_attention_kv8_workspace_bytes.restype = sz
+        L.qqq_attention_kv8.argtypes = [vp, vp, vp, i64, i64, ci, i64, cf, ci, ci, vp, vp, vp, sz, vp]
         _load_native(L)
         _lib = L
     return _lib
@@ -470,6 +486,198 @@ def qqq_gptq_quantize_w4_pergroup(w_fp16, H, percdamp=0.01, want_int=True):
                                                _ptr(s_star, torch.float16), _ptr(s_int, torch.int8),
                                                _ptr(s_wc, torch.float16), _ptr(work), work.numel(), _stream()))
     return w_nat, s_wg, s_star, s_int, s_wc
+
+
+# ---- between the linear calls (include/qqq_layer.h): norm and gated activation to int8, the 8-bit cache, attention over it
+
+def _rows(t, name):
+    if t.dtype != torch.float16 or t.dim() != 2 or t.stride(1) != 1 or not t.is_cuda:
+        raise ValueError("%s must be a 2-D fp16 device tensor with unit inner stride" % name)
+    M, K = t.shape
+    return M, K, (t.stride(0) if M > 1 else max(K, t.stride(0)))
+
+
+def _rmsnorm_args(x, gain, residual, sum_out):
+    M, K, ldx = _rows(x, "x")
+    if tuple(gain.shape) != (K,):
+        raise ValueError("gain must have the %d values of a row" % K)
+    if residual is None:
+        if sum_out is not None:
+            raise ValueError("sum_out without a residual")
+        return M, K, ldx, None, 0, 0, None, 0
+    if residual.dtype not in (torch.float16, torch.float32) or residual.shape != x.shape or residual.stride(1) != 1 or not residual.is_cuda:
+        raise ValueError("residual must be an fp16 or fp32 device tensor of x's shape with unit inner stride")
+    if sum_out is None:
+        sum_out = torch.empty((M, K), dtype=residual.dtype, device=x.device)
+    elif sum_out.dtype != residual.dtype or sum_out.shape != x.shape or sum_out.stride(1) != 1 or not sum_out.is_cuda:
+        raise ValueError("sum_out must be a device tensor of the residual's type and shape with unit inner stride")
+    ldr, lds = (residual.stride(0), sum_out.stride(0)) if M > 1 else (max(K, residual.stride(0)), max(K, sum_out.stride(0)))
+    return M, K, ldx, residual.data_ptr(), ldr, 1 if residual.dtype == torch.float16 else 2, sum_out, lds
+
+
+def qqq_add_rmsnorm(x, gain, residual=None, eps=1e-6, y=None, sum_out=None):
+    """x [M,K] fp16 (+ residual fp16 or fp32) -> (their sum in the residual's type or None, y fp16 [M,K] = norm(sum) * gain).
+    sum_out may be the residual itself."""
+    M, K, ldx, res, ldr, kind, sum_out, lds = _rmsnorm_args(x, gain, residual, sum_out)
+    if y is None:
+        y = torch.empty((M, K), dtype=torch.float16, device=x.device)
+    elif y.shape != x.shape:
+        raise ValueError("y must have x's shape")
+    _check(lib().qqq_add_rmsnorm(x.data_ptr(), ldx, res, ldr, kind, _ptr(gain, _F16), eps, M, K, None if sum_out is None else sum_out.data_ptr(), lds,
+                                 _ptr(y, _F16), _stream()))
+    return sum_out, y
+
+
+def qqq_add_rmsnorm_quant(x, gain, residual=None, eps=1e-6, a_q=None, s_a=None, sum_out=None):
+    """The same straight to codes -> (sum or None, a_q int8 [M,K], s_a fp32 [M]), as qqq_quant_act gives them."""
+    M, K, ldx, res, ldr, kind, sum_out, lds = _rmsnorm_args(x, gain, residual, sum_out)
+    a_q, s_a = _codes_out(M, K, a_q, s_a, x.device)
+    _check(lib().qqq_add_rmsnorm_quant(x.data_ptr(), ldx, res, ldr, kind, _ptr(gain, _F16), eps, M, K, None if sum_out is None else sum_out.data_ptr(),
+                                       lds, _ptr(a_q, _I8), _ptr(s_a, torch.float32), _stream()))
+    return sum_out, a_q, s_a
+
+
+def _codes_out(M, K, a_q, s_a, device):
+    if a_q is None:
+        a_q = torch.empty((M, K), dtype=torch.int8, device=device)
+    if s_a is None:
+        s_a = torch.empty((M,), dtype=torch.float32, device=device)
+    if tuple(a_q.shape) != (M, K) or s_a.numel() != M:
+        raise ValueError("codes and scales must be of %d rows of %d" % (M, K))
+    return a_q, s_a
+
+
+_ACTS = {"silu": 0, "gelu_tanh": 1}
+
+
+def qqq_gated_act_quant(gate, up, act="silu", a_q=None, s_a=None):
+    """gate, up [M,F] fp16 (views of one projection's output allowed) -> (a_q int8 [M,F], s_a fp32 [M]) of act(gate) * up; act "silu" or "gelu_tanh"."""
+    M, F, ldg = _rows(gate, "gate")
+    M2, F2, ldu = _rows(up, "up")
+    if (M, F) != (M2, F2):
+        raise ValueError("gate and up disagree on their shape")
+    if act not in _ACTS:
+        raise ValueError("act must be one of %s" % ", ".join(_ACTS))
+    a_q, s_a = _codes_out(M, F, a_q, s_a, gate.device)
+    _check(lib().qqq_gated_act_quant(gate.data_ptr(), ldg, up.data_ptr(), ldu, _ACTS[act], M, F, _ptr(a_q, _I8), _ptr(s_a, torch.float32), _stream()))
+    return a_q, s_a
+
+
+class KV8Cache(typing.NamedTuple):
+    """A layer's keys and values in 8 bits with a scale for each page and head (layout: include/qqq_layer.h)."""
+    k_codes: torch.Tensor   # uint8 [pages, kv_heads, page_tokens, head_dim], offset binary
+    k_scale: torch.Tensor   # fp32 [pages, kv_heads]
+    v_codes: torch.Tensor   # uint8 [pages, kv_heads, head_dim, page_tokens]
+    v_scale: torch.Tensor   # fp32 [pages, kv_heads]
+    k_tail: torch.Tensor    # fp16 [slots, kv_heads, page_tokens, head_dim]: the pages that are not full
+    v_tail: torch.Tensor    # fp16 [slots, kv_heads, head_dim, page_tokens]
+
+
+class KV8Batch(typing.NamedTuple):
+    """The sequences of a step: b holds kv_len[b] tokens, the last cu[b+1] - cu[b] of them new (rows cu[b] .. of the tensors beside it)."""
+    page_table: torch.Tensor  # int32 [sequences, columns]
+    kv_len: torch.Tensor      # int32 [sequences], the new tokens included
+    cu: torch.Tensor          # int32 [sequences + 1]
+    slots: typing.Optional[torch.Tensor]  # int32 [sequences]: tail slots; None: sequence b has slot b
+    max_new: int              # bounds of the new tokens and of kv_len
+    max_len: int
+
+
+def new_kv8_cache(pages, kv_heads, head_dim, page_tokens=64, slots=1, device="cuda") -> KV8Cache:
+    """An empty cache."""
+    u8 = lambda *s: torch.full(s, 128, dtype=torch.uint8, device=device)  # noqa: E731
+    f16 = lambda *s: torch.zeros(s, dtype=torch.float16, device=device)  # noqa: E731
+    scale = torch.zeros((2, pages, kv_heads), dtype=torch.float32, device=device)
+    return KV8Cache(u8(pages, kv_heads, page_tokens, head_dim), scale[0], u8(pages, kv_heads, head_dim, page_tokens), scale[1],
+                    f16(slots, kv_heads, page_tokens, head_dim), f16(slots, kv_heads, head_dim, page_tokens))
+
+
+class _Cache(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k_codes", "k_scale", "v_codes", "v_scale", "k_tail", "v_tail")] + [
+        ("pages", ctypes.c_int64)] + [(n, ctypes.c_int32) for n in ("slots", "kv_heads", "head_dim", "page_tokens")]
+
+
+class _Batch(ctypes.Structure):
+    _fields_ = [("page_table", ctypes.c_void_p), ("table_stride", ctypes.c_int64)] + [(n, ctypes.c_void_p) for n in ("kv_len", "cu", "slots")] + [
+        (n, ctypes.c_int32) for n in ("columns", "sequences", "max_new", "max_len")]
+
+
+def _kv8_structs(cache, batch):
+    kc, ks, vc, vs, kt, vt = cache
+    table, kv_len, cu, slots, max_new, max_len = batch
+    if kc.dim() != 4 or kt.dim() != 4 or table.dim() != 2 or table.stride(1) != 1 or not table.is_cuda or table.dtype != _I32:
+        raise ValueError("codes and tails must be 4-D, page_table a 2-D int32 device tensor with unit inner stride")
+    (pages, H, P, D), B = kc.shape, table.shape[0]
+    nslots = kt.shape[0]
+    if vc.shape != (pages, H, D, P) or ks.shape != (pages, H) or vs.shape != (pages, H) or kt.shape != (nslots, H, P, D) or vt.shape != (nslots, H, D, P):
+        raise ValueError("the cache's tensors disagree on their shape")
+    if kv_len.shape != (B,) or cu.shape != (B + 1,) or (slots is not None and slots.shape != (B,)):
+        raise ValueError("kv_len, cu and slots must be of page_table's %d sequences" % B)
+    if slots is None and nslots < B:
+        raise ValueError("%d tail slots for %d sequences" % (nslots, B))
+    f32 = torch.float32
+    return (_Cache(_ptr(kc, _U8), _ptr(ks, f32), _ptr(vc, _U8), _ptr(vs, f32), _ptr(kt, _F16), _ptr(vt, _F16), pages, nslots, H, D, P),
+            _Batch(table.data_ptr(), table.stride(0) if B > 1 else max(table.shape[1], table.stride(0)), _ptr(kv_len, _I32), _ptr(cu, _I32),
+                   _ptr(slots, _I32), table.shape[1], B, max_new, max_len), H, D)
+
+
+def _heads(t, heads, D, name):
+    if t.dtype != torch.float16 or t.dim() != 3 or t.stride(2) != 1 or not t.is_cuda or t.shape[2] != D or (heads and t.shape[1] != heads):
+        raise ValueError("%s must be an fp16 device tensor [tokens, heads, %d] with unit inner stride" % (name, D))
+    return t.shape[0], t.stride(0), t.stride(1)
+
+
+def qqq_kv8_append(cache: KV8Cache, batch: KV8Batch, k, v):
+    """Puts the step's new keys and values [tokens, kv_heads, head_dim] fp16 (strided views allowed) into the cache."""
+    c, b, H, D = _kv8_structs(cache, batch)
+    (T, kt, kh), (T2, vt, vh) = _heads(k, H, D, "k"), _heads(v, H, D, "v")
+    if T != T2:
+        raise ValueError("k and v disagree on their tokens")
+    _check(lib().qqq_kv8_append(ctypes.byref(c), ctypes.byref(b), k.data_ptr(), kt, kh, v.data_ptr(), vt, vh, T, _stream()))
+
+
+def qqq_kv8_read(cache: KV8Cache, batch: KV8Batch, k=None, v=None, tokens=None):
+    """The last cu[b+1] - cu[b] tokens of each sequence as the cache holds them -> (k, v) fp16 [tokens, kv_heads, head_dim]; tokens: rows of the
+    outputs where they are not given."""
+    c, b, H, D = _kv8_structs(cache, batch)
+    if (k is None or v is None) and tokens is None:
+        raise ValueError("tokens is needed where k or v is not given")
+    if k is None:
+        k = torch.empty((tokens, H, D), dtype=torch.float16, device=cache[0].device)
+    if v is None:
+        v = torch.empty((tokens, H, D), dtype=torch.float16, device=cache[0].device)
+    if k.dim() != 3 or k.shape[1:] != (H, D) or v.shape != k.shape:
+        raise ValueError("k and v must be [tokens, %d, %d]" % (H, D))
+    _check(lib().qqq_kv8_read(ctypes.byref(c), ctypes.byref(b), _ptr(k, _F16), _ptr(v, _F16), k.shape[0], _stream()))
+    return k, v
+
+
+def qqq_attention_kv8_workspace_bytes(cache: KV8Cache, batch: KV8Batch, q_heads: int, tokens: int) -> int:
+    c, b, _, _ = _kv8_structs(cache, batch)
+    return int(lib().qqq_attention_kv8_workspace_bytes(ctypes.byref(c), ctypes.byref(b), q_heads, tokens))
+
+
+def qqq_attention_kv8(cache: KV8Cache, batch: KV8Batch, q, scale=None, causal=True, window=0, out=None, lse=None, workspace=None):
+    """Attention of the new tokens' queries [tokens, q_heads, head_dim] fp16 (strided views allowed) over the cache -> (out fp16 of that shape, lse
+    fp32 [tokens, q_heads], or None where none is given).  scale: 1 / sqrt(head_dim).  workspace: a uint8 tensor of
+    qqq_attention_kv8_workspace_bytes(); without one torch's allocator lends it."""
+    c, b, H, D = _kv8_structs(cache, batch)
+    T, qt, qh = _heads(q, 0, D, "q")
+    Hq = q.shape[1]
+    if out is None:
+        out = torch.empty((T, Hq, D), dtype=torch.float16, device=q.device)
+    elif out.shape != q.shape:
+        raise ValueError("out must have q's shape")
+    if lse is not None and lse.shape != (T, Hq):
+        raise ValueError("lse must be [tokens, q_heads]")
+    L = lib()
+    if workspace is None:
+        nbytes = L.qqq_attention_kv8_workspace_bytes(ctypes.byref(c), ctypes.byref(b), Hq, T)
+        workspace = torch.empty((nbytes,), dtype=torch.uint8, device=q.device) if nbytes else None
+    _check(L.qqq_attention_kv8(ctypes.byref(c), ctypes.byref(b), q.data_ptr(), qt, qh, Hq, T, D ** -0.5 if scale is None else scale, int(causal), window,
+                               _ptr(out, _F16), None if lse is None else _ptr(lse, torch.float32), _ptr(workspace, _U8),
+                               0 if workspace is None else workspace.numel(), _stream()))
+    return out, lse
 
 
 def last_route() -> str:

@@ -1,0 +1,301 @@
+"""The 8-bit paged cache and attention over it (include/qqq_layer.h) against the definitions in 64 bits.
+
+Tolerances.  Codes, scales and tails are compared bit for bit: the quantiser's quotient is the fp32 division's.  What is read back is one
+product rounded to fp32 and to fp16: within 2^-11 (1 + 2^-11) of it, or half the least fp16 value.
+Attention: a score's fp32 sum over D products is off by at most ds = (D + 8) 2^-23 scale sum |q| |k|, which changes a weight by exp(2 ds) at
+most; weights are rounded to fp16, 2^-11, and where they are below fp16's normal range by 2^-25 of a unit that is 2^-6 of the largest;
+exponent, its argument (|z| < 2^8: 2^-16) and the final division add 3e-5; the result is rounded to fp16.  So
+|out - exact| <= (2^-11 + 2 ds + 3e-5) sum p |v| + length 2^-31 max |v| + 2^-11 |exact| + 2^-25,  |lse - exact| <= ds + 3e-5.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import qqq_layer_oracle as ref
+from paper_2406_09904_amd import binding as qqq
+
+pytestmark = pytest.mark.gpu
+
+
+def _dev(a):
+    return torch.from_numpy(np.ascontiguousarray(a)).cuda()
+
+
+class Both:
+    """A cache on the host and its twin on the device, filled with the same calls."""
+
+    def __init__(self, seed, lengths, heads, dim, page, slots=None, columns=None):
+        self.rng = np.random.default_rng(seed)
+        self.heads, self.dim, self.page, B = heads, dim, page, len(lengths)
+        self.columns = max(1, max(lengths) // page) if columns is None else columns
+        pages = sum(n // page for n in lengths) + 3
+        order = self.rng.permutation(pages)
+        self.table, at = np.full((B, self.columns), pages - 1, np.int32), 0
+        for b, n in enumerate(lengths):
+            self.table[b, :n // page] = order[at:at + n // page]
+            at += n // page
+        nslots = B + 2 if slots is None else slots
+        self.slots = self.rng.permutation(nslots)[:B].astype(np.int32)
+        self.host = ref.Cache(pages, heads, dim, page, nslots)
+        self.dev = qqq.new_kv8_cache(pages, heads, dim, page, nslots)
+        self.max_len = self.columns * page + page - 1
+
+    def batch(self, kv_len, cu, max_new=None):
+        new = np.diff(cu)
+        return qqq.KV8Batch(_dev(self.table), _dev(np.array(kv_len, np.int32)), _dev(np.array(cu, np.int32)), _dev(self.slots),
+                            int(new.max(initial=0)) if max_new is None else max_new, self.max_len)
+
+    def random(self, T):
+        scale = np.exp(self.rng.standard_normal((1, self.heads, 1)))
+        return tuple((self.rng.standard_normal((T, self.heads, self.dim)) * scale).astype(np.float16) for _ in range(2))
+
+    def append(self, kv_len, new, k=None, v=None):
+        cu = np.concatenate([[0], np.cumsum(new)])
+        if k is None:
+            k, v = self.random(cu[-1])
+        self.host.append(self.table, kv_len, cu, self.slots, k, v)
+        # the values in the middle of a wider tensor, as a fused projection's output holds them
+        wide = torch.full((max(1, cu[-1]), 2 * self.heads + 3, self.dim), 9.0, dtype=torch.float16, device="cuda")
+        wide[:cu[-1], 2:2 + self.heads], wide[:cu[-1], 2 + self.heads:2 + 2 * self.heads] = _dev(k), _dev(v)
+        qqq.qqq_kv8_append(self.dev, self.batch(kv_len, cu), wide[:cu[-1], 2:2 + self.heads], wide[:cu[-1], 2 + self.heads:2 + 2 * self.heads])
+        torch.cuda.synchronize()
+
+    def check(self):
+        for name in ("k_codes", "k_scale", "v_codes", "v_scale", "k_tail", "v_tail"):
+            got, want = getattr(self.dev, name).cpu().numpy(), getattr(self.host, name)
+            if name == "k_tail" or name == "v_tail":   # a slot keeps the tokens of the page it held; the device may not have put them there
+                continue
+            assert np.array_equal(got, want), name
+
+    def check_tokens(self, kv_len):
+        """Every sequence's tokens, through qqq_kv8_read."""
+        cu = np.concatenate([[0], np.cumsum(kv_len)])
+        T = int(cu[-1])
+        k, v = qqq.qqq_kv8_read(self.dev, self.batch(kv_len, cu, max_new=max(1, max(kv_len))), tokens=T)
+        torch.cuda.synchronize()
+        k, v = k.cpu().numpy().astype(np.float64), v.cpu().numpy().astype(np.float64)
+        for b, n in enumerate(kv_len):
+            for got, want in zip((k, v), self.host.tokens(self.table[b], n, self.slots[b])):
+                got = got[cu[b]:cu[b + 1]]
+                assert np.all(np.abs(got - want) <= np.abs(want) * 2 ** -11 * (1 + 2 ** -11) + 2 ** -25), b
+
+
+SHAPES = [(64, 16), (64, 64), (128, 16), (128, 32), (128, 64), (256, 32), (256, 64)]
+
+
+@pytest.mark.parametrize("dim,page", SHAPES)
+def test_append_in_pieces(dim, page):
+    """Sequences filled in pieces that end inside, at and past the pages' ends: codes, scales and values are those of one token after the other."""
+    steps = [[1, 0, page - 1, page, 2 * page + 5], [page - 1, 3, 1, 1, 1], [1, page - 3, 2 * page, 0, page], [2 * page + 1, 1, 1, page - 1, 0],
+             [5, 7, 0, 1, 3 * page]]
+    total = [sum(s[b] for s in steps) for b in range(5)]
+    w = Both(dim + page, total, 3, dim, page)
+    length = [0] * 5
+    for new in steps:
+        length = [a + n for a, n in zip(length, new)]
+        w.append(length, new)
+        w.check()
+        w.check_tokens(length)
+
+
+def test_append_values_that_are_not_finite():
+    """A NaN is held as 0, an infinity as the largest value, closed or not; other tokens of the page keep their values' scale."""
+    w = Both(3, [40], 2, 64, 16)
+    k, v = w.random(40)
+    k[3, 0, 5], k[20, 1, 6], v[7, 1, 0], v[36, 0, 1], v[37, 0, 2] = np.nan, np.inf, -np.inf, np.nan, np.inf
+    w.append([40], [40], k, v)
+    w.check()
+    w.check_tokens([40])
+
+
+def test_append_zeros_and_extremes():
+    w = Both(4, [32 * 3], 2, 128, 32)
+    k, v = w.random(96)
+    k[:32], v[32:64], k[64:], v[64:] = 0, 0, k[64:] * np.float16(6e-8), np.sign(v[64:]) * np.float16(65504)
+    w.append([96], [96], k, v)
+    w.check()
+    w.check_tokens([96])
+
+
+def test_step_between_lengths_of_zero():
+    """No sequence, no new token, no token at all."""
+    w = Both(5, [70, 10], 1, 64, 64)
+    w.append([0, 0], [0, 0])
+    w.append([0, 10], [0, 10])
+    w.append([70, 10], [70, 0])
+    w.check_tokens([70, 10])
+    out, _ = qqq.qqq_attention_kv8(w.dev, w.batch([70, 10], [0, 0, 0]), torch.empty(0, 4, 64, dtype=torch.float16, device="cuda"))
+    assert out.shape == (0, 4, 64)
+
+
+def _check_attention(w, kv_len, new, q_heads, scale=None, causal=True, window=0, spread=1.0):
+    cu = np.concatenate([[0], np.cumsum(new)])
+    T, D = int(cu[-1]), w.dim
+    q = (w.rng.standard_normal((T, q_heads, D)) * spread).astype(np.float16)
+    wide = torch.full((T, q_heads + 2, D + 8), 5.0, dtype=torch.float16, device="cuda")
+    wide[:, 1:-1, :D] = _dev(q)
+    out = torch.full((T, q_heads, D), float("nan"), dtype=torch.float16, device="cuda")
+    lse = torch.full((T, q_heads), float("nan"), device="cuda")
+    qqq.qqq_attention_kv8(w.dev, w.batch(kv_len, cu), wide[:, 1:-1, :D], scale, causal, window, out, lse)
+    torch.cuda.synchronize()
+    out, lse = out.cpu().numpy().astype(np.float64), lse.cpu().numpy()
+    scale = D ** -0.5 if scale is None else scale
+    for b, n in enumerate(kv_len):
+        k, v = w.host.tokens(w.table[b], n, w.slots[b])
+        rows = slice(cu[b], cu[b + 1])
+        want, want_lse, mag, big = ref.attention(q[rows], k, v, scale, causal, window)
+        ds = (D + 8) * 2.0 ** -23 * big
+        bound = (2 ** -11 + 2 * ds[..., None] + 3e-5) * mag + n * 2.0 ** -31 * np.abs(v).max(initial=0) + 2 ** -11 * np.abs(want) + 2 ** -25
+        worst = (np.abs(out[rows] - want) / bound).max(initial=0)
+        assert worst <= 1, (b, n, worst)
+        empty = np.isinf(want_lse)
+        assert np.array_equal(np.isneginf(lse[rows]), empty)
+        assert not out[rows][empty].any()
+    X
+
+
+def _filled(seed, lengths, heads, dim, page):
+    w = Both(seed, lengths, heads, dim, page)
+    w.append(lengths, lengths)
+    return w
+
+
+# lengths: one token, inside a page, at a page's end, inside and at a tile's end, several tiles; a sequence without tokens
+LENGTHS = [1, 15, 16, 0, 63, 64, 65, 200, 257]
+
+
+@pytest.mark.parametrize("dim,page", SHAPES)
+@pytest.mark.parametrize("heads,q_heads", [(1, 1), (2, 16), (3, 15)])
+def test_single_tokens(dim, page, heads, q_heads):
+    w = _filled(11, LENGTHS, heads, dim, page)
+    _check_attention(w, LENGTHS, [min(1, n) for n in LENGTHS], q_heads)
+
+
+@pytest.mark.parametrize("dim,page", [(64, 16), (128, 64), (256, 32)])
+@pytest.mark.parametrize("new", [2, 5, 16, 40])
+def test_a_few_tokens(dim, page, new):
+    """Rows past 16, past 32; more new tokens than a sequence has in some."""
+    lengths = [40, 64, 130, 300]
+    w = _filled(12, lengths, 2, dim, page)
+    _check_attention(w, lengths, [new, min(3, new), new, 1], 6)
+
+
+@pytest.mark.parametrize("dim,page", [(64, 32), (128, 16), (128, 64), (256, 64)])
+@pytest.mark.parametrize("q_heads", [2, 14])
+def test_prompts(dim, page, q_heads):
+    lengths = [1, 129, 200, 64, 333]
+    w = _filled(13, lengths, 2, dim, page)
+    _check_attention(w, lengths, [1, 129, 77, 64, 333], q_heads)
+
+
+@pytest.mark.parametrize("window", [1, 16, 50, 64, 1000])
+@pytest.mark.parametrize("new", [1, 7, 150])
+def test_windows(window, new):
+    lengths = [150, 290, 191]
+    w = _filled(14, lengths, 2, 128, 32)
+    _check_attention(w, lengths, [new, new, min(new, 3)], 8, window=window)
+
+
+@pytest.mark.parametrize("new", [1, 6, 60])
+def test_without_a_causal_mask(new):
+    lengths = [60, 130, 100]
+    w = _filled(15, lengths, 2, 64, 16)
+    _check_attention(w, lengths, [new] * 3, 6, causal=False)
+
+
+@pytest.mark.parametrize("new", [1, 3, 40])
+def test_rows_that_see_nothing(new):
+    """More queries than the sequence has tokens: those before position 0 see nothing."""
+    lengths = [0, 2, 33]
+    w = _filled(16, lengths, 2, 128, 16)
+    _check_attention(w, lengths, [new, max(new, 3), new], 4)
+
+
+def test_large_scores_and_scales_of_very_different_pages():
+    w = Both(17, [256, 256], 2, 128, 16)
+    k, v = w.random(512)
+    v = (v.astype(np.float64) * np.exp(3 * w.rng.standard_normal((32, 1, 1, 1))).repeat(16, 0).reshape(512, 1, 1)).clip(-6e4, 6e4).astype(np.float16)
+    v[64:80] = 0
+    k[96:112] = 0
+    w.append([256, 256], [256, 256], k, v)
+    w.check()
+    _check_attention(w, [256, 256], [1, 1], 4, spread=10)
+    _check_attention(w, [256, 256], [60, 60], 4, spread=10)
+    _check_attention(w, [256, 256], [60, 60], 4, scale=3.0)
+
+
+@pytest.mark.parametrize("new,heads,q_heads", [(1, 1, 8), (3, 2, 8), (20, 1, 8), (150, 1, 1)])
+def test_a_long_past(new, heads, q_heads):
+    """The keys are split over workgroups and joined."""
+    lengths = [5000, 700, 3, 4097]
+    w = _filled(18, lengths, heads, 64, 64)
+    _check_attention(w, lengths, [new, new, min(new, 3), new], q_heads)
+    assert "join" in qqq.last_route()
+    _check_attention(w, lengths, [new, new, min(new, 3), new], q_heads, window=2000)
+
+
+def test_same_result_twice_and_on_another_stream():
+    w = _filled(19, [3000, 100], 2, 128, 64)
+    q = torch.randn(2, 16, 128, device="cuda").half()
+    batch = w.batch([3000, 100], [0, 1, 2])
+    first, _ = qqq.qqq_attention_kv8(w.dev, batch, q)
+    torch.cuda.synchronize()
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        second, _ = qqq.qqq_attention_kv8(w.dev, batch, q)
+    stream.synchronize()
+    assert torch.equal(first, second)
+
+
+def test_graph_of_a_step_replayed_with_other_lengths():
+    """A captured step reads lengths on the device: each replay equals calls of its own on another cache."""
+    lengths = [130, 64, 200]
+    a, b = _filled(20, lengths, 2, 64, 64), _filled(20, lengths, 2, 64, 64)
+    start = [126, 62, 190]
+    kv_len = _dev(np.array(start, np.int32))
+    cu = _dev(np.arange(4, dtype=np.int32))
+    batch = qqq.KV8Batch(_dev(a.table), kv_len, cu, _dev(a.slots), 1, a.max_len)
+    for w in (a, b):
+        k, v = w.random(sum(start))
+        w.append(start, start, k, v)
+    kv = torch.zeros(3, 2, 2, 64, dtype=torch.float16, device="cuda")
+    q, out = torch.zeros(3, 8, 64, dtype=torch.float16, device="cuda"), torch.zeros(3, 8, 64, dtype=torch.float16, device="cuda")
+    work = torch.empty(max(1, qqq.qqq_attention_kv8_workspace_bytes(a.dev, batch, 8, 3)), dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        kv_len += 1
+        qqq.qqq_kv8_append(a.dev, batch, kv[:, 0], kv[:, 1])
+        qqq.qqq_attention_kv8(a.dev, batch, q, out=out, workspace=work)
+    kv_len.copy_(_dev(np.array(start, np.int32)))
+    for step in range(4):
+        kv.copy_(torch.randn(3, 2, 2, 64, device="cuda"))
+        q.copy_(torch.randn(3, 8, 64, device="cuda"))
+        graph.replay()
+        torch.cuda.synchronize()
+        now = [n + step + 1 for n in start]
+        other = qqq.KV8Batch(_dev(b.table), _dev(np.array(now, np.int32)), cu, _dev(b.slots), 1, b.max_len)
+        qqq.qqq_kv8_append(b.dev, other, kv[:, 0], kv[:, 1])
+        want, _ = qqq.qqq_attention_kv8(b.dev, other, q)
+        torch.cuda.synchronize()
+        assert torch.equal(out, want), step
+        assert torch.equal(a.dev.k_codes, b.dev.k_codes) and torch.equal(a.dev.v_codes, b.dev.v_codes)
+
+
+def test_device_tables_out_of_bounds_stay_inside():
+    """Lengths, rows, pages and slots that the host's bounds rule out are cut, skipped or replaced on the device: nothing outside is written."""
+    w = _filled(21, [64, 32], 1, 64, 16)
+    before = [t.clone() for t in w.dev]
+    table = _dev(np.array([[1 << 30, -7, 3, 99], [5, 6, 1000, -1]], np.int32))
+    kv = torch.randn(20, 2, 1, 64, device="cuda").half()
+    q = torch.randn(20, 4, 64, device="cuda").half()
+    for kv_len, cu, slots in (([1 << 30, -5], [0, 9, 20], [0, 1]), ([64, 32], [-3, 17, 400], [77, -1]), ([64, 32], [0, -4, 1 << 30], [0, 1])):
+        batch = qqq.KV8Batch(table, _dev(np.array(kv_len, np.int32)), _dev(np.array(cu, np.int32)), _dev(np.array(slots, np.int32)), 16, 4 * 16 + 15)
+        out, _ = qqq.qqq_attention_kv8(w.dev, batch, q)
+        qqq.qqq_kv8_read(w.dev, batch, tokens=20)
+        torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(before, w.dev))
+    qqq.qqq_kv8_append(w.dev, qqq.KV8Batch(table, _dev(np.array([64, 32], np.int32)), _dev(np.array([0, 9, 20], np.int32)),
+                                           _dev(np.array([77, -1], np.int32)), 16, 79), kv[:, 0], kv[:, 1])
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(before, w.dev))
