@@ -151,7 +151,7 @@ def _check_attention(w, kv_len, new, q_heads, scale=None, causal=True, window=0,
         empty = np.isinf(want_lse)
         assert np.array_equal(np.isneginf(lse[rows]), empty)
         assert not out[rows][empty].any()
-    X
+        assert np.all(np.abs(lse[rows][~empty] - want_lse[~empty]) <= (ds + 3e-5)[~empty]), b
 
 
 def _filled(seed, lengths, heads, dim, page):
