@@ -34,7 +34,6 @@ struct AttnParams {
   float2* part_ml;   // [splits][tokens][q_heads]
   float scale_log2;  // scale * log2(e)
   int group, q_heads, causal, window;
-  int lp;            // log2(page_tokens)
   int splits, chunk; // workgroups that share a row's keys, tiles of each
   int row_blocks;    // of the largest sequence
   int sequences;
@@ -89,6 +88,35 @@ __device__ __forceinline__ Factors factors_of(float ks, float vs, float scale_lo
   return f;
 }
 
+// The pages of a tile of 64 tokens (64 / P of them): where they lie in units of a page and head, and their scales.  The tile is the same
+// for a whole wave, so these are scalar loads.  `closed` pages exist; past them any page that does stands in (its codes are not used).
+template <int P>
+struct Pages {
+  static constexpr int N = kTile / P;
+  int32_t id[N];
+};
+template <int P>
+__device__ __forceinline__ Pages<P> pages_of(const Kv8& c, int b, int tile, int closed) {
+  // (always a load, so that the requests behind it are the same on every path)
+  const int32_t* table = closed > 0 ? c.table + b * c.table_stride : c.kv_len + b;
+  Pages<P> g;
+#pragma unroll
+  for (int i = 0; i < Pages<P>::N; ++i) g.id[i] = table[max(0, min(tile * Pages<P>::N + i, closed - 1))];
+  return g;
+}
+// of a 16-token group's page, by the lane's group
+template <int P, typename T>
+__device__ __forceinline__ T of_group(const T* v, int group) {
+  constexpr int N = Pages<P>::N;
+  const T a = v[0], b = v[1 % N], c = v[2 % N], d = v[3 % N];  // (all of them read, so that they stay in registers)
+  if constexpr (P == 64) return a;
+  else if constexpr (P == 32) return group & 2 ? b : a;
+  else {
+    const T lo = group & 1 ? b : a, hi = group & 1 ? d : c;
+    return group & 2 ? hi : lo;
+  }
+}
+
 // ---- a few rows: up to 16 * NT of them a key/value head -----------------------------------------------------------------------------
 //
 // Bound by the cache's bytes: every code is read once, straight into registers, and used by up to 16 * NT rows; a wave takes every W-th
@@ -98,25 +126,66 @@ __device__ __forceinline__ Factors factors_of(float ks, float vs, float scale_lo
 // from 16 g on.  They are its operand of the second product, whose other operand is 16 consecutive tokens of a channel: one 16-byte
 // load of the token-minor codes.  Along the channels of the first product the same holds: a lane loads 16 consecutive ones, the
 // halves of which belong to two steps; the queries are laid out alike.
-template <int D, int NT, int W>
-__global__ __launch_bounds__(64 * W) void attn_rows_kernel(const AttnParams p) {
-  constexpr int J = D / 64, DT = D / 16;
-  __shared__ float join_o[(W / 2) * NT * DT * 4 * 64];
-  __shared__ float join_m[(W / 2) * NT * 64], join_l[(W / 2) * NT * 64];
+//
+// What is in flight is what counts: the next tile's keys are requested as soon as this tile's are in the scores, its values as soon as
+// this tile's are in the result, and nothing that a request depends on is waited for there (loads return in order): page numbers
+// are fetched two tiles ahead, scales one.
+template <int D, int P, int NT, int W>
+__global__ __launch_bounds__(64 * W, D <= 128 ? 2 : 1) void attn_rows_kernel(const AttnParams p) {
+  constexpr int J = D / 64, DT = D / 16, NP = Pages<P>::N;
+  constexpr int kRowO = D + 4;  // (16 bytes over: the lanes' rows start in different banks)
+  __shared__ float join_o[W * 16 * NT * kRowO];
+  __shared__ float2 join_ml[W][16 * NT];
   const Kv8& c = p.c;
-  const int split = blockIdx.x % p.splits, head = (blockIdx.x / p.splits) % c.heads, b = blockIdx.x / p.splits / c.heads;
+  const int head = blockIdx.x, b = blockIdx.z;
+  // Workgroups go to the eight dies in turn, and of short sequences only the first splits have work: turned by the sequence, so that no die gets
+  // all of a split (48 sequences of 17 to 8000 tokens in 8 splits: 124 us without)
+  const int split = (int)((blockIdx.y + b) % gridDim.y);
   const Kv8Seq s = kv8_sequence(c, b);
   if (s.n == 0) return;
   const Range range = range_of(p, s, 0, s.n - 1);
   const int from = split * p.chunk, tiles = min(p.chunk, range.tiles - from);
   if (tiles <= 0 && split > 0) return;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, g = lane >> 4;
-  const int P = 1 << p.lp, closed = s.len >> p.lp, slot = kv8_slot(c, s.slot);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
+  const int closed = s.len / P, slot = kv8_slot(c, s.slot);
+  const int open_tile = s.len > closed * P ? closed * P / kTile : -1;  // the one with tokens in the tail slot
 
-  // queries, and each row's keys [lo, hi)
+  const int gk = n >> 2;  // 16-token group that this lane's row of the first operand is taken from
+  uint4 kraw[4][J], vraw[DT];
+  const uint32_t k_lane = (((16 * gk) & (P - 1)) + (n & 3)) * D + 16 * g, v_lane = n * P + ((16 * g) & (P - 1));
+  auto offsets = [&](const Pages<P>& of, int64_t* at) {
+#pragma unroll
+    for (int i = 0; i < NP; ++i) at[i] = (kv8_page(c, of.id[i]) * c.heads + head) * (P * D);
+  };
+  auto request_k = [&](const Pages<P>& of) {
+    int64_t offset[NP];
+    offsets(of, offset);
+    const uint8_t* at = c.k_codes + of_group<P>(offset, gk) + k_lane;
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int j = 0; j < J; ++j) kraw[t][j] = *reinterpret_cast<const uint4*>(at + 4 * t * D + 64 * j);
+  };
+  auto request_v = [&](const Pages<P>& of) {
+    int64_t offset[NP];
+    offsets(of, offset);
+    const uint8_t* at = c.v_codes + of_group<P>(offset, g) + v_lane;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) vraw[dt] = *reinterpret_cast<const uint4*>(at + dt * 16 * P);
+  };
+  float ks[NP], vs[NP];
+  auto scales = [&](const Pages<P>& of) {
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      const int64_t at = kv8_page(c, of.id[i]) * c.heads + head;
+      ks[i] = c.k_scale[at];
+      vs[i] = c.v_scale[at];
+    }
+  };
+
+  // queries, and each row's keys [lo, hi).  (Requested first: what is waited for in the loop must not lie behind the codes in flight.)
   h8 q[NT][J * 2];
   int lo[NT], hi[NT];
-  int64_t out_at[NT];  // (token, head) of the row, or -1
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
     const int r = nt * 16 + n, i = r / p.group, hq = head * p.group + r % p.group;
@@ -125,13 +194,22 @@ __global__ __launch_bounds__(64 * W) void attn_rows_kernel(const AttnParams p) {
     const int pos = s.len - s.n + i;
     hi[nt] = !there ? 0 : p.causal ? min(s.len, pos + 1) : s.len;
     lo[nt] = p.window ? pos - p.window + 1 : 0;
-    out_at[nt] = there ? row * p.q_heads + hq : -1;
     const uint4* from_q = reinterpret_cast<const uint4*>(p.q + (there ? row * p.q_token + hq * p.q_head : 0));
 #pragma unroll
     for (int j = 0; j < J; ++j)
 #pragma unroll
-      for (int h = 0; h < 2; ++h) q[nt][2 * j + h] = there ? as_h8(from_q[8 * j + 2 * g + h]) : as_h8(make_uint4(0, 0, 0, 0));
+      for (int h = 0; h < 2; ++h) q[nt][2 * j + h] = as_h8(from_q[8 * j + 2 * g + h]);  // (a row that is not there: another's, never written)
   }
+
+  const int first = range.tile0 + from + wave, end = range.tile0 + from + tiles;
+  Pages<P> pages = pages_of<P>(c, b, min(first, end - 1), closed);
+  __builtin_amdgcn_sched_barrier(0);
+  scales(pages);
+  request_k(pages);
+  __builtin_amdgcn_sched_barrier(0);
+  request_v(pages);
+  __builtin_amdgcn_sched_barrier(0);
+  pages = pages_of<P>(c, b, min(first + W, end - 1), closed);
 
   float m[NT], l[NT];
   f4 o[NT][DT];
@@ -143,42 +221,8 @@ __global__ __launch_bounds__(64 * W) void attn_rows_kernel(const AttnParams p) {
     for (int dt = 0; dt < DT; ++dt) o[nt][dt] = f4{0, 0, 0, 0};
   }
 
-  const int gk = n >> 2;  // 16-token group that this lane's row of the first operand is taken from
-  const int32_t* table = c.table + b * c.table_stride;
-  auto page_of = [&](int tile, int group) {
-    const int at = (tile * kTile + 16 * group) >> p.lp;
-    return closed > 0 ? kv8_page(c, table[min(at, closed - 1)]) : (int64_t)0;
-  };
-  uint4 kraw[4][J], vraw[DT];
-  float ks, vs;
-  auto request_k = [&](int64_t page) {
-    const uint8_t* at = c.k_codes + ((page * c.heads + head) * P + ((16 * gk) & (P - 1)) + (n & 3)) * D + 16 * g;
-#pragma unroll
-    for (int t = 0; t < 4; ++t)
-#pragma unroll
-      for (int j = 0; j < J; ++j) kraw[t][j] = *reinterpret_cast<const uint4*>(at + 4 * t * D + 64 * j);
-  };
-  auto request_v = [&](int64_t page) {
-    const int64_t of = page * c.heads + head;
-    const uint8_t* at = c.v_codes + of * P * D + n * P + ((16 * g) & (P - 1));
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt) vraw[dt] = *reinterpret_cast<const uint4*>(at + dt * 16 * P);
-    ks = c.k_scale[of];
-    vs = c.v_scale[of];
-  };
-
-  const int first = range.tile0 + from + wave, end = range.tile0 + from + tiles;
-  if (first < end) {
-    request_k(page_of(first, gk));
-    request_v(page_of(first, g));
-  }
-  for (int tile = first; tile < end; tile += W) {
-    const int next = min(tile + W, end - 1);
-    const int64_t next_k = page_of(next, gk), next_v = page_of(next, g);
-    const bool open = (tile + 1) * kTile > closed << p.lp;           // some of its tokens are in the tail slot, or nowhere
-    const bool edge = (tile + 1) * kTile > range.whole_hi || tile * kTile < range.whole_lo;
-    const bool k_open = open && (tile * kTile + 16 * gk) >> p.lp >= closed, v_open = open && (tile * kTile + 16 * g) >> p.lp >= closed;
-
+  // one tile: k_of(t, j, half) and v_of(dt, half) give the codes' operands; next() requests after the scores and after the result
+  auto step = [&](int tile, const Factors& f, auto k_of, auto v_of, auto next_k, auto next_v) {
     f4 st[NT][4];
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
@@ -186,13 +230,7 @@ __global__ __launch_bounds__(64 * W) void attn_rows_kernel(const AttnParams p) {
       for (int nt = 0; nt < NT; ++nt) st[nt][t] = f4{0, 0, 0, 0};
 #pragma unroll
       for (int j = 0; j < J; ++j) {
-        h8 k0 = codes8_to_halves(kraw[t][j].x, kraw[t][j].y), k1 = codes8_to_halves(kraw[t][j].z, kraw[t][j].w);
-        if (open && k_open) {
-          const int row = ((16 * gk) & (P - 1)) + 4 * t + (n & 3);
-          const uint4* at = reinterpret_cast<const uint4*>(c.k_tail + (((int64_t)slot * c.heads + head) * P + row) * D + 64 * j + 16 * g);
-          k0 = as_h8(at[0]);
-          k1 = as_h8(at[1]);
-        }
+        const h8 k0 = k_of(t, j, 0), k1 = k_of(t, j, 1);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
           st[nt][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k0, q[nt][2 * j], st[nt][t], 0, 0, 0);
@@ -200,9 +238,8 @@ __global__ __launch_bounds__(64 * W) void attn_rows_kernel(const AttnParams p) {
         }
       }
     }
-    const Factors f = factors_of(v_open ? 1.0f : ks, v_open ? 1.0f : vs, p.scale_log2);
-    request_k(next_k);
-
+    next_k();
+    const bool edge = (tile + 1) * kTile > range.whole_hi || tile * kTile < range.whole_lo;
     h8 w[NT][2];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
@@ -236,84 +273,112 @@ __global__ __launch_bounds__(64 * W) void attn_rows_kernel(const AttnParams p) {
           w[nt][t >> 1][(t & 1) * 4 + i] = (_Float16)e;
         }
       l[nt] = __builtin_fmaf(l[nt], alpha, sum * f.rv);
+      if (__any(alpha != 1.0f)) {
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt) o[nt][dt] *= alpha;
+        for (int dt = 0; dt < DT; ++dt) o[nt][dt] *= alpha;
+      }
     }
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) {
-      h8 v0 = codes8_to_halves(vraw[dt].x, vraw[dt].y), v1 = codes8_to_halves(vraw[dt].z, vraw[dt].w);
-      if (open && v_open) {
-        const int t0 = (16 * g) & (P - 1), left = s.len - (tile * kTile + 16 * g);  // tokens of the group that exist
-        const uint4* at = reinterpret_cast<const uint4*>(c.v_tail + (((int64_t)slot * c.heads + head) * D + dt * 16 + n) * P + t0);
-        v0 = as_h8(at[0]);
-        v1 = as_h8(at[1]);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          if (e >= left) v0[e] = (_Float16)0.0f;
-          if (e + 8 >= left) v1[e] = (_Float16)0.0f;
-        }
-      }
+      const h8 v0 = v_of(dt, 0), v1 = v_of(dt, 1);
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         o[nt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, w[nt][0], o[nt][dt], 0, 0, 0);
         o[nt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, w[nt][1], o[nt][dt], 0, 0, 0);
       }
     }
-    request_v(next_v);
+    next_v();
+  };
+  auto k_codes = [&](int t, int j, int half) { return half ? codes8_to_halves(kraw[t][j].z, kraw[t][j].w) : codes8_to_halves(kraw[t][j].x, kraw[t][j].y); };
+  auto v_codes = [&](int dt, int half) { return half ? codes8_to_halves(vraw[dt].z, vraw[dt].w) : codes8_to_halves(vraw[dt].x, vraw[dt].y); };
+
+  int tile = first;
+  for (; tile < end && tile != open_tile; tile += W) {
+    const Factors f = factors_of(of_group<P>(ks, g), of_group<P>(vs, g), p.scale_log2);
+    const Pages<P> after = pages_of<P>(c, b, min(tile + 2 * W, end - 1), closed);
+    step(tile, f, k_codes, v_codes,
+         [&]() {
+           __builtin_amdgcn_sched_barrier(0);
+           scales(pages);
+           request_k(pages);
+           __builtin_amdgcn_sched_barrier(0);
+         },
+         [&]() {
+           __builtin_amdgcn_sched_barrier(0);
+           request_v(pages);
+           __builtin_amdgcn_sched_barrier(0);
+         });
+    pages = after;
+  }
+  if (tile < end) {
+    // the tile that the sequence ends in, its last tokens in the tail slot; where pages are shorter than a tile, others of them may be codes
+    const bool k_open = (tile * kTile + 16 * gk) / P >= closed, v_open = (tile * kTile + 16 * g) / P >= closed;
+    const int64_t tail = ((int64_t)slot * c.heads + head) * (P * D);
+    h8 kt[4][J][2], vt[DT][2];
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int j = 0; j < J; ++j)
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+          kt[t][j][half] = as_h8(*reinterpret_cast<const uint4*>(c.k_tail + tail + k_lane + 4 * t * D + 64 * j + 8 * half));
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int half = 0; half < 2; ++half) vt[dt][half] = as_h8(*reinterpret_cast<const uint4*>(c.v_tail + tail + v_lane + dt * 16 * P + 8 * half));
+    const int left = s.len - (tile * kTile + 16 * g);  // tokens of the lane's group that exist: what lies past them may be anything
+    const Factors f = factors_of(v_open ? 1.0f : of_group<P>(ks, g), v_open ? 1.0f : of_group<P>(vs, g), p.scale_log2);
+    uint4 there[2];
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      auto pair = [&](int e) { return (8 * half + e < left ? 0xFFFFu : 0u) | (8 * half + e + 1 < left ? 0xFFFF0000u : 0u); };
+      there[half] = make_uint4(pair(0), pair(2), pair(4), pair(6));
+    }
+    auto select = [](bool tail, h8 a, h8 b) { return P == kTile || tail ? a : b; };
+    step(tile, f, [&](int t, int j, int half) { return select(k_open, kt[t][j][half], k_codes(t, j, half)); },
+         [&](int dt, int half) {
+           const uint4 v = __builtin_bit_cast(uint4, vt[dt][half]);
+           return select(v_open, as_h8(make_uint4(v.x & there[half].x, v.y & there[half].y, v.z & there[half].z, v.w & there[half].w)), v_codes(dt, half));
+         },
+         []() {}, []() {});
   }
 
-  // join the waves: the upper half of those left hands its results to the lower half, register by register
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt) l[nt] = across16(across32(l[nt], fadd2), fadd2);
-#pragma unroll
-  for (int half = W / 2; half >= 1; half /= 2) {
-    __syncthreads();
-    if (wave >= half && wave < 2 * half) {
-      const int at = wave - half;
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        join_m[(at * NT + nt) * 64 + lane] = m[nt];
-        join_l[(at * NT + nt) * 64 + lane] = l[nt];
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) join_o[(((at * NT + nt) * DT + dt) * 4 + i) * 64 + lane] = o[nt][dt][i];
-      }
-    }
-    __syncthreads();
-    if (wave < half) {
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        const float m2 = join_m[(wave * NT + nt) * 64 + lane], l2 = join_l[(wave * NT + nt) * 64 + lane];
-        const float now = fmaxf(m[nt], m2), base = now == -__builtin_inff() ? 0.0f : now;
-        const float a1 = __builtin_amdgcn_exp2f(m[nt] - base), a2 = __builtin_amdgcn_exp2f(m2 - base);
-        m[nt] = now;
-        l[nt] = l[nt] * a1 + l2 * a2;
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) o[nt][dt][i] = o[nt][dt][i] * a1 + join_o[(((wave * NT + nt) * DT + dt) * 4 + i) * 64 + lane] * a2;
-      }
-    }
-  }
-  if (wave != 0) return;
+  // join the waves: each puts its rows into LDS, four channels of a row are then a thread's
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
-    if (out_at[nt] < 0) continue;
+    l[nt] = across16(across32(l[nt], fadd2), fadd2);
+    if (g == 0) join_ml[wave][nt * 16 + n] = make_float2(m[nt], l[nt]);
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<f4*>(&join_o[(wave * 16 * NT + nt * 16 + n) * kRowO + dt * 16 + 4 * g]) = o[nt][dt];
+  }
+  __syncthreads();
+  const int rows = s.n * p.group;
+  for (int at = threadIdx.x; at < rows * (D / 4); at += 64 * W) {
+    const int r = at / (D / 4), d = at % (D / 4) * 4, i = r / p.group, hq = head * p.group + r % p.group;
+    const int64_t row = s.row + i;
+    float top = -__builtin_inff(), sum = 0.0f;
+#pragma unroll
+    for (int x = 0; x < W; ++x) top = fmaxf(top, join_ml[x][r].x);
+    const float base = top == -__builtin_inff() ? 0.0f : top;
+    f4 all = {0, 0, 0, 0};
+#pragma unroll
+    for (int x = 0; x < W; ++x) {
+      const float2 ml = join_ml[x][r];
+      const float a = __builtin_amdgcn_exp2f(ml.x - base);
+      sum = __builtin_fmaf(ml.y, a, sum);
+      all += *reinterpret_cast<const f4*>(&join_o[(x * 16 * NT + r) * kRowO + d]) * a;
+    }
+    if (row < 0 || row >= c.tokens) continue;
+    const int64_t to = row * p.q_heads + hq;
     if (p.splits == 1) {
-      const float inv = l[nt] > 0.0f ? 1.0f / l[nt] : 0.0f;
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt) {
-        const uint2 v = make_uint2(as_u32(h2{(_Float16)(o[nt][dt][0] * inv), (_Float16)(o[nt][dt][1] * inv)}),
-                                   as_u32(h2{(_Float16)(o[nt][dt][2] * inv), (_Float16)(o[nt][dt][3] * inv)}));
-        *reinterpret_cast<uint2*>(p.out + out_at[nt] * D + dt * 16 + 4 * g) = v;
-      }
-      if (p.lse && g == 0) p.lse[out_at[nt]] = l[nt] > 0.0f ? kLn2 * (__builtin_amdgcn_logf(l[nt]) + (m[nt] - kShift)) : -__builtin_inff();
+      const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+      *reinterpret_cast<uint2*>(p.out + to * D + d) = make_uint2(as_u32(h2{(_Float16)(all[0] * inv), (_Float16)(all[1] * inv)}),
+                                                                 as_u32(h2{(_Float16)(all[2] * inv), (_Float16)(all[3] * inv)}));
+      if (p.lse && d == 0) p.lse[to] = sum > 0.0f ? kLn2 * (__builtin_amdgcn_logf(sum) + (top - kShift)) : -__builtin_inff();
     } else {
-      const int64_t at = (int64_t)split * c.tokens * p.q_heads + out_at[nt];
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<f4*>(p.part_o + at * D + dt * 16 + 4 * g) = o[nt][dt];
-      if (g == 0) p.part_ml[at] = make_float2(m[nt], l[nt]);
+      const int64_t part = (int64_t)split * c.tokens * p.q_heads + to;
+      *reinterpret_cast<f4*>(p.part_o + part * D + d) = all;
+      if (d == 0) p.part_ml[part] = make_float2(top, sum);
     }
   }
 }
@@ -336,7 +401,7 @@ struct TileLds {
   float c[4], lv[4], rv[4];
 };
 
-template <int D>
+template <int D, int P>
 __global__ __launch_bounds__(kBlockThreads, D <= 128 ? 2 : 1) void attn_block_kernel(const AttnParams p) {
   constexpr int KC = D / 64, VC = D / 64;  // chunks of 16 codes of a thread, of each tile's keys and values
   constexpr int KS = D / 16, DT = D / 32;
@@ -351,8 +416,8 @@ __global__ __launch_bounds__(kBlockThreads, D <= 128 ? 2 : 1) void attn_block_ke
   const Range range = range_of(p, s, row0 / p.group, min(row0 + kBlockRows - 1, rows - 1) / p.group);
   const int from = split * p.chunk, tiles = min(p.chunk, range.tiles - from);
   if (tiles <= 0 && split > 0) return;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 31, h = lane >> 5;
-  const int P = 1 << p.lp, closed = s.len >> p.lp, slot = kv8_slot(c, s.slot);
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, h = lane >> 5;
+  const int closed = s.len / P, slot = kv8_slot(c, s.slot);
 
   const int r = row0 + wave * 32 + n, i = r / p.group, hq = head * p.group + r % p.group;
   const int64_t row = s.row + i;
@@ -363,70 +428,97 @@ __global__ __launch_bounds__(kBlockThreads, D <= 128 ? 2 : 1) void attn_block_ke
   {
     const uint4* from_q = reinterpret_cast<const uint4*>(p.q + (there ? row * p.q_token + hq * p.q_head : 0));
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) q[ks] = there ? as_h8(from_q[2 * ks + h]) : as_h8(make_uint4(0, 0, 0, 0));
+    for (int ks = 0; ks < KS; ++ks) q[ks] = as_h8(from_q[2 * ks + h]);  // (a row that is not there: another's, never written)
   }
 
   // staging: thread's chunks of 16 codes
-  const int32_t* table = c.table + b * c.table_stride;
-  auto page_of = [&](int tile, int group) {
-    const int at = (tile * kTile + 16 * group) >> p.lp;
-    return closed > 0 ? kv8_page(c, table[min(at, closed - 1)]) : (int64_t)0;
-  };
+  constexpr int NP = Pages<P>::N;
   uint4 kraw[KC], vraw[VC];
   float ks_raw = 0.0f, vs_raw = 0.0f;
-  auto request = [&](int tile) {
+  auto request = [&](const Pages<P>& of) {
+    int64_t offset[NP];
+#pragma unroll
+    for (int x = 0; x < NP; ++x) offset[x] = (kv8_page(c, of.id[x]) * c.heads + head) * (P * D);
 #pragma unroll
     for (int j = 0; j < KC; ++j) {
       const int at = tid + kBlockThreads * j, t = at / (D / 16), d = at % (D / 16) * 16;
-      kraw[j] = *reinterpret_cast<const uint4*>(c.k_codes + ((page_of(tile, t >> 4) * c.heads + head) * P + (t & (P - 1))) * D + d);
+      kraw[j] = *reinterpret_cast<const uint4*>(c.k_codes + of_group<P>(offset, t >> 4) + (t & (P - 1)) * D + d);
     }
 #pragma unroll
     for (int j = 0; j < VC; ++j) {
       const int at = tid + kBlockThreads * j, d = at >> 2, grp = at & 3;
-      vraw[j] = *reinterpret_cast<const uint4*>(c.v_codes + ((page_of(tile, grp) * c.heads + head) * D + d) * P + ((16 * grp) & (P - 1)));
+      vraw[j] = *reinterpret_cast<const uint4*>(c.v_codes + of_group<P>(offset, grp) + d * P + ((16 * grp) & (P - 1)));
     }
     if (tid < 4) {
-      const int64_t of = page_of(tile, tid) * c.heads + head;
-      ks_raw = c.k_scale[of];
-      vs_raw = c.v_scale[of];
+      const int64_t at = kv8_page(c, of_group<P>(of.id, tid)) * c.heads + head;
+      ks_raw = c.k_scale[at];
+      vs_raw = c.v_scale[at];
     }
   };
+  const int open_tile = s.len > closed * P ? closed * P / kTile : -1;  // the one with tokens in the tail slot
   auto stage = [&](int tile, TileLds<D>& to) {
-    const bool open = (tile + 1) * kTile > closed << p.lp;
+    h8 k[KC][2], v[VC][2];
+#pragma unroll
+    for (int j = 0; j < KC; ++j) {
+      k[j][0] = codes8_to_halves(kraw[j].x, kraw[j].y);
+      k[j][1] = codes8_to_halves(kraw[j].z, kraw[j].w);
+    }
+#pragma unroll
+    for (int j = 0; j < VC; ++j) {
+      v[j][0] = codes8_to_halves(vraw[j].x, vraw[j].y);
+      v[j][1] = codes8_to_halves(vraw[j].z, vraw[j].w);
+    }
+    if (tile == open_tile) {
+      const int64_t tail = ((int64_t)slot * c.heads + head) * (P * D);
+      uint4 kt[KC][2], vt[VC][2];
+#pragma unroll
+      for (int j = 0; j < KC; ++j) {
+        const int at = tid + kBlockThreads * j, t = at / (D / 16), d = at % (D / 16) * 16;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) kt[j][half] = *reinterpret_cast<const uint4*>(c.k_tail + tail + (t & (P - 1)) * D + d + 8 * half);
+      }
+#pragma unroll
+      for (int j = 0; j < VC; ++j) {
+        const int at = tid + kBlockThreads * j, d = at >> 2, grp = at & 3;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) vt[j][half] = *reinterpret_cast<const uint4*>(c.v_tail + tail + d * P + ((16 * grp) & (P - 1)) + 8 * half);
+      }
+#pragma unroll
+      for (int j = 0; j < KC; ++j) {
+        const int t = (tid + kBlockThreads * j) / (D / 16);
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+          if ((tile * kTile + t) / P >= closed) k[j][half] = as_h8(kt[j][half]);
+      }
+#pragma unroll
+      for (int j = 0; j < VC; ++j) {
+        const int grp = (tid + kBlockThreads * j) & 3, left = s.len - (tile * kTile + 16 * grp);  // tokens that exist
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+          if ((tile * kTile + 16 * grp) / P >= closed) {
+            v[j][half] = as_h8(vt[j][half]);
+#pragma unroll
+            for (int x = 0; x < 8; ++x)
+              if (8 * half + x >= left) v[j][half][x] = (_Float16)0.0f;
+          }
+      }
+    }
 #pragma unroll
     for (int j = 0; j < KC; ++j) {
       const int at = tid + kBlockThreads * j, t = at / (D / 16), d = at % (D / 16) * 16;
-      h8 a = codes8_to_halves(kraw[j].x, kraw[j].y), e = codes8_to_halves(kraw[j].z, kraw[j].w);
-      if (open && (tile * kTile + t) >> p.lp >= closed) {
-        const uint4* tail = reinterpret_cast<const uint4*>(c.k_tail + (((int64_t)slot * c.heads + head) * P + (t & (P - 1))) * D + d);
-        a = as_h8(tail[0]);
-        e = as_h8(tail[1]);
-      }
       uint4* put = reinterpret_cast<uint4*>(&to.k[t * TileLds<D>::kRowK + d]);
-      put[0] = __builtin_bit_cast(uint4, a);
-      put[1] = __builtin_bit_cast(uint4, e);
+      put[0] = __builtin_bit_cast(uint4, k[j][0]);
+      put[1] = __builtin_bit_cast(uint4, k[j][1]);
     }
 #pragma unroll
     for (int j = 0; j < VC; ++j) {
       const int at = tid + kBlockThreads * j, d = at >> 2, grp = at & 3;
-      h8 a = codes8_to_halves(vraw[j].x, vraw[j].y), e = codes8_to_halves(vraw[j].z, vraw[j].w);
-      if (open && (tile * kTile + 16 * grp) >> p.lp >= closed) {
-        const int left = s.len - (tile * kTile + 16 * grp);
-        const uint4* tail = reinterpret_cast<const uint4*>(c.v_tail + (((int64_t)slot * c.heads + head) * D + d) * P + ((16 * grp) & (P - 1)));
-        a = as_h8(tail[0]);
-        e = as_h8(tail[1]);
-#pragma unroll
-        for (int x = 0; x < 8; ++x) {
-          if (x >= left) a[x] = (_Float16)0.0f;
-          if (x + 8 >= left) e[x] = (_Float16)0.0f;
-        }
-      }
       uint4* put = reinterpret_cast<uint4*>(&to.v[d * TileLds<D>::kRowV + 16 * grp]);
-      put[0] = __builtin_bit_cast(uint4, a);
-      put[1] = __builtin_bit_cast(uint4, e);
+      put[0] = __builtin_bit_cast(uint4, v[j][0]);
+      put[1] = __builtin_bit_cast(uint4, v[j][1]);
     }
     if (tid < 4) {
-      const bool tail = open && (tile * kTile + 16 * tid) >> p.lp >= closed;
+      const bool tail = tile == open_tile && (tile * kTile + 16 * tid) / P >= closed;
       const Factors f = factors_of(tail ? 1.0f : ks_raw, tail ? 1.0f : vs_raw, p.scale_log2);
       to.c[tid] = f.c;
       to.lv[tid] = f.lv;
@@ -442,10 +534,13 @@ __global__ __launch_bounds__(kBlockThreads, D <= 128 ? 2 : 1) void attn_block_ke
     for (int x = 0; x < 16; ++x) o[dt][x] = 0.0f;
 
   const int first = range.tile0 + from, end = first + tiles;
+  Pages<P> pages;   // of the tile after the one whose codes are on their way
   if (tiles > 0) {
-    request(first);
+    request(pages_of<P>(c, b, first, closed));
+    pages = pages_of<P>(c, b, min(first + 1, end - 1), closed);
     stage(first, lds[0]);
-    request(min(first + 1, end - 1));
+    request(pages);
+    pages = pages_of<P>(c, b, min(first + 2, end - 1), closed);
     lds_barrier();
   }
   const int token_of_row = 16 * (n >> 4) + 8 * ((n >> 2) & 1) + 4 * ((n >> 3) & 1) + (n & 3);
@@ -510,7 +605,8 @@ __global__ __launch_bounds__(kBlockThreads, D <= 128 ? 2 : 1) void attn_block_ke
       }
     if (tile + 1 < end) {
       stage(tile + 1, lds[(tile + 1 - first) & 1]);
-      request(min(tile + 2, end - 1));
+      request(pages);
+      pages = pages_of<P>(c, b, min(tile + 3, end - 1), closed);
     }
     lds_barrier();
   }
@@ -539,91 +635,185 @@ __global__ __launch_bounds__(kBlockThreads, D <= 128 ? 2 : 1) void attn_block_ke
   }
 }
 
-// Joins the splits of every row, in their order.  One wave a row.
-constexpr int kJoinRows = 4;
+// How many splits a row (new token i, head hq) was computed in: its workgroup's tiles as that one counted them.
+__device__ __forceinline__ int parts_of(const AttnParams& p, const Kv8Seq& s, int i, int hq, int block_rows) {
+  const int r = i * p.group + hq % p.group, row0 = block_rows ? r / block_rows * block_rows : 0;
+  const int last = block_rows ? min(row0 + block_rows, s.n * p.group) - 1 : s.n * p.group - 1;
+  const Range range = range_of(p, s, row0 / p.group, last / p.group);
+  return min(max(1, (range.tiles + p.chunk - 1) / p.chunk), p.splits);
+}
+
+// Joins the splits of every row, one workgroup a row: each wave sums every kJoinWaves-th split, always in the same order.
+constexpr int kJoinWaves = 8, kJoinMost = 1024;  // (splits: plan_of keeps below that)
 template <int D>
-__global__ __launch_bounds__(64 * kJoinRows) void attn_join_kernel(const AttnParams p, int block_rows) {
+__global__ __launch_bounds__(64 * kJoinWaves) void attn_join_kernel(const AttnParams p, int block_rows) {
+  constexpr int E = D / 64;
+  typedef float fe __attribute__((ext_vector_type(E)));
+  __shared__ float weight[kJoinMost];
+  __shared__ float2 most[kJoinWaves];
+  __shared__ float sums[kJoinWaves][D];
+  const Kv8& c = p.c;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int hq = (int)(blockIdx.x % p.q_heads), i = (int)(blockIdx.x / p.q_heads % c.max_new), b = (int)(blockIdx.x / p.q_heads / c.max_new);
+  const Kv8Seq s = kv8_sequence(c, b);
+  const int64_t row = s.row + i;
+  if (i >= s.n || row < 0 || row >= c.tokens) return;
+  const int parts = parts_of(p, s, i, hq, block_rows);
+  const int64_t at = row * p.q_heads + hq, step = c.tokens * p.q_heads;
+  const float* part = p.part_o + at * D + lane * E;
+  fe first = {};  // (on its way while the weights are made)
+  if (wave < parts) first = *reinterpret_cast<const fe*>(part + wave * step * D);
+  float2 ml[kJoinMost / 64 / kJoinWaves];
+  float m = -__builtin_inff(), l = 0.0f;
+#pragma unroll
+  for (int j = 0; j < kJoinMost / 64 / kJoinWaves; ++j) {
+    const int k = tid + 64 * kJoinWaves * j;
+    ml[j] = k < parts ? p.part_ml[at + k * step] : make_float2(-__builtin_inff(), 0.0f);
+    m = fmaxf(m, ml[j].x);
+  }
+#pragma unroll
+  for (int x = 1; x < 64; x *= 2) m = fmaxf(m, __shfl_xor(m, x));
+  if (lane == 0) most[wave].x = m;
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < kJoinWaves; ++j) m = fmaxf(m, most[j].x);
+  const float base = m == -__builtin_inff() ? 0.0f : m;
+#pragma unroll
+  for (int j = 0; j < kJoinMost / 64 / kJoinWaves; ++j) {
+    const int k = tid + 64 * kJoinWaves * j;
+    const float a = __builtin_amdgcn_exp2f(ml[j].x - base);
+    if (k < parts) weight[k] = a;
+    l = __builtin_fmaf(ml[j].y, a, l);
+  }
+#pragma unroll
+  for (int x = 1; x < 64; x *= 2) l += __shfl_xor(l, x);
+  if (lane == 0) most[wave].y = l;
+  __syncthreads();
+  fe o = first * (wave < parts ? weight[wave] : 0.0f);
+#pragma unroll 8
+  for (int k = wave + kJoinWaves; k < parts; k += kJoinWaves) o += *reinterpret_cast<const fe*>(part + k * step * D) * weight[k];
+#pragma unroll
+  for (int j = 0; j < E; ++j) sums[wave][lane * E + j] = o[j];
+  __syncthreads();
+  if (tid >= D) return;
+  l = 0.0f;
+  float sum = 0.0f;
+#pragma unroll
+  for (int j = 0; j < kJoinWaves; ++j) {
+    l += most[j].y;
+    sum += sums[j][tid];
+  }
+  p.out[at * D + tid] = __builtin_bit_cast(uint16_t, (_Float16)(l > 0.0f ? sum / l : 0.0f));
+  if (p.lse && tid == 0) p.lse[at] = l > 0.0f ? kLn2 * (__builtin_amdgcn_logf(l) + (m - kShift)) : -__builtin_inff();
+}
+
+// The same of a few splits: one wave a row, nothing to be joined but what it holds.
+constexpr int kJoinFew = 8;
+template <int D>
+__global__ __launch_bounds__(256) void attn_join_few_kernel(const AttnParams p, int block_rows) {
+  constexpr int E = D / 64;
+  typedef float fe __attribute__((ext_vector_type(E)));
+  typedef _Float16 he __attribute__((ext_vector_type(E)));
   const Kv8& c = p.c;
   const int lane = threadIdx.x & 63;
-  const int64_t id = (int64_t)blockIdx.x * kJoinRows + (threadIdx.x >> 6);  // (sequence, new token, head)
+  const int64_t id = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int hq = (int)(id % p.q_heads), i = (int)(id / p.q_heads % c.max_new);
   const int64_t b = id / p.q_heads / c.max_new;
   if (b >= p.sequences) return;
   const Kv8Seq s = kv8_sequence(c, (int)b);
   const int64_t row = s.row + i;
   if (i >= s.n || row < 0 || row >= c.tokens) return;
-  // the tiles of the row's workgroup, as that one counted them
-  const int r = i * p.group + hq % p.group, row0 = block_rows ? r / block_rows * block_rows : 0;
-  const int last = block_rows ? min(row0 + block_rows, s.n * p.group) - 1 : s.n * p.group - 1;
-  const Range range = range_of(p, s, row0 / p.group, last / p.group);
-  const int parts = max(1, (range.tiles + p.chunk - 1) / p.chunk);
+  const int parts = parts_of(p, s, i, hq, block_rows);
   const int64_t at = row * p.q_heads + hq, step = c.tokens * p.q_heads;
-  float m = -__builtin_inff();
-  for (int k = lane; k < parts; k += 64) m = fmaxf(m, p.part_ml[at + k * step].x);
+  fe o[kJoinFew];
+  float2 ml[kJoinFew];
 #pragma unroll
-  for (int x = 1; x < 64; x *= 2) m = fmaxf(m, __shfl_xor(m, x));
+  for (int k = 0; k < kJoinFew; ++k) {
+    const int64_t from = at + (k < parts ? k : 0) * step;
+    ml[k] = p.part_ml[from];
+    o[k] = *reinterpret_cast<const fe*>(p.part_o + from * D + lane * E);
+  }
+  float m = -__builtin_inff(), l = 0.0f;
+#pragma unroll
+  for (int k = 0; k < kJoinFew; ++k) m = fmaxf(m, ml[k].x);
   const float base = m == -__builtin_inff() ? 0.0f : m;
-  float l = 0.0f, o[D / 64];
+  fe sum = {};
 #pragma unroll
-  for (int j = 0; j < D / 64; ++j) o[j] = 0.0f;
-  for (int k = 0; k < parts; ++k) {
-    const float2 ml = p.part_ml[at + k * step];
-    const float a = __builtin_amdgcn_exp2f(ml.x - base);
-    l = __builtin_fmaf(ml.y, a, l);
-    const float* from = p.part_o + (at + k * step) * D + lane * (D / 64);
-#pragma unroll
-    for (int j = 0; j < D / 64; ++j) o[j] = __builtin_fmaf(from[j], a, o[j]);
+  for (int k = 0; k < kJoinFew; ++k) {
+    const float a = k < parts ? __builtin_amdgcn_exp2f(ml[k].x - base) : 0.0f;
+    l = __builtin_fmaf(ml[k].y, a, l);
+    sum += o[k] * a;
   }
   const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-  uint16_t* out = p.out + at * D + lane * (D / 64);
+  he out;
 #pragma unroll
-  for (int j = 0; j < D / 64; ++j) out[j] = __builtin_bit_cast(uint16_t, (_Float16)(o[j] * inv));
+  for (int j = 0; j < E; ++j) out[j] = (_Float16)(sum[j] * inv);
+  *reinterpret_cast<he*>(p.out + at * D + lane * E) = out;
   if (p.lse && lane == 0) p.lse[at] = l > 0.0f ? kLn2 * (__builtin_amdgcn_logf(l) + (m - kShift)) : -__builtin_inff();
 }
 
 // What a call launches, from sizes that the host knows.
 struct Plan {
   int nt;          // 16-row tiles of the few-rows kernel, or 0: the many-rows kernel
+  int waves;       // of the few-rows kernel
   int row_blocks;
   int splits, chunk;
   int most;        // splits that no call of a smaller span exceeds
 };
-constexpr int kRowsWaves = 4;
 
 Plan plan_of(int heads, int group, int sequences, int max_new, int max_len, int window, int D) {
   Plan f;
   const int64_t rows = (int64_t)max_new * group;
   f.nt = rows <= 16 ? 1 : rows <= 32 && D <= 128 ? 2 : 0;
   f.row_blocks = f.nt ? 1 : (int)((rows + kBlockRows - 1) / kBlockRows);
-  const int64_t span = window > 0 && (int64_t)window + max_new < max_len ? (int64_t)window + max_new : max_len;
-  const int64_t tiles = (span + kTile - 1) / kTile + 1;  // (a window's keys may start inside a tile)
+  const bool windowed = window > 0 && (int64_t)window + max_new < max_len;
+  // (a window's keys may start inside a tile)
+  const int64_t tiles = windowed ? ((int64_t)window + max_new + kTile - 1) / kTile + 1 : (max_len + kTile - 1) / kTile;
   const int64_t groups = (int64_t)sequences * heads * f.row_blocks;
-  // enough workgroups to fill the chip, but at least two tiles for each wave
-  const int64_t want = (int64_t)num_cus() * (f.nt ? 6 : 2), least = f.nt ? 2 * kRowsWaves : 8;
+  // Few rows: with one sequence every workgroup has as many tiles, and one round of resident ones is best (131000 keys, 8 heads: 57.7 us with two
+  // a CU, 60.5 with four, 66 with eight); lengths of several differ, and shorter pieces level them (48 of 17 to 8000 keys: 105 us,
+  // 95, 91 with eight, 98 with twelve).  A wave should have two tiles at least.
+  const int64_t want = (int64_t)num_cus() * (f.nt && sequences > 1 ? 8 : 2), least = 8;
   int64_t splits = groups >= want ? 1 : (want + groups - 1) / groups;
+  if (splits > kJoinMost) splits = kJoinMost;
   f.most = (int)(splits < (tiles + least - 1) / least ? splits : (tiles + least - 1) / least);
+  if (f.most < 1) f.most = 1;
   int64_t chunk = (tiles + splits - 1) / splits;
   if (chunk < least) chunk = least;
   if (chunk >= tiles) chunk = tiles;
+  if (chunk < 1) chunk = 1;
   f.chunk = (int)chunk;
-  f.splits = (int)((tiles + chunk - 1) / chunk);
+  f.splits = tiles > 0 ? (int)((tiles + chunk - 1) / chunk) : 1;
+  f.waves = f.nt == 1 && D <= 128 && f.splits == 1 && groups <= num_cus() ? 8 : 4;
   return f;
 }
 
-template <int D>
+template <int D, int P>
 int launch_attention_t(const AttnParams& p, const Plan& f, hipStream_t st) {
   const int64_t blocks = (int64_t)p.sequences * p.c.heads * f.row_blocks * f.splits;
-  const int64_t joins = ((int64_t)p.sequences * p.c.max_new * p.q_heads + kJoinRows - 1) / kJoinRows;
-  if (blocks > 0x7FFFFFFF || joins > 0x7FFFFFFF) return set_error(QQQ_ERR_SHAPE, "attention_kv8: too many workgroups");
-  if (f.nt == 1) hipLaunchKernelGGL((attn_rows_kernel<D, 1, kRowsWaves>), dim3((unsigned)blocks), dim3(64 * kRowsWaves), 0, st, p);
-  else if (f.nt == 2) {
-    if constexpr (D <= 128) hipLaunchKernelGGL((attn_rows_kernel<D, 2, kRowsWaves>), dim3((unsigned)blocks), dim3(64 * kRowsWaves), 0, st, p);
-  } else hipLaunchKernelGGL((attn_block_kernel<D>), dim3((unsigned)blocks), dim3(kBlockThreads), 0, st, p);
-  if (f.splits > 1) hipLaunchKernelGGL((attn_join_kernel<D>), dim3((unsigned)joins), dim3(64 * kJoinRows), 0, st, p, f.nt ? 0 : kBlockRows);
+  const int64_t joins = (int64_t)p.sequences * p.c.max_new * p.q_heads;
+  if (blocks > 0x7FFFFFFF || (f.splits > 1 && joins > 0x7FFFFFFF)) return set_error(QQQ_ERR_SHAPE, "attention_kv8: too many workgroups");
+  if (f.nt && p.sequences > 65535) return set_error(QQQ_ERR_SHAPE, "attention_kv8: %d sequences", p.sequences);
+#define QQQ_ROWS(NT, W) hipLaunchKernelGGL((attn_rows_kernel<D, P, NT, W>), dim3(p.c.heads, f.splits, p.sequences), dim3(64 * W), 0, st, p)
+  if (f.nt == 0) hipLaunchKernelGGL((attn_block_kernel<D, P>), dim3((unsigned)blocks), dim3(kBlockThreads), 0, st, p);
+  else if constexpr (D <= 128) {
+    if (f.nt == 2) QQQ_ROWS(2, 4);
+    else if (f.waves == 8) QQQ_ROWS(1, 8);
+    else QQQ_ROWS(1, 4);
+  } else QQQ_ROWS(1, 4);
+#undef QQQ_ROWS
+  const int block_rows = f.nt ? 0 : kBlockRows;
+  if (f.splits > kJoinFew) hipLaunchKernelGGL((attn_join_kernel<D>), dim3((unsigned)joins), dim3(64 * kJoinWaves), 0, st, p, block_rows);
+  else if (f.splits > 1) hipLaunchKernelGGL((attn_join_few_kernel<D>), dim3((unsigned)((joins + 3) / 4)), dim3(256), 0, st, p, block_rows);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return set_error(QQQ_ERR_HIP, "attention_kv8 launch: %s", hipGetErrorString(e));
   route_note("attention_kv8 %s x%d%s", f.nt ? "rows" : "blocks", f.splits, f.splits > 1 ? " + join" : "");
   return QQQ_OK;
+}
+
+template <int D>
+int launch_attention_p(const AttnParams& p, int P, const Plan& f, hipStream_t st) {
+  return P == 16 ? launch_attention_t<D, 16>(p, f, st) : P == 32 ? launch_attention_t<D, 32>(p, f, st) : launch_attention_t<D, 64>(p, f, st);
 }
 
 size_t partial_bytes(int splits, int64_t tokens, int q_heads, int D) {
@@ -655,12 +845,11 @@ int launch_attention_kv8(const Kv8& c, int D, int P, int sequences, const void* 
   p.q_heads = q_heads;
   p.causal = causal;
   p.window = window;
-  p.lp = P == 16 ? 4 : P == 32 ? 5 : 6;
   p.splits = f.splits;
   p.chunk = f.chunk;
   p.row_blocks = f.row_blocks;
   p.sequences = sequences;
-  return D == 64 ? launch_attention_t<64>(p, f, st) : D == 128 ? launch_attention_t<128>(p, f, st) : launch_attention_t<256>(p, f, st);
+  return D == 64 ? launch_attention_p<64>(p, P, f, st) : D == 128 ? launch_attention_p<128>(p, P, f, st) : launch_attention_p<256>(p, P, f, st);
 }
 
 }  // namespace qqq
