@@ -55,7 +55,7 @@ def _no_native(*args):
     return None
 
 
-_native_linear = _no_native
+_native_linear = _native_rmsnorm = _native_gated = _native_append = _native_read = _native_attention = _no_native
 
 
 def _call_path():
@@ -64,8 +64,9 @@ def _call_path():
 
 
 def _load_native(library):
-    """The extension that takes the linear calls from tensors to the library (csrc/qqq_torch_call.cpp).  Without it they are marshalled here."""
-    global _native_linear
+    """The extension that takes the linear calls and those of include/qqq_layer.h from tensors to the library (csrc/qqq_torch_call.cpp).  Without
+    it they are marshalled here."""
+    global _native_linear, _native_rmsnorm, _native_gated, _native_append, _native_read, _native_attention
     path = _call_path()
     try:
         spec = importlib.util.spec_from_file_location("_qqq_call", path)
@@ -76,7 +77,9 @@ def _load_native(library):
                       % (os.path.basename(path), e), RuntimeWarning, stacklevel=3)
         return
     module.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (library.qqq_linear_w4a8_perchannel, library.qqq_linear_w4a8_pergroup)))
-    _native_linear = module.linear
+    module.bind_layer(*(ctypes.cast(getattr(library, n), ctypes.c_void_p).value for n in LAYER_SYMBOLS))
+    _native_linear, _native_rmsnorm, _native_gated = module.linear, module.rmsnorm, module.gated
+    _native_append, _native_read, _native_attention = module.append, module.read, module.attention
 
 
 def lib():
@@ -497,6 +500,13 @@ def _rows(t, name):
     return M, K, (t.stride(0) if M > 1 else max(K, t.stride(0)))
 
 
+def _checked(out):
+    """What the extension gives: the outputs, or the library's error code."""
+    if out.__class__ is int:
+        _check(out)
+    return out
+
+
 def _rmsnorm_args(x, gain, residual, sum_out):
     M, K, ldx = _rows(x, "x")
     if tuple(gain.shape) != (K,):
@@ -518,6 +528,9 @@ def _rmsnorm_args(x, gain, residual, sum_out):
 def qqq_add_rmsnorm(x, gain, residual=None, eps=1e-6, y=None, sum_out=None):
     """x [M,K] fp16 (+ residual fp16 or fp32) -> (their sum in the residual's type or None, y fp16 [M,K] = norm(sum) * gain).
     sum_out may be the residual itself."""
+    out = _native_rmsnorm(x, gain, residual, eps, sum_out, y, None, False, _raw_stream(_device())) if _lib and x.is_cuda else None
+    if out is not None:
+        return _checked(out)
     M, K, ldx, res, ldr, kind, sum_out, lds = _rmsnorm_args(x, gain, residual, sum_out)
     if y is None:
         y = torch.empty((M, K), dtype=torch.float16, device=x.device)
@@ -530,6 +543,9 @@ def qqq_add_rmsnorm(x, gain, residual=None, eps=1e-6, y=None, sum_out=None):
 
 def qqq_add_rmsnorm_quant(x, gain, residual=None, eps=1e-6, a_q=None, s_a=None, sum_out=None):
     """The same straight to codes -> (sum or None, a_q int8 [M,K], s_a fp32 [M]), as qqq_quant_act gives them."""
+    out = _native_rmsnorm(x, gain, residual, eps, sum_out, a_q, s_a, True, _raw_stream(_device())) if _lib and x.is_cuda else None
+    if out is not None:
+        return _checked(out)
     M, K, ldx, res, ldr, kind, sum_out, lds = _rmsnorm_args(x, gain, residual, sum_out)
     a_q, s_a = _codes_out(M, K, a_q, s_a, x.device)
     _check(lib().qqq_add_rmsnorm_quant(x.data_ptr(), ldx, res, ldr, kind, _ptr(gain, _F16), eps, M, K, None if sum_out is None else sum_out.data_ptr(),
@@ -552,12 +568,15 @@ _ACTS = {"silu": 0, "gelu_tanh": 1}
 
 def qqq_gated_act_quant(gate, up, act="silu", a_q=None, s_a=None):
     """gate, up [M,F] fp16 (views of one projection's output allowed) -> (a_q int8 [M,F], s_a fp32 [M]) of act(gate) * up; act "silu" or "gelu_tanh"."""
+    if act not in _ACTS:
+        raise ValueError("act must be one of %s" % ", ".join(_ACTS))
+    out = _native_gated(gate, up, _ACTS[act], a_q, s_a, _raw_stream(_device())) if _lib and gate.is_cuda else None
+    if out is not None:
+        return _checked(out)
     M, F, ldg = _rows(gate, "gate")
     M2, F2, ldu = _rows(up, "up")
     if (M, F) != (M2, F2):
         raise ValueError("gate and up disagree on their shape")
-    if act not in _ACTS:
-        raise ValueError("act must be one of %s" % ", ".join(_ACTS))
     a_q, s_a = _codes_out(M, F, a_q, s_a, gate.device)
     _check(lib().qqq_gated_act_quant(gate.data_ptr(), ldg, up.data_ptr(), ldu, _ACTS[act], M, F, _ptr(a_q, _I8), _ptr(s_a, torch.float32), _stream()))
     return a_q, s_a
@@ -629,6 +648,9 @@ def _heads(t, heads, D, name):
 
 def qqq_kv8_append(cache: KV8Cache, batch: KV8Batch, k, v):
     """Puts the step's new keys and values [tokens, kv_heads, head_dim] fp16 (strided views allowed) into the cache."""
+    rc = _native_append(cache, batch, k, v, _raw_stream(_device())) if _lib and k.is_cuda else None
+    if rc is not None:
+        return _check(rc)
     c, b, H, D = _kv8_structs(cache, batch)
     (T, kt, kh), (T2, vt, vh) = _heads(k, H, D, "k"), _heads(v, H, D, "v")
     if T != T2:
@@ -639,6 +661,11 @@ def qqq_kv8_append(cache: KV8Cache, batch: KV8Batch, k, v):
 def qqq_kv8_read(cache: KV8Cache, batch: KV8Batch, k=None, v=None, tokens=None):
     """The last cu[b+1] - cu[b] tokens of each sequence as the cache holds them -> (k, v) fp16 [tokens, kv_heads, head_dim]; tokens: rows of the
     outputs where they are not given."""
+    if k is not None and v is not None and _lib and k.is_cuda:
+        rc = _native_read(cache, batch, k, v, _raw_stream(_device()))
+        if rc is not None:
+            _check(rc)
+            return k, v
     c, b, H, D = _kv8_structs(cache, batch)
     if (k is None or v is None) and tokens is None:
         raise ValueError("tokens is needed where k or v is not given")
@@ -661,6 +688,9 @@ def qqq_attention_kv8(cache: KV8Cache, batch: KV8Batch, q, scale=None, causal=Tr
     """Attention of the new tokens' queries [tokens, q_heads, head_dim] fp16 (strided views allowed) over the cache -> (out fp16 of that shape, lse
     fp32 [tokens, q_heads], or None where none is given).  scale: 1 / sqrt(head_dim).  workspace: a uint8 tensor of
     qqq_attention_kv8_workspace_bytes(); without one torch's allocator lends it."""
+    given = _native_attention(cache, batch, q, scale, causal, window, out, lse, workspace, _raw_stream(_device())) if _lib and q.is_cuda else None
+    if given is not None:
+        return _checked(given)
     c, b, H, D = _kv8_structs(cache, batch)
     T, qt, qh = _heads(q, 0, D, "q")
     Hq = q.shape[1]

@@ -44,7 +44,7 @@ def build_call() -> str:
     tmp = target + ".tmp.%d" % os.getpid()
     # NDEBUG: pybind11 keeps a thread-local counter without it.  A library with a thread-local variable of its own that nothing reads makes every other
     # library's (torch's, HIP's) slower from its loading on, glibc looking through all of them at each access: two ctypes calls 14.5 -> 16.8 us.
-    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-DNDEBUG", "-I", sysconfig.get_paths()["include"], "-isystem", inc,
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-DNDEBUG", "-I", sysconfig.get_paths()["include"], "-I", os.path.join(ROOT, "include"), "-isystem", inc,
            "-isystem", os.path.join(inc, "torch", "csrc", "api", "include"),
            "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI), os.path.join(CSRC, "qqq_torch_call.cpp"), "-o", tmp,
            "-L", os.path.join(base, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"]
