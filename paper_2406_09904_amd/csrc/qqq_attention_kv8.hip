@@ -22,6 +22,7 @@ typedef float f16v __attribute__((ext_vector_type(16)));
 
 constexpr int kTile = 64;         // tokens of a step over the keys
 constexpr float kShift = 6.0f;    // weights are up to 2^6: fp16 keeps all their bits down to 2^-20 of the largest
+constexpr float kSlack = 8.0f;    // the many-rows kernel lets weights grow by 2^8 before it rescales: up to 2^14 then, fp16 ends at 2^16
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
 struct AttnParams {
@@ -455,74 +456,69 @@ __global__ __launch_bounds__(kBlockThreads, D <= 128 ? 2 : 1) void attn_block_ke
       vs_raw = c.v_scale[at];
     }
   };
-  const int open_tile = s.len > closed * P ? closed * P / kTile : -1;  // the one with tokens in the tail slot
-  auto stage = [&](int tile, TileLds<D>& to) {
-    h8 k[KC][2], v[VC][2];
-#pragma unroll
-    for (int j = 0; j < KC; ++j) {
-      k[j][0] = codes8_to_halves(kraw[j].x, kraw[j].y);
-      k[j][1] = codes8_to_halves(kraw[j].z, kraw[j].w);
-    }
-#pragma unroll
-    for (int j = 0; j < VC; ++j) {
-      v[j][0] = codes8_to_halves(vraw[j].x, vraw[j].y);
-      v[j][1] = codes8_to_halves(vraw[j].z, vraw[j].w);
-    }
-    if (tile == open_tile) {
-      const int64_t tail = ((int64_t)slot * c.heads + head) * (P * D);
-      uint4 kt[KC][2], vt[VC][2];
-#pragma unroll
-      for (int j = 0; j < KC; ++j) {
-        const int at = tid + kBlockThreads * j, t = at / (D / 16), d = at % (D / 16) * 16;
-#pragma unroll
-        for (int half = 0; half < 2; ++half) kt[j][half] = *reinterpret_cast<const uint4*>(c.k_tail + tail + (t & (P - 1)) * D + d + 8 * half);
-      }
-#pragma unroll
-      for (int j = 0; j < VC; ++j) {
-        const int at = tid + kBlockThreads * j, d = at >> 2, grp = at & 3;
-#pragma unroll
-        for (int half = 0; half < 2; ++half) vt[j][half] = *reinterpret_cast<const uint4*>(c.v_tail + tail + d * P + ((16 * grp) & (P - 1)) + 8 * half);
-      }
-#pragma unroll
-      for (int j = 0; j < KC; ++j) {
-        const int t = (tid + kBlockThreads * j) / (D / 16);
-#pragma unroll
-        for (int half = 0; half < 2; ++half)
-          if ((tile * kTile + t) / P >= closed) k[j][half] = as_h8(kt[j][half]);
-      }
-#pragma unroll
-      for (int j = 0; j < VC; ++j) {
-        const int grp = (tid + kBlockThreads * j) & 3, left = s.len - (tile * kTile + 16 * grp);  // tokens that exist
-#pragma unroll
-        for (int half = 0; half < 2; ++half)
-          if ((tile * kTile + 16 * grp) / P >= closed) {
-            v[j][half] = as_h8(vt[j][half]);
-#pragma unroll
-            for (int x = 0; x < 8; ++x)
-              if (8 * half + x >= left) v[j][half][x] = (_Float16)0.0f;
-          }
-      }
-    }
+  // codes to fp16, into LDS
+  auto stage = [&](TileLds<D>& to) {
 #pragma unroll
     for (int j = 0; j < KC; ++j) {
       const int at = tid + kBlockThreads * j, t = at / (D / 16), d = at % (D / 16) * 16;
       uint4* put = reinterpret_cast<uint4*>(&to.k[t * TileLds<D>::kRowK + d]);
-      put[0] = __builtin_bit_cast(uint4, k[j][0]);
-      put[1] = __builtin_bit_cast(uint4, k[j][1]);
+      put[0] = __builtin_bit_cast(uint4, codes8_to_halves(kraw[j].x, kraw[j].y));
+      put[1] = __builtin_bit_cast(uint4, codes8_to_halves(kraw[j].z, kraw[j].w));
     }
 #pragma unroll
     for (int j = 0; j < VC; ++j) {
       const int at = tid + kBlockThreads * j, d = at >> 2, grp = at & 3;
       uint4* put = reinterpret_cast<uint4*>(&to.v[d * TileLds<D>::kRowV + 16 * grp]);
-      put[0] = __builtin_bit_cast(uint4, v[j][0]);
-      put[1] = __builtin_bit_cast(uint4, v[j][1]);
+      put[0] = __builtin_bit_cast(uint4, codes8_to_halves(vraw[j].x, vraw[j].y));
+      put[1] = __builtin_bit_cast(uint4, codes8_to_halves(vraw[j].z, vraw[j].w));
     }
     if (tid < 4) {
-      const bool tail = tile == open_tile && (tile * kTile + 16 * tid) / P >= closed;
-      const Factors f = factors_of(tail ? 1.0f : ks_raw, tail ? 1.0f : vs_raw, p.scale_log2);
+      const Factors f = factors_of(ks_raw, vs_raw, p.scale_log2);
       to.c[tid] = f.c;
       to.lv[tid] = f.lv;
       to.rv[tid] = f.rv;
+    }
+  };
+  // and over it what the tail slot holds of the tile that the sequence ends in (each thread over its own chunks)
+  const int open_tile = s.len > closed * P ? closed * P / kTile : -1;
+  auto stage_tail = [&](TileLds<D>& to) {
+    const int64_t tail = ((int64_t)slot * c.heads + head) * (P * D);
+    uint4 kt[KC][2], vt[VC][2];
+#pragma unroll
+    for (int j = 0; j < KC; ++j) {
+      const int at = tid + kBlockThreads * j, t = at / (D / 16), d = at % (D / 16) * 16;
+#pragma unroll
+      for (int half = 0; half < 2; ++half) kt[j][half] = *reinterpret_cast<const uint4*>(c.k_tail + tail + (t & (P - 1)) * D + d + 8 * half);
+    }
+#pragma unroll
+    for (int j = 0; j < VC; ++j) {
+      const int at = tid + kBlockThreads * j, d = at >> 2, grp = at & 3;
+#pragma unroll
+      for (int half = 0; half < 2; ++half) vt[j][half] = *reinterpret_cast<const uint4*>(c.v_tail + tail + d * P + ((16 * grp) & (P - 1)) + 8 * half);
+    }
+#pragma unroll
+    for (int j = 0; j < KC; ++j) {
+      const int at = tid + kBlockThreads * j, t = at / (D / 16), d = at % (D / 16) * 16;
+      if ((open_tile * kTile + t) / P < closed) continue;
+      uint4* put = reinterpret_cast<uint4*>(&to.k[t * TileLds<D>::kRowK + d]);
+      put[0] = kt[j][0];
+      put[1] = kt[j][1];
+    }
+#pragma unroll
+    for (int j = 0; j < VC; ++j) {
+      const int at = tid + kBlockThreads * j, d = at >> 2, grp = at & 3;
+      if ((open_tile * kTile + 16 * grp) / P < closed) continue;
+      const int left = s.len - (open_tile * kTile + 16 * grp);  // tokens that exist: what lies past them may be anything
+      auto pair = [&](uint32_t w, int e) { return w & ((e < left ? 0xFFFFu : 0u) | (e + 1 < left ? 0xFFFF0000u : 0u)); };
+      uint4* put = reinterpret_cast<uint4*>(&to.v[d * TileLds<D>::kRowV + 16 * grp]);
+#pragma unroll
+      for (int half = 0; half < 2; ++half)
+        put[half] = make_uint4(pair(vt[j][half].x, 8 * half), pair(vt[j][half].y, 8 * half + 2), pair(vt[j][half].z, 8 * half + 4), pair(vt[j][half].w, 8 * half + 6));
+    }
+    if (tid < 4 && (open_tile * kTile + 16 * tid) / P >= closed) {
+      to.c[tid] = p.scale_log2;
+      to.lv[tid] = 0.0f;
+      to.rv[tid] = 1.0f;
     }
   };
 
@@ -538,7 +534,10 @@ __global__ __launch_bounds__(kBlockThreads, D <= 128 ? 2 : 1) void attn_block_ke
   if (tiles > 0) {
     request(pages_of<P>(c, b, first, closed));
     pages = pages_of<P>(c, b, min(first + 1, end - 1), closed);
-    stage(first, lds[0]);
+    // everything so far, the queries too: left to the loop, their wait would be one for the codes in flight in every tile
+    __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
+    stage(lds[0]);
+    if (first == open_tile) stage_tail(lds[0]);
     request(pages);
     pages = pages_of<P>(c, b, min(first + 2, end - 1), closed);
     lds_barrier();
@@ -546,17 +545,47 @@ __global__ __launch_bounds__(kBlockThreads, D <= 128 ? 2 : 1) void attn_block_ke
   const int token_of_row = 16 * (n >> 4) + 8 * ((n >> 2) & 1) + 4 * ((n >> 3) & 1) + (n & 3);
   for (int tile = first; tile < end; ++tile) {
     const TileLds<D>& t = lds[(tile - first) & 1];
+    TileLds<D>& next = lds[(tile + 1 - first) & 1];
+    auto k_of = [&](int x) {  // x: step and 32-token subtile (in turn, so that no product waits for the one before it)
+      return as_h8(*reinterpret_cast<const uint4*>(&t.k[(32 * (x & 1) + token_of_row) * TileLds<D>::kRowK + 16 * (x >> 1) + 8 * h]));
+    };
+    auto v_of = [&](int x) {  // x: step of 16 tokens and 32 channels
+      return as_h8(*reinterpret_cast<const uint4*>(&t.v[(32 * (x % DT) + n) * TileLds<D>::kRowV + 16 * (x / DT) + 8 * h]));
+    };
+    constexpr int kAhead = D == 128 ? 8 : 4;  // operands on their way from LDS
     f16v sc[2];
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
+    for (int u = 0; u < 2; ++u)
 #pragma unroll
       for (int x = 0; x < 16; ++x) sc[u][x] = 0.0f;
+    {
+      h8 a[2 * KS];
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        const h8 a = as_h8(*reinterpret_cast<const uint4*>(&t.k[(32 * u + token_of_row) * TileLds<D>::kRowK + 16 * ks + 8 * h]));
-        sc[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a, q[ks], sc[u], 0, 0, 0);
+      for (int x = 0; x < kAhead; ++x) a[x] = k_of(x);
+#pragma unroll
+      for (int x = 0; x < 2 * KS; ++x) {
+        if (x + kAhead < 2 * KS) a[x + kAhead] = k_of(x + kAhead);
+        sc[x & 1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[x], q[x >> 1], sc[x & 1], 0, 0, 0);
+      }
+      __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);
+#pragma unroll
+      for (int x = 0; x < 2 * KS; ++x) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        if (x + kAhead < 2 * KS) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
       }
     }
+    __builtin_amdgcn_sched_barrier(0);
+    h8 v[4 * DT];
+#pragma unroll
+    for (int x = 0; x < kAhead; ++x) v[x] = v_of(x);  // on their way while the weights are made
+    float fc[4], flv[4], frv[4];
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      fc[g] = t.c[g];
+      flv[g] = t.lv[g];
+      frv[g] = t.rv[g];
+    }
+    __builtin_amdgcn_sched_barrier(0);
     if ((tile + 1) * kTile > range.whole_hi || tile * kTile < range.whole_lo) {
 #pragma unroll
       for (int u = 0; u < 2; ++u)
@@ -572,42 +601,41 @@ __global__ __launch_bounds__(kBlockThreads, D <= 128 ? 2 : 1) void attn_block_ke
       float tg = sc[g >> 1][8 * (g & 1)];
 #pragma unroll
       for (int x = 1; x < 8; ++x) tg = fmaxf(tg, sc[g >> 1][8 * (g & 1) + x]);
-      top = fmaxf(top, __builtin_fmaf(tg, t.c[g], t.lv[g]));
+      top = fmaxf(top, __builtin_fmaf(tg, fc[g], flv[g]));
     }
     top = across32(top, fmax2);
-    const float was = m, now = fmaxf(was, top), base = now == -__builtin_inff() ? 0.0f : now;
-    const float alpha = __builtin_amdgcn_exp2f(was - base);
-    m = now;
+    if (__any(top > m + kSlack)) {
+      const float now = top > m + kSlack ? top : m, alpha = __builtin_amdgcn_exp2f(m - now);  // (m finite or now above it: not NaN)
+      const float by = m == now ? 1.0f : alpha;
+      m = now;
+      l *= by;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) o[dt] *= by;
+    }
+    const float base = m == -__builtin_inff() ? 0.0f : m;   // a row that has seen nothing yet: weights 2^-inf = 0
     h8 w[4];
-    l *= alpha;
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
-      const float add = t.lv[g] - base + kShift, cg = t.c[g];
+      const float add = flv[g] - base + kShift;
       float sum = 0.0f;
 #pragma unroll
       for (int x = 0; x < 8; ++x) {
-        const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[g >> 1][8 * (g & 1) + x], cg, add));
+        const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[g >> 1][8 * (g & 1) + x], fc[g], add));
         sum += e;
         w[g][x] = (_Float16)e;
       }
-      l = __builtin_fmaf(sum, t.rv[g], l);
+      l = __builtin_fmaf(sum, frv[g], l);
     }
-    if (__any(alpha != 1.0f)) {
+    // the second product; beside it the next tile's codes become fp16 (past the last tile: some codes again, never read)
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt) o[dt] *= alpha;
+    for (int x = 0; x < 4 * DT; ++x) {
+      if (x + kAhead < 4 * DT) v[x + kAhead] = v_of(x + kAhead);
+      o[x % DT] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v[x], w[x / DT], o[x % DT], 0, 0, 0);
     }
-#pragma unroll
-    for (int g = 0; g < 4; ++g)
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt) {
-        const h8 a = as_h8(*reinterpret_cast<const uint4*>(&t.v[(32 * dt + n) * TileLds<D>::kRowV + 16 * g + 8 * h]));
-        o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a, w[g], o[dt], 0, 0, 0);
-      }
-    if (tile + 1 < end) {
-      stage(tile + 1, lds[(tile + 1 - first) & 1]);
-      request(pages);
-      pages = pages_of<P>(c, b, min(tile + 3, end - 1), closed);
-    }
+    stage(next);
+    if (tile + 1 == open_tile) stage_tail(next);
+    request(pages);
+    pages = pages_of<P>(c, b, min(tile + 3, end - 1), closed);
     lds_barrier();
   }
   l = across32(l, fadd2);
