@@ -22,7 +22,7 @@ typedef float f16v __attribute__((ext_vector_type(16)));
 
 constexpr int kTile = 64;         // tokens of a step over the keys
 constexpr float kShift = 6.0f;    // weights are up to 2^6: fp16 keeps all their bits down to 2^-20 of the largest
-constexpr float kSlack = 8.0f;    // the many-rows kernel lets weights grow by 2^8 before it rescales: up to 2^14 then, fp16 ends at 2^16
+constexpr float kMost = 0x1p14f;  // sums of weights up to which the many-rows kernel leaves its reference alone (fp16 ends at 2^16)
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
 struct AttnParams {
@@ -99,7 +99,8 @@ struct Pages {
 template <int P>
 __device__ __forceinline__ Pages<P> pages_of(const Kv8& c, int b, int tile, int closed) {
   // (always a load, so that the requests behind it are the same on every path)
-  const int32_t* table = closed > 0 ? c.table + b * c.table_stride : c.kv_len + b;
+  typedef const int32_t __attribute__((address_space(4))) * Constant;  // (scalar loads, whatever stands between them)
+  const Constant table = (Constant)(uintptr_t)(closed > 0 ? c.table + b * c.table_stride : c.kv_len + b);
   Pages<P> g;
 #pragma unroll
   for (int i = 0; i < Pages<P>::N; ++i) g.id[i] = table[max(0, min(tile * Pages<P>::N + i, closed - 1))];
@@ -530,19 +531,20 @@ __global__ __launch_bounds__(kBlockThreads, D <= 128 ? 2 : 1) void attn_block_ke
     for (int x = 0; x < 16; ++x) o[dt][x] = 0.0f;
 
   const int first = range.tile0 + from, end = first + tiles;
-  Pages<P> pages;   // of the tile after the one whose codes are on their way
-  if (tiles > 0) {
-    request(pages_of<P>(c, b, first, closed));
-    pages = pages_of<P>(c, b, min(first + 1, end - 1), closed);
-    // everything so far, the queries too: left to the loop, their wait would be one for the codes in flight in every tile
-    __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
-    stage(lds[0]);
-    if (first == open_tile) stage_tail(lds[0]);
-    request(pages);
-    pages = pages_of<P>(c, b, min(first + 2, end - 1), closed);
-    lds_barrier();
-  }
+  auto pages_at = [&](int tile) { return pages_of<P>(c, b, min(tile, end - 1), closed); };
+  Pages<P> pages = pages_at(first);   // of the tile after the one whose codes are on their way
+  request(pages);
+  pages = pages_at(first + 1);
+  // everything so far, the queries too: left to the loop, their wait would be one for the codes in flight in every tile
+  __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
+  __builtin_amdgcn_sched_barrier(0);
+  stage(lds[0]);
+  if (first == open_tile) stage_tail(lds[0]);
+  request(pages);
+  pages = pages_at(first + 2);
+  lds_barrier();
   const int token_of_row = 16 * (n >> 4) + 8 * ((n >> 2) & 1) + 4 * ((n >> 3) & 1) + (n & 3);
+  bool unseen = true;  // some row of the wave has seen nothing yet
   for (int tile = first; tile < end; ++tile) {
     const TileLds<D>& t = lds[(tile - first) & 1];
     TileLds<D>& next = lds[(tile + 1 - first) & 1];
@@ -552,7 +554,7 @@ __global__ __launch_bounds__(kBlockThreads, D <= 128 ? 2 : 1) void attn_block_ke
     auto v_of = [&](int x) {  // x: step of 16 tokens and 32 channels
       return as_h8(*reinterpret_cast<const uint4*>(&t.v[(32 * (x % DT) + n) * TileLds<D>::kRowV + 16 * (x / DT) + 8 * h]));
     };
-    constexpr int kAhead = D == 128 ? 8 : 4;  // operands on their way from LDS
+    constexpr int kAhead = 4;  // operands on their way from LDS
     f16v sc[2];
 #pragma unroll
     for (int u = 0; u < 2; ++u)
@@ -595,37 +597,45 @@ __global__ __launch_bounds__(kBlockThreads, D <= 128 ? 2 : 1) void attn_block_ke
           if (!(key >= lo && key < hi)) sc[u][x] = -__builtin_inff();
         }
     }
-    float top = -__builtin_inff();
+    // Weights relative to the reference as it stands.  Sums of a lane's weights that stay small say that each of them does; where they do not, or
+    // where a row has seen nothing yet, the reference is raised to the row's largest contribution, and they are made again.
+    h8 w[4];
+    float sums[4];
+    auto weigh = [&]() {
+      const float base = m == -__builtin_inff() ? 0.0f : m;   // a row that has seen nothing yet: weights 2^-inf = 0
 #pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      float tg = sc[g >> 1][8 * (g & 1)];
+      for (int g = 0; g < 4; ++g) {
+        const float add = flv[g] - base + kShift;
+        sums[g] = 0.0f;
 #pragma unroll
-      for (int x = 1; x < 8; ++x) tg = fmaxf(tg, sc[g >> 1][8 * (g & 1) + x]);
-      top = fmaxf(top, __builtin_fmaf(tg, fc[g], flv[g]));
-    }
-    top = across32(top, fmax2);
-    if (__any(top > m + kSlack)) {
-      const float now = top > m + kSlack ? top : m, alpha = __builtin_amdgcn_exp2f(m - now);  // (m finite or now above it: not NaN)
-      const float by = m == now ? 1.0f : alpha;
+        for (int x = 0; x < 8; ++x) {
+          const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[g >> 1][8 * (g & 1) + x], fc[g], add));
+          sums[g] += e;
+          w[g][x] = (_Float16)e;
+        }
+      }
+    };
+    weigh();
+    if (unseen || __any(fmaxf(fmaxf(sums[0], sums[1]), fmaxf(sums[2], sums[3])) > kMost)) {
+      float top = -__builtin_inff();
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        float tg = sc[g >> 1][8 * (g & 1)];
+#pragma unroll
+        for (int x = 1; x < 8; ++x) tg = fmaxf(tg, sc[g >> 1][8 * (g & 1) + x]);
+        top = fmaxf(top, __builtin_fmaf(tg, fc[g], flv[g]));
+      }
+      top = across32(top, fmax2);
+      const float now = fmaxf(m, top), by = m == now ? 1.0f : __builtin_amdgcn_exp2f(m - now);
       m = now;
       l *= by;
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) o[dt] *= by;
+      unseen = __any(m == -__builtin_inff());
+      weigh();
     }
-    const float base = m == -__builtin_inff() ? 0.0f : m;   // a row that has seen nothing yet: weights 2^-inf = 0
-    h8 w[4];
 #pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      const float add = flv[g] - base + kShift;
-      float sum = 0.0f;
-#pragma unroll
-      for (int x = 0; x < 8; ++x) {
-        const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[g >> 1][8 * (g & 1) + x], fc[g], add));
-        sum += e;
-        w[g][x] = (_Float16)e;
-      }
-      l = __builtin_fmaf(sum, frv[g], l);
-    }
+    for (int g = 0; g < 4; ++g) l = __builtin_fmaf(sums[g], frv[g], l);
     // the second product; beside it the next tile's codes become fp16 (past the last tile: some codes again, never read)
 #pragma unroll
     for (int x = 0; x < 4 * DT; ++x) {
@@ -635,7 +645,7 @@ __global__ __launch_bounds__(kBlockThreads, D <= 128 ? 2 : 1) void attn_block_ke
     stage(next);
     if (tile + 1 == open_tile) stage_tail(next);
     request(pages);
-    pages = pages_of<P>(c, b, min(tile + 3, end - 1), closed);
+    pages = pages_at(tile + 3);
     lds_barrier();
   }
   l = across32(l, fadd2);
