@@ -10,6 +10,8 @@
 // S is computed transposed (keys x rows), and so is O (channels x rows): a lane of S^T's accumulator holds keys of ONE row, which is
 // how the second product wants its operand, so that the weights go from the one to the other in registers.  What makes that fit is
 // which token each row of the first product's operand is taken from (token_of_row below).
+#include <type_traits>
+
 #include "qqq_kv8.h"
 
 namespace qqq {
@@ -545,9 +547,9 @@ __global__ __launch_bounds__(kBlockThreads, D <= 128 ? 2 : 1) void attn_block_ke
   lds_barrier();
   const int token_of_row = 16 * (n >> 4) + 8 * ((n >> 2) & 1) + 4 * ((n >> 3) & 1) + (n & 3);
   bool unseen = true;  // some row of the wave has seen nothing yet
-  for (int tile = first; tile < end; ++tile) {
-    const TileLds<D>& t = lds[(tile - first) & 1];
-    TileLds<D>& next = lds[(tile + 1 - first) & 1];
+  auto step = [&](int tile, auto buffer) {
+    const TileLds<D>& t = lds[decltype(buffer)::value];
+    TileLds<D>& next = lds[1 - decltype(buffer)::value];
     auto k_of = [&](int x) {  // x: step and 32-token subtile (in turn, so that no product waits for the one before it)
       return as_h8(*reinterpret_cast<const uint4*>(&t.k[(32 * (x & 1) + token_of_row) * TileLds<D>::kRowK + 16 * (x >> 1) + 8 * h]));
     };
@@ -555,11 +557,8 @@ __global__ __launch_bounds__(kBlockThreads, D <= 128 ? 2 : 1) void attn_block_ke
       return as_h8(*reinterpret_cast<const uint4*>(&t.v[(32 * (x % DT) + n) * TileLds<D>::kRowV + 16 * (x / DT) + 8 * h]));
     };
     constexpr int kAhead = 4;  // operands on their way from LDS
+    const f16v zero = {};
     f16v sc[2];
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-      for (int x = 0; x < 16; ++x) sc[u][x] = 0.0f;
     {
       h8 a[2 * KS];
 #pragma unroll
@@ -567,7 +566,7 @@ __global__ __launch_bounds__(kBlockThreads, D <= 128 ? 2 : 1) void attn_block_ke
 #pragma unroll
       for (int x = 0; x < 2 * KS; ++x) {
         if (x + kAhead < 2 * KS) a[x + kAhead] = k_of(x + kAhead);
-        sc[x & 1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[x], q[x >> 1], sc[x & 1], 0, 0, 0);
+        sc[x & 1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[x], q[x >> 1], x < 2 ? zero : sc[x & 1], 0, 0, 0);
       }
       __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);
 #pragma unroll
@@ -647,6 +646,11 @@ __global__ __launch_bounds__(kBlockThreads, D <= 128 ? 2 : 1) void attn_block_ke
     request(pages);
     pages = pages_at(tile + 3);
     lds_barrier();
+  };
+  // (two at a time: which buffer is which is then a constant, and LDS addresses offsets of the instructions)
+  for (int tile = first; tile < end; tile += 2) {
+    step(tile, std::integral_constant<int, 0>{});
+    if (tile + 1 < end) step(tile + 1, std::integral_constant<int, 1>{});
   }
   l = across32(l, fadd2);
   if (!there) return;
