@@ -67,7 +67,7 @@ int qqq_gated_act_quant(const void* gate_fp16, int64_t ldg, const void* up_fp16,
  *   k_codes [pages, kv_heads, page_tokens, head_dim],  v_codes [pages, kv_heads, head_dim, page_tokens]  uint8
  *   k_scale, v_scale [pages, kv_heads] fp32
  *   k_tail [slots, kv_heads, page_tokens, head_dim],  v_tail [slots, kv_heads, head_dim, page_tokens]  fp16
- * page_tokens 16, 32 or 64; head_dim 64, 128 or 256; kv_heads >= 1.  (Values lie token by token: eight values of one channel are
+ * page_tokens 16, 32 or 64; head_dim 64, 128 or 256; kv_heads >= 1; pages * kv_heads < 2^31.  (Values lie token by token: eight values of one channel are
  * then an operand of the matrix instruction as they are.)
  */
 typedef struct qqq_kv8_cache {

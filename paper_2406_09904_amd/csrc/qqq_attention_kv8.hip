@@ -87,7 +87,7 @@ __device__ __forceinline__ Factors factors_of(float ks, float vs, float scale_lo
   f.c = fmaxf(ks * scale_log2, 0x1p-100f);
   const float v = vs > 0.0f ? vs : 1.0f;
   f.lv = __builtin_amdgcn_logf(v);
-  f.rv = 1.0f / v;
+  f.rv = __builtin_amdgcn_rcpf(v);
   return f;
 }
 
@@ -159,7 +159,7 @@ __global__ __launch_bounds__(64 * W, D <= 128 ? 2 : 1) void attn_rows_kernel(con
   const uint32_t k_lane = (((16 * gk) & (P - 1)) + (n & 3)) * D + 16 * g, v_lane = n * P + ((16 * g) & (P - 1));
   auto offsets = [&](const Pages<P>& of, int64_t* at) {
 #pragma unroll
-    for (int i = 0; i < NP; ++i) at[i] = (kv8_page(c, of.id[i]) * c.heads + head) * (P * D);
+    for (int i = 0; i < NP; ++i) at[i] = kv8_block(c, of.id[i], head) * (P * D);
   };
   auto request_k = [&](const Pages<P>& of) {
     int64_t offset[NP];
@@ -181,7 +181,7 @@ __global__ __launch_bounds__(64 * W, D <= 128 ? 2 : 1) void attn_rows_kernel(con
   auto scales = [&](const Pages<P>& of) {
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
-      const int64_t at = kv8_page(c, of.id[i]) * c.heads + head;
+      const int64_t at = kv8_block(c, of.id[i], head);
       ks[i] = c.k_scale[at];
       vs[i] = c.v_scale[at];
     }
@@ -442,7 +442,7 @@ __global__ __launch_bounds__(kBlockThreads, D <= 128 ? 2 : 1) void attn_block_ke
   auto request = [&](const Pages<P>& of) {
     int64_t offset[NP];
 #pragma unroll
-    for (int x = 0; x < NP; ++x) offset[x] = (kv8_page(c, of.id[x]) * c.heads + head) * (P * D);
+    for (int x = 0; x < NP; ++x) offset[x] = kv8_block(c, of.id[x], head) * (P * D);
 #pragma unroll
     for (int j = 0; j < KC; ++j) {
       const int at = tid + kBlockThreads * j, t = at / (D / 16), d = at % (D / 16) * 16;
@@ -454,7 +454,7 @@ __global__ __launch_bounds__(kBlockThreads, D <= 128 ? 2 : 1) void attn_block_ke
       vraw[j] = *reinterpret_cast<const uint4*>(c.v_codes + of_group<P>(offset, grp) + d * P + ((16 * grp) & (P - 1)));
     }
     if (tid < 4) {
-      const int64_t at = kv8_page(c, of_group<P>(of.id, tid)) * c.heads + head;
+      const int64_t at = kv8_block(c, of_group<P>(of.id, tid), head);
       ks_raw = c.k_scale[at];
       vs_raw = c.v_scale[at];
     }

@@ -31,9 +31,11 @@ __device__ __forceinline__ Kv8Seq kv8_sequence(const Kv8& c, int b) {
   s.slot = c.slots ? c.slots[b] : b;
   return s;
 }
-__device__ __forceinline__ bool kv8_has_page(const Kv8& c, int page) { return (uint32_t)page < (uint64_t)c.pages; }
+__device__ __forceinline__ bool kv8_has_page(const Kv8& c, int page) { return (uint32_t)page < (uint32_t)c.pages; }
 // for reads: one that exists in the place of one that does not
-__device__ __forceinline__ int64_t kv8_page(const Kv8& c, int page) { return kv8_has_page(c, page) ? page : c.pages - 1; }
+__device__ __forceinline__ uint32_t kv8_page(const Kv8& c, int page) { return min((uint32_t)page, (uint32_t)c.pages - 1u); }
+// a page's place for a head, in units of P * D values and of scales (pages * heads is below 2^31)
+__device__ __forceinline__ int64_t kv8_block(const Kv8& c, int page, int head) { return kv8_page(c, page) * (uint32_t)c.heads + (uint32_t)head; }
 __device__ __forceinline__ int kv8_slot(const Kv8& c, int slot) { return (uint32_t)slot < (uint32_t)c.nslots ? slot : c.nslots - 1; }
 
 // Four codes (offset binary bytes) as fp16 code values: byte u under the exponent of 1024 is 1024 + u, less 1152 it is u - 128, exactly.

@@ -172,7 +172,7 @@ __global__ __launch_bounds__(kThreads) void kv8_read_kernel(const ReadParams p) 
   const int start = s.len - s.n, closed = s.len / P, page = start / P + unit;
   if (s.n == 0 || page * P >= s.len) return;
   const bool is_tail = page >= closed;
-  const int64_t at = (int64_t)(is_tail ? kv8_slot(c, s.slot) : kv8_page(c, c.table[b * c.table_stride + page])) * c.heads + head;
+  const int64_t at = is_tail ? (int64_t)kv8_slot(c, s.slot) * c.heads + head : kv8_block(c, c.table[b * c.table_stride + page], head);
   uint16_t* out = (values ? p.v : p.k) + head * D;
   auto put = [&](int t, int d8, uint4 w) {
     const int pos = page * P + t;

@@ -52,7 +52,7 @@ int rmsnorm(const char* name, const void* x, int64_t ldx, const void* residual, 
 int check_cache(const char* name, const qqq_kv8_cache* c, const qqq_kv8_batch* b, int64_t tokens) {
   if (!c || !b) return set_error(QQQ_ERR_NULL, "%s: NULL struct", name);
   if ((c->page_tokens != 16 && c->page_tokens != 32 && c->page_tokens != 64) || (c->head_dim != 64 && c->head_dim != 128 && c->head_dim != 256) ||
-      c->kv_heads < 1 || c->pages < 1 || c->pages > 0x7FFFFFFF || c->slots < 1)
+      c->kv_heads < 1 || c->pages < 1 || c->pages > 0x7FFFFFFF / c->kv_heads || c->slots < 1)
     return set_error(QQQ_ERR_SHAPE, "%s: unsupported cache: %lld pages of %d tokens, %d heads of %d, %d slots", name, (long long)c->pages,
                      c->page_tokens, c->kv_heads, c->head_dim, c->slots);
   if (b->sequences < 0 || tokens < 0 || tokens > kMaxTokens || b->max_new < 0 || b->max_new > kMaxTokens || b->max_len < 0 || b->max_len > kMaxTokens ||
