@@ -806,7 +806,7 @@ struct Plan {
 Plan plan_of(int heads, int group, int sequences, int max_new, int max_len, int window, int D) {
   Plan f;
   const int64_t rows = (int64_t)max_new * group;
-  f.nt = rows <= 16 ? 1 : rows <= 32 && D <= 128 ? 2 : 0;
+  f.nt = rows <= 16 ? 1 : rows <= 32 ? 2 : 0;
   f.row_blocks = f.nt ? 1 : (int)((rows + kBlockRows - 1) / kBlockRows);
   const bool windowed = window > 0 && (int64_t)window + max_new < max_len;
   // (a window's keys may start inside a tile)
@@ -838,11 +838,9 @@ int launch_attention_t(const AttnParams& p, const Plan& f, hipStream_t st) {
   if (f.nt && p.sequences > 65535) return set_error(QQQ_ERR_SHAPE, "attention_kv8: %d sequences", p.sequences);
 #define QQQ_ROWS(NT, W) hipLaunchKernelGGL((attn_rows_kernel<D, P, NT, W>), dim3(p.c.heads, f.splits, p.sequences), dim3(64 * W), 0, st, p)
   if (f.nt == 0) hipLaunchKernelGGL((attn_block_kernel<D, P>), dim3((unsigned)blocks), dim3(kBlockThreads), 0, st, p);
-  else if constexpr (D <= 128) {
-    if (f.nt == 2) QQQ_ROWS(2, 4);
-    else if (f.waves == 8) QQQ_ROWS(1, 8);
-    else QQQ_ROWS(1, 4);
-  } else QQQ_ROWS(1, 4);
+  else if (f.nt == 2) QQQ_ROWS(2, 4);
+  else if (f.waves == 4) QQQ_ROWS(1, 4);
+  else if constexpr (D <= 128) QQQ_ROWS(1, 8);
 #undef QQQ_ROWS
   const int block_rows = f.nt ? 0 : kBlockRows;
   if (f.splits > kJoinFew) hipLaunchKernelGGL((attn_join_kernel<D>), dim3((unsigned)joins), dim3(64 * kJoinWaves), 0, st, p, block_rows);
