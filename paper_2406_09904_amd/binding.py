@@ -643,7 +643,7 @@ def _kv8_structs(cache, batch):
 def _heads(t, heads, D, name):
     if t.dtype != torch.float16 or t.dim() != 3 or t.stride(2) != 1 or not t.is_cuda or t.shape[2] != D or (heads and t.shape[1] != heads):
         raise ValueError("%s must be an fp16 device tensor [tokens, heads, %d] with unit inner stride" % (name, D))
-    return t.shape[0], t.stride(0), t.stride(1)
+    return t.shape[0], t.stride(0) if t.shape[0] > 1 else 0, t.stride(1) if t.shape[1] > 1 else 0
 
 
 def qqq_kv8_append(cache: KV8Cache, batch: KV8Batch, k, v):

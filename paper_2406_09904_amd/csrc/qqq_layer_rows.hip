@@ -5,6 +5,11 @@
 // Norm: y = h rho gain, rho = 1/sqrt(mean h^2 + eps).  rho is common to a row, so codes = rne(h gain / S), S = max |h gain| / 127,
 // and s_a = S rho: the sum of squares and the maximum come out of the same pass, and no code depends on how the sum was ordered.
 // h gain is exact in fp32 where h is fp16 (11 + 11 bits).
+//
+// Both are bound by their bytes from some hundred rows on, below that by how soon a row is done (a launch from a graph alone is 1.6 us).
+// Norm, fp16 residual, codes: M = 1, K = 4096 2.7 us; M = 777, K = 5120 6.2; M = 4096, K = 8192 37 to 44 (5.3 to 6.3 TB/s, by what the last-level
+// cache still holds); fp32 residual, fp16 output: M = 777, K = 5120 9.4, M = 4096, K = 8192 74.  Gated activation: M = 16, F = 11008 3.7 us;
+// M = 4096, F = 28672 113 (5.2 TB/s).
 #include "qqq_internal.h"
 #include "qqq_layer.h"
 
@@ -212,7 +217,12 @@ void launch_rmsnorm_t(const NormParams& p, int64_t M, hipStream_t st) {
 #define QQQ_NORM(V, T) hipLaunchKernelGGL((rmsnorm_kernel<RES, QUANT, V, T>), dim3((unsigned)M), dim3(T), 0, st, p)
   if (p.nvec <= 64) QQQ_NORM(1, 64);
   else if (p.nvec <= 256) QQQ_NORM(1, 256);
-  else if (p.nvec <= 512) QQQ_NORM(2, 256);
+  else if (M <= num_cus() && p.nvec <= 2048) {
+    // A row per CU at most: what counts is how soon it is done (M = 1, K = 8192 3.1 us against 3.6 with 256 threads; M = 200 4.2 against 4.5)
+    if (p.nvec <= 512) QQQ_NORM(1, 512);
+    else if (p.nvec <= 1024) QQQ_NORM(1, 1024);
+    else QQQ_NORM(2, 1024);
+  } else if (p.nvec <= 512) QQQ_NORM(2, 256);
   else if (p.nvec <= 1024) QQQ_NORM(4, 256);
   else if (p.nvec <= 2048) QQQ_NORM(4, 512);
   else if (p.nvec <= 4096) QQQ_NORM(4, 1024);

@@ -191,9 +191,13 @@ PyObject* rmsnorm(PyObject*, PyObject* const* args, Py_ssize_t n) {
     const int kind = !has ? QQQ_RESIDUAL_NONE : res->scalar_type() == at::kHalf ? QQQ_RESIDUAL_FP16 : QQQ_RESIDUAL_FP32;
     const void *px = x->data_ptr(), *pr = has ? res->data_ptr() : nullptr, *pg = gain->data_ptr();
     void *ps = has ? sum->data_ptr() : nullptr, *po = out->data_ptr();
+    float* pa = quantise ? static_cast<float*>(s_a->data_ptr()) : nullptr;
     const int64_t ldx = row_stride(*x), ldr = has ? row_stride(*res) : 0, lds = has ? row_stride(*sum) : 0;
-    const int rc = quantise ? layer.norm_quant(px, ldx, pr, ldr, kind, pg, eps, M, K, ps, lds, static_cast<int8_t*>(po), static_cast<float*>(s_a->data_ptr()), stream)
-                            : layer.norm(px, ldx, pr, ldr, kind, pg, eps, M, K, ps, lds, po, stream);
+    int rc;
+    Py_BEGIN_ALLOW_THREADS;
+    rc = quantise ? layer.norm_quant(px, ldx, pr, ldr, kind, pg, eps, M, K, ps, lds, static_cast<int8_t*>(po), pa, stream)
+                  : layer.norm(px, ldx, pr, ldr, kind, pg, eps, M, K, ps, lds, po, stream);
+    Py_END_ALLOW_THREADS;
     if (rc != 0) return PyLong_FromLong(rc);
     PyObject* total = has ? given_or(args[4], made_sum) : none();
     return quantise ? tuple_of(total, given_or(args[5], made_out), given_or(args[6], made_s)) : tuple_of(total, given_or(args[5], made_out));
@@ -220,8 +224,14 @@ PyObject* gated(PyObject*, PyObject* const* args, Py_ssize_t n) {
       Py_RETURN_NONE;
     }
     if (!a_q || !s_a) Py_RETURN_NONE;
-    const int rc = layer.gated(gate->data_ptr(), row_stride(*gate), up->data_ptr(), row_stride(*up), (int)act, M, F,
-                               static_cast<int8_t*>(a_q->data_ptr()), static_cast<float*>(s_a->data_ptr()), stream);
+    const void *pg = gate->data_ptr(), *pu = up->data_ptr();
+    int8_t* pq = static_cast<int8_t*>(a_q->data_ptr());
+    float* ps = static_cast<float*>(s_a->data_ptr());
+    const int64_t ldg = row_stride(*gate), ldu = row_stride(*up);
+    int rc;
+    Py_BEGIN_ALLOW_THREADS;
+    rc = layer.gated(pg, ldg, pu, ldu, (int)act, M, F, pq, ps, stream);
+    Py_END_ALLOW_THREADS;
     if (rc != 0) return PyLong_FromLong(rc);
     return tuple_of(given_or(args[3], made_q), given_or(args[4], made_s));
   } catch (const std::exception&) {
@@ -262,6 +272,10 @@ const at::Tensor* heads_of(PyObject* o, int64_t heads, int64_t D) {
   return t && t->dim() == 3 && t->stride(2) == 1 && t->size(2) == D && (heads == 0 || t->size(1) == heads) ? t : nullptr;
 }
 
+// strides of [tokens, heads, D]; of an axis of one entry it may be anything, and is not used
+int64_t token_stride(const at::Tensor& t) { return t.size(0) > 1 ? t.stride(0) : 0; }
+int64_t head_stride(const at::Tensor& t) { return t.size(1) > 1 ? t.stride(1) : 0; }
+
 // append(cache, batch, k, v, stream) -> an error code (0 too), or None
 PyObject* append(PyObject*, PyObject* const* args, Py_ssize_t n) {
   if (n != 5 || !layer.append) Py_RETURN_NONE;
@@ -277,7 +291,13 @@ PyObject* append(PyObject*, PyObject* const* args, Py_ssize_t n) {
       Py_RETURN_NONE;
     }
     if (!k || !v || k->size(0) != v->size(0)) Py_RETURN_NONE;
-    return PyLong_FromLong(layer.append(&c, &b, k->data_ptr(), k->stride(0), k->stride(1), v->data_ptr(), v->stride(0), v->stride(1), k->size(0), stream));
+    const void *pk = k->data_ptr(), *pv = v->data_ptr();
+    const int64_t kt = token_stride(*k), kh = head_stride(*k), vt = token_stride(*v), vh = head_stride(*v), T = k->size(0);
+    int rc;
+    Py_BEGIN_ALLOW_THREADS;
+    rc = layer.append(&c, &b, pk, kt, kh, pv, vt, vh, T, stream);
+    Py_END_ALLOW_THREADS;
+    return PyLong_FromLong(rc);
   } catch (const std::exception&) {
     PyErr_Clear();
     Py_RETURN_NONE;
@@ -299,7 +319,13 @@ PyObject* read(PyObject*, PyObject* const* args, Py_ssize_t n) {
       Py_RETURN_NONE;
     }
     if (!k || !v || k->dim() != 3 || !is_shape(*k, {k->size(0), c.kv_heads, c.head_dim}) || !is_shape(*v, k->sizes())) Py_RETURN_NONE;
-    return PyLong_FromLong(layer.read(&c, &b, k->data_ptr(), v->data_ptr(), k->size(0), stream));
+    void *pk = k->data_ptr(), *pv = v->data_ptr();
+    const int64_t T = k->size(0);
+    int rc;
+    Py_BEGIN_ALLOW_THREADS;
+    rc = layer.read(&c, &b, pk, pv, T, stream);
+    Py_END_ALLOW_THREADS;
+    return PyLong_FromLong(rc);
   } catch (const std::exception&) {
     PyErr_Clear();
     Py_RETURN_NONE;
@@ -343,8 +369,15 @@ PyObject* attention(PyObject*, PyObject* const* args, Py_ssize_t n) {
       work = w->data_ptr();
       bytes = (size_t)w->numel();
     }
-    const int rc = layer.attention(&c, &b, q->data_ptr(), q->stride(0), q->stride(1), (int)Hq, T, scale, args[4] == Py_True, (int)window, out->data_ptr(),
-                                   lse ? static_cast<float*>(lse->data_ptr()) : nullptr, work, bytes, stream);
+    const void* pq = q->data_ptr();
+    void* po = out->data_ptr();
+    float* pl = lse ? static_cast<float*>(lse->data_ptr()) : nullptr;
+    const int64_t qt = token_stride(*q), qh = head_stride(*q);
+    const int causal = args[4] == Py_True;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS;
+    rc = layer.attention(&c, &b, pq, qt, qh, (int)Hq, T, scale, causal, (int)window, po, pl, work, bytes, stream);
+    Py_END_ALLOW_THREADS;
     if (rc != 0) return PyLong_FromLong(rc);
     Py_INCREF(args[7]);
     return tuple_of(given_or(args[6], made), args[7]);

@@ -172,7 +172,7 @@ def test_single_tokens(dim, page, heads, q_heads):
 
 
 @pytest.mark.parametrize("dim,page", [(64, 16), (128, 64), (256, 32)])
-@pytest.mark.parametrize("new", [2, 5, 16, 40])
+@pytest.mark.parametrize("new", [2, 5, 9, 16, 40])
 def test_a_few_tokens(dim, page, new):
     """Rows past 16, past 32; more new tokens than a sequence has in some."""
     lengths = [40, 64, 130, 300]
@@ -299,3 +299,71 @@ def test_device_tables_out_of_bounds_stay_inside():
                                            _dev(np.array([77, -1], np.int32)), 16, 79), kv[:, 0], kv[:, 1])
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(before, w.dev))
+
+
+def test_caches_whose_offsets_pass_32_bits():
+    """The same pages at the end of a cache of over 4 GiB of codes as at the start of a small one: append, read and attention give the same bits."""
+    H, D, P, B = 8, 128, 64, 2
+    pages = (1 << 32) // (H * D * P) + 40
+    rng = np.random.default_rng(22)
+    lengths = [300, 129]
+    order = rng.permutation(12)
+    i32 = lambda a: _dev(np.asarray(a, np.int32))  # noqa: E731
+    tables = [np.concatenate([order[:4], order[4:8]]).reshape(2, 4), pages - 1 - np.concatenate([order[:4], order[4:8]]).reshape(2, 4)]
+    k, v = (torch.randn(sum(lengths), H, D, device="cuda").half() for _ in range(2))
+    q1, q2 = torch.randn(2, 16, D, device="cuda").half(), torch.randn(sum(lengths), 16, D, device="cuda").half()
+    got = []
+    for table, n in zip(tables, (12, pages)):
+        cache = qqq.KV8Cache(torch.empty(n, H, P, D, dtype=torch.uint8, device="cuda"), torch.empty(n, H, device="cuda"), torch.empty(n, H, D, P, dtype=torch.uint8, device="cuda"),
+                             torch.empty(n, H, device="cuda"), *(torch.zeros(B, H, *s, dtype=torch.float16, device="cuda") for s in ((P, D), (D, P))))
+        assert n == 12 or cache.k_codes.numel() > 1 << 32
+        whole = qqq.KV8Batch(i32(table), i32(lengths), i32([0, 300, 429]), None, 300, 300)
+        qqq.qqq_kv8_append(cache, whole, k, v)
+        one, _ = qqq.qqq_attention_kv8(cache, whole._replace(cu=i32([0, 1, 2]), max_new=1), q1)
+        many, _ = qqq.qqq_attention_kv8(cache, whole, q2)
+        got.append((*qqq.qqq_kv8_read(cache, whole, tokens=429), one, many))
+        torch.cuda.synchronize()
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
+
+
+def test_marshalled_in_python(monkeypatch):
+    """Without the extension the calls are the same, refusals included."""
+    w = _filled(23, [100, 40], 2, 64, 32)
+    batch = w.batch([100, 40], [0, 3, 5])
+    q, kv = torch.randn(5, 4, 64, device="cuda").half(), torch.randn(5, 2, 64, device="cuda").half()
+    lse = [torch.empty(5, 4, device="cuda") for _ in range(2)]
+    x, r, gain = torch.randn(5, 256, device="cuda").half(), torch.randn(5, 256, device="cuda"), torch.ones(256, device="cuda").half()
+
+    def all_calls(i):
+        qqq.qqq_kv8_append(w.dev, batch, kv, kv)   # (no page is filled by it: it can be done again)
+        outs = [*qqq.qqq_attention_kv8(w.dev, batch, q, lse=lse[i]), *qqq.qqq_kv8_read(w.dev, batch, *(torch.empty(5, 2, 64, device="cuda").half() for _ in range(2)))]
+        outs += [*qqq.qqq_add_rmsnorm(x, gain, r), *qqq.qqq_add_rmsnorm_quant(x, gain, r), *qqq.qqq_add_rmsnorm_quant(x, gain)[1:], *qqq.qqq_gated_act_quant(x, r.half(), "gelu_tanh")]
+        torch.cuda.synchronize()
+        return [t.clone() for t in outs] + [t.clone() for t in w.dev]
+
+    def refusals():
+        with pytest.raises(ValueError):
+            qqq.qqq_add_rmsnorm(x, gain[:100])
+        with pytest.raises(ValueError):
+            qqq.qqq_gated_act_quant(x, r)
+        with pytest.raises(ValueError):
+            qqq.qqq_attention_kv8(w.dev, batch, q[..., :32])
+        with pytest.raises(ValueError):
+            qqq.qqq_kv8_append(w.dev, batch, kv, kv[:4])
+        with pytest.raises(ValueError):
+            qqq.qqq_kv8_append(w.dev._replace(k_scale=w.dev.k_scale[:1]), batch, kv, kv)
+        for call in (lambda: qqq.qqq_add_rmsnorm_quant(x, gain, r, eps=-1.0), lambda: qqq.qqq_attention_kv8(w.dev, batch, q[:, :3].contiguous()),
+                     lambda: qqq.qqq_attention_kv8(w.dev, batch._replace(max_len=1000), q), lambda: qqq.qqq_attention_kv8(w.dev, batch, q, window=4, causal=False),
+                     lambda: qqq.qqq_add_rmsnorm(torch.empty(5 * 256 + 1, device="cuda").half()[1:].view(5, 256), gain)):
+            with pytest.raises(qqq.QQQError) as e:
+                call()
+            assert e.value.code == 2
+    first = all_calls(0)
+    refusals()
+    for name in ("rmsnorm", "gated", "append", "read", "attention"):
+        monkeypatch.setattr(qqq, "_native_" + name, qqq._no_native)
+    second = all_calls(1)
+    refusals()
+    for a, b in zip(first, second):
+        assert torch.equal(a, b)
