@@ -123,7 +123,8 @@ int qqq_kv8_read(const qqq_kv8_cache* cache, const qqq_kv8_batch* batch, void* k
  * Query i of sequence b stands at position pos = kv_len[b] - n_b + i and sees key j iff
  *   0 <= j < kv_len[b],  j <= pos if causal,  j > pos - window if window > 0.
  *   out[t,h,:] = sum_j softmax_j(scale * <q[t,h], k_j>) v_j,   lse[t,h] = log sum_j exp(scale * <q[t,h], k_j>);
- *   a query that sees nothing gives out = 0, lse = -infinity.  q_heads / kv_heads query heads in a row share a key/value head.
+ *   a query that sees nothing gives out = 0, lse = -infinity, one with a NaN gives NaN in its row; rows that belong to no sequence are
+ *   left as they are.  q_heads / kv_heads query heads in a row share a key/value head.
  * Products of fp16 and of codes with fp32 accumulation; probabilities are rounded to fp16 (relative to the row's largest
  * contribution) for the second product, their sum is not.
  *   q_fp16: token t, head h at t * q_token_stride + h * q_head_stride (elements, % 8 == 0); out_fp16 [tokens, q_heads, head_dim] dense;

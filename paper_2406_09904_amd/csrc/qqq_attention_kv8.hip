@@ -375,10 +375,10 @@ __global__ __launch_bounds__(64 * W, D <= 128 ? 2 : 1) void attn_rows_kernel(con
     if (row < 0 || row >= c.tokens) continue;
     const int64_t to = row * p.q_heads + hq;
     if (p.splits == 1) {
-      const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+      const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;  // (0: it sees nothing; a NaN stays one)
       *reinterpret_cast<uint2*>(p.out + to * D + d) = make_uint2(as_u32(h2{(_Float16)(all[0] * inv), (_Float16)(all[1] * inv)}),
                                                                  as_u32(h2{(_Float16)(all[2] * inv), (_Float16)(all[3] * inv)}));
-      if (p.lse && d == 0) p.lse[to] = sum > 0.0f ? kLn2 * (__builtin_amdgcn_logf(sum) + (top - kShift)) : -__builtin_inff();
+      if (p.lse && d == 0) p.lse[to] = sum == 0.0f ? -__builtin_inff() : kLn2 * (__builtin_amdgcn_logf(sum) + (top - kShift));
     } else {
       const int64_t part = (int64_t)split * c.tokens * p.q_heads + to;
       *reinterpret_cast<f4*>(p.part_o + part * D + d) = all;
@@ -656,7 +656,7 @@ __global__ __launch_bounds__(kBlockThreads, D <= 128 ? 2 : 1) void attn_block_ke
   if (!there) return;
   const int64_t at = row * p.q_heads + hq;
   if (p.splits == 1) {
-    const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
@@ -665,7 +665,7 @@ __global__ __launch_bounds__(kBlockThreads, D <= 128 ? 2 : 1) void attn_block_ke
                                    as_u32(h2{(_Float16)(o[dt][x + 2] * inv), (_Float16)(o[dt][x + 3] * inv)}));
         *reinterpret_cast<uint2*>(p.out + at * D + 32 * dt + 2 * x + 4 * h) = v;
       }
-    if (p.lse && h == 0) p.lse[at] = l > 0.0f ? kLn2 * (__builtin_amdgcn_logf(l) + (m - kShift)) : -__builtin_inff();
+    if (p.lse && h == 0) p.lse[at] = l == 0.0f ? -__builtin_inff() : kLn2 * (__builtin_amdgcn_logf(l) + (m - kShift));
   } else {
     const int64_t part = (int64_t)split * c.tokens * p.q_heads + at;
 #pragma unroll
@@ -745,8 +745,8 @@ __global__ __launch_bounds__(64 * kJoinWaves) void attn_join_kernel(const AttnPa
     l += most[j].y;
     sum += sums[j][tid];
   }
-  p.out[at * D + tid] = __builtin_bit_cast(uint16_t, (_Float16)(l > 0.0f ? sum / l : 0.0f));
-  if (p.lse && tid == 0) p.lse[at] = l > 0.0f ? kLn2 * (__builtin_amdgcn_logf(l) + (m - kShift)) : -__builtin_inff();
+  p.out[at * D + tid] = __builtin_bit_cast(uint16_t, (_Float16)(l == 0.0f ? 0.0f : sum / l));
+  if (p.lse && tid == 0) p.lse[at] = l == 0.0f ? -__builtin_inff() : kLn2 * (__builtin_amdgcn_logf(l) + (m - kShift));
 }
 
 // The same of a few splits: one wave a row, nothing to be joined but what it holds.
@@ -786,12 +786,12 @@ __global__ __launch_bounds__(256) void attn_join_few_kernel(const AttnParams p, 
     l = __builtin_fmaf(ml[k].y, a, l);
     sum += o[k] * a;
   }
-  const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
   he out;
 #pragma unroll
   for (int j = 0; j < E; ++j) out[j] = (_Float16)(sum[j] * inv);
   *reinterpret_cast<he*>(p.out + at * D + lane * E) = out;
-  if (p.lse && lane == 0) p.lse[at] = l > 0.0f ? kLn2 * (__builtin_amdgcn_logf(l) + (m - kShift)) : -__builtin_inff();
+  if (p.lse && lane == 0) p.lse[at] = l == 0.0f ? -__builtin_inff() : kLn2 * (__builtin_amdgcn_logf(l) + (m - kShift));
 }
 
 // What a call launches, from sizes that the host knows.

@@ -26,7 +26,7 @@ __device__ __forceinline__ Kv8Seq kv8_sequence(const Kv8& c, int b) {
   Kv8Seq s;
   const int from = c.cu[b], to = c.cu[b + 1];
   s.row = from;
-  s.n = to > from ? min(to - from, c.max_new) : 0;
+  s.n = to > from ? (int)min((uint32_t)to - (uint32_t)from, (uint32_t)c.max_new) : 0;
   s.len = min(max(c.kv_len[b], 0), c.max_len);
   s.slot = c.slots ? c.slots[b] : b;
   return s;

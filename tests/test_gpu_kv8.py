@@ -234,6 +234,27 @@ def test_a_long_past(new, heads, q_heads):
     _check_attention(w, lengths, [new, new, min(new, 3), new], q_heads, window=2000)
 
 
+@pytest.mark.parametrize("new,length", [(1, 40), (1, 700), (1, 5000), (40, 100), (40, 2000), (300, 3500)])
+def test_a_query_that_is_not_a_number(new, length):
+    """It gives NaN in its own row, in what the sum's logarithm is as well, whole or joined from splits."""
+    w = _filled(25, [length], 1, 64, 64)
+    q = torch.randn(new, 4, 64, device="cuda").half()
+    batch = w.batch([length], [0, new])
+    want, want_lse = torch.empty_like(q), torch.empty(new, 4, device="cuda")
+    out, lse = torch.empty_like(q), torch.empty(new, 4, device="cuda")
+    qqq.qqq_attention_kv8(w.dev, batch, q, out=want, lse=want_lse)
+    q[new // 2, 2, 7] = float("nan")
+    qqq.qqq_attention_kv8(w.dev, batch, q, out=out, lse=lse)
+    torch.cuda.synchronize()
+    here = torch.zeros(new, 4, dtype=torch.bool, device="cuda")
+    here[new // 2, 2] = True
+    assert out[here].isnan().all() and lse[here].isnan().all()
+    assert torch.isfinite(out[~here]).all()
+    # (the many-rows kernel may take another reference for the rows beside it: as far from the formula's as before)
+    assert (out[~here].float() - want[~here].float()).abs().max() <= 2 ** -9 * want.float().abs().max()
+    assert (lse[~here] - want_lse[~here]).abs().max() <= 1e-4
+
+
 def test_same_result_twice_and_on_another_stream():
     w = _filled(19, [3000, 100], 2, 128, 64)
     q = torch.randn(2, 16, 128, device="cuda").half()
