@@ -123,8 +123,11 @@ __device__ __forceinline__ T of_group(const T* v, int group) {
 
 // ---- a few rows: up to 16 * NT of them a key/value head -----------------------------------------------------------------------------
 //
-// Bound by the cache's bytes: every code is read once, straight into registers, and used by up to 16 * NT rows; a wave takes every W-th
-// tile of its workgroup's chunk by itself, the waves' results are joined through LDS.
+// Bound by the cache's bytes: every code is read once, straight into registers, and used by up to 16 * NT rows; a wave takes every fourth
+// tile of its workgroup's chunk by itself, the waves' results are joined through LDS.  One token of a session of 131000, 8 heads of 128
+// read by 64: 49 us, 5.5 TB/s (a plain read stream reaches 6.2); of 48 sessions of 17 to 8000: 84 us, 4.7 TB/s, the rest being what their
+// lengths leave unbalanced.  A short past is latency: 500 tokens 7.4 us, of which 2.2 are an empty launch, and 0.3 a tile; with eight waves
+// instead of four, so that no wave has two tiles, 8.5, since a compute unit's four SIMDs issue the same instructions either way.
 // A tile of 64 tokens, 16 x 16 x 32 products.  Lane l = 16 g + n.  S^T: operand row r of 16-token subtile t is token
 // 16 (r / 4) + 4 t + r % 4, so that lane (g, n) gets the scores of row n with tokens 16 g + 4 t + i, i = 0..3: over t, the 16 tokens
 // from 16 g on.  They are its operand of the second product, whose other operand is 16 consecutive tokens of a channel: one 16-byte
@@ -134,8 +137,9 @@ __device__ __forceinline__ T of_group(const T* v, int group) {
 // What is in flight is what counts: the next tile's keys are requested as soon as this tile's are in the scores, its values as soon as
 // this tile's are in the result, and nothing that a request depends on is waited for there (loads return in order): page numbers
 // are fetched two tiles ahead, scales one.
-template <int D, int P, int NT, int W>
-__global__ __launch_bounds__(64 * W, D <= 128 ? 2 : 1) void attn_rows_kernel(const AttnParams p) {
+constexpr int W = 4, kRowsThreads = 64 * W;
+template <int D, int P, int NT>
+__global__ __launch_bounds__(kRowsThreads, D <= 128 ? 2 : 1) void attn_rows_kernel(const AttnParams p) {
   constexpr int J = D / 64, DT = D / 16, NP = Pages<P>::N;
   constexpr int kRowO = D + 4;  // (16 bytes over: the lanes' rows start in different banks)
   __shared__ float join_o[W * 16 * NT * kRowO];
@@ -207,13 +211,6 @@ __global__ __launch_bounds__(64 * W, D <= 128 ? 2 : 1) void attn_rows_kernel(con
 
   const int first = range.tile0 + from + wave, end = range.tile0 + from + tiles;
   Pages<P> pages = pages_of<P>(c, b, min(first, end - 1), closed);
-  __builtin_amdgcn_sched_barrier(0);
-  scales(pages);
-  request_k(pages);
-  __builtin_amdgcn_sched_barrier(0);
-  request_v(pages);
-  __builtin_amdgcn_sched_barrier(0);
-  pages = pages_of<P>(c, b, min(first + W, end - 1), closed);
 
   float m[NT], l[NT];
   f4 o[NT][DT];
@@ -297,22 +294,31 @@ __global__ __launch_bounds__(64 * W, D <= 128 ? 2 : 1) void attn_rows_kernel(con
   auto v_codes = [&](int dt, int half) { return half ? codes8_to_halves(vraw[dt].z, vraw[dt].w) : codes8_to_halves(vraw[dt].x, vraw[dt].y); };
 
   int tile = first;
-  for (; tile < end && tile != open_tile; tile += W) {
-    const Factors f = factors_of(of_group<P>(ks, g), of_group<P>(vs, g), p.scale_log2);
-    const Pages<P> after = pages_of<P>(c, b, min(tile + 2 * W, end - 1), closed);
-    step(tile, f, k_codes, v_codes,
-         [&]() {
-           __builtin_amdgcn_sched_barrier(0);
-           scales(pages);
-           request_k(pages);
-           __builtin_amdgcn_sched_barrier(0);
-         },
-         [&]() {
-           __builtin_amdgcn_sched_barrier(0);
-           request_v(pages);
-           __builtin_amdgcn_sched_barrier(0);
-         });
-    pages = after;
+  if (first < end && (P < kTile || first != open_tile)) {  // (a wave that has but the tail slot goes there at once: 500 tokens 9.0 us, 9.4 through codes that it does not use)
+    __builtin_amdgcn_sched_barrier(0);
+    scales(pages);
+    request_k(pages);
+    __builtin_amdgcn_sched_barrier(0);
+    request_v(pages);
+    __builtin_amdgcn_sched_barrier(0);
+    pages = pages_of<P>(c, b, min(first + W, end - 1), closed);
+    for (; tile < end && tile != open_tile; tile += W) {
+      const Factors f = factors_of(of_group<P>(ks, g), of_group<P>(vs, g), p.scale_log2);
+      const Pages<P> after = pages_of<P>(c, b, min(tile + 2 * W, end - 1), closed);
+      step(tile, f, k_codes, v_codes,
+           [&]() {
+             __builtin_amdgcn_sched_barrier(0);
+             scales(pages);
+             request_k(pages);
+             __builtin_amdgcn_sched_barrier(0);
+           },
+           [&]() {
+             __builtin_amdgcn_sched_barrier(0);
+             request_v(pages);
+             __builtin_amdgcn_sched_barrier(0);
+           });
+      pages = after;
+    }
   }
   if (tile < end) {
     // the tile that the sequence ends in, its last tokens in the tail slot; where pages are shorter than a tile, others of them may be codes
@@ -357,7 +363,7 @@ __global__ __launch_bounds__(64 * W, D <= 128 ? 2 : 1) void attn_rows_kernel(con
   }
   __syncthreads();
   const int rows = s.n * p.group;
-  for (int at = threadIdx.x; at < rows * (D / 4); at += 64 * W) {
+  for (int at = threadIdx.x; at < rows * (D / 4); at += kRowsThreads) {
     const int r = at / (D / 4), d = at % (D / 4) * 4, i = r / p.group, hq = head * p.group + r % p.group;
     const int64_t row = s.row + i;
     float top = -__builtin_inff(), sum = 0.0f;
@@ -389,9 +395,13 @@ __global__ __launch_bounds__(64 * W, D <= 128 ? 2 : 1) void attn_rows_kernel(con
 
 // ---- many rows ----------------------------------------------------------------------------------------------------------------------
 //
-// Bound by the matrix instructions and, as much, by the exponentials beside them: 128 rows of one key/value head (tokens times the
-// heads that share it) a workgroup, 32 a wave, over tiles of 64 tokens that the workgroup converts to fp16 in LDS once for its four
-// waves (two buffers, one barrier a tile, the next tile's codes on their way meanwhile).
+// 128 rows of one key/value head (tokens times the heads that share it) a workgroup, 32 a wave, over tiles of 64 tokens that the
+// workgroup converts to fp16 in LDS once for its four waves (two buffers, one barrier a tile, the next tile's codes on their way
+// meanwhile).  A prompt of 8000 tokens, 64 heads of 128 over 8: 1.07 to 1.13 ms, 930 to 980 TFLOP/s, where a large library product of
+// fp16 reaches 1411.  Bound by the power that the matrix instructions draw together with the exponentials beside them: the same
+// instructions on data of zeros take 0.88 ms.  Heads of 64 have twice the exponentials for a product: 660 TFLOP/s; heads of 256 fit but one wave
+// a SIMD: 620.  64 rows a wave (accumulators in the other register file, and copies to and fro) took 1.41 ms, values straight from memory
+// instead of through LDS 2.6 (spilled), the two products of neighbouring tiles interleaved 1.21.
 // 32 x 32 x 16 products, lane l = 32 h + n.  S^T: operand row r of a 32-token subtile is token 16 (r / 16) + 8 ((r / 4) % 2) + 4 ((r / 8) % 2)
 // + r % 4, so that lane (h, n) gets the scores of row n with tokens 16 s + 8 h + 0..7 in registers 8 s .. 8 s + 7: its operand of step s
 // of the second product.
@@ -685,7 +695,8 @@ __device__ __forceinline__ int parts_of(const AttnParams& p, const Kv8Seq& s, in
   return min(max(1, (range.tiles + p.chunk - 1) / p.chunk), p.splits);
 }
 
-// Joins the splits of every row, one workgroup a row: each wave sums every kJoinWaves-th split, always in the same order.
+// Joins the splits of every row, one workgroup a row: each wave sums every kJoinWaves-th split, always in the same order.  64 splits of
+// 64 rows: 6 us (55 by one wave that takes them one after another).
 constexpr int kJoinWaves = 8, kJoinMost = 1024;  // (splits: plan_of keeps below that)
 template <int D>
 __global__ __launch_bounds__(64 * kJoinWaves) void attn_join_kernel(const AttnParams p, int block_rows) {
@@ -749,7 +760,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void attn_join_kernel(const AttnPa
   if (p.lse && tid == 0) p.lse[at] = l == 0.0f ? -__builtin_inff() : kLn2 * (__builtin_amdgcn_logf(l) + (m - kShift));
 }
 
-// The same of a few splits: one wave a row, nothing to be joined but what it holds.
+// The same of few splits or many rows: one wave a row, eight splits at a time.
 constexpr int kJoinFew = 8;
 template <int D>
 __global__ __launch_bounds__(256) void attn_join_few_kernel(const AttnParams p, int block_rows) {
@@ -767,24 +778,29 @@ __global__ __launch_bounds__(256) void attn_join_few_kernel(const AttnParams p, 
   if (i >= s.n || row < 0 || row >= c.tokens) return;
   const int parts = parts_of(p, s, i, hq, block_rows);
   const int64_t at = row * p.q_heads + hq, step = c.tokens * p.q_heads;
-  fe o[kJoinFew];
-  float2 ml[kJoinFew];
-#pragma unroll
-  for (int k = 0; k < kJoinFew; ++k) {
-    const int64_t from = at + (k < parts ? k : 0) * step;
-    ml[k] = p.part_ml[from];
-    o[k] = *reinterpret_cast<const fe*>(p.part_o + from * D + lane * E);
-  }
   float m = -__builtin_inff(), l = 0.0f;
-#pragma unroll
-  for (int k = 0; k < kJoinFew; ++k) m = fmaxf(m, ml[k].x);
-  const float base = m == -__builtin_inff() ? 0.0f : m;
   fe sum = {};
+  for (int k0 = 0; k0 < parts; k0 += kJoinFew) {
+    fe o[kJoinFew];
+    float2 ml[kJoinFew];
 #pragma unroll
-  for (int k = 0; k < kJoinFew; ++k) {
-    const float a = k < parts ? __builtin_amdgcn_exp2f(ml[k].x - base) : 0.0f;
-    l = __builtin_fmaf(ml[k].y, a, l);
-    sum += o[k] * a;
+    for (int k = 0; k < kJoinFew; ++k) {
+      const int64_t from = at + (k0 + k < parts ? k0 + k : k0) * step;
+      ml[k] = p.part_ml[from];
+      o[k] = *reinterpret_cast<const fe*>(p.part_o + from * D + lane * E);
+    }
+    const float was = m;
+#pragma unroll
+    for (int k = 0; k < kJoinFew; ++k) m = fmaxf(m, ml[k].x);
+    const float base = m == -__builtin_inff() ? 0.0f : m, by = __builtin_amdgcn_exp2f(was - base);
+    l *= by;
+    sum *= by;
+#pragma unroll
+    for (int k = 0; k < kJoinFew; ++k) {
+      const float a = k0 + k < parts ? __builtin_amdgcn_exp2f(ml[k].x - base) : 0.0f;
+      l = __builtin_fmaf(ml[k].y, a, l);
+      sum += o[k] * a;
+    }
   }
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
   he out;
@@ -797,36 +813,44 @@ __global__ __launch_bounds__(256) void attn_join_few_kernel(const AttnParams p, 
 // What a call launches, from sizes that the host knows.
 struct Plan {
   int nt;          // 16-row tiles of the few-rows kernel, or 0: the many-rows kernel
-  int waves;       // of the few-rows kernel
   int row_blocks;
   int splits, chunk;
   int most;        // splits that no call of a smaller span exceeds
 };
 
-Plan plan_of(int heads, int group, int sequences, int max_new, int max_len, int window, int D) {
+Plan plan_of(int heads, int group, int sequences, int max_new, int max_len, int window) {
   Plan f;
   const int64_t rows = (int64_t)max_new * group;
+  // Up to 32 rows the codes go to the few-rows kernel (32 rows of 8 heads of 128, 8 sequences of 4000: 22.9 us against 33.2 in the many-rows one;
+  // 48 of them 98 against 147; 20 rows, 400 tokens 9.0 against 14.9).  More are not worth a third tile of registers.
   f.nt = rows <= 16 ? 1 : rows <= 32 ? 2 : 0;
   f.row_blocks = f.nt ? 1 : (int)((rows + kBlockRows - 1) / kBlockRows);
   const bool windowed = window > 0 && (int64_t)window + max_new < max_len;
   // (a window's keys may start inside a tile)
   const int64_t tiles = windowed ? ((int64_t)window + max_new + kTile - 1) / kTile + 1 : (max_len + kTile - 1) / kTile;
   const int64_t groups = (int64_t)sequences * heads * f.row_blocks;
-  // Few rows: with one sequence every workgroup has as many tiles, and one round of resident ones is best (131000 keys, 8 heads: 57.7 us with two
-  // a CU, 60.5 with four, 66 with eight); lengths of several differ, and shorter pieces level them (48 of 17 to 8000 keys: 105 us,
-  // 95, 91 with eight, 98 with twelve).  A wave should have two tiles at least.
-  const int64_t want = (int64_t)num_cus() * (f.nt && sequences > 1 ? 8 : 2), least = 8;
+  // How the keys are split.  A workgroup a CU, in pieces of four tiles at least (one a wave), and only into three or more, since a join costs
+  // as much as some seven tiles.  One sequence, 8 heads of 128 read by 64: 1000 tokens 8.5 us (whole 10.1, pieces of eight tiles or more 10.2),
+  // 8000 10.3 (10.9); 16 sequences of 1000 11.0 (pieces of eight 12.6); 128 new tokens behind 8000 36 (49 with two workgroups a CU).
+  // Pieces would be longer than 32 tiles: then more, so that the bytes in flight last (131000 tokens 49.0, a workgroup a CU 55.0) and,
+  // where several sequences' lengths differ, shorter ones level them (48 of 17 to 8000: 91 us with eight workgroups a CU, 95 with four, 105 with two,
+  // 98 with twelve).
+  const int64_t cus = num_cus(), want = cus * (f.nt && sequences > 1 ? 8 : 2);
   int64_t splits = groups >= want ? 1 : (want + groups - 1) / groups;
   if (splits > kJoinMost) splits = kJoinMost;
-  f.most = (int)(splits < (tiles + least - 1) / least ? splits : (tiles + least - 1) / least);
-  if (f.most < 1) f.most = 1;
-  int64_t chunk = (tiles + splits - 1) / splits;
-  if (chunk < least) chunk = least;
-  if (chunk >= tiles) chunk = tiles;
+  int64_t chunk = (tiles * groups + cus - 1) / cus;
+  if (chunk <= 32) {
+    if (chunk < 4) chunk = 4;
+    if (tiles <= 2 * chunk) chunk = tiles;
+  } else {
+    chunk = (tiles + splits - 1) / splits;
+    if (chunk < 8) chunk = 8;
+  }
   if (chunk < 1) chunk = 1;
+  // (neither rule makes more of a shorter span: a workgroup a CU is at most `splits` for a head, pieces are four tiles or more, two of them are one)
+  f.most = (int)(tiles <= 8 ? 1 : splits < (tiles + 3) / 4 ? splits : (tiles + 3) / 4);
   f.chunk = (int)chunk;
   f.splits = tiles > 0 ? (int)((tiles + chunk - 1) / chunk) : 1;
-  f.waves = f.nt == 1 && D <= 128 && f.splits == 1 && groups <= num_cus() ? 8 : 4;
   return f;
 }
 
@@ -836,14 +860,13 @@ int launch_attention_t(const AttnParams& p, const Plan& f, hipStream_t st) {
   const int64_t joins = (int64_t)p.sequences * p.c.max_new * p.q_heads;
   if (blocks > 0x7FFFFFFF || (f.splits > 1 && joins > 0x7FFFFFFF)) return set_error(QQQ_ERR_SHAPE, "attention_kv8: too many workgroups");
   if (f.nt && p.sequences > 65535) return set_error(QQQ_ERR_SHAPE, "attention_kv8: %d sequences", p.sequences);
-#define QQQ_ROWS(NT, W) hipLaunchKernelGGL((attn_rows_kernel<D, P, NT, W>), dim3(p.c.heads, f.splits, p.sequences), dim3(64 * W), 0, st, p)
+  const dim3 grid(p.c.heads, f.splits, p.sequences);
   if (f.nt == 0) hipLaunchKernelGGL((attn_block_kernel<D, P>), dim3((unsigned)blocks), dim3(kBlockThreads), 0, st, p);
-  else if (f.nt == 2) QQQ_ROWS(2, 4);
-  else if (f.waves == 4) QQQ_ROWS(1, 4);
-  else if constexpr (D <= 128) QQQ_ROWS(1, 8);
-#undef QQQ_ROWS
+  else if (f.nt == 1) hipLaunchKernelGGL((attn_rows_kernel<D, P, 1>), grid, dim3(kRowsThreads), 0, st, p);
+  else hipLaunchKernelGGL((attn_rows_kernel<D, P, 2>), grid, dim3(kRowsThreads), 0, st, p);
   const int block_rows = f.nt ? 0 : kBlockRows;
-  if (f.splits > kJoinFew) hipLaunchKernelGGL((attn_join_kernel<D>), dim3((unsigned)joins), dim3(64 * kJoinWaves), 0, st, p, block_rows);
+  // (many rows have waves enough: 4096 rows of 16 splits, 16000 keys, 55 us in all against 65 with a workgroup a row)
+  if (f.splits > kJoinFew && joins < 4 * (int64_t)num_cus()) hipLaunchKernelGGL((attn_join_kernel<D>), dim3((unsigned)joins), dim3(64 * kJoinWaves), 0, st, p, block_rows);
   else if (f.splits > 1) hipLaunchKernelGGL((attn_join_few_kernel<D>), dim3((unsigned)((joins + 3) / 4)), dim3(256), 0, st, p, block_rows);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return set_error(QQQ_ERR_HIP, "attention_kv8 launch: %s", hipGetErrorString(e));
@@ -863,12 +886,12 @@ size_t partial_bytes(int splits, int64_t tokens, int q_heads, int D) {
 }  // namespace
 
 size_t attention_kv8_bytes(int heads, int q_heads, int D, int sequences, int max_new, int max_len, int64_t tokens) {
-  return partial_bytes(plan_of(heads, q_heads / heads, sequences, max_new, max_len, 0, D).most, tokens, q_heads, D);
+  return partial_bytes(plan_of(heads, q_heads / heads, sequences, max_new, max_len, 0).most, tokens, q_heads, D);
 }
 
 int launch_attention_kv8(const Kv8& c, int D, int P, int sequences, const void* q, int64_t q_token, int64_t q_head, int q_heads, float scale,
                          int causal, int window, void* out, float* lse, void* workspace, size_t workspace_bytes, hipStream_t st) {
-  const Plan f = plan_of(c.heads, q_heads / c.heads, sequences, c.max_new, c.max_len, window, D);
+  const Plan f = plan_of(c.heads, q_heads / c.heads, sequences, c.max_new, c.max_len, window);
   if (partial_bytes(f.splits, c.tokens, q_heads, D) > workspace_bytes)
     return set_error(QQQ_ERR_WORKSPACE, "attention_kv8: workspace of %zu bytes, %zu needed", workspace_bytes, partial_bytes(f.splits, c.tokens, q_heads, D));
   AttnParams p;

@@ -234,6 +234,16 @@ def test_a_long_past(new, heads, q_heads):
     _check_attention(w, lengths, [new, new, min(new, 3), new], q_heads, window=2000)
 
 
+@pytest.mark.parametrize("dim,new,q_heads", [(64, 130, 8), (128, 33, 32), (256, 1030, 1)])
+def test_many_rows_of_many_splits(dim, new, q_heads):
+    """More than eight splits of 1024 rows and more: a wave joins a row's, eight at a time."""
+    w = _filled(24, [2700], 1, dim, 64)
+    _check_attention(w, [2700], [new], q_heads)
+    splits = int(qqq.last_route().split(" x")[1].split()[0])
+    assert splits > 8 and "join" in qqq.last_route()
+    _check_attention(w, [2700], [new], q_heads, window=2300)
+
+
 @pytest.mark.parametrize("new,length", [(1, 40), (1, 700), (1, 5000), (40, 100), (40, 2000), (300, 3500)])
 def test_a_query_that_is_not_a_number(new, length):
     """It gives NaN in its own row, in what the sum's logarithm is as well, whole or joined from splits."""
