@@ -10,6 +10,7 @@
 // S is computed transposed (keys x rows), and so is O (channels x rows): a lane of S^T's accumulator holds keys of ONE row, which is
 // how the second product wants its operand, so that the weights go from the one to the other in registers.  What makes that fit is
 // which token each row of the first product's operand is taken from (token_of_row below).
+#include <algorithm>
 #include <type_traits>
 
 #include "qqq_kv8.h"
@@ -23,6 +24,7 @@ typedef float f4 __attribute__((ext_vector_type(4)));
 typedef float f16v __attribute__((ext_vector_type(16)));
 
 constexpr int kTile = 64;         // tokens of a step over the keys
+constexpr int kJoinMost = 1024;   // parts of a row
 constexpr float kShift = 6.0f;    // weights are up to 2^6: fp16 keeps all their bits down to 2^-20 of the largest
 constexpr float kMost = 0x1p14f;  // sums of weights up to which the many-rows kernel leaves its reference alone (fp16 ends at 2^16)
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
@@ -33,11 +35,13 @@ struct AttnParams {
   int64_t q_token, q_head;
   uint16_t* out;
   float* lse;
-  float* part_o;     // [splits][tokens][q_heads][D], where the keys are split
-  float2* part_ml;   // [splits][tokens][q_heads]
+  // where the keys are split; many rows: [splits][tokens][q_heads], few: [2 * splits][rows of a key/value head][heads] (see Share)
+  float* part_o;     // [..][D]
+  float2* part_ml;
+  int2* part_of;     // few rows: a sequence's first workgroup, twice, + 1 if its second place; how many share it  [sequences]
   float scale_log2;  // scale * log2(e)
   int group, q_heads, causal, window;
-  int splits, chunk; // workgroups that share a row's keys, tiles of each
+  int splits, chunk; // many rows: workgroups that share a row's keys, tiles of each; few rows: workgroups of a head, where parts are written; tiles of each
   int row_blocks;    // of the largest sequence
   int sequences;
 };
@@ -46,6 +50,17 @@ __device__ __forceinline__ h8 as_h8(uint4 v) { return __builtin_bit_cast(h8, v);
 __device__ __forceinline__ h8 codes8_to_halves(uint32_t a, uint32_t b) {
   const uint2 lo = codes4_to_halves(a), hi = codes4_to_halves(b);
   return as_h8(make_uint4(lo.x, lo.y, hi.x, hi.y));
+}
+
+// 16 codes; ONCE: past the caches, which need not keep what no other workgroup reads.
+template <bool ONCE>
+__device__ __forceinline__ uint4 load_codes(const uint8_t* from) {
+  typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+  const u4* at = reinterpret_cast<const u4*>(from);
+  u4 v;
+  if constexpr (ONCE) v = __builtin_nontemporal_load(at);
+  else v = *at;
+  return make_uint4(v.x, v.y, v.z, v.w);
 }
 
 // maximum / sum over the lanes l, l ^ 16, l ^ 32, l ^ 48 and over l, l ^ 32
@@ -121,12 +136,82 @@ __device__ __forceinline__ T of_group(const T* v, int group) {
   }
 }
 
+// What a workgroup of the few-rows kernel has of a head's keys, all sequences' tiles in a row and cut into equal shares: so every workgroup
+// ends at the same time whatever the lengths are, which the host does not know.  A sequence counts one tile at least, for what is written of it.  A
+// workgroup that has all of a sequence writes its result; of one that it shares it writes a part, into its first place where its share starts with
+// it, otherwise (the share ends with it) into its second.
+struct Share {
+  int b, from, tiles;  // first sequence, its tiles that others have, tiles in all
+  int start;           // among all
+  int each, longer;    // shares of each tiles, the first `longer` of them of one more
+};
+__device__ __forceinline__ int weight_of(const AttnParams& p, int b) {
+  const Kv8Seq s = kv8_sequence(p.c, b);
+  return s.n > 0 ? max(1, range_of(p, s, 0, s.n - 1).tiles) : 0;
+}
+__device__ __forceinline__ int share_at(const Share& s, int x) {  // the workgroup that has tile x
+  const int of_longer = s.longer * (s.each + 1);
+  return x < of_longer ? x / (s.each + 1) : s.longer + (x - of_longer) / s.each;
+}
+template <int T>
+__device__ __forceinline__ Share share_of(const AttnParams& p, int w) {
+  __shared__ int sums[T / 64], found[2];
+  Share s;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  int weight = 0, upto = 0, total = 0;
+  auto scan = [&](int base) {  // weights of T sequences, their running sum in each wave, each wave's sum
+    weight = base + tid < p.sequences ? weight_of(p, base + tid) : 0;
+    upto = weight;
+#pragma unroll
+    for (int x = 1; x < 64; x *= 2) {
+      const int v = __shfl_up(upto, x);
+      upto += lane >= x ? v : 0;
+    }
+    __syncthreads();
+    if (lane == 63) sums[wave] = upto;
+    __syncthreads();
+  };
+  auto before = [&](int waves) {
+    int sum = 0;
+    for (int x = 0; x < waves; ++x) sum += sums[x];
+    return sum;
+  };
+  for (int base = 0; base < p.sequences; base += T) {
+    scan(base);
+    total += before(T / 64);
+  }
+  total = __builtin_amdgcn_readfirstlane(total);
+  const int shares = max(1, min(p.splits, max(total / 4, p.sequences)));
+  s.each = total / shares;
+  s.longer = total - s.each * shares;
+  s.start = w * s.each + min(w, s.longer);
+  s.tiles = w < shares ? s.each + (w < s.longer ? 1 : 0) : 0;
+  s.b = 0;
+  s.from = s.start;
+  if (s.tiles > 0) {
+    int at = 0;
+    for (int base = 0; base < p.sequences; base += T) {
+      if (p.sequences > T) scan(base);
+      const int first = at + before(wave) + upto - weight;
+      if (first <= s.start && s.start < first + weight) {
+        found[0] = base + tid;
+        found[1] = s.start - first;
+      }
+      at += before(T / 64);
+    }
+    __syncthreads();
+    s.b = __builtin_amdgcn_readfirstlane(found[0]);
+    s.from = __builtin_amdgcn_readfirstlane(found[1]);
+  }
+  return s;
+}
+
 // ---- a few rows: up to 16 * NT of them a key/value head -----------------------------------------------------------------------------
 //
 // Bound by the cache's bytes: every code is read once, straight into registers, and used by up to 16 * NT rows; a wave takes every fourth
 // tile of its workgroup's chunk by itself, the waves' results are joined through LDS.  One token of a session of 131000, 8 heads of 128
-// read by 64: 49 us, 5.5 TB/s (a plain read stream reaches 6.2); of 48 sessions of 17 to 8000: 84 us, 4.7 TB/s, the rest being what their
-// lengths leave unbalanced.  A short past is latency: 500 tokens 7.4 us, of which 2.2 are an empty launch, and 0.3 a tile; with eight waves
+// read by 64: 47 us, 5.7 TB/s (a plain read stream reaches 6.2); of 48 sessions of 17 to 8000: 75 us, 5.3 TB/s, the rest being where a share
+// goes from one sequence to the next.  A short past is latency: 500 tokens 7.4 us, of which 2.2 are an empty launch, and 0.3 a tile; with eight waves
 // instead of four, so that no wave has two tiles, 8.5, since a compute unit's four SIMDs issue the same instructions either way.
 // A tile of 64 tokens, 16 x 16 x 32 products.  Lane l = 16 g + n.  S^T: operand row r of 16-token subtile t is token
 // 16 (r / 4) + 4 t + r % 4, so that lane (g, n) gets the scores of row n with tokens 16 g + 4 t + i, i = 0..3: over t, the 16 tokens
@@ -138,258 +223,292 @@ __device__ __forceinline__ T of_group(const T* v, int group) {
 // this tile's are in the result, and nothing that a request depends on is waited for there (loads return in order): page numbers
 // are fetched two tiles ahead, scales one.
 constexpr int W = 4, kRowsThreads = 64 * W;
-template <int D, int P, int NT>
+template <int D, int P, int NT, bool SHARED, bool ONCE>
 __global__ __launch_bounds__(kRowsThreads, D <= 128 ? 2 : 1) void attn_rows_kernel(const AttnParams p) {
   constexpr int J = D / 64, DT = D / 16, NP = Pages<P>::N;
   constexpr int kRowO = D + 4;  // (16 bytes over: the lanes' rows start in different banks)
   __shared__ float join_o[W * 16 * NT * kRowO];
   __shared__ float2 join_ml[W][16 * NT];
   const Kv8& c = p.c;
-  const int head = blockIdx.x, b = blockIdx.z;
-  // Workgroups go to the eight dies in turn, and of short sequences only the first splits have work: turned by the sequence, so that no die gets
-  // all of a split (48 sequences of 17 to 8000 tokens in 8 splits: 124 us without)
-  const int split = (int)((blockIdx.y + b) % gridDim.y);
-  const Kv8Seq s = kv8_sequence(c, b);
-  if (s.n == 0) return;
-  const Range range = range_of(p, s, 0, s.n - 1);
-  const int from = split * p.chunk, tiles = min(p.chunk, range.tiles - from);
-  if (tiles <= 0 && split > 0) return;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
-  const int closed = s.len / P, slot = kv8_slot(c, s.slot);
-  const int open_tile = s.len > closed * P ? closed * P / kTile : -1;  // the one with tokens in the tail slot
-
-  const int gk = n >> 2;  // 16-token group that this lane's row of the first operand is taken from
-  uint4 kraw[4][J], vraw[DT];
-  const uint32_t k_lane = (((16 * gk) & (P - 1)) + (n & 3)) * D + 16 * g, v_lane = n * P + ((16 * g) & (P - 1));
-  auto offsets = [&](const Pages<P>& of, int64_t* at) {
-#pragma unroll
-    for (int i = 0; i < NP; ++i) at[i] = kv8_block(c, of.id[i], head) * (P * D);
-  };
-  auto request_k = [&](const Pages<P>& of) {
-    int64_t offset[NP];
-    offsets(of, offset);
-    const uint8_t* at = c.k_codes + of_group<P>(offset, gk) + k_lane;
-#pragma unroll
-    for (int t = 0; t < 4; ++t)
-#pragma unroll
-      for (int j = 0; j < J; ++j) kraw[t][j] = *reinterpret_cast<const uint4*>(at + 4 * t * D + 64 * j);
-  };
-  auto request_v = [&](const Pages<P>& of) {
-    int64_t offset[NP];
-    offsets(of, offset);
-    const uint8_t* at = c.v_codes + of_group<P>(offset, g) + v_lane;
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt) vraw[dt] = *reinterpret_cast<const uint4*>(at + dt * 16 * P);
-  };
-  float ks[NP], vs[NP];
-  auto scales = [&](const Pages<P>& of) {
-#pragma unroll
-    for (int i = 0; i < NP; ++i) {
-      const int64_t at = kv8_block(c, of.id[i], head);
-      ks[i] = c.k_scale[at];
-      vs[i] = c.v_scale[at];
+  const int head = blockIdx.x;
+  Share share = {};
+  share.b = blockIdx.z;
+  if constexpr (SHARED) {
+    share = share_of<kRowsThreads>(p, blockIdx.y);
+    if (share.tiles == 0) return;
+  }
+  int left = share.tiles;
+  for (int b = share.b; b < p.sequences; ++b) {
+    const Kv8Seq s = kv8_sequence(c, b);
+    if (s.n == 0) {
+      if constexpr (SHARED) continue;
+      return;
     }
-  };
+    const Range range = range_of(p, s, 0, s.n - 1);
+    const int weight = max(1, range.tiles), from = SHARED ? (b == share.b ? share.from : 0) : (int)blockIdx.y * p.chunk;
+    const int take = min(SHARED ? left : p.chunk, weight - from);
+    if (take <= 0) return;
+    const int tiles = min(take, range.tiles - from);  // (0 of a sequence that has none)
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
+    const int closed = s.len / P, slot = kv8_slot(c, s.slot);
+    const int open_tile = s.len > closed * P ? closed * P / kTile : -1;  // the one with tokens in the tail slot
 
-  // queries, and each row's keys [lo, hi).  (Requested first: what is waited for in the loop must not lie behind the codes in flight.)
-  h8 q[NT][J * 2];
-  int lo[NT], hi[NT];
+    const int gk = n >> 2;  // 16-token group that this lane's row of the first operand is taken from
+    uint4 kraw[4][J], vraw[DT];
+    const uint32_t k_lane = (((16 * gk) & (P - 1)) + (n & 3)) * D + 16 * g, v_lane = n * P + ((16 * g) & (P - 1));
+    auto offsets = [&](const Pages<P>& of, int64_t* at) {
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    const int r = nt * 16 + n, i = r / p.group, hq = head * p.group + r % p.group;
-    const int64_t row = s.row + i;
-    const bool there = i < s.n && row >= 0 && row < c.tokens;
-    const int pos = s.len - s.n + i;
-    hi[nt] = !there ? 0 : p.causal ? min(s.len, pos + 1) : s.len;
-    lo[nt] = p.window ? pos - p.window + 1 : 0;
-    const uint4* from_q = reinterpret_cast<const uint4*>(p.q + (there ? row * p.q_token + hq * p.q_head : 0));
+      for (int i = 0; i < NP; ++i) at[i] = kv8_block(c, of.id[i], head) * (P * D);
+    };
+    auto request_k = [&](const Pages<P>& of) {
+      int64_t offset[NP];
+      offsets(of, offset);
+      const uint8_t* at = c.k_codes + of_group<P>(offset, gk) + k_lane;
 #pragma unroll
-    for (int j = 0; j < J; ++j)
+      for (int t = 0; t < 4; ++t)
 #pragma unroll
-      for (int h = 0; h < 2; ++h) q[nt][2 * j + h] = as_h8(from_q[8 * j + 2 * g + h]);  // (a row that is not there: another's, never written)
-  }
-
-  const int first = range.tile0 + from + wave, end = range.tile0 + from + tiles;
-  Pages<P> pages = pages_of<P>(c, b, min(first, end - 1), closed);
-
-  float m[NT], l[NT];
-  f4 o[NT][DT];
+        for (int j = 0; j < J; ++j) kraw[t][j] = load_codes<ONCE>(at + 4 * t * D + 64 * j);
+    };
+    auto request_v = [&](const Pages<P>& of) {
+      int64_t offset[NP];
+      offsets(of, offset);
+      const uint8_t* at = c.v_codes + of_group<P>(offset, g) + v_lane;
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    m[nt] = -__builtin_inff();
-    l[nt] = 0.0f;
+      for (int dt = 0; dt < DT; ++dt) vraw[dt] = load_codes<ONCE>(at + dt * 16 * P);
+    };
+    float ks[NP], vs[NP];
+    auto scales = [&](const Pages<P>& of) {
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt) o[nt][dt] = f4{0, 0, 0, 0};
-  }
-
-  // one tile: k_of(t, j, half) and v_of(dt, half) give the codes' operands; next() requests after the scores and after the result
-  auto step = [&](int tile, const Factors& f, auto k_of, auto v_of, auto next_k, auto next_v) {
-    f4 st[NT][4];
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) st[nt][t] = f4{0, 0, 0, 0};
-#pragma unroll
-      for (int j = 0; j < J; ++j) {
-        const h8 k0 = k_of(t, j, 0), k1 = k_of(t, j, 1);
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          st[nt][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k0, q[nt][2 * j], st[nt][t], 0, 0, 0);
-          st[nt][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, q[nt][2 * j + 1], st[nt][t], 0, 0, 0);
-        }
+      for (int i = 0; i < NP; ++i) {
+        const int64_t at = kv8_block(c, of.id[i], head);
+        ks[i] = c.k_scale[at];
+        vs[i] = c.v_scale[at];
       }
-    }
-    next_k();
-    const bool edge = (tile + 1) * kTile > range.whole_hi || tile * kTile < range.whole_lo;
-    h8 w[NT][2];
+    };
+
+    // queries, and each row's keys [lo, hi).  (Requested first: what is waited for in the loop must not lie behind the codes in flight.)
+    h8 q[NT][J * 2];
+    int lo[NT], hi[NT];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      if (edge) {
+      const int r = nt * 16 + n, i = r / p.group, hq = head * p.group + r % p.group;
+      const int64_t row = s.row + i;
+      const bool there = i < s.n && row >= 0 && row < c.tokens;
+      const int pos = s.len - s.n + i;
+      hi[nt] = !there ? 0 : p.causal ? min(s.len, pos + 1) : s.len;
+      lo[nt] = p.window ? pos - p.window + 1 : 0;
+      const uint4* from_q = reinterpret_cast<const uint4*>(p.q + (there ? row * p.q_token + hq * p.q_head : 0));
+#pragma unroll
+      for (int j = 0; j < J; ++j)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) q[nt][2 * j + h] = as_h8(from_q[8 * j + 2 * g + h]);  // (a row that is not there: another's, never written)
+    }
+
+    const int first = range.tile0 + from + wave, end = range.tile0 + from + tiles;
+    Pages<P> pages = pages_of<P>(c, b, min(first, end - 1), closed);
+
+    float m[NT], l[NT];
+    f4 o[NT][DT];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      m[nt] = -__builtin_inff();
+      l[nt] = 0.0f;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) o[nt][dt] = f4{0, 0, 0, 0};
+    }
+
+    // one tile: k_of(t, j, half) and v_of(dt, half) give the codes' operands; next() requests after the scores and after the result
+    auto step = [&](int tile, const Factors& f, auto k_of, auto v_of, auto next_k, auto next_v) {
+      f4 st[NT][4];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) st[nt][t] = f4{0, 0, 0, 0};
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+          const h8 k0 = k_of(t, j, 0), k1 = k_of(t, j, 1);
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            st[nt][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k0, q[nt][2 * j], st[nt][t], 0, 0, 0);
+            st[nt][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, q[nt][2 * j + 1], st[nt][t], 0, 0, 0);
+          }
+        }
+      }
+      next_k();
+      const bool edge = (tile + 1) * kTile > range.whole_hi || tile * kTile < range.whole_lo;
+      h8 w[NT][2];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        if (edge) {
+#pragma unroll
+          for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int key = tile * kTile + 16 * g + 4 * t + i;
+              if (!(key >= lo[nt] && key < hi[nt])) st[nt][t][i] = -__builtin_inff();
+            }
+        }
+        float top = -__builtin_inff();
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) top = fmaxf(top, st[nt][t][i]);
+        top = __builtin_fmaf(top, f.c, f.lv);
+        top = across16(across32(top, fmax2), fmax2);
+        const float was = m[nt], now = fmaxf(was, top);
+        const float base = now == -__builtin_inff() ? 0.0f : now;   // a row that has seen nothing yet: weights 2^-inf = 0
+        const float alpha = __builtin_amdgcn_exp2f(was - base), add = f.lv - base + kShift;
+        m[nt] = now;
+        float sum = 0.0f;
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const int key = tile * kTile + 16 * g + 4 * t + i;
-            if (!(key >= lo[nt] && key < hi[nt])) st[nt][t][i] = -__builtin_inff();
+            const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(st[nt][t][i], f.c, add));
+            sum += e;
+            w[nt][t >> 1][(t & 1) * 4 + i] = (_Float16)e;
           }
-      }
-      float top = -__builtin_inff();
+        l[nt] = __builtin_fmaf(l[nt], alpha, sum * f.rv);
+        if (__any(alpha != 1.0f)) {
 #pragma unroll
-      for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) top = fmaxf(top, st[nt][t][i]);
-      top = __builtin_fmaf(top, f.c, f.lv);
-      top = across16(across32(top, fmax2), fmax2);
-      const float was = m[nt], now = fmaxf(was, top);
-      const float base = now == -__builtin_inff() ? 0.0f : now;   // a row that has seen nothing yet: weights 2^-inf = 0
-      const float alpha = __builtin_amdgcn_exp2f(was - base), add = f.lv - base + kShift;
-      m[nt] = now;
-      float sum = 0.0f;
-#pragma unroll
-      for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(st[nt][t][i], f.c, add));
-          sum += e;
-          w[nt][t >> 1][(t & 1) * 4 + i] = (_Float16)e;
+          for (int dt = 0; dt < DT; ++dt) o[nt][dt] *= alpha;
         }
-      l[nt] = __builtin_fmaf(l[nt], alpha, sum * f.rv);
-      if (__any(alpha != 1.0f)) {
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt) o[nt][dt] *= alpha;
       }
-    }
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt) {
-      const h8 v0 = v_of(dt, 0), v1 = v_of(dt, 1);
+      for (int dt = 0; dt < DT; ++dt) {
+        const h8 v0 = v_of(dt, 0), v1 = v_of(dt, 1);
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        o[nt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, w[nt][0], o[nt][dt], 0, 0, 0);
-        o[nt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, w[nt][1], o[nt][dt], 0, 0, 0);
+        for (int nt = 0; nt < NT; ++nt) {
+          o[nt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, w[nt][0], o[nt][dt], 0, 0, 0);
+          o[nt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, w[nt][1], o[nt][dt], 0, 0, 0);
+        }
       }
-    }
-    next_v();
-  };
-  auto k_codes = [&](int t, int j, int half) { return half ? codes8_to_halves(kraw[t][j].z, kraw[t][j].w) : codes8_to_halves(kraw[t][j].x, kraw[t][j].y); };
-  auto v_codes = [&](int dt, int half) { return half ? codes8_to_halves(vraw[dt].z, vraw[dt].w) : codes8_to_halves(vraw[dt].x, vraw[dt].y); };
+      next_v();
+    };
+    auto k_codes = [&](int t, int j, int half) { return half ? codes8_to_halves(kraw[t][j].z, kraw[t][j].w) : codes8_to_halves(kraw[t][j].x, kraw[t][j].y); };
+    auto v_codes = [&](int dt, int half) { return half ? codes8_to_halves(vraw[dt].z, vraw[dt].w) : codes8_to_halves(vraw[dt].x, vraw[dt].y); };
 
-  int tile = first;
-  if (first < end && (P < kTile || first != open_tile)) {  // (a wave that has but the tail slot goes there at once: 500 tokens 9.0 us, 9.4 through codes that it does not use)
-    __builtin_amdgcn_sched_barrier(0);
-    scales(pages);
-    request_k(pages);
-    __builtin_amdgcn_sched_barrier(0);
-    request_v(pages);
-    __builtin_amdgcn_sched_barrier(0);
-    pages = pages_of<P>(c, b, min(first + W, end - 1), closed);
-    for (; tile < end && tile != open_tile; tile += W) {
-      const Factors f = factors_of(of_group<P>(ks, g), of_group<P>(vs, g), p.scale_log2);
-      const Pages<P> after = pages_of<P>(c, b, min(tile + 2 * W, end - 1), closed);
-      step(tile, f, k_codes, v_codes,
-           [&]() {
-             __builtin_amdgcn_sched_barrier(0);
-             scales(pages);
-             request_k(pages);
-             __builtin_amdgcn_sched_barrier(0);
+    int tile = first;
+    if (first < end && (P < kTile || first != open_tile)) {  // (a wave that has but the tail slot goes there at once: 500 tokens 9.0 us, 9.4 through codes that it does not use)
+      __builtin_amdgcn_sched_barrier(0);
+      scales(pages);
+      request_k(pages);
+      __builtin_amdgcn_sched_barrier(0);
+      request_v(pages);
+      __builtin_amdgcn_sched_barrier(0);
+      pages = pages_of<P>(c, b, min(first + W, end - 1), closed);
+      for (; tile < end && tile != open_tile; tile += W) {
+        const Factors f = factors_of(of_group<P>(ks, g), of_group<P>(vs, g), p.scale_log2);
+        const Pages<P> after = pages_of<P>(c, b, min(tile + 2 * W, end - 1), closed);
+        step(tile, f, k_codes, v_codes,
+             [&]() {
+               __builtin_amdgcn_sched_barrier(0);
+               scales(pages);
+               request_k(pages);
+               __builtin_amdgcn_sched_barrier(0);
+             },
+             [&]() {
+               __builtin_amdgcn_sched_barrier(0);
+               request_v(pages);
+               __builtin_amdgcn_sched_barrier(0);
+             });
+        pages = after;
+      }
+    }
+    if (tile < end) {
+      // the tile that the sequence ends in, its last tokens in the tail slot; where pages are shorter than a tile, others of them may be codes
+      const bool k_open = (tile * kTile + 16 * gk) / P >= closed, v_open = (tile * kTile + 16 * g) / P >= closed;
+      const int64_t tail = ((int64_t)slot * c.heads + head) * (P * D);
+      h8 kt[4][J][2], vt[DT][2];
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int j = 0; j < J; ++j)
+#pragma unroll
+          for (int half = 0; half < 2; ++half)
+            kt[t][j][half] = as_h8(*reinterpret_cast<const uint4*>(c.k_tail + tail + k_lane + 4 * t * D + 64 * j + 8 * half));
+      auto request_vt = [&]() {
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+          for (int half = 0; half < 2; ++half) vt[dt][half] = as_h8(*reinterpret_cast<const uint4*>(c.v_tail + tail + v_lane + dt * 16 * P + 8 * half));
+      };
+      // (pages shorter than a tile, shared: beside the codes there are not registers enough for both; 48 sequences in pages of 32 78 us, 98 spilled;
+      // where there are, a second wait is 1 us of a short call)
+      constexpr bool kValuesLater = SHARED && P < kTile && D >= 128;
+      if constexpr (!kValuesLater) request_vt();
+      const int left = s.len - (tile * kTile + 16 * g);  // tokens of the lane's group that exist: what lies past them may be anything
+      const Factors f = factors_of(v_open ? 1.0f : of_group<P>(ks, g), v_open ? 1.0f : of_group<P>(vs, g), p.scale_log2);
+      uint4 there[2];
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        auto pair = [&](int e) { return (8 * half + e < left ? 0xFFFFu : 0u) | (8 * half + e + 1 < left ? 0xFFFF0000u : 0u); };
+        there[half] = make_uint4(pair(0), pair(2), pair(4), pair(6));
+      }
+      auto select = [](bool tail, h8 a, h8 b) { return P == kTile || tail ? a : b; };
+      step(tile, f, [&](int t, int j, int half) { return select(k_open, kt[t][j][half], k_codes(t, j, half)); },
+           [&](int dt, int half) {
+             const uint4 v = __builtin_bit_cast(uint4, vt[dt][half]);
+             return select(v_open, as_h8(make_uint4(v.x & there[half].x, v.y & there[half].y, v.z & there[half].z, v.w & there[half].w)), v_codes(dt, half));
            },
            [&]() {
-             __builtin_amdgcn_sched_barrier(0);
-             request_v(pages);
-             __builtin_amdgcn_sched_barrier(0);
-           });
-      pages = after;
+             if constexpr (kValuesLater) {
+               __builtin_amdgcn_sched_barrier(0);
+               request_vt();
+               __builtin_amdgcn_sched_barrier(0);
+             }
+           },
+           []() {});
     }
-  }
-  if (tile < end) {
-    // the tile that the sequence ends in, its last tokens in the tail slot; where pages are shorter than a tile, others of them may be codes
-    const bool k_open = (tile * kTile + 16 * gk) / P >= closed, v_open = (tile * kTile + 16 * g) / P >= closed;
-    const int64_t tail = ((int64_t)slot * c.heads + head) * (P * D);
-    h8 kt[4][J][2], vt[DT][2];
-#pragma unroll
-    for (int t = 0; t < 4; ++t)
-#pragma unroll
-      for (int j = 0; j < J; ++j)
-#pragma unroll
-        for (int half = 0; half < 2; ++half)
-          kt[t][j][half] = as_h8(*reinterpret_cast<const uint4*>(c.k_tail + tail + k_lane + 4 * t * D + 64 * j + 8 * half));
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-      for (int half = 0; half < 2; ++half) vt[dt][half] = as_h8(*reinterpret_cast<const uint4*>(c.v_tail + tail + v_lane + dt * 16 * P + 8 * half));
-    const int left = s.len - (tile * kTile + 16 * g);  // tokens of the lane's group that exist: what lies past them may be anything
-    const Factors f = factors_of(v_open ? 1.0f : of_group<P>(ks, g), v_open ? 1.0f : of_group<P>(vs, g), p.scale_log2);
-    uint4 there[2];
-#pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      auto pair = [&](int e) { return (8 * half + e < left ? 0xFFFFu : 0u) | (8 * half + e + 1 < left ? 0xFFFF0000u : 0u); };
-      there[half] = make_uint4(pair(0), pair(2), pair(4), pair(6));
-    }
-    auto select = [](bool tail, h8 a, h8 b) { return P == kTile || tail ? a : b; };
-    step(tile, f, [&](int t, int j, int half) { return select(k_open, kt[t][j][half], k_codes(t, j, half)); },
-         [&](int dt, int half) {
-           const uint4 v = __builtin_bit_cast(uint4, vt[dt][half]);
-           return select(v_open, as_h8(make_uint4(v.x & there[half].x, v.y & there[half].y, v.z & there[half].z, v.w & there[half].w)), v_codes(dt, half));
-         },
-         []() {}, []() {});
-  }
 
-  // join the waves: each puts its rows into LDS, four channels of a row are then a thread's
+    // join the waves: each puts its rows into LDS, four channels of a row are then a thread's
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    l[nt] = across16(across32(l[nt], fadd2), fadd2);
-    if (g == 0) join_ml[wave][nt * 16 + n] = make_float2(m[nt], l[nt]);
+    for (int nt = 0; nt < NT; ++nt) {
+      l[nt] = across16(across32(l[nt], fadd2), fadd2);
+      if (g == 0) join_ml[wave][nt * 16 + n] = make_float2(m[nt], l[nt]);
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<f4*>(&join_o[(wave * 16 * NT + nt * 16 + n) * kRowO + dt * 16 + 4 * g]) = o[nt][dt];
-  }
-  __syncthreads();
-  const int rows = s.n * p.group;
-  for (int at = threadIdx.x; at < rows * (D / 4); at += kRowsThreads) {
-    const int r = at / (D / 4), d = at % (D / 4) * 4, i = r / p.group, hq = head * p.group + r % p.group;
-    const int64_t row = s.row + i;
-    float top = -__builtin_inff(), sum = 0.0f;
-#pragma unroll
-    for (int x = 0; x < W; ++x) top = fmaxf(top, join_ml[x][r].x);
-    const float base = top == -__builtin_inff() ? 0.0f : top;
-    f4 all = {0, 0, 0, 0};
-#pragma unroll
-    for (int x = 0; x < W; ++x) {
-      const float2 ml = join_ml[x][r];
-      const float a = __builtin_amdgcn_exp2f(ml.x - base);
-      sum = __builtin_fmaf(ml.y, a, sum);
-      all += *reinterpret_cast<const f4*>(&join_o[(x * 16 * NT + r) * kRowO + d]) * a;
+      for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<f4*>(&join_o[(wave * 16 * NT + nt * 16 + n) * kRowO + dt * 16 + 4 * g]) = o[nt][dt];
     }
-    if (row < 0 || row >= c.tokens) continue;
-    const int64_t to = row * p.q_heads + hq;
-    if (p.splits == 1) {
-      const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;  // (0: it sees nothing; a NaN stays one)
-      *reinterpret_cast<uint2*>(p.out + to * D + d) = make_uint2(as_u32(h2{(_Float16)(all[0] * inv), (_Float16)(all[1] * inv)}),
-                                                                 as_u32(h2{(_Float16)(all[2] * inv), (_Float16)(all[3] * inv)}));
-      if (p.lse && d == 0) p.lse[to] = sum == 0.0f ? -__builtin_inff() : kLn2 * (__builtin_amdgcn_logf(sum) + (top - kShift));
-    } else {
-      const int64_t part = (int64_t)split * c.tokens * p.q_heads + to;
-      *reinterpret_cast<f4*>(p.part_o + part * D + d) = all;
-      if (d == 0) p.part_ml[part] = make_float2(top, sum);
+    __syncthreads();
+    const int rows = s.n * p.group;
+    const bool whole = take == weight;
+    const int place = SHARED ? 2 * (int)blockIdx.y + (b == share.b ? 0 : 1) : 2 * (int)(blockIdx.z * gridDim.y + blockIdx.y);
+    for (int at = threadIdx.x; at < rows * (D / 4); at += kRowsThreads) {
+      const int r = at / (D / 4), d = at % (D / 4) * 4, i = r / p.group, hq = head * p.group + r % p.group;
+      const int64_t row = s.row + i;
+      float top = -__builtin_inff(), sum = 0.0f;
+#pragma unroll
+      for (int x = 0; x < W; ++x) top = fmaxf(top, join_ml[x][r].x);
+      const float base = top == -__builtin_inff() ? 0.0f : top;
+      f4 all = {0, 0, 0, 0};
+#pragma unroll
+      for (int x = 0; x < W; ++x) {
+        const float2 ml = join_ml[x][r];
+        const float a = __builtin_amdgcn_exp2f(ml.x - base);
+        sum = __builtin_fmaf(ml.y, a, sum);
+        all += *reinterpret_cast<const f4*>(&join_o[(x * 16 * NT + r) * kRowO + d]) * a;
+      }
+      if (row < 0 || row >= c.tokens) continue;
+      const int64_t to = row * p.q_heads + hq;
+      if (whole) {
+        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;  // (0: it sees nothing; a NaN stays one)
+        *reinterpret_cast<uint2*>(p.out + to * D + d) = make_uint2(as_u32(h2{(_Float16)(all[0] * inv), (_Float16)(all[1] * inv)}),
+                                                                   as_u32(h2{(_Float16)(all[2] * inv), (_Float16)(all[3] * inv)}));
+        if (p.lse && d == 0) p.lse[to] = sum == 0.0f ? -__builtin_inff() : kLn2 * (__builtin_amdgcn_logf(sum) + (top - kShift));
+      } else {
+        const int64_t part = ((int64_t)place * (c.max_new * p.group) + r) * c.heads + head;
+        *reinterpret_cast<f4*>(p.part_o + part * D + d) = all;
+        if (d == 0) p.part_ml[part] = make_float2(top, sum);
+      }
     }
+    if (p.splits > 1 && from == 0 && head == 0 && threadIdx.x == 0) {
+      const int last = SHARED ? share_at(share, share.start + share.tiles - left + weight - 1) : (weight - 1) / p.chunk;
+      p.part_of[b] = make_int2(place, last - (int)blockIdx.y + 1);
+    }
+    if constexpr (!SHARED) return;
+    left -= take;
+    if (left <= 0) return;
+    __syncthreads();  // (the joined rows have been read)
   }
 }
 
@@ -687,17 +806,37 @@ __global__ __launch_bounds__(kBlockThreads, D <= 128 ? 2 : 1) void attn_block_ke
   }
 }
 
-// How many splits a row (new token i, head hq) was computed in: its workgroup's tiles as that one counted them.
-__device__ __forceinline__ int parts_of(const AttnParams& p, const Kv8Seq& s, int i, int hq, int block_rows) {
-  const int r = i * p.group + hq % p.group, row0 = block_rows ? r / block_rows * block_rows : 0;
-  const int last = block_rows ? min(row0 + block_rows, s.n * p.group) - 1 : s.n * p.group - 1;
-  const Range range = range_of(p, s, row0 / p.group, last / p.group);
-  return min(max(1, (range.tiles + p.chunk - 1) / p.chunk), p.splits);
+// Where the parts of a row (new token i, head hq) lie: the first, and the others at equal distances.
+struct RowParts {
+  int n;
+  int64_t first, second, step;
+  __device__ __forceinline__ int64_t operator[](int k) const { return k == 0 ? first : second + (k - 1) * step; }
+};
+__device__ __forceinline__ RowParts parts_of(const AttnParams& p, const Kv8Seq& s, int b, int i, int hq, int64_t at, int block_rows) {
+  RowParts parts;
+  const int r = i * p.group + hq % p.group;
+  if (block_rows) {  // of the many-rows kernel: its workgroup's tiles as that one counted them
+    const int row0 = r / block_rows * block_rows;
+    const Range range = range_of(p, s, row0 / p.group, (min(row0 + block_rows, s.n * p.group) - 1) / p.group);
+    parts.n = min(max(1, (range.tiles + p.chunk - 1) / p.chunk), p.splits);
+    parts.first = at;
+    parts.step = p.c.tokens * p.q_heads;
+    parts.second = at + parts.step;
+  } else {  // (one: it is written already)
+    const int2 of = p.part_of[b];
+    const int rows = p.c.max_new * p.group, head = hq / p.group;
+    const int place = (int)min((uint32_t)of.x, 2u * p.splits - 1u);
+    parts.n = of.y > 1 ? min(min(of.y, p.splits - place / 2), kJoinMost) : 0;
+    parts.step = (int64_t)2 * rows * p.c.heads;
+    parts.first = ((int64_t)place * rows + r) * p.c.heads + head;
+    parts.second = ((int64_t)(place / 2 + 1) * 2 * rows + r) * p.c.heads + head;
+  }
+  return parts;
 }
 
 // Joins the splits of every row, one workgroup a row: each wave sums every kJoinWaves-th split, always in the same order.  64 splits of
 // 64 rows: 6 us (55 by one wave that takes them one after another).
-constexpr int kJoinWaves = 8, kJoinMost = 1024;  // (splits: plan_of keeps below that)
+constexpr int kJoinWaves = 8;
 template <int D>
 __global__ __launch_bounds__(64 * kJoinWaves) void attn_join_kernel(const AttnParams p, int block_rows) {
   constexpr int E = D / 64;
@@ -711,17 +850,19 @@ __global__ __launch_bounds__(64 * kJoinWaves) void attn_join_kernel(const AttnPa
   const Kv8Seq s = kv8_sequence(c, b);
   const int64_t row = s.row + i;
   if (i >= s.n || row < 0 || row >= c.tokens) return;
-  const int parts = parts_of(p, s, i, hq, block_rows);
-  const int64_t at = row * p.q_heads + hq, step = c.tokens * p.q_heads;
-  const float* part = p.part_o + at * D + lane * E;
+  const int64_t at = row * p.q_heads + hq;
+  const RowParts place = parts_of(p, s, b, i, hq, at, block_rows);
+  const int parts = place.n;
+  if (parts == 0) return;
+  const float* part = p.part_o + lane * E;
   fe first = {};  // (on its way while the weights are made)
-  if (wave < parts) first = *reinterpret_cast<const fe*>(part + wave * step * D);
+  if (wave < parts) first = *reinterpret_cast<const fe*>(part + place[wave] * D);
   float2 ml[kJoinMost / 64 / kJoinWaves];
   float m = -__builtin_inff(), l = 0.0f;
 #pragma unroll
   for (int j = 0; j < kJoinMost / 64 / kJoinWaves; ++j) {
     const int k = tid + 64 * kJoinWaves * j;
-    ml[j] = k < parts ? p.part_ml[at + k * step] : make_float2(-__builtin_inff(), 0.0f);
+    ml[j] = k < parts ? p.part_ml[place[k]] : make_float2(-__builtin_inff(), 0.0f);
     m = fmaxf(m, ml[j].x);
   }
 #pragma unroll
@@ -744,7 +885,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void attn_join_kernel(const AttnPa
   __syncthreads();
   fe o = first * (wave < parts ? weight[wave] : 0.0f);
 #pragma unroll 8
-  for (int k = wave + kJoinWaves; k < parts; k += kJoinWaves) o += *reinterpret_cast<const fe*>(part + k * step * D) * weight[k];
+  for (int k = wave + kJoinWaves; k < parts; k += kJoinWaves) o += *reinterpret_cast<const fe*>(part + place[k] * D) * weight[k];
 #pragma unroll
   for (int j = 0; j < E; ++j) sums[wave][lane * E + j] = o[j];
   __syncthreads();
@@ -776,8 +917,10 @@ __global__ __launch_bounds__(256) void attn_join_few_kernel(const AttnParams p, 
   const Kv8Seq s = kv8_sequence(c, (int)b);
   const int64_t row = s.row + i;
   if (i >= s.n || row < 0 || row >= c.tokens) return;
-  const int parts = parts_of(p, s, i, hq, block_rows);
-  const int64_t at = row * p.q_heads + hq, step = c.tokens * p.q_heads;
+  const int64_t at = row * p.q_heads + hq;
+  const RowParts place = parts_of(p, s, (int)b, i, hq, at, block_rows);
+  const int parts = place.n;
+  if (parts == 0) return;
   float m = -__builtin_inff(), l = 0.0f;
   fe sum = {};
   for (int k0 = 0; k0 < parts; k0 += kJoinFew) {
@@ -785,7 +928,7 @@ __global__ __launch_bounds__(256) void attn_join_few_kernel(const AttnParams p, 
     float2 ml[kJoinFew];
 #pragma unroll
     for (int k = 0; k < kJoinFew; ++k) {
-      const int64_t from = at + (k0 + k < parts ? k0 + k : k0) * step;
+      const int64_t from = place[k0 + k < parts ? k0 + k : k0];
       ml[k] = p.part_ml[from];
       o[k] = *reinterpret_cast<const fe*>(p.part_o + from * D + lane * E);
     }
@@ -815,6 +958,8 @@ struct Plan {
   int nt;          // 16-row tiles of the few-rows kernel, or 0: the many-rows kernel
   int row_blocks;
   int splits, chunk;
+  bool shared;     // few rows: whether workgroups take equal shares of all sequences' keys
+  bool once;       // few rows: codes past the caches (of shares always)
   int most;        // splits that no call of a smaller span exceeds
 };
 
@@ -829,17 +974,21 @@ Plan plan_of(int heads, int group, int sequences, int max_new, int max_len, int 
   // (a window's keys may start inside a tile)
   const int64_t tiles = windowed ? ((int64_t)window + max_new + kTile - 1) / kTile + 1 : (max_len + kTile - 1) / kTile;
   const int64_t groups = (int64_t)sequences * heads * f.row_blocks;
-  // How the keys are split.  A workgroup a CU, in pieces of four tiles at least (one a wave), and only into three or more, since a join costs
-  // as much as some seven tiles.  One sequence, 8 heads of 128 read by 64: 1000 tokens 8.5 us (whole 10.1, pieces of eight tiles or more 10.2),
-  // 8000 10.3 (10.9); 16 sequences of 1000 11.0 (pieces of eight 12.6); 128 new tokens behind 8000 36 (49 with two workgroups a CU).
-  // Pieces would be longer than 32 tiles: then more, so that the bytes in flight last (131000 tokens 49.0, a workgroup a CU 55.0) and,
-  // where several sequences' lengths differ, shorter ones level them (48 of 17 to 8000: 91 us with eight workgroups a CU, 95 with four, 105 with two,
-  // 98 with twelve).
-  const int64_t cus = num_cus(), want = cus * (f.nt && sequences > 1 ? 8 : 2);
-  int64_t splits = groups >= want ? 1 : (want + groups - 1) / groups;
+  // How the keys are split.  Up to 32 tiles for a workgroup a CU: one a CU, in pieces of four tiles at least (one a wave), and only into three or
+  // more, since a join costs as much as some seven tiles.  One sequence, 8 heads of 128 read by 64: 1000 tokens 8.5 us (whole 10.1, pieces
+  // of eight tiles or more 10.2), 8000 10.3 (10.9); 16 sequences of 1000 11.0 (pieces of eight 12.6); 128 new tokens behind 8000 36 (49
+  // with two workgroups a CU).
+  // Beyond, two workgroups a CU, so that the bytes in flight last (131000 tokens 49.0, one 55.0, four 60); few rows of several sequences in equal
+  // shares: 48 of 17 to 8000 tokens 82 us (pieces of each sequence, eight workgroups a CU 92, four 95, two 105; shares for one workgroup a CU 86,
+  // four 91), 64 of 50 to 16000 89 (103), eight of 1000 and one of 60000 37 (43).  Of equal lengths pieces would do (16 of 8000: 47, shares 53),
+  // but the host knows only the longest; and short ones are better off with them (six of 300 to 900: 8.7, 13.4).
+  // Codes past the caches: 192000 tokens 70.0 us (76.0), 48 sequences 82 (87); a workgroup that waits for each of its loads is the better for
+  // what a cache may have kept (16 sequences of 2000, read a moment before, 16.5 us; past the caches 20.6).
+  const int64_t cus = num_cus(), per_cu = (tiles * groups + cus - 1) / cus;
+  const bool few = per_cu <= 32;
+  int64_t chunk = per_cu, splits = groups >= 2 * cus ? 1 : (2 * cus + groups - 1) / groups;
   if (splits > kJoinMost) splits = kJoinMost;
-  int64_t chunk = (tiles * groups + cus - 1) / cus;
-  if (chunk <= 32) {
+  if (few) {
     if (chunk < 4) chunk = 4;
     if (tiles <= 2 * chunk) chunk = tiles;
   } else {
@@ -847,10 +996,23 @@ Plan plan_of(int heads, int group, int sequences, int max_new, int max_len, int 
     if (chunk < 8) chunk = 8;
   }
   if (chunk < 1) chunk = 1;
-  // (neither rule makes more of a shorter span: a workgroup a CU is at most `splits` for a head, pieces are four tiles or more, two of them are one)
-  f.most = (int)(tiles <= 8 ? 1 : splits < (tiles + 3) / 4 ? splits : (tiles + 3) / 4);
   f.chunk = (int)chunk;
   f.splits = tiles > 0 ? (int)((tiles + chunk - 1) / chunk) : 1;
+  // (neither rule makes more of a shorter span: a workgroup a CU is at most `splits` for a head, pieces are four tiles or more, two of them are one)
+  f.most = (int)(tiles <= 8 ? 1 : splits < (tiles + 3) / 4 ? splits : (tiles + 3) / 4);
+  f.shared = false;
+  f.once = sequences == 1 && per_cu >= 8;
+  if (f.nt && sequences > 1) {
+    // (shares of many sequences: at 8 workgroups a CU there are enough of whole ones)
+    const bool many = groups >= 8 * cus || tiles * sequences > 0x7FFFFFFF;
+    const int64_t shares = std::min<int64_t>((2 * cus + heads - 1) / heads, kJoinMost);
+    if (!few) {
+      f.shared = !many;
+      if (many) f.chunk = (int)tiles;
+    }
+    f.splits = f.shared ? (int)shares : many || f.splits == 1 ? 1 : f.splits * sequences;
+    f.most = many ? 1 : (int)std::max(few ? 1 : shares, f.most > 1 ? (int64_t)f.most * sequences : 1);
+  }
   return f;
 }
 
@@ -859,14 +1021,22 @@ int launch_attention_t(const AttnParams& p, const Plan& f, hipStream_t st) {
   const int64_t blocks = (int64_t)p.sequences * p.c.heads * f.row_blocks * f.splits;
   const int64_t joins = (int64_t)p.sequences * p.c.max_new * p.q_heads;
   if (blocks > 0x7FFFFFFF || (f.splits > 1 && joins > 0x7FFFFFFF)) return set_error(QQQ_ERR_SHAPE, "attention_kv8: too many workgroups");
-  if (f.nt && p.sequences > 65535) return set_error(QQQ_ERR_SHAPE, "attention_kv8: %d sequences", p.sequences);
-  const dim3 grid(p.c.heads, f.splits, p.sequences);
+  if (f.nt && !f.shared && p.sequences > 65535) return set_error(QQQ_ERR_SHAPE, "attention_kv8: %d sequences", p.sequences);
+  const dim3 grid(p.c.heads, f.shared ? f.splits : std::max(1, f.splits / p.sequences), f.shared ? 1 : p.sequences);
+#define QQQ_ROWS(SHARED, ONCE)                                                                                                  \
+  do {                                                                                                                          \
+    if (f.nt == 1) hipLaunchKernelGGL((attn_rows_kernel<D, P, 1, SHARED, ONCE>), grid, dim3(kRowsThreads), 0, st, p);           \
+    else hipLaunchKernelGGL((attn_rows_kernel<D, P, 2, SHARED, ONCE>), grid, dim3(kRowsThreads), 0, st, p);                     \
+  } while (0)
   if (f.nt == 0) hipLaunchKernelGGL((attn_block_kernel<D, P>), dim3((unsigned)blocks), dim3(kBlockThreads), 0, st, p);
-  else if (f.nt == 1) hipLaunchKernelGGL((attn_rows_kernel<D, P, 1>), grid, dim3(kRowsThreads), 0, st, p);
-  else hipLaunchKernelGGL((attn_rows_kernel<D, P, 2>), grid, dim3(kRowsThreads), 0, st, p);
+  else if (f.shared) QQQ_ROWS(true, true);
+  else if (f.once) QQQ_ROWS(false, true);
+  else QQQ_ROWS(false, false);
+#undef QQQ_ROWS
   const int block_rows = f.nt ? 0 : kBlockRows;
   // (many rows have waves enough: 4096 rows of 16 splits, 16000 keys, 55 us in all against 65 with a workgroup a row)
-  if (f.splits > kJoinFew && joins < 4 * (int64_t)num_cus()) hipLaunchKernelGGL((attn_join_kernel<D>), dim3((unsigned)joins), dim3(64 * kJoinWaves), 0, st, p, block_rows);
+  const int parts = f.nt && !f.shared ? f.splits / p.sequences : f.splits;  // (of a row, at most)
+  if (parts > kJoinFew && joins < 4 * (int64_t)num_cus()) hipLaunchKernelGGL((attn_join_kernel<D>), dim3((unsigned)joins), dim3(64 * kJoinWaves), 0, st, p, block_rows);
   else if (f.splits > 1) hipLaunchKernelGGL((attn_join_few_kernel<D>), dim3((unsigned)((joins + 3) / 4)), dim3(256), 0, st, p, block_rows);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return set_error(QQQ_ERR_HIP, "attention_kv8 launch: %s", hipGetErrorString(e));
@@ -879,21 +1049,26 @@ int launch_attention_p(const AttnParams& p, int P, const Plan& f, hipStream_t st
   return P == 16 ? launch_attention_t<D, 16>(p, f, st) : P == 32 ? launch_attention_t<D, 32>(p, f, st) : launch_attention_t<D, 64>(p, f, st);
 }
 
-size_t partial_bytes(int splits, int64_t tokens, int q_heads, int D) {
-  return splits > 1 ? (size_t)splits * (size_t)tokens * (size_t)q_heads * ((size_t)D * 4 + 8) : 0;
+// Parts of rows, of D and two floats each, and for few rows where each sequence's are.
+size_t parts_rows(const Plan& f, int splits, int64_t tokens, int max_new, int q_heads) {
+  return splits == 1 ? 0 : (size_t)splits * (size_t)q_heads * (f.nt ? 2 * (size_t)max_new : (size_t)tokens);
+}
+size_t partial_bytes(const Plan& f, int splits, int64_t tokens, int sequences, int max_new, int q_heads, int D) {
+  return splits == 1 ? 0 : parts_rows(f, splits, tokens, max_new, q_heads) * ((size_t)D * 4 + 8) + (f.nt ? (size_t)sequences * 8 : 0);
 }
 
 }  // namespace
 
 size_t attention_kv8_bytes(int heads, int q_heads, int D, int sequences, int max_new, int max_len, int64_t tokens) {
-  return partial_bytes(plan_of(heads, q_heads / heads, sequences, max_new, max_len, 0).most, tokens, q_heads, D);
+  const Plan f = plan_of(heads, q_heads / heads, sequences, max_new, max_len, 0);
+  return partial_bytes(f, f.most, tokens, sequences, max_new, q_heads, D);
 }
 
 int launch_attention_kv8(const Kv8& c, int D, int P, int sequences, const void* q, int64_t q_token, int64_t q_head, int q_heads, float scale,
                          int causal, int window, void* out, float* lse, void* workspace, size_t workspace_bytes, hipStream_t st) {
   const Plan f = plan_of(c.heads, q_heads / c.heads, sequences, c.max_new, c.max_len, window);
-  if (partial_bytes(f.splits, c.tokens, q_heads, D) > workspace_bytes)
-    return set_error(QQQ_ERR_WORKSPACE, "attention_kv8: workspace of %zu bytes, %zu needed", workspace_bytes, partial_bytes(f.splits, c.tokens, q_heads, D));
+  const size_t need = partial_bytes(f, f.splits, c.tokens, sequences, c.max_new, q_heads, D), rows = parts_rows(f, f.splits, c.tokens, c.max_new, q_heads);
+  if (need > workspace_bytes) return set_error(QQQ_ERR_WORKSPACE, "attention_kv8: workspace of %zu bytes, %zu needed", workspace_bytes, need);
   AttnParams p;
   p.c = c;
   p.q = (const uint16_t*)q;
@@ -902,7 +1077,8 @@ int launch_attention_kv8(const Kv8& c, int D, int P, int sequences, const void* 
   p.out = (uint16_t*)out;
   p.lse = lse;
   p.part_o = (float*)workspace;
-  p.part_ml = (float2*)((char*)workspace + (size_t)f.splits * c.tokens * q_heads * D * 4);
+  p.part_ml = (float2*)(p.part_o + rows * D);
+  p.part_of = (int2*)(p.part_ml + rows);
   p.scale_log2 = scale * kLog2e;
   p.group = q_heads / c.heads;
   p.q_heads = q_heads;

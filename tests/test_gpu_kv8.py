@@ -244,6 +244,30 @@ def test_many_rows_of_many_splits(dim, new, q_heads):
     _check_attention(w, [2700], [new], q_heads, window=2300)
 
 
+@pytest.mark.parametrize("window", [0, 100])
+@pytest.mark.parametrize("q_heads", [1, 9])
+def test_equal_shares_of_many_sequences(q_heads, window):
+    """More sequences than a workgroup has threads, long, short and empty, some without a new token: shares begin and end inside of them."""
+    rng = np.random.default_rng(26)
+    lengths = [int(n) for n in rng.integers(0, 150, 300)]
+    lengths[7], lengths[8], lengths[200], lengths[299] = 2500, 0, 3333, 64
+    new = [int(rng.integers(0, 4)) for _ in lengths]
+    new[7], new[8], new[199], new[200], new[299] = 3, 2, 0, 1, 1
+    w = _filled(27, lengths, 1, 64, 64)
+    _check_attention(w, lengths, new, q_heads, window=window)
+    if not window:
+        assert "rows x512 + join" in qqq.last_route()
+
+
+@pytest.mark.parametrize("lengths,new", [([5, 0, 70], [1, 1, 1]), ([0, 0, 0], [1, 2, 0]), ([1, 900, 3], [0, 4, 0]), ([640, 640, 640], [1, 1, 1]), ([257, 1, 512], [2, 1, 1])])
+def test_equal_shares_of_less_than_was_announced(lengths, new):
+    """Bounds that promise far more tokens than there are: most shares are empty."""
+    w = Both(28, lengths, 8, 128, 64, columns=1100)
+    w.append(lengths, lengths)
+    _check_attention(w, lengths, new, 32)
+    assert "rows x64 + join" in qqq.last_route()
+
+
 @pytest.mark.parametrize("new,length", [(1, 40), (1, 700), (1, 5000), (40, 100), (40, 2000), (300, 3500)])
 def test_a_query_that_is_not_a_number(new, length):
     """It gives NaN in its own row, in what the sum's logarithm is as well, whole or joined from splits."""
