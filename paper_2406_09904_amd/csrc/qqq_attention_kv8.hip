@@ -14,6 +14,7 @@
 #include <type_traits>
 
 #include "qqq_kv8.h"
+#include "qqq_past.h"
 
 namespace qqq {
 
@@ -50,17 +51,6 @@ __device__ __forceinline__ h8 as_h8(uint4 v) { return __builtin_bit_cast(h8, v);
 __device__ __forceinline__ h8 codes8_to_halves(uint32_t a, uint32_t b) {
   const uint2 lo = codes4_to_halves(a), hi = codes4_to_halves(b);
   return as_h8(make_uint4(lo.x, lo.y, hi.x, hi.y));
-}
-
-// 16 codes; ONCE: past the caches, which need not keep what no other workgroup reads.
-template <bool ONCE>
-__device__ __forceinline__ uint4 load_codes(const uint8_t* from) {
-  typedef uint32_t u4 __attribute__((ext_vector_type(4)));
-  const u4* at = reinterpret_cast<const u4*>(from);
-  u4 v;
-  if constexpr (ONCE) v = __builtin_nontemporal_load(at);
-  else v = *at;
-  return make_uint4(v.x, v.y, v.z, v.w);
 }
 
 // maximum / sum over the lanes l, l ^ 16, l ^ 32, l ^ 48 and over l, l ^ 32
@@ -223,7 +213,7 @@ __device__ __forceinline__ Share share_of(const AttnParams& p, int w) {
 // this tile's are in the result, and nothing that a request depends on is waited for there (loads return in order): page numbers
 // are fetched two tiles ahead, scales one.
 constexpr int W = 4, kRowsThreads = 64 * W;
-template <int D, int P, int NT, bool SHARED, bool ONCE>
+template <int D, int P, int NT, bool SHARED, bool PAST>
 __global__ __launch_bounds__(kRowsThreads, D <= 128 ? 2 : 1) void attn_rows_kernel(const AttnParams p) {
   constexpr int J = D / 64, DT = D / 16, NP = Pages<P>::N;
   constexpr int kRowO = D + 4;  // (16 bytes over: the lanes' rows start in different banks)
@@ -267,14 +257,14 @@ __global__ __launch_bounds__(kRowsThreads, D <= 128 ? 2 : 1) void attn_rows_kern
 #pragma unroll
       for (int t = 0; t < 4; ++t)
 #pragma unroll
-        for (int j = 0; j < J; ++j) kraw[t][j] = load_codes<ONCE>(at + 4 * t * D + 64 * j);
+        for (int j = 0; j < J; ++j) kraw[t][j] = load16<PAST>(at + 4 * t * D + 64 * j);
     };
     auto request_v = [&](const Pages<P>& of) {
       int64_t offset[NP];
       offsets(of, offset);
       const uint8_t* at = c.v_codes + of_group<P>(offset, g) + v_lane;
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt) vraw[dt] = load_codes<ONCE>(at + dt * 16 * P);
+      for (int dt = 0; dt < DT; ++dt) vraw[dt] = load16<PAST>(at + dt * 16 * P);
     };
     float ks[NP], vs[NP];
     auto scales = [&](const Pages<P>& of) {
@@ -959,7 +949,7 @@ struct Plan {
   int row_blocks;
   int splits, chunk;
   bool shared;     // few rows: whether workgroups take equal shares of all sequences' keys
-  bool once;       // few rows: codes past the caches (of shares always)
+  bool past;       // few rows: codes past the caches (of shares always)
   int most;        // splits that no call of a smaller span exceeds
 };
 
@@ -1001,7 +991,7 @@ Plan plan_of(int heads, int group, int sequences, int max_new, int max_len, int 
   // (neither rule makes more of a shorter span: a workgroup a CU is at most `splits` for a head, pieces are four tiles or more, two of them are one)
   f.most = (int)(tiles <= 8 ? 1 : splits < (tiles + 3) / 4 ? splits : (tiles + 3) / 4);
   f.shared = false;
-  f.once = sequences == 1 && per_cu >= 8;
+  f.past = sequences == 1 && per_cu >= 8;
   if (f.nt && sequences > 1) {
     // (shares of many sequences: at 8 workgroups a CU there are enough of whole ones)
     const bool many = groups >= 8 * cus || tiles * sequences > 0x7FFFFFFF;
@@ -1023,14 +1013,14 @@ int launch_attention_t(const AttnParams& p, const Plan& f, hipStream_t st) {
   if (blocks > 0x7FFFFFFF || (f.splits > 1 && joins > 0x7FFFFFFF)) return set_error(QQQ_ERR_SHAPE, "attention_kv8: too many workgroups");
   if (f.nt && !f.shared && p.sequences > 65535) return set_error(QQQ_ERR_SHAPE, "attention_kv8: %d sequences", p.sequences);
   const dim3 grid(p.c.heads, f.shared ? f.splits : std::max(1, f.splits / p.sequences), f.shared ? 1 : p.sequences);
-#define QQQ_ROWS(SHARED, ONCE)                                                                                                  \
+#define QQQ_ROWS(SHARED, PAST)                                                                                                  \
   do {                                                                                                                          \
-    if (f.nt == 1) hipLaunchKernelGGL((attn_rows_kernel<D, P, 1, SHARED, ONCE>), grid, dim3(kRowsThreads), 0, st, p);           \
-    else hipLaunchKernelGGL((attn_rows_kernel<D, P, 2, SHARED, ONCE>), grid, dim3(kRowsThreads), 0, st, p);                     \
+    if (f.nt == 1) hipLaunchKernelGGL((attn_rows_kernel<D, P, 1, SHARED, PAST>), grid, dim3(kRowsThreads), 0, st, p);           \
+    else hipLaunchKernelGGL((attn_rows_kernel<D, P, 2, SHARED, PAST>), grid, dim3(kRowsThreads), 0, st, p);                     \
   } while (0)
   if (f.nt == 0) hipLaunchKernelGGL((attn_block_kernel<D, P>), dim3((unsigned)blocks), dim3(kBlockThreads), 0, st, p);
   else if (f.shared) QQQ_ROWS(true, true);
-  else if (f.once) QQQ_ROWS(false, true);
+  else if (f.past) QQQ_ROWS(false, true);
   else QQQ_ROWS(false, false);
 #undef QQQ_ROWS
   const int block_rows = f.nt ? 0 : kBlockRows;

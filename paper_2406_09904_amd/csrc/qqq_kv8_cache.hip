@@ -5,8 +5,10 @@
 // step of single tokens): the workgroup's four waves share a page, since a call lasts as long as its slowest page.  Append: the page's fp16
 // values (the open page's from the tail slot, the others from the new rows) are read once into registers, |max| is reduced over the
 // wave, and codes = 128 + rne(x / s) are written.  A lane holds four tokens of eight channels; values are turned token-minor as codes, in
-// registers (4 x 4 bytes) and through LDS.
+// registers (4 x 4 bytes) and through LDS.  12000 tokens of 40 heads of 128 in pages of 16: appended (376 MB) in 79 us, 4.7 TB/s, read back (445 MB)
+// in 62, 7.1 TB/s with the codes still in the last-level cache; a token each of 64 sequences, 8 heads, pages of 64: 6.1 us.
 #include "qqq_kv8.h"
+#include "qqq_past.h"
 
 namespace qqq {
 
@@ -96,7 +98,7 @@ struct AppendParams {
   int units, sequences;  // pages a sequence may touch
 };
 
-template <int D, int P, int C>
+template <int D, int P, int C, bool PAST>
 __global__ __launch_bounds__(64 * kWaves) void kv8_append_kernel(const AppendParams p) {
   using S = PageShape<D, P, C>;
   __shared__ uint32_t turned[kWaves / C][D * S::kRow / 4];
@@ -116,7 +118,7 @@ __global__ __launch_bounds__(64 * kWaves) void kv8_append_kernel(const AppendPar
   uint16_t* tail = const_cast<uint16_t*>(w.values ? c.v_tail : c.k_tail) + ((int64_t)s.slot * c.heads + w.head) * (P * D);
   auto new_values = [&](int pos, int d8) {  // eight values of a new token as they came; a row outside the tensor reads as zeros
     const int64_t row = s.row + (pos - start);
-    return row >= 0 && row < c.tokens ? *reinterpret_cast<const uint4*>(in + row * token_stride + d8 * 8) : make_uint4(0, 0, 0, 0);
+    return row >= 0 && row < c.tokens ? load16<PAST>(in + row * token_stride + d8 * 8) : make_uint4(0, 0, 0, 0);
   };
 
   if (page < closed) {
@@ -225,7 +227,7 @@ __device__ __forceinline__ uint4 scaled_halves(uint2 codes, float s) {
   return make_uint4(mul(a.x), mul(a.y), mul(b.x), mul(b.y));
 }
 
-template <int D, int P, int C>
+template <int D, int P, int C, bool PAST>
 __global__ __launch_bounds__(64 * kWaves) void kv8_read_kernel(const ReadParams p) {
   using S = PageShape<D, P, C>;
   __shared__ uint32_t turned[kWaves / C][D * S::kRow / 4];
@@ -245,7 +247,7 @@ __global__ __launch_bounds__(64 * kWaves) void kv8_read_kernel(const ReadParams 
   auto put = [&](int t, int d8, uint4 x) {
     const int pos = page * P + t;
     const int64_t row = s.row + (pos - start);
-    if (pos >= start && pos < s.len && row >= 0 && row < c.tokens) *reinterpret_cast<uint4*>(out + row * c.heads * D + d8 * 8) = x;
+    if (pos >= start && pos < s.len && row >= 0 && row < c.tokens) store16<PAST>(out + row * c.heads * D + d8 * 8, x);
   };
   if (is_tail) {
     const uint16_t* tail = (w.values ? c.v_tail : c.k_tail) + ((int64_t)kv8_slot(c, s.slot) * c.heads + w.head) * (P * D);
@@ -275,7 +277,7 @@ __global__ __launch_bounds__(64 * kWaves) void kv8_read_kernel(const ReadParams 
       const int i = lane + S::kStep * j, t = i / (D / 8) * 4, d8 = i % (D / 8);
 #pragma unroll
       for (int k = 0; k < 4; ++k)
-        if (i < S::kQuads) q[j][k] = reinterpret_cast<const uint2*>(codes)[(t + k) * (D / 8) + d8];
+        if (i < S::kQuads) q[j][k] = load8<PAST>(codes + ((t + k) * (D / 8) + d8) * 8);
     }
 #pragma unroll
     for (int j = 0; j < S::kPerLane; ++j) {
@@ -291,7 +293,7 @@ __global__ __launch_bounds__(64 * kWaves) void kv8_read_kernel(const ReadParams 
 #pragma unroll
   for (int j = 0; j < S::kVectors; ++j) {
     const int i = lane + S::kStep * j;
-    if (i < S::kBytes / 16) raw[j] = reinterpret_cast<const uint4*>(codes)[i];
+    if (i < S::kBytes / 16) raw[j] = load16<PAST>(codes + i * 16);
   }
 #pragma unroll
   for (int j = 0; j < S::kVectors; ++j) {
@@ -319,8 +321,11 @@ __global__ __launch_bounds__(64 * kWaves) void kv8_read_kernel(const ReadParams 
 }
 
 // Whether a page is shared: while that gives a CU eight workgroups at most, keys' and values' (64 sequences, 8 heads of 128, pages of 64: a token
-// appended 6.1 us against 9.9, 65 read 9.8 against 11.4; 12000 tokens of 40 heads in pages of 16: 140 and 117 us against 102 and 68)
+// appended 6.1 us against 9.9, 65 read 9.8 against 11.4; 12000 tokens of 40 heads in pages of 16: 140 and 117 us against 102 and 68, before either went past the caches)
 bool shared_pages(int64_t pages) { return pages <= (int64_t)num_cus() * 4; }
+// Whether fp16 values and codes read go past the caches (codes that are written do not: attention reads them next): where a call's operands,
+// fp16 and codes of `tokens` keys and values, are more than the last of them.  12000 tokens of 40 heads, 376 MB appended and 445 MB read: 79 and 62 us against 102 and 67.
+bool past_caches(const Kv8& c, int D) { return c.tokens * c.heads * D * 6 > kLastCacheBytes; }
 
 template <typename Params, typename Kernel>
 int launch_pages(Kernel kernel, const Params& p, bool shared, const char* name, hipStream_t st) {
@@ -349,7 +354,11 @@ int launch_kv8_append(const Kv8& c, int D, int P, int sequences, const void* k, 
                       int64_t v_token, int64_t v_head, hipStream_t st) {
   const AppendParams p = {c, (const uint16_t*)k, (const uint16_t*)v, k_token, k_head, v_token, v_head, units_of(c.max_new, P), sequences};
   const bool shared = shared_pages((int64_t)p.units * c.heads * sequences);
-#define QQQ_APPEND(D_, P_) return shared ? launch_pages(kv8_append_kernel<D_, P_, kWaves>, p, true, "kv8_append", st) : launch_pages(kv8_append_kernel<D_, P_, 1>, p, false, "kv8_append", st)
+  const bool past = past_caches(c, D);
+#define QQQ_APPEND(D_, P_)                                                                                    \
+  return shared ? launch_pages(kv8_append_kernel<D_, P_, kWaves, false>, p, true, "kv8_append", st)          \
+         : past ? launch_pages(kv8_append_kernel<D_, P_, 1, true>, p, false, "kv8_append", st)               \
+                : launch_pages(kv8_append_kernel<D_, P_, 1, false>, p, false, "kv8_append", st)
   QQQ_KV8_SHAPES(QQQ_APPEND)
 #undef QQQ_APPEND
 }
@@ -357,7 +366,11 @@ int launch_kv8_append(const Kv8& c, int D, int P, int sequences, const void* k, 
 int launch_kv8_read(const Kv8& c, int D, int P, int sequences, void* k, void* v, hipStream_t st) {
   const ReadParams p = {c, (uint16_t*)k, (uint16_t*)v, units_of(c.max_new, P), sequences};
   const bool shared = shared_pages((int64_t)p.units * c.heads * sequences);
-#define QQQ_READ(D_, P_) return shared ? launch_pages(kv8_read_kernel<D_, P_, kWaves>, p, true, "kv8_read", st) : launch_pages(kv8_read_kernel<D_, P_, 1>, p, false, "kv8_read", st)
+  const bool past = past_caches(c, D);
+#define QQQ_READ(D_, P_)                                                                                      \
+  return shared ? launch_pages(kv8_read_kernel<D_, P_, kWaves, false>, p, true, "kv8_read", st)              \
+         : past ? launch_pages(kv8_read_kernel<D_, P_, 1, true>, p, false, "kv8_read", st)                   \
+                : launch_pages(kv8_read_kernel<D_, P_, 1, false>, p, false, "kv8_read", st)
   QQQ_KV8_SHAPES(QQQ_READ)
 #undef QQQ_READ
 }

@@ -8,14 +8,19 @@
 //
 // Both are bound by their bytes from some hundred rows on, below that by how soon a row is done (a launch from a graph alone is 1.6 us).
 // Norm, fp16 residual, codes: M = 1, K = 4096 2.7 us; M = 777, K = 5120 6.2; M = 4096, K = 8192 37 to 44 (5.3 to 6.3 TB/s, by what the last-level
-// cache still holds); fp32 residual, fp16 output: M = 777, K = 5120 9.4, M = 4096, K = 8192 74.  Gated activation: M = 16, F = 11008 3.7 us;
-// M = 4096, F = 28672 113 (5.2 TB/s).
-#include "qqq_internal.h"
+// cache still holds); fp32 residual, fp16 output: M = 777, K = 5120 9.4, M = 4096, K = 8192 66.  Gated activation: M = 16, F = 11008 3.7 us;
+// M = 4096, F = 28672 108 (5.4 TB/s).
+//
+// Inputs are read past the caches (qqq_past.h) where all operands are more than the last of them: gated activation, M = 4096, F = 28672 (587 MB)
+// and a reader of its codes 356 us, 424 otherwise; norm, fp32 residual, M = 4096, K = 8192 (403 MB) 66 against 74.  Smaller calls would lose what
+// the call before them has left there: gated, F = 11008 (225 MB) 41 against 34, norm, fp16 residual (235 MB) 43 against 37.
+#include "qqq_past.h"
 #include "qqq_layer.h"
 
 namespace qqq {
 
 namespace {
+
 
 constexpr float kLeastScale = 0x1p-120f;  // below it a reciprocal would leave fp32's range: the row counts as zero
 
@@ -88,7 +93,7 @@ struct NormParams {
 };
 
 // RES: QQQ_RESIDUAL_*.  VPT > 0: the row is VPT vectors of 8 values per thread; VPT == 0: any K, the row is read twice.
-template <int RES, bool QUANT, int VPT, int T>
+template <int RES, bool QUANT, int VPT, int T, bool PAST>
 __global__ __launch_bounds__(T) void rmsnorm_kernel(const NormParams p) {
   __shared__ float2 smem[T / 64];
   const int64_t m = blockIdx.x;
@@ -101,10 +106,10 @@ __global__ __launch_bounds__(T) void rmsnorm_kernel(const NormParams p) {
     uint4 x, r[RV];
   };
   auto request = [&](int idx, Raw& w) {
-    w.x = x[idx];
+    w.x = load16<PAST>(x + idx);
     if constexpr (RES != QQQ_RESIDUAL_NONE) {
 #pragma unroll
-      for (int i = 0; i < RV; ++i) w.r[i] = res[(int64_t)idx * RV + i];
+      for (int i = 0; i < RV; ++i) w.r[i] = load16<PAST>(res + (int64_t)idx * RV + i);
     }
   };
   // the sum as it is stored, in fp32
@@ -213,8 +218,12 @@ __global__ __launch_bounds__(T) void rmsnorm_kernel(const NormParams p) {
 }
 
 template <int RES, bool QUANT>
-void launch_rmsnorm_t(const NormParams& p, int64_t M, hipStream_t st) {
-#define QQQ_NORM(V, T) hipLaunchKernelGGL((rmsnorm_kernel<RES, QUANT, V, T>), dim3((unsigned)M), dim3(T), 0, st, p)
+void launch_rmsnorm_t(const NormParams& p, int64_t M, bool past, hipStream_t st) {
+#define QQQ_NORM(V, T)                                                                                                  \
+  do {                                                                                                                  \
+    if (V == 0 || !past) hipLaunchKernelGGL((rmsnorm_kernel<RES, QUANT, V, T, false>), dim3((unsigned)M), dim3(T), 0, st, p); \
+    else hipLaunchKernelGGL((rmsnorm_kernel<RES, QUANT, V, T, V != 0>), dim3((unsigned)M), dim3(T), 0, st, p);              \
+  } while (0)
   if (p.nvec <= 64) QQQ_NORM(1, 64);
   else if (p.nvec <= 256) QQQ_NORM(1, 256);
   else if (M <= num_cus() && p.nvec <= 2048) {
@@ -249,7 +258,7 @@ struct GatedParams {
   int nvec;
 };
 
-template <int ACT, int VPT, int T>
+template <int ACT, int VPT, int T, bool PAST>
 __global__ __launch_bounds__(T) void gated_act_kernel(const GatedParams p) {
   __shared__ float2 smem[T / 64];
   const int64_t m = blockIdx.x;
@@ -282,8 +291,8 @@ __global__ __launch_bounds__(T) void gated_act_kernel(const GatedParams p) {
     for (int j = 0; j < VPT; ++j) {
       const int idx = threadIdx.x + T * j;
       if (idx < p.nvec) {
-        vg[j] = gate[idx];
-        vu[j] = up[idx];
+        vg[j] = load16<PAST>(gate + idx);
+        vu[j] = load16<PAST>(up + idx);
       }
     }
 #pragma unroll
@@ -316,8 +325,12 @@ __global__ __launch_bounds__(T) void gated_act_kernel(const GatedParams p) {
 }
 
 template <int ACT>
-void launch_gated_t(const GatedParams& p, int64_t M, hipStream_t st) {
-#define QQQ_GATED(V, T) hipLaunchKernelGGL((gated_act_kernel<ACT, V, T>), dim3((unsigned)M), dim3(T), 0, st, p)
+void launch_gated_t(const GatedParams& p, int64_t M, bool past, hipStream_t st) {
+#define QQQ_GATED(V, T)                                                                                             \
+  do {                                                                                                              \
+    if (V == 0 || !past) hipLaunchKernelGGL((gated_act_kernel<ACT, V, T, false>), dim3((unsigned)M), dim3(T), 0, st, p); \
+    else hipLaunchKernelGGL((gated_act_kernel<ACT, V, T, V != 0>), dim3((unsigned)M), dim3(T), 0, st, p);                \
+  } while (0)
   if (p.nvec <= 64) QQQ_GATED(1, 64);
   else if (p.nvec <= 256) QQQ_GATED(1, 256);
   else if (p.nvec <= 512) QQQ_GATED(2, 256);
@@ -347,9 +360,11 @@ int launch_rmsnorm(const void* x, int64_t ldx, const void* residual, int64_t ldr
   p.inv_k = 1.0f / (float)K;
   p.nvec = (int)(K / 8);
   const bool q = a_q != nullptr;
-  if (residual_type == QQQ_RESIDUAL_NONE) q ? launch_rmsnorm_t<QQQ_RESIDUAL_NONE, true>(p, M, st) : launch_rmsnorm_t<QQQ_RESIDUAL_NONE, false>(p, M, st);
-  else if (residual_type == QQQ_RESIDUAL_FP16) q ? launch_rmsnorm_t<QQQ_RESIDUAL_FP16, true>(p, M, st) : launch_rmsnorm_t<QQQ_RESIDUAL_FP16, false>(p, M, st);
-  else q ? launch_rmsnorm_t<QQQ_RESIDUAL_FP32, true>(p, M, st) : launch_rmsnorm_t<QQQ_RESIDUAL_FP32, false>(p, M, st);
+  const int of_residual = residual_type == QQQ_RESIDUAL_NONE ? 0 : residual_type == QQQ_RESIDUAL_FP16 ? 4 : 8;  // bytes read and written of a value
+  const bool past = M * K * (2 + of_residual + (q ? 1 : 2)) > kLastCacheBytes;
+  if (residual_type == QQQ_RESIDUAL_NONE) q ? launch_rmsnorm_t<QQQ_RESIDUAL_NONE, true>(p, M, past, st) : launch_rmsnorm_t<QQQ_RESIDUAL_NONE, false>(p, M, past, st);
+  else if (residual_type == QQQ_RESIDUAL_FP16) q ? launch_rmsnorm_t<QQQ_RESIDUAL_FP16, true>(p, M, past, st) : launch_rmsnorm_t<QQQ_RESIDUAL_FP16, false>(p, M, past, st);
+  else q ? launch_rmsnorm_t<QQQ_RESIDUAL_FP32, true>(p, M, past, st) : launch_rmsnorm_t<QQQ_RESIDUAL_FP32, false>(p, M, past, st);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return set_error(QQQ_ERR_HIP, "rmsnorm launch: %s", hipGetErrorString(e));
   route_note("rmsnorm");
@@ -366,7 +381,8 @@ int launch_gated_act(const void* gate, int64_t ldg, const void* up, int64_t ldu,
   p.ldg = ldg / 8;
   p.ldu = ldu / 8;
   p.nvec = (int)(F / 8);
-  act == QQQ_ACT_SILU ? launch_gated_t<QQQ_ACT_SILU>(p, M, st) : launch_gated_t<QQQ_ACT_GELU_TANH>(p, M, st);
+  const bool past = M * F * 5 > kLastCacheBytes;
+  act == QQQ_ACT_SILU ? launch_gated_t<QQQ_ACT_SILU>(p, M, past, st) : launch_gated_t<QQQ_ACT_GELU_TANH>(p, M, past, st);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return set_error(QQQ_ERR_HIP, "gated_act launch: %s", hipGetErrorString(e));
   route_note("gated_act");
