@@ -149,6 +149,7 @@ __device__ __forceinline__ Share share_of(const AttnParams& p, int w) {
   Share s;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   int weight = 0, upto = 0, total = 0;
+  if (tid == 0) found[0] = p.sequences;  // (none: should the lengths change under the call)
   auto scan = [&](int base) {  // weights of T sequences, their running sum in each wave, each wave's sum
     weight = base + tid < p.sequences ? weight_of(p, base + tid) : 0;
     upto = weight;
