@@ -129,7 +129,7 @@ int qqq_kv8_read(const qqq_kv8_cache* cache, const qqq_kv8_batch* batch, void* k
  * contribution) for the second product, their sum is not.
  *   q_fp16: token t, head h at t * q_token_stride + h * q_head_stride (elements, % 8 == 0); out_fp16 [tokens, q_heads, head_dim] dense;
  *   lse [tokens, q_heads] fp32 or NULL.  scale > 0, finite.  window needs causal.
- *   q_heads % kv_heads == 0.
+ *   q_heads % kv_heads == 0.  At most 65535 sequences where a key/value head has up to 32 rows (max_new * q_heads / kv_heads).
  *   workspace: qqq_attention_kv8_workspace_bytes() bytes (partial results of calls that split the keys; 0 where none is needed), its
  *   contents irrelevant on entry; not shared by calls that may run concurrently.
  */

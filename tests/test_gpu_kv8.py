@@ -268,6 +268,46 @@ def test_equal_shares_of_less_than_was_announced(lengths, new):
     assert "rows x64 + join" in qqq.last_route()
 
 
+@pytest.mark.parametrize("dim,page", SHAPES + [(256, 16)])
+@pytest.mark.parametrize("new", [1, 4])
+def test_equal_shares_of_every_shape(dim, page, new):
+    """Shares that end inside of sequences, with tail slots beside pages shorter than a tile; 7 and 28 rows of a head."""
+    lengths = [300, 0, 129 + page, 64, 700]
+    w = Both(29, lengths, 2, dim, page, columns=900 * 64 // page)
+    w.append(lengths, lengths)
+    _check_attention(w, lengths, [min(new, n) for n in lengths], 14)
+    assert "rows x256 + join" in qqq.last_route()
+
+
+@pytest.mark.parametrize("dim,page", [(64, 16), (128, 32), (128, 64)])
+@pytest.mark.parametrize("new", [1, 17])
+def test_one_long_sequence_of_many_heads(dim, page, new):
+    w = _filled(30, [4200], 32, dim, page)
+    _check_attention(w, [4200], [new], 32)
+    assert "join" in qqq.last_route()
+
+
+def test_more_values_than_the_last_level_cache():
+    """A call that goes past the caches: the same bits as in pieces that do not."""
+    H, D, P, n = 40, 128, 16, 9000
+    pages = n // P
+    table = torch.randperm(pages, device="cuda").int().view(1, -1)
+    k, v = (torch.randn(n, H, D, device="cuda").half() for _ in range(2))
+    whole, pieces = (qqq.new_kv8_cache(pages, H, D, P, 1) for _ in range(2))
+    step = lambda length, new: qqq.KV8Batch(table, torch.tensor([length], dtype=torch.int32, device="cuda"),  # noqa: E731
+                                            torch.tensor([0, new], dtype=torch.int32, device="cuda"), None, new, n)
+    qqq.qqq_kv8_append(whole, step(n, n), k, v)
+    for at in range(0, n, 3000):
+        qqq.qqq_kv8_append(pieces, step(at + 3000, 3000), k[at:at + 3000], v[at:at + 3000])
+    torch.cuda.synchronize()
+    for name in ("k_codes", "k_scale", "v_codes", "v_scale", "k_tail", "v_tail"):
+        assert torch.equal(getattr(whole, name), getattr(pieces, name)), name
+    got = qqq.qqq_kv8_read(whole, step(n, n), tokens=n)
+    for at in range(0, n, 3000):
+        for a, b in zip(got, qqq.qqq_kv8_read(pieces, step(at + 3000, 3000), tokens=3000)):
+            assert torch.equal(a[at:at + 3000], b), at
+
+
 @pytest.mark.parametrize("new,length", [(1, 40), (1, 700), (1, 5000), (40, 100), (40, 2000), (300, 3500)])
 def test_a_query_that_is_not_a_number(new, length):
     """It gives NaN in its own row, in what the sum's logarithm is as well, whole or joined from splits."""

@@ -167,3 +167,29 @@ def test_another_stream_and_graph_replays():
         torch.cuda.synchronize()
         for a, b in zip(got, (*want, *want2)):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("residual", [None, torch.float16, torch.float32])
+def test_more_rows_than_the_last_level_cache_holds(residual):
+    """Calls that read past the caches: the same bits as calls of a thousand rows, which do not."""
+    M, K = 17000, 5120
+    x, gain = torch.randn(M, K, device="cuda").half(), torch.randn(K, device="cuda").half()
+    r = None if residual is None else torch.randn(M, K, device="cuda", dtype=residual)
+    h, a, s = qqq.qqq_add_rmsnorm_quant(x, gain, r)
+    h2, y = qqq.qqq_add_rmsnorm(x, gain, r)
+    for at in range(0, M, 1000):
+        part = slice(at, at + 1000)
+        ph, pa, ps = qqq.qqq_add_rmsnorm_quant(x[part], gain, None if r is None else r[part])
+        _, py = qqq.qqq_add_rmsnorm(x[part], gain, None if r is None else r[part])
+        assert torch.equal(pa, a[part]) and torch.equal(ps, s[part]) and torch.equal(py, y[part]), at
+        assert r is None or (torch.equal(ph, h[part]) and torch.equal(ph, h2[part])), at
+
+
+@pytest.mark.parametrize("F", [8200, 28672])
+def test_more_gated_rows_than_the_last_level_cache_holds(F):
+    M = 7000
+    x = torch.randn(M, 2 * F, device="cuda").half()
+    a, s = qqq.qqq_gated_act_quant(x[:, :F], x[:, F:])
+    for at in range(0, M, 1000):
+        pa, ps = qqq.qqq_gated_act_quant(x[at:at + 1000, :F], x[at:at + 1000, F:])
+        assert torch.equal(pa, a[at:at + 1000]) and torch.equal(ps, s[at:at + 1000]), at
