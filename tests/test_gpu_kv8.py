@@ -268,7 +268,7 @@ def test_equal_shares_of_less_than_was_announced(lengths, new):
     assert "rows x64 + join" in qqq.last_route()
 
 
-@pytest.mark.parametrize("dim,page", SHAPES + [(256, 16)])
+@pytest.mark.parametrize("dim,page", SHAPES + [(256, 16), (64, 32)])
 @pytest.mark.parametrize("new", [1, 4])
 def test_equal_shares_of_every_shape(dim, page, new):
     """Shares that end inside of sequences, with tail slots beside pages shorter than a tile; 7 and 28 rows of a head."""
@@ -277,6 +277,17 @@ def test_equal_shares_of_every_shape(dim, page, new):
     w.append(lengths, lengths)
     _check_attention(w, lengths, [min(new, n) for n in lengths], 14)
     assert "rows x256 + join" in qqq.last_route()
+
+
+@pytest.mark.parametrize("dim,page", SHAPES + [(256, 16), (64, 32)])
+@pytest.mark.parametrize("new", [1, 4, 40])
+@pytest.mark.parametrize("announced", [1100, 70000, 1 << 21])
+def test_one_sequence_of_every_shape(dim, page, new, announced):
+    """7, 28 and 280 rows of a head, by what the bounds announce whole, in pieces, and in many; the last tokens in the tail slot."""
+    w = Both(31, [1000], 2, dim, page, columns=announced // page)
+    w.append([1000], [1000])
+    _check_attention(w, [1000], [new], 14)
+    _check_attention(w, [1000], [new], 14, window=100)
 
 
 @pytest.mark.parametrize("dim,page", [(64, 16), (128, 32), (128, 64)])
