@@ -962,8 +962,9 @@ Plan plan_of(int heads, int group, int sequences, int max_new, int max_len, int 
   f.nt = rows <= 16 ? 1 : rows <= 32 ? 2 : 0;
   f.row_blocks = f.nt ? 1 : (int)((rows + kBlockRows - 1) / kBlockRows);
   const bool windowed = window > 0 && (int64_t)window + max_new < max_len;
-  // (a window's keys may start inside a tile)
-  const int64_t tiles = windowed ? ((int64_t)window + max_new + kTile - 1) / kTile + 1 : (max_len + kTile - 1) / kTile;
+  // (a window's keys may start inside a tile, but there are no more of them than of all keys)
+  const int64_t all_tiles = ((int64_t)max_len + kTile - 1) / kTile;
+  const int64_t tiles = windowed ? std::min(((int64_t)window + max_new + kTile - 1) / kTile + 1, all_tiles) : all_tiles;
   const int64_t groups = (int64_t)sequences * heads * f.row_blocks;
   // How the keys are split.  Up to 32 tiles for a workgroup a CU: one a CU, in pieces of four tiles at least (one a wave), and only into three or
   // more, since a join costs as much as some seven tiles.  One sequence, 8 heads of 128 read by 64: 1000 tokens 8.5 us (whole 10.1, pieces

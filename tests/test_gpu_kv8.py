@@ -196,6 +196,15 @@ def test_windows(window, new):
     _check_attention(w, lengths, [new, new, min(new, 3)], 8, window=window)
 
 
+@pytest.mark.parametrize("lengths,new,q_heads,window", [([1024], 1, 64, 1000), ([512], 1, 64, 480), ([512], 1, 32, 500), ([2048], 1, 64, 2000), ([1024, 1024], 1, 64, 1000),
+                                                        ([512], 40, 64, 440), ([3827, 90, 3000], 3, 64, 3799)])
+def test_windows_a_little_shorter_than_the_past(lengths, new, q_heads, window):
+    """The bound of the lengths is that of the window's last whole tile: no more pieces than the workspace query, which knows no window, counts."""
+    w = _filled(32, lengths, 8, 128, 64)
+    w.max_len = max(lengths)
+    _check_attention(w, lengths, [new] * len(lengths), q_heads, window=window)
+
+
 @pytest.mark.parametrize("new", [1, 6, 60])
 def test_without_a_causal_mask(new):
     lengths = [60, 130, 100]

@@ -131,6 +131,27 @@ def test_a_window_never_needs_more_workspace(L):
                     assert b <= a, (sequences, max_new, tiles, window)
 
 
+def _windowed_call(L, sequences, max_new, max_len, window, kv_heads, q_heads, tokens):
+    """The code of a call with a window and a workspace of the queried size.  Without a device it is never enqueued."""
+    c = _cache(kv_heads=kv_heads, page_tokens=64, pages=100, slots=1000)
+    b = _batch(columns=max_len // 64, table_stride=max(1, max_len // 64), max_len=max_len, sequences=sequences, max_new=max_new)
+    need = L.qqq_attention_kv8_workspace_bytes(ctypes.byref(c), ctypes.byref(b), q_heads, tokens)
+    return _attend(L, c, b, heads=q_heads, T=tokens, window=window, work=BAD if need else None, nbytes=need)
+
+
+@pytest.mark.skipif(torch.cuda.device_count() > 0, reason="made-up pointers: only where nothing can be launched")
+def test_the_queried_workspace_is_enough_for_the_call_with_any_window(L):
+    """Windows a little shorter than the past among them, whose first key may lie inside a tile."""
+    for sequences in (1, 2, 3, 16, 48, 300):
+        for max_new in (1, 3, 40, 300):
+            for kv_heads, q_heads in ((1, 1), (8, 64), (32, 32)):
+                for max_len in (400, 512, 1000, 1024, 2048, 3827, 60000):
+                    for less in (0, 1, 12, 28, 32, 62, 63, 64, 72, 100, 400, 2000):
+                        window = max(1, max_len - less)
+                        rc = _windowed_call(L, sequences, max_new, max_len, window, kv_heads, q_heads, sequences * max_new)
+                        assert rc not in (NULL, SHAPE, WORKSPACE), (sequences, max_new, kv_heads, q_heads, max_len, window, L.qqq_last_error())
+
+
 def test_binding_refuses_cpu_tensors_and_shapes_that_disagree():
     x = torch.zeros((2, 64), dtype=torch.float16)
     gain = torch.ones(64, dtype=torch.float16)
