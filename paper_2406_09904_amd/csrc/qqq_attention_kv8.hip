@@ -995,15 +995,15 @@ Plan plan_of(int heads, int group, int sequences, int max_new, int max_len, int 
   f.shared = false;
   f.past = sequences == 1 && per_cu >= 8;
   if (f.nt && sequences > 1) {
-    // (shares of many sequences: at 8 workgroups a CU there are enough of whole ones)
-    const bool many = groups >= 8 * cus || tiles * sequences > 0x7FFFFFFF;
+    // (shares of many sequences: at 8 workgroups a CU there are enough of whole ones; of 2^31 tiles they could not be counted, but of a window's they may)
+    const bool enough = groups >= 8 * cus, many = enough || tiles * sequences > 0x7FFFFFFF;
     const int64_t shares = std::min<int64_t>((2 * cus + heads - 1) / heads, kJoinMost);
     if (!few) {
       f.shared = !many;
       if (many) f.chunk = (int)tiles;
     }
     f.splits = f.shared ? (int)shares : many || f.splits == 1 ? 1 : f.splits * sequences;
-    f.most = many ? 1 : (int)std::max(few ? 1 : shares, f.most > 1 ? (int64_t)f.most * sequences : 1);
+    f.most = enough ? 1 : (int)std::max(few ? 1 : shares, f.most > 1 ? (int64_t)f.most * sequences : 1);
   }
   return f;
 }

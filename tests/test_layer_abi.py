@@ -152,6 +152,16 @@ def test_the_queried_workspace_is_enough_for_the_call_with_any_window(L):
                         assert rc not in (NULL, SHAPE, WORKSPACE), (sequences, max_new, kv_heads, q_heads, max_len, window, L.qqq_last_error())
 
 
+@pytest.mark.skipif(torch.cuda.device_count() > 0, reason="made-up pointers: only where nothing can be launched")
+@pytest.mark.parametrize("sequences,max_len", [(199, 734743714), (300, 1 << 29), (3000, 50_000_000)])
+def test_the_queried_workspace_is_enough_with_a_window_where_all_tiles_pass_31_bits(L, sequences, max_len):
+    """Without a window the keys of such calls are not split; with one they are."""
+    for window in (1000, 100_000, max_len // 2):
+        for kv_heads, q_heads in ((1, 8), (7, 21)):
+            rc = _windowed_call(L, sequences, 1, max_len, window, kv_heads, q_heads, sequences)
+            assert rc not in (NULL, SHAPE, WORKSPACE), (window, kv_heads, L.qqq_last_error())
+
+
 def test_binding_refuses_cpu_tensors_and_shapes_that_disagree():
     x = torch.zeros((2, 64), dtype=torch.float16)
     gain = torch.ones(64, dtype=torch.float16)
