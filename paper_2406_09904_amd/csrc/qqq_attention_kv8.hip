@@ -83,14 +83,16 @@ __device__ __forceinline__ Range range_of(const AttnParams& p, const Kv8Seq& s, 
   return r;
 }
 
-// A page's factors: of the exponent, log2 of the values' scale, and one over it.  A scale of zero stands for codes that are all zero.
+// A page's factors: of the exponent, log2 of the values' scale, and one over it.  A scale of zero stands for codes that are all zero: whatever it
+// is taken for, they add nothing.  It is taken for the least that a page has (2^-24 / 127), so that such a page's scores do not stand for the row's
+// largest contribution, beside which the others' weights would lose their bits (as 1, with values of 1e-3 and scores 10 below the zeros': half of the result).
 struct Factors {
   float c, lv, rv;
 };
 __device__ __forceinline__ Factors factors_of(float ks, float vs, float scale_log2) {
   Factors f;
   f.c = fmaxf(ks * scale_log2, 0x1p-100f);
-  const float v = vs > 0.0f ? vs : 1.0f;
+  const float v = vs > 0.0f ? vs : 0x1p-31f;
   f.lv = __builtin_amdgcn_logf(v);
   f.rv = __builtin_amdgcn_rcpf(v);
   return f;

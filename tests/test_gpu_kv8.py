@@ -233,6 +233,42 @@ def test_large_scores_and_scales_of_very_different_pages():
     _check_attention(w, [256, 256], [60, 60], 4, scale=3.0)
 
 
+def _small_values_beside(seed, dim, page, length, size, lead, first, last):
+    """One sequence with values of one sign, `size` in magnitude, whose tokens first .. last - 1 score `lead` (natural logarithm) above the others' mean
+    for every query -> (cache, queries' common part).  (Bounds that announce far more, so that many tiles are one wave's.)"""
+    w = Both(seed, [length], 1, dim, page, columns=1 << 15)
+    k, v = (w.rng.standard_normal((length, 1, dim)) * 0.1).astype(np.float16), (size * (0.5 + 0.5 * w.rng.random((length, 1, dim)))).astype(np.float16)
+    toward = np.where(w.rng.random(dim) < 0.5, -1.0, 1.0)
+    k[first:last, 0] += (toward * lead / dim ** 0.5).astype(np.float16)
+    return w, k, v, toward
+
+
+def _check_given_queries(w, length, q):
+    """As _check_attention, of the last tokens' given queries of one sequence."""
+    n, q_heads, D = q.shape
+    out, lse = qqq.qqq_attention_kv8(w.dev, w.batch([length], [0, n]), _dev(q), lse=torch.empty(n, q_heads, device="cuda"))
+    torch.cuda.synchronize()
+    out, lse = out.cpu().numpy().astype(np.float64), lse.cpu().numpy()
+    k, v = w.host.tokens(w.table[0], length, w.slots[0])
+    want, want_lse, mag, big = ref.attention(q, k, v, D ** -0.5)
+    ds = (D + 8) * 2.0 ** -23 * big
+    bound = (2 ** -11 + 2 * ds[..., None] + 3e-5) * mag + length * 2.0 ** -31 * np.abs(v).max() + 2 ** -11 * np.abs(want) + 2 ** -25
+    assert (np.abs(out - want) / bound).max() <= 1, (np.abs(out - want) / bound).max()
+    assert np.all(np.abs(lse - want_lse) <= ds + 3e-5)
+
+
+@pytest.mark.parametrize("size", [1.0, 1e-3, 1e-4])
+@pytest.mark.parametrize("dim,page,new,q_heads", [(64, 64, 1, 2), (128, 16, 3, 2), (128, 64, 40, 1), (64, 16, 150, 1), (256, 32, 40, 1)])
+def test_small_values_beside_a_page_of_zeros(dim, page, new, q_heads, size):
+    """Zeros that score far higher than the values: what the values add is as exact as without them."""
+    length = 4096
+    w, k, v, toward = _small_values_beside(33, dim, page, length, size, 10.0, 2048, 2048 + page)
+    v[2048:2048 + page] = 0
+    w.append([length], [length], k, v)
+    w.check()
+    _check_given_queries(w, length, (toward + 0.1 * w.rng.standard_normal((new, q_heads, dim))).astype(np.float16))
+
+
 @pytest.mark.parametrize("new,heads,q_heads", [(1, 1, 8), (3, 2, 8), (20, 1, 8), (150, 1, 1)])
 def test_a_long_past(new, heads, q_heads):
     """The keys are split over workgroups and joined."""
