@@ -310,8 +310,9 @@ __global__ __launch_bounds__(kRowsThreads, D <= 128 ? 2 : 1) void attn_rows_kern
       for (int dt = 0; dt < DT; ++dt) o[nt][dt] = f4{0, 0, 0, 0};
     }
 
-    // one tile: k_of(t, j, half) and v_of(dt, half) give the codes' operands; next() requests after the scores and after the result
-    auto step = [&](int tile, const Factors& f, auto k_of, auto v_of, auto next_k, auto next_v) {
+    // one tile's keys from `key_lo` and up to `key_hi`: k_of(t, j, half) and v_of(dt, half) give the codes' operands; next() requests after the scores
+    // and after the result
+    auto step = [&](int tile, int key_lo, int key_hi, const Factors& f, auto k_of, auto v_of, auto next_k, auto next_v) {
       f4 st[NT][4];
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
@@ -333,12 +334,13 @@ __global__ __launch_bounds__(kRowsThreads, D <= 128 ? 2 : 1) void attn_rows_kern
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         if (edge) {
+          const int least = max(lo[nt], key_lo), most = min(hi[nt], key_hi);
 #pragma unroll
           for (int t = 0; t < 4; ++t)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               const int key = tile * kTile + 16 * g + 4 * t + i;
-              if (!(key >= lo[nt] && key < hi[nt])) st[nt][t][i] = -__builtin_inff();
+              if (!(key >= least && key < most)) st[nt][t][i] = -__builtin_inff();
             }
         }
         float top = -__builtin_inff();
@@ -381,8 +383,13 @@ __global__ __launch_bounds__(kRowsThreads, D <= 128 ? 2 : 1) void attn_rows_kern
     auto k_codes = [&](int t, int j, int half) { return half ? codes8_to_halves(kraw[t][j].z, kraw[t][j].w) : codes8_to_halves(kraw[t][j].x, kraw[t][j].y); };
     auto v_codes = [&](int dt, int half) { return half ? codes8_to_halves(vraw[dt].z, vraw[dt].w) : codes8_to_halves(vraw[dt].x, vraw[dt].y); };
 
-    int tile = first;
-    if (first < end && (P < kTile || first != open_tile)) {  // (a wave that has but the tail slot goes there at once: 500 tokens 9.0 us, 9.4 through codes that it does not use)
+    // Tokens in the tail slot are a step of their own, a wave's last: their values are not relative to a page's scale, and in one step with closed pages of
+    // small values (pages shorter than a tile) their scores would stand for more than they contribute and take those pages' weights their bits (values of
+    // 1e-4 to 1e-3: 0.3 % of the result).  The step costs a short call in small pages 0.4 us (500 tokens 8.0 us); codes and slot never share registers (four tokens
+    // of 48 sequences in pages of 16 109 us, 116 in one step; one of 16 sequences, heads of 64 18.5, 23.3).
+    const bool has_tail = open_tile >= first && open_tile < end && (open_tile - first) % W == 0;
+    const int code_end = min(end, (closed * P + kTile - 1) / kTile);
+    if (first < code_end) {  // (a wave that has but the tail slot goes there at once: 500 tokens 9.0 us, 9.4 through codes that it does not use)
       __builtin_amdgcn_sched_barrier(0);
       scales(pages);
       request_k(pages);
@@ -390,10 +397,10 @@ __global__ __launch_bounds__(kRowsThreads, D <= 128 ? 2 : 1) void attn_rows_kern
       request_v(pages);
       __builtin_amdgcn_sched_barrier(0);
       pages = pages_of<P>(c, b, min(first + W, end - 1), closed);
-      for (; tile < end && tile != open_tile; tile += W) {
+      for (int tile = first; tile < code_end; tile += W) {
         const Factors f = factors_of(of_group<P>(ks, g), of_group<P>(vs, g), p.scale_log2);
         const Pages<P> after = pages_of<P>(c, b, min(tile + 2 * W, end - 1), closed);
-        step(tile, f, k_codes, v_codes,
+        step(tile, 0, closed * P, f, k_codes, v_codes,
              [&]() {
                __builtin_amdgcn_sched_barrier(0);
                scales(pages);
@@ -408,9 +415,7 @@ __global__ __launch_bounds__(kRowsThreads, D <= 128 ? 2 : 1) void attn_rows_kern
         pages = after;
       }
     }
-    if (tile < end) {
-      // the tile that the sequence ends in, its last tokens in the tail slot; where pages are shorter than a tile, others of them may be codes
-      const bool k_open = (tile * kTile + 16 * gk) / P >= closed, v_open = (tile * kTile + 16 * g) / P >= closed;
+    if (has_tail) {
       const int64_t tail = ((int64_t)slot * c.heads + head) * (P * D);
       h8 kt[4][J][2], vt[DT][2];
 #pragma unroll
@@ -420,38 +425,24 @@ __global__ __launch_bounds__(kRowsThreads, D <= 128 ? 2 : 1) void attn_rows_kern
 #pragma unroll
           for (int half = 0; half < 2; ++half)
             kt[t][j][half] = as_h8(*reinterpret_cast<const uint4*>(c.k_tail + tail + k_lane + 4 * t * D + 64 * j + 8 * half));
-      auto request_vt = [&]() {
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt)
+      for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-          for (int half = 0; half < 2; ++half) vt[dt][half] = as_h8(*reinterpret_cast<const uint4*>(c.v_tail + tail + v_lane + dt * 16 * P + 8 * half));
-      };
-      // (pages shorter than a tile, shared: beside the codes there are not registers enough for both; 48 sequences in pages of 32 78 us, 98 spilled;
-      // where there are, a second wait is 1 us of a short call)
-      constexpr bool kValuesLater = SHARED && P < kTile && D >= 128;
-      if constexpr (!kValuesLater) request_vt();
-      const int left = s.len - (tile * kTile + 16 * g);  // tokens of the lane's group that exist: what lies past them may be anything
-      const Factors f = factors_of(v_open ? 1.0f : of_group<P>(ks, g), v_open ? 1.0f : of_group<P>(vs, g), p.scale_log2);
+        for (int half = 0; half < 2; ++half) vt[dt][half] = as_h8(*reinterpret_cast<const uint4*>(c.v_tail + tail + v_lane + dt * 16 * P + 8 * half));
+      // tokens of the lane's group that are in the slot: what lies past them may be anything
+      const int left = open_tile * kTile + 16 * g >= closed * P ? s.len - (open_tile * kTile + 16 * g) : 0;
       uint4 there[2];
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
         auto pair = [&](int e) { return (8 * half + e < left ? 0xFFFFu : 0u) | (8 * half + e + 1 < left ? 0xFFFF0000u : 0u); };
         there[half] = make_uint4(pair(0), pair(2), pair(4), pair(6));
       }
-      auto select = [](bool tail, h8 a, h8 b) { return P == kTile || tail ? a : b; };
-      step(tile, f, [&](int t, int j, int half) { return select(k_open, kt[t][j][half], k_codes(t, j, half)); },
+      step(open_tile, closed * P, s.len, factors_of(1.0f, 1.0f, p.scale_log2), [&](int t, int j, int half) { return kt[t][j][half]; },
            [&](int dt, int half) {
              const uint4 v = __builtin_bit_cast(uint4, vt[dt][half]);
-             return select(v_open, as_h8(make_uint4(v.x & there[half].x, v.y & there[half].y, v.z & there[half].z, v.w & there[half].w)), v_codes(dt, half));
+             return as_h8(make_uint4(v.x & there[half].x, v.y & there[half].y, v.z & there[half].z, v.w & there[half].w));
            },
-           [&]() {
-             if constexpr (kValuesLater) {
-               __builtin_amdgcn_sched_barrier(0);
-               request_vt();
-               __builtin_amdgcn_sched_barrier(0);
-             }
-           },
-           []() {});
+           []() {}, []() {});
     }
 
     // join the waves: each puts its rows into LDS, four channels of a row are then a thread's
@@ -604,7 +595,8 @@ __global__ __launch_bounds__(kBlockThreads, D <= 128 ? 2 : 1) void attn_block_ke
       to.rv[tid] = f.rv;
     }
   };
-  // and over it what the tail slot holds of the tile that the sequence ends in (each thread over its own chunks)
+  // and over it what the tail slot holds of the tile that the sequence ends in (each thread over its own chunks): where that tile has closed pages too, in
+  // a step of its own after theirs (see the few-rows kernel)
   const int open_tile = s.len > closed * P ? closed * P / kTile : -1;
   auto stage_tail = [&](TileLds<D>& to) {
     const int64_t tail = ((int64_t)slot * c.heads + head) * (P * D);
@@ -654,7 +646,9 @@ __global__ __launch_bounds__(kBlockThreads, D <= 128 ? 2 : 1) void attn_block_ke
 #pragma unroll
     for (int x = 0; x < 16; ++x) o[dt][x] = 0.0f;
 
-  const int first = range.tile0 + from, end = first + tiles;
+  const int first = range.tile0 + from, last = first + tiles;
+  const int tail_step = open_tile < first || open_tile >= last ? -1 : P < kTile && closed * P > open_tile * kTile ? open_tile + 1 : open_tile;
+  const int end = max(last, tail_step + 1);  // steps are tiles, but for the tail slot's
   auto pages_at = [&](int tile) { return pages_of<P>(c, b, min(tile, end - 1), closed); };
   Pages<P> pages = pages_at(first);   // of the tile after the one whose codes are on their way
   request(pages);
@@ -663,13 +657,15 @@ __global__ __launch_bounds__(kBlockThreads, D <= 128 ? 2 : 1) void attn_block_ke
   __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
   __builtin_amdgcn_sched_barrier(0);
   stage(lds[0]);
-  if (first == open_tile) stage_tail(lds[0]);
+  if (first == tail_step) stage_tail(lds[0]);
   request(pages);
   pages = pages_at(first + 2);
   lds_barrier();
   const int token_of_row = 16 * (n >> 4) + 8 * ((n >> 2) & 1) + 4 * ((n >> 3) & 1) + (n & 3);
   bool unseen = true;  // some row of the wave has seen nothing yet
-  auto step = [&](int tile, auto buffer) {
+  auto step = [&](int at, auto buffer) {
+    const bool is_tail = at == tail_step;
+    const int tile = is_tail ? open_tile : at;
     const TileLds<D>& t = lds[decltype(buffer)::value];
     TileLds<D>& next = lds[1 - decltype(buffer)::value];
     auto k_of = [&](int x) {  // x: step and 32-token subtile (in turn, so that no product waits for the one before it)
@@ -710,12 +706,13 @@ __global__ __launch_bounds__(kBlockThreads, D <= 128 ? 2 : 1) void attn_block_ke
     }
     __builtin_amdgcn_sched_barrier(0);
     if ((tile + 1) * kTile > range.whole_hi || tile * kTile < range.whole_lo) {
+      const int least = P < kTile && is_tail ? max(lo, closed * P) : lo, most = P < kTile && !is_tail ? min(hi, closed * P) : hi;
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
         for (int x = 0; x < 16; ++x) {
           const int key = tile * kTile + 32 * u + 16 * (x >> 3) + 8 * h + (x & 7);
-          if (!(key >= lo && key < hi)) sc[u][x] = -__builtin_inff();
+          if (!(key >= least && key < most)) sc[u][x] = -__builtin_inff();
         }
     }
     // Weights relative to the reference as it stands.  Sums of a lane's weights that stay small say that each of them does; where they do not, or
@@ -764,15 +761,15 @@ __global__ __launch_bounds__(kBlockThreads, D <= 128 ? 2 : 1) void attn_block_ke
       o[x % DT] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v[x], w[x / DT], o[x % DT], 0, 0, 0);
     }
     stage(next);
-    if (tile + 1 == open_tile) stage_tail(next);
+    if (at + 1 == tail_step) stage_tail(next);
     request(pages);
-    pages = pages_at(tile + 3);
+    pages = pages_at(at + 3);
     lds_barrier();
   };
   // (two at a time: which buffer is which is then a constant, and LDS addresses offsets of the instructions)
-  for (int tile = first; tile < end; tile += 2) {
-    step(tile, std::integral_constant<int, 0>{});
-    if (tile + 1 < end) step(tile + 1, std::integral_constant<int, 1>{});
+  for (int at = first; at < end; at += 2) {
+    step(at, std::integral_constant<int, 0>{});
+    if (at + 1 < end) step(at + 1, std::integral_constant<int, 1>{});
   }
   l = across32(l, fadd2);
   if (!there) return;

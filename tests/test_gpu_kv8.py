@@ -269,6 +269,16 @@ def test_small_values_beside_a_page_of_zeros(dim, page, new, q_heads, size):
     _check_given_queries(w, length, (toward + 0.1 * w.rng.standard_normal((new, q_heads, dim))).astype(np.float16))
 
 
+@pytest.mark.parametrize("size", [1.0, 1e-3, 1e-4, 1e4])
+@pytest.mark.parametrize("dim,page,length,new,q_heads", [(64, 16, 4017, 1, 2), (128, 16, 4017, 3, 2), (128, 32, 4001, 1, 16), (128, 64, 4020, 1, 2), (64, 16, 4017, 40, 1), (128, 32, 4001, 40, 2),
+                                                         (128, 64, 4020, 40, 1), (256, 16, 4017, 1, 20), (256, 32, 4001, 40, 1)])
+def test_small_values_beside_an_open_page(dim, page, length, new, q_heads, size):
+    """The tail slot's tokens score far higher than the closed pages before them, in the same tile and others: those add what they should."""
+    w, k, v, toward = _small_values_beside(34, dim, page, length, size, 10.0, length // page * page, length)
+    w.append([length], [length], k, v)
+    _check_given_queries(w, length, (toward + 0.1 * w.rng.standard_normal((new, q_heads, dim))).astype(np.float16))
+
+
 @pytest.mark.parametrize("new,heads,q_heads", [(1, 1, 8), (3, 2, 8), (20, 1, 8), (150, 1, 1)])
 def test_a_long_past(new, heads, q_heads):
     """The keys are split over workgroups and joined."""
