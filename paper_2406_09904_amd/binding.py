@@ -272,10 +272,14 @@ def qqq_gemm_workspace_bytes(M: int, N: int, K: int) -> int:
     return int(lib().qqq_gemm_workspace_bytes(M, N, K))
 
 
+def qqq_gemm_workspace_zero_bytes(M: int, N: int, K: int) -> int:
+    return int(lib().qqq_gemm_workspace_zero_bytes(M, N, K))
+
+
 def split_k_part(workspace: torch.Tensor, M: int, N: int, K: int) -> torch.Tensor:
     """The part of a GEMM workspace that every call leaves zero (arrival counters and split-K partial
     sums of the decode kernel); what follows it is scratch of the prefill kernels with no invariant."""
-    return workspace[:int(lib().qqq_gemm_workspace_zero_bytes(M, N, K))]
+    return workspace[:qqq_gemm_workspace_zero_bytes(M, N, K)]
 
 
 def new_workspace(M: int, N: int, K: int, device="cuda") -> torch.Tensor:

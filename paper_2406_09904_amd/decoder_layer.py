@@ -7,9 +7,18 @@ Run as a program it serves a few sessions on random weights: prompts in pieces, 
 """
 from __future__ import annotations
 
+import functools
+import typing
+
 import torch
 
 from . import binding as qqq
+
+
+@functools.lru_cache(maxsize=4096)
+def _workspace_sizes(rows, N, K):
+    """(bytes of a linear call's workspace, those of its part that is to be zero)"""
+    return max(qqq.qqq_linear_workspace_bytes(rows, N, K), 16), qqq.qqq_gemm_workspace_zero_bytes(rows, N, K)
 
 
 class _Linear:
@@ -19,18 +28,29 @@ class _Linear:
         self.N, self.K = weight.shape
         w_nat, self.scale = qqq.qqq_quantize_w4_perchannel(weight)
         self.packed = qqq.qqq_pack_w4(w_nat, self.K)
-        self._work = {}
+        self.empty = torch.empty((0,), dtype=torch.uint8, device=self.packed.device)
 
-    def _workspace(self, M):
-        if M not in self._work:
-            self._work[M] = qqq.new_linear_workspace(M, self.N, self.K)
-        return self._work[M]
+    def workspace(self, rows):
+        """Of a call with that many rows.  Its first part is to be zero, and every call leaves it so."""
+        nbytes, zero = _workspace_sizes(rows, self.N, self.K)
+        work = self.empty.new_empty(nbytes)
+        work[:zero].zero_()
+        return work
 
-    def of_codes(self, a_q, s_a):
-        return qqq.qqq_gemm_w4a8_perchannel(a_q, s_a, self.packed, self.scale, self._workspace(a_q.shape[0]))
+    def of_codes(self, a_q, s_a, workspace=None):
+        return qqq.qqq_gemm_w4a8_perchannel(a_q, s_a, self.packed, self.scale, self.workspace(a_q.shape[0]) if workspace is None else workspace)
 
-    def __call__(self, x):
-        return qqq.qqq_linear_w4a8_perchannel(x, self.packed, self.scale, self._workspace(x.shape[0]))
+    def __call__(self, x, workspace=None):
+        return qqq.qqq_linear_w4a8_perchannel(x, self.packed, self.scale, self.workspace(x.shape[0]) if workspace is None else workspace)
+
+
+class Workspaces(typing.NamedTuple):
+    """The linear calls' workspaces of steps of so many tokens (DecoderLayer.new_workspaces)."""
+    tokens: int
+    qkv: torch.Tensor
+    o: torch.Tensor
+    gate_up: torch.Tensor
+    down: torch.Tensor
 
 
 class DecoderLayer:
@@ -50,22 +70,30 @@ class DecoderLayer:
         a, b = x.float().chunk(2, dim=-1)
         return torch.cat((a * cos - b * sin, b * cos + a * sin), dim=-1).half()
 
-    def __call__(self, x, residual, cache: qqq.KV8Cache, batch: qqq.KV8Batch, positions):
+    def new_workspaces(self, tokens) -> Workspaces:
+        """For a program that keeps them over steps of `tokens` tokens, which saves each step their clearing.  They hold counters and partial sums: steps that may
+        run at the same time, on other streams or in other graphs, need workspaces of their own, and those of a graph are made outside of its capture."""
+        return Workspaces(tokens, *(m.workspace(tokens) for m in (self.qkv, self.o, self.gate_up, self.down)))
+
+    def __call__(self, x, residual, cache: qqq.KV8Cache, batch: qqq.KV8Batch, positions, workspaces: typing.Optional[Workspaces] = None):
         """x [tokens, hidden] fp16, the layer before's output, residual the stream that it is to be added to (None: x is the stream), positions [tokens]
-        -> (x, residual) for the next layer; the residual is updated in place."""
+        -> (x, residual) for the next layer; the residual is updated in place.  Without workspaces torch's allocator lends them for the call."""
         H, Hk, D = self.q_heads, self.kv_heads, self.head_dim
+        if workspaces is not None and workspaces.tokens != x.shape[0]:
+            raise ValueError("workspaces of %d tokens for %d" % (workspaces.tokens, x.shape[0]))
+        work = workspaces or Workspaces(x.shape[0], None, None, None, None)
         total, a_q, s_a = qqq.qqq_add_rmsnorm_quant(x, self.gain_attention, residual, self.eps, sum_out=residual)
         residual = x if total is None else total
-        qkv = self.qkv.of_codes(a_q, s_a).view(-1, H + 2 * Hk, D)
+        qkv = self.qkv.of_codes(a_q, s_a, work.qkv).view(-1, H + 2 * Hk, D)
         q, k = self.rotate(qkv[:, :H], positions), self.rotate(qkv[:, H:H + Hk], positions)
         qqq.qqq_kv8_append(cache, batch, k, qkv[:, H + Hk:])
         attended, _ = qqq.qqq_attention_kv8(cache, batch, q, window=self.window)
-        y = self.o(attended.view(-1, H * D))
+        y = self.o(attended.view(-1, H * D), work.o)
         residual, a_q, s_a = qqq.qqq_add_rmsnorm_quant(y, self.gain_ffn, residual, self.eps)
-        gate_up = self.gate_up.of_codes(a_q, s_a)
+        gate_up = self.gate_up.of_codes(a_q, s_a, work.gate_up)
         ffn = self.down.K
         a_q, s_a = qqq.qqq_gated_act_quant(gate_up[:, :ffn], gate_up[:, ffn:])
-        return self.down.of_codes(a_q, s_a), residual
+        return self.down.of_codes(a_q, s_a, work.down), residual
 
 
 def random_layer(hidden=4096, q_heads=32, kv_heads=8, head_dim=128, ffn=11008, seed=0, device="cuda", **more) -> DecoderLayer:
@@ -98,12 +126,13 @@ def main():
     # single tokens: one captured step, replayed
     x, residual = torch.randn(sessions, 4096, device="cuda").half(), torch.zeros(sessions, 4096, device="cuda").half()
     batch = qqq.KV8Batch(table, kv_len, torch.arange(sessions + 1, dtype=torch.int32, device="cuda"), None, 1, prompt + steps)
-    layer(x, residual.clone(), cache, batch._replace(kv_len=kv_len + 1), kv_len)   # (workspaces are made outside the graph; the step below writes the same token again)
+    work = layer.new_workspaces(sessions)   # (the graph's own)
+    layer(x, residual.clone(), cache, batch._replace(kv_len=kv_len + 1), kv_len, work)   # (once outside of the capture; the step below writes the same token again)
     torch.cuda.synchronize()
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
         kv_len += 1
-        y, stream = layer(x, residual, cache, batch, kv_len - 1)
+        y, stream = layer(x, residual, cache, batch, kv_len - 1, work)
     kv_len.fill_(prompt)
     start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
     start.record()

@@ -101,3 +101,83 @@ def test_residual_in_place_over_two_layers():
     torch.cuda.synchronize()
     assert r2.data_ptr() != r.data_ptr() and torch.equal(r, (kept.float() + y.float()).half())
     assert torch.isfinite(y2).all() and torch.isfinite(r2).all()
+
+
+def _token_step(layer, sessions, seed, past=30):
+    """A step of one token of each of some sessions behind a prompt -> what the layer is called with (the step can be repeated: it writes the same tokens again)."""
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    table, pages = dl.pages_in_order(sessions, 64, 16)
+    cache = qqq.new_kv8_cache(pages, HK, D, 16, sessions)
+    i32 = lambda v: torch.full((sessions,), v, dtype=torch.int32, device="cuda")  # noqa: E731
+    cu = torch.arange(sessions + 1, dtype=torch.int32, device="cuda")
+    kv = torch.randn(sessions * past, 2, HK, D, generator=gen, device="cuda").half()
+    qqq.qqq_kv8_append(cache, qqq.KV8Batch(table, i32(past), cu * past, None, past, 64), kv[:, 0], kv[:, 1])
+    x, residual = (torch.randn(sessions, HIDDEN, generator=gen, device="cuda").half() for _ in range(2))
+    return x, residual, cache, qqq.KV8Batch(table, i32(past + 1), cu, None, 1, 64), i32(past)
+
+
+def _run(layer, step, **more):
+    x, residual, cache, batch, positions = step
+    return layer(x, residual.clone(), cache, batch, positions, **more)
+
+
+def test_no_workspace_stays_behind():
+    """Steps of ever other numbers of rows leave nothing allocated."""
+    layer = dl.random_layer(HIDDEN, HQ, HK, D, FFN, seed=7)
+    steps = [_token_step(layer, n, n) for n in (1, 5, 20, 70, 150)]
+    _run(layer, steps[0])
+    torch.cuda.synchronize()
+    before = torch.cuda.memory_allocated()
+    for step in steps:
+        _run(layer, step)
+    torch.cuda.synchronize()
+    assert torch.cuda.memory_allocated() == before
+
+
+@pytest.mark.parametrize("sessions", [3, 16, 40])
+def test_steps_on_two_streams_at_once(sessions):
+    layer = dl.random_layer(HIDDEN, HQ, HK, D, FFN, seed=8)
+    steps = [_token_step(layer, sessions, seed) for seed in (1, 2)]
+    want = [_run(layer, s) for s in steps]
+    kept = [layer.new_workspaces(sessions) for _ in steps]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in steps]
+    got = [[], []]
+    for turn in range(10):
+        for i, stream in enumerate(streams):
+            with torch.cuda.stream(stream):
+                got[i].append(_run(layer, steps[i], workspaces=kept[i] if turn % 2 else None))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for y, r in got[i]:
+            assert torch.equal(y, want[i][0]) and torch.equal(r, want[i][1])
+
+
+@pytest.mark.parametrize("sessions,keep", [(4, False), (4, True), (24, False), (100, False)])
+def test_a_captured_step_between_eager_ones(sessions, keep):
+    """A number of rows that is first met inside of a capture; eager steps of as many before the first replay and between the others."""
+    layer = dl.random_layer(HIDDEN, HQ, HK, D, FFN, seed=9)
+    step, other = _token_step(layer, sessions, 3), _token_step(layer, sessions + 1, 4)
+    x, residual, cache, batch, positions = step
+    work = layer.new_workspaces(sessions) if keep else None
+    into = residual.clone()
+    _run(layer, other)   # (another number of rows: torch's own libraries are ready)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        into.copy_(residual)
+        y, r = layer(x, into, cache, batch, positions, work)
+    want_y, want_r = _run(layer, step)
+    torch.cuda.synchronize()
+    for _ in range(4):
+        graph.replay()
+        again = _run(layer, step)
+        torch.cuda.synchronize()
+        assert torch.equal(y, want_y) and torch.equal(r, want_r)
+        assert torch.equal(again[0], want_y) and torch.equal(again[1], want_r)
+
+
+def test_workspaces_of_another_number_of_tokens_are_refused():
+    layer = dl.random_layer(HIDDEN, HQ, HK, D, FFN, seed=10)
+    with pytest.raises(ValueError):
+        _run(layer, _token_step(layer, 3, 5), workspaces=layer.new_workspaces(4))
