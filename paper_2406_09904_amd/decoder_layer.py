@@ -77,7 +77,8 @@ class DecoderLayer:
 
     def __call__(self, x, residual, cache: qqq.KV8Cache, batch: qqq.KV8Batch, positions, workspaces: typing.Optional[Workspaces] = None):
         """x [tokens, hidden] fp16, the layer before's output, residual the stream that it is to be added to (None: x is the stream), positions [tokens]
-        -> (x, residual) for the next layer; the residual is updated in place.  Without workspaces torch's allocator lends them for the call."""
+        -> (x, residual) for the next layer, the residual a new tensor; the one that was given holds its sum with x then, without what attention adds.
+        Without workspaces torch's allocator lends them for the call."""
         H, Hk, D = self.q_heads, self.kv_heads, self.head_dim
         if workspaces is not None and workspaces.tokens != x.shape[0]:
             raise ValueError("workspaces of %d tokens for %d" % (workspaces.tokens, x.shape[0]))
