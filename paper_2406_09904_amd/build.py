@@ -13,14 +13,13 @@ LIB = os.path.join(HERE, "libqqq.so")
 SOURCES = ["qqq_api.hip", "qqq_pack.hip", "qqq_quant_act.hip", "qqq_gemm_skinny.hip",
            "qqq_gemm_prefill_dma.hip", "qqq_gemm_prefill_ring.hip", "qqq_group_bias.hip", "qqq_quant_weight.hip", "qqq_probes.hip", "qqq_calib.hip",
            "qqq_hessian.hip", "qqq_compensate.hip", "qqq_layer_api.hip", "qqq_layer_rows.hip", "qqq_kv8_cache.hip", "qqq_attention_kv8.hip"]
+# The last flag but the include paths: by default the compiler leaves out the restoring of the execution mask at the end of a branch that ends together with the
+# one around it.  Where registers are short it then puts a copy of a live value into that place, for the lanes of the inner branch only: attention with 32
+# rows of heads of 256 in equal shares lost a zero in the other lanes so, and stored to an address made with what was there instead.  No other kernel's assembly
+# had such a copy; all are compiled without the omission, which changes no time and no result of theirs (the twelve cases of perf/cases.py).
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
-         "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
+         "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-mllvm", "-amdgpu-remove-redundant-endcf=0",
          "-I", os.path.join(ROOT, "include"), "-I", CSRC]
-# By default the compiler leaves out the restoring of the execution mask at the end of a branch that ends together with the one around it.  Where registers are
-# short it then puts a copy of a live value into that place, for the lanes of the inner branch only: attention with 32 rows of heads of 256 in equal shares
-# lost a zero in the other lanes so, and stored to an address made with what was there instead.
-LAYER_FLAGS = ["-mllvm", "-amdgpu-remove-redundant-endcf=0"]
-FLAGS_OF = {src: LAYER_FLAGS for src in ("qqq_layer_rows.hip", "qqq_kv8_cache.hip", "qqq_attention_kv8.hip")}
 
 
 def hipcc() -> str:
@@ -70,7 +69,7 @@ def build(verbose: bool = False, extra_flags=(), out_dir: str = None) -> str:
 
     def one(src):
         obj = os.path.join(objdir, src.replace(".hip", ".o"))
-        cmd = [cc, *FLAGS, *FLAGS_OF.get(src, ()), *extra_flags, "-c", os.path.join(CSRC, src), "-o", obj]
+        cmd = [cc, *FLAGS, *extra_flags, "-c", os.path.join(CSRC, src), "-o", obj]
         r = subprocess.run(cmd, capture_output=True, text=True)
         out = "\n".join(l for l in (r.stdout + r.stderr).splitlines()
                         if "packed-fp32-ops" not in l)
