@@ -98,6 +98,22 @@ def test_append_in_pieces(dim, page):
         w.check_tokens(length)
 
 
+@pytest.mark.parametrize("dim,page", SHAPES)
+def test_tail_slots_hold_the_open_pages_tokens(dim, page):
+    """Bit for bit, of what is in the slot: the tokens of the page that is not full."""
+    steps = [[1, page - 1, 3], [page - 1, 2, page], [5, 0, page - 4], [1, page, 2 * page + 7]]
+    w = Both(dim * page, [sum(s[b] for s in steps) for b in range(3)], 2, dim, page)
+    length = [0] * 3
+    for new in steps:
+        length = [a + n for a, n in zip(length, new)]
+        w.append(length, new)
+        k_tail, v_tail = w.dev.k_tail.cpu().numpy(), w.dev.v_tail.cpu().numpy()
+        for b, slot in enumerate(w.slots):
+            held = length[b] % page
+            assert np.array_equal(k_tail[slot, :, :held], w.host.k_tail[slot, :, :held]), (b, length)
+            assert np.array_equal(v_tail[slot, :, :, :held], w.host.v_tail[slot, :, :, :held]), (b, length)
+
+
 def test_append_values_that_are_not_finite():
     """A NaN is held as 0, an infinity as the largest value, closed or not; other tokens of the page keep their values' scale."""
     w = Both(3, [40], 2, 64, 16)

@@ -70,6 +70,13 @@ def test_norm(M, K, residual):
     assert np.all(np.abs(got - y) <= np.abs(y) * (2 ** -11 + REL) + 2 ** -25)
 
 
+@pytest.mark.parametrize("residual", ["none", "fp16", "fp32"])
+@pytest.mark.parametrize("M,K", [(300, 5128), (300, 8192), (280, 12296), (280, 16384)])
+def test_norm_of_more_rows_than_compute_units(M, K, residual):
+    """Rows of more than 4096 values, four vectors a thread: prompts of the larger models."""
+    test_norm(M, K, residual)
+
+
 def test_norm_sum_in_the_residuals_place():
     rng = np.random.default_rng(5)
     for K in (1024, 40000):
@@ -111,6 +118,12 @@ def test_gated(M, F, act):
     a_q, s_a = qqq.qqq_gated_act_quant(d[:, :F], d[:, F:], act)
     torch.cuda.synchronize()
     _check_codes(y, a_q, s_a, 127 * REL)
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu_tanh"])
+@pytest.mark.parametrize("M,F", [(7, 2056), (300, 4096), (5, 4104), (300, 8192), (3, 8200)])
+def test_gated_rows_of_every_length_class(M, F, act):
+    test_gated(M, F, act)
 
 
 def test_gated_products_past_fp16_and_rows_of_nothing():
