@@ -203,8 +203,8 @@ __device__ __forceinline__ Share share_of(const AttnParams& p, int w) {
 //
 // Bound by the cache's bytes: every code is read once, straight into registers, and used by up to 16 * NT rows; a wave takes every fourth
 // tile of its workgroup's chunk by itself, the waves' results are joined through LDS.  One token of a session of 131000, 8 heads of 128
-// read by 64: 47 us, 5.7 TB/s (a plain read stream reaches 6.2); of 48 sessions of 17 to 8000: 75 us, 5.3 TB/s, the rest being where a share
-// goes from one sequence to the next.  A short past is latency: 500 tokens 7.4 us, of which 2.2 are an empty launch, and 0.3 a tile; with eight waves
+// read by 64: 48 us, 5.6 TB/s (a plain read stream reaches 6.2); of 48 sessions of 17 to 8000: 77 us, 5.2 TB/s, the rest being where a share
+// goes from one sequence to the next.  A short past is latency: 500 tokens 7.8 to 8.1 us, of which 1.6 are an empty launch, and 0.3 a tile; with eight waves
 // instead of four, so that no wave has two tiles, 8.5, since a compute unit's four SIMDs issue the same instructions either way.
 // A tile of 64 tokens, 16 x 16 x 32 products.  Lane l = 16 g + n.  S^T: operand row r of 16-token subtile t is token
 // 16 (r / 4) + 4 t + r % 4, so that lane (g, n) gets the scores of row n with tokens 16 g + 4 t + i, i = 0..3: over t, the 16 tokens
@@ -501,9 +501,9 @@ __global__ __launch_bounds__(kRowsThreads, D <= 128 ? 2 : 1) void attn_rows_kern
 // 128 rows of one key/value head (tokens times the heads that share it) a workgroup, 32 a wave, over tiles of 64 tokens that the
 // workgroup converts to fp16 in LDS once for its four waves (two buffers, one barrier a tile, the next tile's codes on their way
 // meanwhile).  A prompt of 8000 tokens, 64 heads of 128 over 8: 1.07 to 1.13 ms, 930 to 980 TFLOP/s, where a large library product of
-// fp16 reaches 1411.  Bound by the power that the matrix instructions draw together with the exponentials beside them: the same
-// instructions on data of zeros take 0.88 ms.  Heads of 64 have twice the exponentials for a product: 660 TFLOP/s; heads of 256 fit but one wave
-// a SIMD: 620.  64 rows a wave (accumulators in the other register file, and copies to and fro) took 1.41 ms, values straight from memory
+// fp16 reaches 1411.  The matrix units are busy half of the cycles: the exponentials and conversions beside them take their issue.  Power is the rest: the
+// same instructions on data of zeros take 0.88 ms.  Heads of 64 have twice the exponentials for a product: 800 TFLOP/s; heads of 256 (32 over 4) fit but one wave
+// a SIMD, with 60 to 70 registers spilled and copies between the register files: 710.  64 rows a wave (accumulators in the other register file, and copies to and fro) took 1.41 ms, values straight from memory
 // instead of through LDS 2.6 (spilled), the two products of neighbouring tiles interleaved 1.21.
 // 32 x 32 x 16 products, lane l = 32 h + n.  S^T: operand row r of a 32-token subtile is token 16 (r / 16) + 8 ((r / 4) % 2) + 4 ((r / 8) % 2)
 // + r % 4, so that lane (h, n) gets the scores of row n with tokens 16 s + 8 h + 0..7 in registers 8 s .. 8 s + 7: its operand of step s

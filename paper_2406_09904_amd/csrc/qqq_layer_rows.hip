@@ -7,8 +7,8 @@
 // h gain is exact in fp32 where h is fp16 (11 + 11 bits).
 //
 // Both are bound by their bytes from some hundred rows on, below that by how soon a row is done (a launch from a graph alone is 1.6 us).
-// Norm, fp16 residual, codes: M = 1, K = 4096 2.7 us; M = 777, K = 5120 6.2; M = 4096, K = 8192 37 to 44 (5.3 to 6.3 TB/s, by what the last-level
-// cache still holds); fp32 residual, fp16 output: M = 777, K = 5120 9.4, M = 4096, K = 8192 66.  Gated activation: M = 16, F = 11008 3.7 us;
+// Norm, fp16 residual, codes: M = 1, K = 4096 2.2 to 2.4 us; M = 777, K = 5120 6.2; M = 4096, K = 8192 37 to 44 (5.3 to 6.3 TB/s, by what the last-level
+// cache still holds); fp32 residual, fp16 output: M = 777, K = 5120 9.7 to 10.8, M = 4096, K = 8192 66.  Gated activation: M = 16, F = 11008 3.8 to 4.0 us;
 // M = 4096, F = 28672 108 (5.4 TB/s).
 //
 // Inputs are read past the caches (qqq_past.h) where all operands are more than the last of them: gated activation, M = 4096, F = 28672 (587 MB)

@@ -5,8 +5,8 @@
 
 namespace qqq {
 
-// A call whose operands are more than the last-level cache reads its inputs past it: none of them can be there still, and what it writes then
-// is, for the call that reads that.
+// A call of the norm, the activation or the cache (append, read) whose operands are more than the last-level cache reads its inputs past it: none of them can be
+// there still, and what it writes then is, for the call that reads that.  (Attention over few rows has a rule of its own, by how it splits the keys: see plan_of.)
 constexpr int64_t kLastCacheBytes = 256 << 20;
 
 typedef uint32_t u2v __attribute__((ext_vector_type(2)));
