@@ -1,0 +1,68 @@
+/*
+ * qqq_serve.h — C ABI of the two ends of a serving step, before the first decoder layer and behind the last, MI355X (gfx950):
+ *
+ *   what sessions hold and bring --qqq_kv8_plan--> page tables, lengths, places of the rows (the qqq_kv8_batch of qqq_layer.h); --qqq_kv8_release--> pages free again
+ *
+ * Conventions as in qqq.h: every pointer inside is a DEVICE pointer owned by the caller, `stream` is a hipStream_t passed as void*, a call only enqueues
+ * kernels, never allocates, synchronises or throws; return QQQ_OK or an error code with nothing enqueued.  Forward only: the path serves quantised
+ * weights, nothing on it has a gradient.  Results do not depend on the order in which workgroups run.
+ */
+#ifndef QQQ_SERVE_H_
+#define QQQ_SERVE_H_
+
+#include "qqq_layer.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/*
+ * What a program keeps of its sessions on the GPU, so that a step's tables can be made there (and a captured step replayed) without the host.
+ *   pages [sessions, pages_stride] int32: the first held / page_tokens of a row's `columns` entries are the session's closed pages in order
+ *   held [sessions] int32: tokens in the cache
+ *   free_pages [pool] int32, free_count [1] int32: the pages that no session has, a stack; the last of the first free_count entries is taken first
+ *   held_after, free_count_after: where a call writes what holds after it; the same pointers, or others (then held and free_count stay as they are, and of
+ *   held_after only the step's sessions are written)
+ * All 4-byte aligned.  page_tokens 16, 32 or 64, as in qqq_kv8_cache.  The struct is a host struct, read before the call returns.
+ */
+typedef struct qqq_kv8_sessions {
+  int32_t* pages;
+  int64_t pages_stride;
+  const int32_t* held;
+  int32_t* held_after;
+  int32_t* free_pages;
+  const int32_t* free_count;
+  int32_t* free_count_after;
+  int64_t pool;
+  int32_t sessions, columns, page_tokens;
+} qqq_kv8_sessions;
+
+/*
+ * The tables of a step in which sequence b is session batch->slots[b] (slots NULL: session b) and brings new_tokens[b] tokens, in the order of the sequences:
+ *   n_b = new_tokens[b], cut to 0 .. max_new, to max_len - held and to the rows that are left;  len_b = held + n_b;  cu[b] = n_0 + .. + n_(b-1)
+ *   fresh_b = len_b / page_tokens - held / page_tokens pages come from the stack's top, the first sequence's first
+ * Written: batch->kv_len [sequences], batch->cu [sequences + 1], batch->page_table (of row b the first len_b / page_tokens entries: the session's pages, then the
+ * fresh ones), the fresh ones in sessions->pages too, held_after, free_count_after, and, where they are not NULL,
+ *   sequence [tokens], positions [tokens] int32: of each row its sequence in the step and its place in it, held .. len_b - 1; rows behind cu[sequences] are left as they are
+ *   lacking [1] int32: pages that were wanted and not there.  Their entries are -1, which is no page: append drops what it would write to them, so a program
+ *   gives up or repeats that step's last sequences.  One that admits no more than free_count covers never sees it.
+ * batch is a qqq_kv8_batch as the calls of qqq_layer.h take it, its tensors written here.  page_table may be sessions->pages itself (with its stride) where slots is NULL;
+ * no other outputs may overlap.  max_len / page_tokens <= columns of both tables.  A session that does not exist brings nothing; one that is there twice, or held and free_count
+ * that are out of bounds, give wrong tables, never an access outside.
+ *   workspace: qqq_kv8_plan_workspace_bytes() bytes, 4-byte aligned, contents irrelevant on entry; not shared by calls that may run concurrently.
+ */
+size_t qqq_kv8_plan_workspace_bytes(const qqq_kv8_sessions* sessions, const qqq_kv8_batch* batch);
+int qqq_kv8_plan(const qqq_kv8_sessions* sessions, const qqq_kv8_batch* batch, const int32_t* new_tokens, int64_t tokens,
+                 int32_t* sequence, int32_t* positions, int32_t* lacking, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Sessions ids[0 .. count-1] (NULL: 0 .. count-1) end: their pages go to the stack in that order, a session's in their own, and they hold nothing.  In place only: held_after is
+ * held and free_count_after is free_count.  Entries that are no page (-1) are dropped, and so is what the stack has no room for; a session that does not exist
+ * is skipped, one that is there twice is released once.
+ */
+int qqq_kv8_release(const qqq_kv8_sessions* sessions, const int32_t* ids, int64_t count, void* stream);
+
+#ifdef __cplusplus
+}
+#endif
+#endif /* QQQ_SERVE_H_ */

@@ -1,5 +1,6 @@
 """Thin ctypes binding over libqqq.so (the C ABI declared in include/qqq.h; the offline stage in include/qqq_calib.h, what lies
-between a decoder layer's linear calls in include/qqq_layer.h, tuning and diagnostic controls in include/qqq_tuning.h).
+between a decoder layer's linear calls in include/qqq_layer.h, the two ends of a serving step in include/qqq_serve.h, tuning and diagnostic
+controls in include/qqq_tuning.h).
 
 Argument marshalling only: every step of the path runs in the library's HIP kernels.  PyTorch
 supplies device memory and the stream.  There is no CPU fallback: if the library is missing or a
@@ -39,6 +40,11 @@ SYMBOLS = [
 LAYER_SYMBOLS = [
     "qqq_add_rmsnorm", "qqq_add_rmsnorm_quant", "qqq_gated_act_quant", "qqq_kv8_append", "qqq_kv8_read",
     "qqq_attention_kv8_workspace_bytes", "qqq_attention_kv8",
+]
+
+# the entry points of include/qqq_serve.h
+SERVE_SYMBOLS = [
+    "qqq_kv8_plan_workspace_bytes", "qqq_kv8_plan", "qqq_kv8_release",
 ]
 
 _lib = None
@@ -148,6 +154,10 @@ def lib():
         L.qqq_attention_kv8_workspace_bytes.argtypes = [vp, vp, ci, i64]
         L.qqq_attention_kv8_workspace_bytes.restype = sz
         L.qqq_attention_kv8.argtypes = [vp, vp, vp, i64, i64, ci, i64, cf, ci, ci, vp, vp, vp, sz, vp]
+        L.qqq_kv8_plan_workspace_bytes.argtypes = [vp, vp]
+        L.qqq_kv8_plan_workspace_bytes.restype = sz
+        L.qqq_kv8_plan.argtypes = [vp, vp, vp, i64, vp, vp, vp, vp, sz, vp]
+        L.qqq_kv8_release.argtypes = [vp, vp, i64, vp]
         _load_native(L)
         _lib = L
     return _lib
@@ -712,6 +722,105 @@ def qqq_attention_kv8(cache: KV8Cache, batch: KV8Batch, q, scale=None, causal=Tr
                                _ptr(out, _F16), None if lse is None else _ptr(lse, torch.float32), _ptr(workspace, _U8),
                                0 if workspace is None else workspace.numel(), _stream()))
     return out, lse
+
+
+# ---- the two ends of a serving step (include/qqq_serve.h): tables made on the GPU, the int8 product of the output head, log probabilities
+
+def _here(*tensors):
+    """The calls run on the current device's current stream: a tensor of another device is refused, as one of the host is."""
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.get_device() != _device()):
+            raise ValueError("libqqq takes tensors of the current device only")
+
+
+def _row_stride(t):
+    """Of a 2-D tensor; of one row or none it may be anything."""
+    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], t.stride(0))
+
+
+class KV8Sessions(typing.NamedTuple):
+    """What a program keeps of its sessions on the GPU (layout: include/qqq_serve.h)."""
+    pages: torch.Tensor       # int32 [sessions, columns]: each session's closed pages in order
+    held: torch.Tensor        # int32 [sessions]: tokens in the cache
+    free: torch.Tensor        # int32 [pages]: the pages that no session has, a stack
+    free_count: torch.Tensor  # int32 [1]: its height
+
+
+def new_kv8_sessions(sessions, columns, pages, device="cuda") -> KV8Sessions:
+    """Sessions that hold nothing, over a cache of that many pages (taken from page 0 on)."""
+    i32 = lambda *s: torch.zeros(s, dtype=_I32, device=device)  # noqa: E731
+    return KV8Sessions(i32(sessions, columns), i32(sessions), torch.arange(pages - 1, -1, -1, dtype=_I32, device=device),
+                       torch.full((1,), pages, dtype=_I32, device=device))
+
+
+def new_kv8_batch(sequences, columns, max_new, max_len, slots=None, device="cuda") -> KV8Batch:
+    """For qqq_kv8_plan to fill; slots: the step's sessions, int32 [sequences] (None: session b is sequence b)."""
+    i32 = lambda *s: torch.zeros(s, dtype=_I32, device=device)  # noqa: E731
+    return KV8Batch(i32(sequences, columns), i32(sequences), i32(sequences + 1), slots, max_new, max_len)
+
+
+class _Sessions(ctypes.Structure):
+    _fields_ = [("pages", ctypes.c_void_p), ("pages_stride", ctypes.c_int64)] + [
+        (n, ctypes.c_void_p) for n in ("held", "held_after", "free_pages", "free_count", "free_count_after")] + [("pool", ctypes.c_int64)] + [
+        (n, ctypes.c_int32) for n in ("sessions", "columns", "page_tokens")]
+
+
+def _sessions_struct(sessions, page_tokens, after=None):
+    pages, held, free, count = sessions
+    held_after, count_after = (held, count) if after is None else after
+    _here(pages, held, free, count, held_after, count_after)
+    if pages.dim() != 2 or pages.dtype != _I32 or (pages.numel() and pages.stride(1) != 1):
+        raise ValueError("pages must be a 2-D int32 device tensor with unit inner stride")
+    S, columns = pages.shape
+    if held.shape != (S,) or held_after.shape != (S,) or free.dim() != 1 or count.numel() != 1 or count_after.numel() != 1:
+        raise ValueError("held must be of pages' %d sessions, free 1-D, free_count one number" % S)
+    return _Sessions(pages.data_ptr(), _row_stride(pages), _ptr(held, _I32), _ptr(held_after, _I32),
+                     _ptr(free, _I32), _ptr(count, _I32), _ptr(count_after, _I32), free.numel(), S, columns, page_tokens)
+
+
+def qqq_kv8_plan(sessions: KV8Sessions, batch: KV8Batch, new, page_tokens, sequence=None, positions=None, lacking=None, after=None, tokens=None, workspace=None) -> KV8Batch:
+    """Fills batch (page_table, kv_len, cu) for a step in which sequence b is session batch.slots[b] and brings new[b] tokens (int32 [sequences]), and takes their pages.
+    sequence, positions: int32 [tokens], of each row its sequence and its position; lacking: int32 [1], pages that were not there.  tokens: rows of the
+    step's tensors, where neither is given (none: as many as come).  after: (held, free_count) of after the step in tensors of their own; without it in place.  workspace: a
+    uint8 tensor of qqq_kv8_plan_workspace_bytes(); without one torch's allocator lends it."""
+    s = _sessions_struct(sessions, page_tokens, after)
+    table, kv_len, cu, slots, max_new, max_len = batch
+    _here(table, kv_len, cu, slots, new, sequence, positions, lacking, workspace)
+    if table.dim() != 2 or table.dtype != _I32 or (table.numel() and table.stride(1) != 1):
+        raise ValueError("page_table must be a 2-D int32 device tensor with unit inner stride")
+    B = table.shape[0]
+    if kv_len.shape != (B,) or cu.shape != (B + 1,) or new.shape != (B,) or (slots is not None and slots.shape != (B,)):
+        raise ValueError("kv_len, cu, slots and new must be of page_table's %d sequences" % B)
+    for t in (sequence, positions):
+        if t is not None and (t.dim() != 1 or (tokens is not None and t.numel() != tokens)):
+            raise ValueError("sequence and positions must be 1-D, of the step's rows")
+        tokens = t.numel() if t is not None else tokens
+    if lacking is not None and lacking.numel() != 1:
+        raise ValueError("lacking must be one number")
+    b = _Batch(table.data_ptr(), _row_stride(table), _ptr(kv_len, _I32), _ptr(cu, _I32), _ptr(slots, _I32), table.shape[1], B, max_new, max_len)
+    L = lib()
+    if workspace is None:
+        nbytes = L.qqq_kv8_plan_workspace_bytes(ctypes.byref(s), ctypes.byref(b))
+        workspace = torch.empty((nbytes,), dtype=_U8, device=table.device) if nbytes else None
+    _check(L.qqq_kv8_plan(ctypes.byref(s), ctypes.byref(b), _ptr(new, _I32), 1 << 30 if tokens is None else tokens, _ptr(sequence, _I32), _ptr(positions, _I32),
+                          _ptr(lacking, _I32), _ptr(workspace, _U8), 0 if workspace is None else workspace.numel(), _stream()))
+    return batch
+
+
+def qqq_kv8_plan_workspace_bytes(sessions: KV8Sessions, batch: KV8Batch, page_tokens: int) -> int:
+    s, table = _sessions_struct(sessions, page_tokens), batch.page_table
+    b = _Batch(None, _row_stride(table), None, None, None if batch.slots is None else batch.slots.data_ptr(), table.shape[1], table.shape[0], batch.max_new,
+               batch.max_len)
+    return int(lib().qqq_kv8_plan_workspace_bytes(ctypes.byref(s), ctypes.byref(b)))
+
+
+def qqq_kv8_release(sessions: KV8Sessions, page_tokens, ids=None):
+    """Sessions ids (int32 [count]; None: all) end: their pages are free again and they hold nothing."""
+    s = _sessions_struct(sessions, page_tokens)
+    _here(ids)
+    if ids is not None and ids.dim() != 1:
+        raise ValueError("ids must be 1-D")
+    _check(lib().qqq_kv8_release(ctypes.byref(s), _ptr(ids, _I32), sessions.held.numel() if ids is None else ids.numel(), _stream()))
 
 
 def last_route() -> str:

@@ -1,0 +1,124 @@
+// C-ABI entry points of qqq_serve.h: argument validation (host code only).
+#include "qqq_plan.h"
+#include "qqq_serve.h"
+
+namespace qqq {
+namespace {
+
+constexpr int64_t kMost = 1 << 30;  // tokens of a sequence, rows of a call, pages: places stay in 32 bits
+
+bool aligned(const void* p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
+
+int check_sessions(const char* name, const qqq_kv8_sessions* s) {
+  if (!s) return set_error(QQQ_ERR_NULL, "%s: NULL struct", name);
+  if ((s->page_tokens != 16 && s->page_tokens != 32 && s->page_tokens != 64) || s->sessions < 1 || s->columns < 0 || s->pages_stride < s->columns ||
+      s->pool < 0 || s->pool > kMost)
+    return set_error(QQQ_ERR_SHAPE, "%s: unsupported sessions: %d of %d page columns of stride %lld, pages of %d tokens, a stack of %lld", name, s->sessions,
+                     s->columns, (long long)s->pages_stride, s->page_tokens, (long long)s->pool);
+  return QQQ_OK;
+}
+int check_session_pointers(const char* name, const qqq_kv8_sessions* s) {
+  if (!s->held || !s->held_after || !s->free_count || !s->free_count_after || (s->columns > 0 && !s->pages) || (s->pool > 0 && !s->free_pages))
+    return set_error(QQQ_ERR_NULL, "%s: NULL pointer in a struct", name);
+  if (!aligned(s->pages, 4) || !aligned(s->held, 4) || !aligned(s->held_after, 4) || !aligned(s->free_pages, 4) || !aligned(s->free_count, 4) ||
+      !aligned(s->free_count_after, 4))
+    return set_error(QQQ_ERR_SHAPE, "%s: misaligned pointer in a struct", name);
+  return QQQ_OK;
+}
+int check_plan(const char* name, const qqq_kv8_sessions* s, const qqq_kv8_batch* b) {
+  if (int rc = check_sessions(name, s)) return rc;
+  if (!b) return set_error(QQQ_ERR_NULL, "%s: NULL struct", name);
+  if (b->sequences < 0 || b->max_new < 0 || b->max_new > kMost || b->max_len < 0 || b->max_len > kMost || b->columns < 0 || b->table_stride < b->columns ||
+      b->max_len / s->page_tokens > b->columns || b->max_len / s->page_tokens > s->columns)
+    return set_error(QQQ_ERR_SHAPE, "%s: unsupported batch: %d sequences, at most %d new of %d tokens, %d page columns of stride %lld (the sessions' table: %d)", name,
+                     b->sequences, b->max_new, b->max_len, b->columns, (long long)b->table_stride, s->columns);
+  if (!b->slots && b->sequences > s->sessions) return set_error(QQQ_ERR_SHAPE, "%s: %d sequences of %d sessions", name, b->sequences, s->sessions);
+  return QQQ_OK;
+}
+PlanArgs session_args(const qqq_kv8_sessions* s) {
+  PlanArgs p = {};
+  p.pages = s->pages;
+  p.pages_stride = s->pages_stride;
+  p.held = s->held;
+  p.free_pages = s->free_pages;
+  p.free_count = s->free_count;
+  p.held_after = s->held_after;
+  p.free_count_after = s->free_count_after;
+  p.free_out = s->free_pages;
+  p.pool = (int32_t)s->pool;
+  p.sessions = s->sessions;
+  p.columns = s->columns;
+  p.shift = s->page_tokens == 16 ? 4 : s->page_tokens == 32 ? 5 : 6;
+  return p;
+}
+// The call's arguments but for the rows, which the workspace does not depend on
+PlanArgs plan_args(const qqq_kv8_sessions* s, const qqq_kv8_batch* b) {
+  PlanArgs p = session_args(s);
+  p.ids = b->slots;
+  p.table = const_cast<int32_t*>(b->page_table);
+  p.table_stride = b->table_stride;
+  p.kv_len = const_cast<int32_t*>(b->kv_len);
+  p.cu = const_cast<int32_t*>(b->cu);
+  p.sequences = b->sequences;
+  p.max_new = b->max_new;
+  p.max_len = b->max_len;
+  p.same_table = b->page_table == s->pages;
+  return p;
+}
+
+}  // namespace
+}  // namespace qqq
+
+using namespace qqq;
+
+extern "C" {
+
+size_t qqq_kv8_plan_workspace_bytes(const qqq_kv8_sessions* sessions, const qqq_kv8_batch* batch) {
+  if (check_plan("qqq_kv8_plan_workspace_bytes", sessions, batch)) return 0;
+  return kv8_plan_bytes(plan_args(sessions, batch));
+}
+
+int qqq_kv8_plan(const qqq_kv8_sessions* sessions, const qqq_kv8_batch* batch, const int32_t* new_tokens, int64_t tokens, int32_t* sequence,
+                 int32_t* positions, int32_t* lacking, void* workspace, size_t workspace_bytes, void* stream) {
+  const char* name = "qqq_kv8_plan";
+  if (int rc = check_plan(name, sessions, batch)) return rc;
+  if (tokens < 0 || tokens > kMost) return set_error(QQQ_ERR_SHAPE, "%s: %lld rows", name, (long long)tokens);
+  if (int rc = check_session_pointers(name, sessions)) return rc;
+  if (!batch->cu || (batch->sequences > 0 && (!batch->kv_len || !new_tokens || (!batch->page_table && batch->max_len >= sessions->page_tokens))))
+    return set_error(QQQ_ERR_NULL, "%s: NULL pointer", name);
+  if (!aligned(batch->page_table, 4) || !aligned(batch->kv_len, 4) || !aligned(batch->cu, 4) || !aligned(batch->slots, 4) || !aligned(new_tokens, 4) ||
+      !aligned(sequence, 4) || !aligned(positions, 4) || !aligned(lacking, 4) || !aligned(workspace, 4))
+    return set_error(QQQ_ERR_SHAPE, "%s: misaligned pointer", name);
+  PlanArgs p = plan_args(sessions, batch);
+  if (p.same_table && p.table && (p.ids || p.table_stride != p.pages_stride))
+    return set_error(QQQ_ERR_SHAPE, "%s: the sessions' own table with %s", name, p.ids ? "slots" : "another stride");
+  p.new_tokens = new_tokens;
+  p.tokens = (int32_t)tokens;
+  p.sequence = sequence;
+  p.positions = positions;
+  p.lacking = lacking;
+  p.top = static_cast<int32_t*>(workspace);
+  const size_t need = kv8_plan_bytes(p);
+  if (need && (!workspace || workspace_bytes < need))
+    return set_error(QQQ_ERR_WORKSPACE, "%s: workspace %zu bytes < %zu needed", name, workspace ? workspace_bytes : 0, need);
+  route_reset();
+  return launch_kv8_plan(p, (hipStream_t)stream);
+}
+
+int qqq_kv8_release(const qqq_kv8_sessions* sessions, const int32_t* ids, int64_t count, void* stream) {
+  const char* name = "qqq_kv8_release";
+  if (int rc = check_sessions(name, sessions)) return rc;
+  if (count < 0 || count > kMost || (!ids && count > sessions->sessions)) return set_error(QQQ_ERR_SHAPE, "%s: %lld of %d sessions", name, (long long)count, sessions->sessions);
+  if (count == 0) return QQQ_OK;
+  if (int rc = check_session_pointers(name, sessions)) return rc;
+  if (!aligned(ids, 4)) return set_error(QQQ_ERR_SHAPE, "%s: misaligned pointer", name);
+  if (sessions->held != sessions->held_after || sessions->free_count != sessions->free_count_after)
+    return set_error(QQQ_ERR_SHAPE, "%s: not in place", name);
+  PlanArgs p = session_args(sessions);
+  p.ids = ids;
+  p.sequences = (int32_t)count;
+  route_reset();
+  return launch_kv8_release(p, (hipStream_t)stream);
+}
+
+}  // extern "C"

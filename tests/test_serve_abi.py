@@ -1,0 +1,94 @@
+"""CPU-only checks of include/qqq_serve.h's boundary: exports, and arguments that are refused on the host before anything is enqueued."""
+import ctypes
+import os
+import re
+
+import pytest
+import torch
+
+from paper_2406_09904_amd import binding
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+BAD = ctypes.c_void_p(0x1000)   # never dereferenced: every call below fails validation, or has nothing to do
+NULL, SHAPE, WORKSPACE = 1, 2, 3
+
+
+@pytest.fixture(scope="module")
+def L():
+    if not os.path.exists(binding.LIB_PATH):
+        from paper_2406_09904_amd import build
+        build.build()
+    return binding.lib()
+
+
+def test_header_functions_are_exported(L):
+    src = re.sub(r"/\*.*?\*/", "", open(os.path.join(ROOT, "include", "qqq_serve.h")).read(), flags=re.S)
+    names = sorted(set(re.findall(r"\b(qqq_[a-z0-9_]+)\s*\(", src)))
+    assert names == sorted(binding.SERVE_SYMBOLS)
+    for n in names:
+        assert hasattr(L, n), n
+
+
+def _sessions(**more):
+    s = dict(pages=0x1000, pages_stride=4, held=0x1000, held_after=0x1000, free_pages=0x1000, free_count=0x1000, free_count_after=0x1000, pool=10, sessions=3, columns=4,
+             page_tokens=32)
+    s.update(more)
+    return binding._Sessions(**s)
+
+
+def _batch(**more):
+    b = dict(page_table=0x2000, table_stride=4, kv_len=0x1000, cu=0x1000, slots=None, columns=4, sequences=2, max_new=3, max_len=4 * 32 + 31)
+    b.update(more)
+    return binding._Batch(**b)
+
+
+def _plan(L, s, b, new=BAD, tokens=6, sequence=BAD, positions=BAD, lacking=BAD, work=BAD, nbytes=1 << 20):
+    return L.qqq_kv8_plan(ctypes.byref(s) if s is not None else None, ctypes.byref(b) if b is not None else None, new, tokens, sequence, positions, lacking, work, nbytes, None)
+
+
+SESSION_REFUSALS = [dict(page_tokens=8), dict(page_tokens=48), dict(sessions=0), dict(columns=-1), dict(pages_stride=3), dict(pool=-1), dict(pool=(1 << 30) + 1)]
+
+
+def test_plan_refusals(L):
+    for bad in SESSION_REFUSALS + [dict(columns=3), dict(sessions=1), dict(pages=0x1002), dict(held=0x1001), dict(held_after=0x1002), dict(free_pages=0x1002), dict(free_count=0x1002),
+                                   dict(free_count_after=0x1002)]:
+        assert _plan(L, _sessions(**bad), _batch()) == SHAPE, bad
+    for missing in ("pages", "held", "held_after", "free_pages", "free_count", "free_count_after"):
+        assert _plan(L, _sessions(**{missing: None}), _batch()) == NULL, missing
+    for bad in (dict(sequences=-1), dict(max_new=-1), dict(max_new=(1 << 30) + 1), dict(max_len=-1), dict(max_len=5 * 32), dict(columns=-1), dict(table_stride=3), dict(columns=3),
+                dict(sequences=4), dict(page_table=0x2002), dict(kv_len=0x1001), dict(cu=0x1002), dict(slots=0x1002),
+                dict(page_table=0x1000, slots=0x1000), dict(page_table=0x1000, table_stride=5)):    # the last two: the sessions' own table with slots, with another stride
+        assert _plan(L, _sessions(), _batch(**bad)) == SHAPE, bad
+    for missing in ("page_table", "kv_len", "cu"):
+        assert _plan(L, _sessions(), _batch(**{missing: None})) == NULL, missing
+    for bad in (dict(tokens=-1), dict(tokens=(1 << 30) + 1), dict(new=ctypes.c_void_p(0x1001)), dict(sequence=ctypes.c_void_p(0x1002)), dict(positions=ctypes.c_void_p(0x1002)),
+                dict(lacking=ctypes.c_void_p(0x1002)), dict(work=ctypes.c_void_p(0x1002))):
+        assert _plan(L, _sessions(), _batch(), **bad) == SHAPE, bad
+    assert _plan(L, None, _batch()) == NULL and _plan(L, _sessions(), None) == NULL and _plan(L, _sessions(), _batch(), new=None) == NULL
+    # large tables are made in two launches, which need a workspace
+    s, b = _sessions(sessions=3000, columns=4000, pages_stride=4000), _batch(sequences=3000, columns=4000, table_stride=4000, max_len=4000 * 32)
+    need = L.qqq_kv8_plan_workspace_bytes(ctypes.byref(s), ctypes.byref(b))
+    assert need == 3000 * 4
+    assert _plan(L, s, b, work=None) == WORKSPACE and _plan(L, s, b, nbytes=need - 1) == WORKSPACE
+    assert b"workspace" in L.qqq_last_error()
+    assert L.qqq_kv8_plan_workspace_bytes(ctypes.byref(_sessions()), ctypes.byref(_batch())) == 0
+    assert L.qqq_kv8_plan_workspace_bytes(ctypes.byref(_sessions(page_tokens=7)), ctypes.byref(b)) == 0
+
+
+def test_release_refusals(L):
+    def call(ids=BAD, count=2, **more):
+        return L.qqq_kv8_release(ctypes.byref(_sessions(**more)), ids, count, None)
+    for bad in SESSION_REFUSALS + [dict(held_after=0x1004), dict(free_count_after=0x1004), dict(count=-1), dict(count=4, ids=None), dict(ids=ctypes.c_void_p(0x1002)), dict(held=0x1002, held_after=0x1002)]:
+        assert call(**bad) == SHAPE, bad
+    assert call(held=None) == NULL and call(free_pages=None) == NULL and call(pages=None) == NULL
+    assert L.qqq_kv8_release(None, BAD, 1, None) == NULL
+    assert call(count=0) == 0
+
+
+def test_binding_refuses_cpu_tensors_and_shapes_that_disagree():
+    i32 = lambda *s: torch.zeros(s, dtype=torch.int32)  # noqa: E731
+    sessions = binding.KV8Sessions(i32(2, 3), i32(2), i32(9), i32(1))
+    batch = binding.KV8Batch(i32(2, 3), i32(2), i32(3), None, 4, 50)
+    for call in (lambda: binding.qqq_kv8_plan(sessions, batch, i32(2), 16), lambda: binding.qqq_kv8_release(sessions, 16), lambda: binding.qqq_kv8_plan_workspace_bytes(sessions, batch, 16)):
+        with pytest.raises(ValueError):
+            call()
