@@ -2,6 +2,7 @@
  * qqq_serve.h — C ABI of the two ends of a serving step, before the first decoder layer and behind the last, MI355X (gfx950):
  *
  *   what sessions hold and bring --qqq_kv8_plan--> page tables, lengths, places of the rows (the qqq_kv8_batch of qqq_layer.h); --qqq_kv8_release--> pages free again
+ *   logits --qqq_logprobs--> log probabilities, entropies, likeliest tokens
  *
  * Conventions as in qqq.h: every pointer inside is a DEVICE pointer owned by the caller, `stream` is a hipStream_t passed as void*, a call only enqueues
  * kernels, never allocates, synchronises or throws; return QQQ_OK or an error code with nothing enqueued.  Forward only: the path serves quantised
@@ -61,6 +62,27 @@ int qqq_kv8_plan(const qqq_kv8_sessions* sessions, const qqq_kv8_batch* batch, c
  * is skipped, one that is there twice is released once.
  */
 int qqq_kv8_release(const qqq_kv8_sessions* sessions, const int32_t* ids, int64_t count, void* stream);
+
+/*
+ * What is asked of the logits x[m, 0 .. V-1] of M rows:
+ *   lse[m] = log sum_v exp(x[m,v]);  logprob[m] = x[m, tokens[m]] - lse[m];  entropy[m] = -sum_v p_v log p_v,  p_v = exp(x[m,v] - lse[m])
+ *   top_tokens[m, 0 .. top-1]: the largest logits' places, in falling order, of equal ones (-0 and 0 are equal) the lowest place first; top_logprobs: their x - lse.  Places that V
+ *   does not have give -1 and -infinity.
+ * A logit of -infinity is masked: its probability is 0 and it adds nothing to the entropy.  A row of nothing else gives lse = -infinity, entropy 0 and log probabilities of
+ * -infinity.  A row with a NaN or +infinity gives NaN in all its numbers; among the top tokens NaN counts as larger than everything.  A token below 0 is none: its logprob is 0,
+ * whatever the row holds; one past V - 1 gives NaN.  All sums are fp32, relative to the largest logit.
+ *   logits [M,ld] fp16 or fp32 by type, aligned to it, ld >= V; 1 <= V < 2^30; tokens [M] int32 or NULL (then logprob is NULL); 0 <= top <= QQQ_MAX_TOP, top_tokens [M,top] int32
+ *   and top_logprobs [M,top] fp32 where top > 0; logprob, entropy, lse [M] fp32, each may be NULL.
+ *   workspace: qqq_logprobs_workspace_bytes() bytes, 16-byte aligned (0 where rows are not split over workgroups), contents irrelevant on entry; not shared by calls
+ *   that may run concurrently.
+ */
+#define QQQ_LOGITS_FP16 0
+#define QQQ_LOGITS_FP32 1
+#define QQQ_MAX_TOP 64
+size_t qqq_logprobs_workspace_bytes(int64_t M, int64_t V, int type);
+int qqq_logprobs(const void* logits, int64_t ld, int type, int64_t M, int64_t V, const int32_t* tokens, int top, float* logprob,
+                 float* entropy, float* lse, int32_t* top_tokens, float* top_logprobs, void* workspace, size_t workspace_bytes,
+                 void* stream);
 
 #ifdef __cplusplus
 }

@@ -52,3 +52,29 @@ class Sessions:
                     count += 1
             self.held[s] = 0
         self.count = count
+
+
+def logprobs(x, tokens, top):
+    """x [M,V] -> (logprob, entropy, lse, top_tokens, top_logprobs) in 64 bits, row by row."""
+    M, V = x.shape
+    logprob, entropy, lse = np.zeros(M), np.zeros(M), np.zeros(M)
+    top_tokens, top_logprobs = np.full((M, top), -1, np.int32), np.full((M, top), -np.inf)
+    for m in range(M):
+        r = x[m].astype(np.float64)
+        broken, nothing = bool(np.isnan(r).any() or (r == np.inf).any()), bool((r == -np.inf).all())
+        if broken:
+            lse[m] = entropy[m] = np.nan
+        elif nothing:
+            lse[m], entropy[m] = -np.inf, 0.0
+        else:
+            largest = r.max()                    # (taken off first: 64 bits do not hold 3e38 and log V)
+            seen = r[r > -np.inf] - largest
+            log_z = np.log(np.exp(seen).sum())
+            lse[m] = largest + log_z
+            entropy[m] = -np.sum(np.exp(seen - log_z) * (seen - log_z))
+        relative = np.full(V, -np.inf) if nothing else np.full(V, np.nan) if broken else (r - largest) - log_z
+        t = -1 if tokens is None else int(tokens[m])
+        logprob[m] = 0.0 if t < 0 else relative[t] if t < V else np.nan
+        order = np.lexsort((np.arange(V), -np.where(np.isnan(r), 0.0, r), ~np.isnan(r)))[:top]
+        top_tokens[m, :len(order)], top_logprobs[m, :len(order)] = order, relative[order]
+    return logprob, entropy, lse, top_tokens, top_logprobs

@@ -44,7 +44,7 @@ LAYER_SYMBOLS = [
 
 # the entry points of include/qqq_serve.h
 SERVE_SYMBOLS = [
-    "qqq_kv8_plan_workspace_bytes", "qqq_kv8_plan", "qqq_kv8_release",
+    "qqq_kv8_plan_workspace_bytes", "qqq_kv8_plan", "qqq_kv8_release", "qqq_logprobs_workspace_bytes", "qqq_logprobs",
 ]
 
 _lib = None
@@ -158,6 +158,9 @@ def lib():
         L.qqq_kv8_plan_workspace_bytes.restype = sz
         L.qqq_kv8_plan.argtypes = [vp, vp, vp, i64, vp, vp, vp, vp, sz, vp]
         L.qqq_kv8_release.argtypes = [vp, vp, i64, vp]
+        L.qqq_logprobs_workspace_bytes.argtypes = [i64, i64, ci]
+        L.qqq_logprobs_workspace_bytes.restype = sz
+        L.qqq_logprobs.argtypes = [vp, i64, ci, i64, i64, vp, ci, vp, vp, vp, vp, vp, vp, sz, vp]
         _load_native(L)
         _lib = L
     return _lib
@@ -821,6 +824,51 @@ def qqq_kv8_release(sessions: KV8Sessions, page_tokens, ids=None):
     if ids is not None and ids.dim() != 1:
         raise ValueError("ids must be 1-D")
     _check(lib().qqq_kv8_release(ctypes.byref(s), _ptr(ids, _I32), sessions.held.numel() if ids is None else ids.numel(), _stream()))
+
+
+class LogProbs(typing.NamedTuple):
+    """Of M rows of logits."""
+    logprob: typing.Optional[torch.Tensor]       # fp32 [M], of the given tokens
+    entropy: typing.Optional[torch.Tensor]       # fp32 [M]
+    lse: typing.Optional[torch.Tensor]           # fp32 [M]: log of the exponentials' sum
+    top_tokens: typing.Optional[torch.Tensor]    # int32 [M, top], the likeliest first, of equal ones the lowest
+    top_logprobs: typing.Optional[torch.Tensor]  # fp32 [M, top]
+
+
+MAX_TOP = 64
+_LOGITS = {torch.float16: 0, torch.float32: 1}
+
+
+def qqq_logprobs_workspace_bytes(M: int, V: int, dtype=torch.float16) -> int:
+    return int(lib().qqq_logprobs_workspace_bytes(M, V, _LOGITS[dtype]))
+
+
+def qqq_logprobs(logits, tokens=None, top=0, out: LogProbs = None, workspace=None) -> LogProbs:
+    """logits [M,V] fp16 or fp32 (row stride allowed) -> log probabilities of tokens (int32 [M]; below 0: none, 0), entropies, the logarithms of the sums and the `top` likeliest
+    tokens (up to MAX_TOP).  out: what to write into, None where a number is not wanted.  workspace: a uint8 tensor of qqq_logprobs_workspace_bytes(); without one
+    torch's allocator lends it."""
+    if logits.dtype not in _LOGITS or logits.dim() != 2 or (logits.numel() and logits.stride(1) != 1):
+        raise ValueError("logits must be a 2-D fp16 or fp32 device tensor with unit inner stride")
+    _here(logits, tokens, workspace)
+    M, V = logits.shape
+    if tokens is not None and tokens.shape != (M,):
+        raise ValueError("tokens must be of the %d rows" % M)
+    if out is None:
+        f32 = lambda *s: torch.empty(s, dtype=torch.float32, device=logits.device)  # noqa: E731
+        out = LogProbs(None if tokens is None else f32(M), f32(M), f32(M), torch.empty((M, top), dtype=_I32, device=logits.device) if top > 0 else None,
+                       f32(M, top) if top > 0 else None)
+    _here(*out)
+    for t, shape in zip(out, ((M,), (M,), (M,), (M, top), (M, top))):
+        if t is not None and t.shape != shape:
+            raise ValueError("outputs must be of %d rows, with %d tokens each" % (M, top))
+    L = lib()
+    if workspace is None:
+        nbytes = L.qqq_logprobs_workspace_bytes(M, V, _LOGITS[logits.dtype])
+        workspace = torch.empty((nbytes,), dtype=_U8, device=logits.device) if nbytes else None
+    f32 = torch.float32
+    _check(L.qqq_logprobs(logits.data_ptr(), _row_stride(logits), _LOGITS[logits.dtype], M, V, _ptr(tokens, _I32), top, _ptr(out[0], f32), _ptr(out[1], f32), _ptr(out[2], f32),
+                          _ptr(out[3], _I32), _ptr(out[4], f32), _ptr(workspace, _U8), 0 if workspace is None else workspace.numel(), _stream()))
+    return out
 
 
 def last_route() -> str:

@@ -1,0 +1,522 @@
+// Log probabilities, entropy and the largest logits of rows of V values (qqq_serve.h): each logit is read once.
+//
+// One pass keeps, per thread and relative to the largest logit m it has met,  z = sum e^(x-m)  and  t = sum (x-m) e^(x-m);  a larger m' turns them into
+// z f  and  (t + (m-m') z) f,  f = e^(m-m').  Then  lse = m + log z,  H = log z - t / z: no difference of large numbers is left in either.
+//
+// The largest `top` logits need nothing in that pass but the threads' maxima.  64 groups of threads hold disjoint parts of the row, so the top-th largest of the groups' maxima is
+// a lower bound of the row's top-th largest value, and only threads with a maximum of at least that look at their values again: 24 of them are expected for the
+// largest 20 of 64 groups, whatever V is.  What passes the bound goes into a list of up to 64 entries held in a wave's lanes in falling order; the waves' lists are
+// joined by counting, for each entry, how many are larger.  Entries are ordered by (value, lower place first), so equal values have one order and no result depends on
+// which wave came first.
+//
+// Many rows: a workgroup a row.  Few rows: a row is split, the parts leave their sums and their groups' maxima in the workspace, and a second kernel joins
+// them and looks again at the groups that pass.
+#include <float.h>
+
+#include "qqq_past.h"
+#include "qqq_serve.h"
+
+namespace qqq {
+
+namespace {
+
+constexpr int kSplitThreads = 256, kJoinThreads = 1024, kUnroll = 4;
+constexpr int kGroups = 64;              // of a workgroup's threads
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kFar = -1000.0f;         // e^kFar is 0: further than that is as far, and stays finite
+
+struct LogprobArgs {
+  const char* logits;
+  int64_t row_bytes;
+  const int32_t* tokens;
+  float *logprob, *entropy, *lse, *top_logprobs;
+  int32_t* top_tokens;
+  float* parts;   // split rows: of each part its sums (3 values), then its groups' maxima (kGroups)
+  int V, top, splits, blocks_per_part;
+};
+constexpr int kPartValues = 3 + kGroups;
+
+// fp16: 8 values in 16 bytes; fp32: 4
+template <bool F32>
+struct Row {
+  static constexpr int kVec = F32 ? 4 : 8, kSize = F32 ? 4 : 2;
+  const char* at;
+  int lead, blocks, tail;  // values before the first whole 16 aligned bytes, those 16 bytes, values behind the last
+  __device__ __forceinline__ Row(const LogprobArgs& p, int64_t row) {
+    at = p.logits + row * p.row_bytes;
+    lead = min((int)((16 - (reinterpret_cast<uintptr_t>(at) & 15)) & 15) / kSize, p.V);
+    blocks = (p.V - lead) / kVec;
+    tail = p.V - lead - blocks * kVec;
+  }
+  __device__ __forceinline__ float value(int i) const {
+    if constexpr (F32) return reinterpret_cast<const float*>(at)[i];
+    else return (float)reinterpret_cast<const _Float16*>(at)[i];
+  }
+  // the i-th of the lead's and the tail's values, and its place
+  __device__ __forceinline__ int place_of_odd(int i) const { return i < lead ? i : i + blocks * kVec; }
+  template <bool PAST>
+  __device__ __forceinline__ uint4 block(int b) const { return load16<PAST>(at + lead * kSize + (int64_t)b * 16); }
+  __device__ __forceinline__ int place_of_block(int b) const { return lead + b * kVec; }
+  static __device__ __forceinline__ uint4 masked_block() {
+    constexpr uint32_t w = F32 ? 0xFF800000u : 0xFC00FC00u;  // -infinity
+    return make_uint4(w, w, w, w);
+  }
+  static __device__ __forceinline__ void unpack(uint4 v, float* x) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < kVec; ++i)
+      x[i] = F32 ? __builtin_bit_cast(float, w[i]) : half_bits_to_float(i & 1 ? w[i >> 1] >> 16 : w[i >> 1] & 0xFFFFu);
+  }
+  static __device__ __forceinline__ float largest(const uint4* v) {  // of kUnroll blocks; not a NaN unless all are
+    if constexpr (F32) {
+      float m = __builtin_bit_cast(float, v[0].x);
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) {
+        const uint32_t w[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) m = fmaxf(m, __builtin_bit_cast(float, w[i]));
+      }
+      return m;
+    } else {
+      h2 m = as_h2(v[0].x);
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) {
+        const uint32_t w[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) m = __builtin_elementwise_max(m, as_h2(w[i]));
+      }
+      return fmaxf((float)m[0], (float)m[1]);
+    }
+  }
+};
+
+struct Sums {
+  float m = -FLT_MAX, z = 0.0f, t = 0.0f;
+  __device__ __forceinline__ void raise(float to) {  // m becomes the larger of the two; a NaN leaves it
+    const float larger = fmaxf(m, to), d = fmaxf(m - larger, kFar), f = __builtin_amdgcn_exp2f(d * kLog2e);
+    t = (t + d * z) * f;
+    z *= f;
+    m = larger;
+  }
+  __device__ __forceinline__ void add(float x) {  // x <= m, or a NaN or infinity, which makes z a NaN
+    const float d = x - m, e = __builtin_amdgcn_exp2f(d * kLog2e);
+    z += e;
+    t = __builtin_fmaf(fmaxf(d, kFar), e, t);
+  }
+};
+
+template <int CTRL>
+__device__ __forceinline__ float moved(float v) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xF, 0xF, false));
+}
+// over groups of G lanes, in each of them
+template <int G>
+__device__ __forceinline__ float group_max(float v) {
+  if constexpr (G >= 2) v = fmaxf(v, moved<0xB1>(v));   // quad_perm [1,0,3,2]
+  if constexpr (G >= 4) v = fmaxf(v, moved<0x4E>(v));   // quad_perm [2,3,0,1]
+  if constexpr (G >= 8) v = fmaxf(v, moved<0x141>(v));  // row_half_mirror
+  if constexpr (G >= 16) v = fmaxf(v, moved<0x140>(v)); // row_mirror
+  return v;
+}
+__device__ __forceinline__ float lane_value(float v, int lane) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane)); }
+__device__ __forceinline__ float wave_max(float v) {
+  v = group_max<16>(v);
+  return fmaxf(fmaxf(lane_value(v, 0), lane_value(v, 16)), fmaxf(lane_value(v, 32), lane_value(v, 48)));
+}
+__device__ __forceinline__ float wave_sum(float v) {
+  v += moved<0xB1>(v);
+  v += moved<0x4E>(v);
+  v += moved<0x141>(v);
+  v += moved<0x140>(v);
+  return (lane_value(v, 0) + lane_value(v, 16)) + (lane_value(v, 32) + lane_value(v, 48));
+}
+// of all lanes, in each of them; the order is fixed
+__device__ __forceinline__ Sums wave_sums(Sums s) {
+  s.raise(wave_max(s.m));
+  s.z = wave_sum(s.z);
+  s.t = wave_sum(s.t);
+  return s;
+}
+template <int WAVES>
+__device__ __forceinline__ Sums join_waves(const float (*of_wave)[3]) {
+  Sums all;
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) all.m = fmaxf(all.m, of_wave[w][0]);
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) {
+    Sums s;
+    s.m = of_wave[w][0];
+    s.z = of_wave[w][1];
+    s.t = of_wave[w][2];
+    s.raise(all.m);
+    all.z += s.z;
+    all.t += s.t;
+  }
+  return all;
+}
+
+// ---- order.  Values by 32 bits that order as they do: a NaN above everything, -0 as 0
+__device__ __forceinline__ uint32_t order_of(float x) {
+  const uint32_t b = __builtin_bit_cast(uint32_t, x + 0.0f);
+  return x != x ? 0xFFFFFFFFu : b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float value_of(uint32_t order) {
+  return __builtin_bit_cast(float, order & 0x80000000u ? order ^ 0x80000000u : ~order);
+}
+
+// A lower bound of the top-th largest of the lanes' values (none of them a NaN): the largest number of 20 leading bits that `top` lanes reach.
+// Where it is no more than the value that threads start from, everything passes, -infinity too.
+__device__ __forceinline__ float bound_of(float v, int top) {
+  const uint32_t order = order_of(v);
+  uint32_t bound = 0;
+#pragma unroll
+  for (int bit = 31; bit >= 12; --bit) {
+    const uint32_t raised = bound | 1u << bit;
+    if (__popcll(__ballot(order >= raised)) >= top) bound = raised;
+  }
+  return bound <= 0x00800000u ? -__builtin_inff() : value_of(bound);
+}
+
+// The largest entries so far, in the wave's lanes in falling order: (order of the value, bits of the place inverted); 0, 0: none
+struct List {
+  uint32_t order = 0, place = 0;
+  __device__ __forceinline__ static bool above(uint32_t a_order, uint32_t a_place, uint32_t b_order, uint32_t b_place) {
+    return a_order > b_order || (a_order == b_order && a_place > b_place);
+  }
+  // Lanes offer a value each: those that belong into the first `top` are put there, one after the other.
+  __device__ __forceinline__ void offer(bool has, float x, int at, int top, float& bound) {
+    if (!__ballot(has && !(x < bound))) return;
+    const uint32_t o = order_of(x), q = ~(uint32_t)at;
+    uint64_t some;
+    while ((some = __ballot(has && above(o, q, (uint32_t)__builtin_amdgcn_readlane((int)order, top - 1), (uint32_t)__builtin_amdgcn_readlane((int)place, top - 1)) && !(x < bound)))) {
+      const int from = __builtin_ctzll(some), lane = threadIdx.x & 63;
+      const uint32_t new_order = (uint32_t)__builtin_amdgcn_readlane((int)o, from), new_place = (uint32_t)__builtin_amdgcn_readlane((int)q, from);
+      const int to = __popcll(__ballot(above(order, place, new_order, new_place)));
+      const uint32_t order_before = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)order, 0x138, 0xF, 0xF, false);  // wave_shr:1
+      const uint32_t place_before = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)place, 0x138, 0xF, 0xF, false);
+      order = lane < to ? order : lane == to ? new_order : order_before;
+      place = lane < to ? place : lane == to ? new_place : place_before;
+      if (lane == from) has = false;
+    }
+    // what is below the last of a full list need not be offered
+    const uint32_t last = (uint32_t)__builtin_amdgcn_readlane((int)order, top - 1);
+    if (last != 0 && last != 0xFFFFFFFFu) bound = fmaxf(bound, value_of(last));
+  }
+};
+
+// The waves' lists as one: entries to LDS, each one's rank counted, the first `top` written.
+template <int T>
+__device__ __forceinline__ void write_top(const LogprobArgs& p, int64_t row, const List& list, const Sums& all, float log_z, uint2* entries, int* count) {
+  const int lane = threadIdx.x & 63;
+  const bool has = lane < p.top && (list.order | list.place) != 0;
+  const uint64_t some = __ballot(has);
+  int base = 0;
+  if (lane == 0 && some) base = atomicAdd(count, __popcll(some));  // (in LDS; the entries' order decides nothing)
+  base = __builtin_amdgcn_readfirstlane(base);
+  if (has) entries[base + lane] = make_uint2(list.order, list.place);
+  __syncthreads();
+  const int n = *count;
+  for (int i = threadIdx.x; i < max(n, p.top); i += T) {
+    if (i < n) {
+      const uint2 mine = entries[i];
+      int rank = 0;
+      for (int j = 0; j < n; ++j) {
+        const uint2 other = entries[j];
+        rank += List::above(other.x, other.y, mine.x, mine.y);
+      }
+      if (rank < p.top) {
+        p.top_tokens[row * p.top + rank] = (int32_t)~mine.y;
+        p.top_logprobs[row * p.top + rank] = all.z == 0.0f ? -__builtin_inff() : (value_of(mine.x) - all.m) - log_z;
+      }
+    } else {  // fewer values than that
+      p.top_tokens[row * p.top + i] = -1;
+      p.top_logprobs[row * p.top + i] = -__builtin_inff();
+    }
+  }
+}
+
+template <bool F32>
+__device__ __forceinline__ void write_numbers(const LogprobArgs& p, int64_t row, const Row<F32>& r, const Sums& all, float log_z) {
+  const bool none = all.z == 0.0f;  // everything masked
+  if (p.lse) p.lse[row] = none ? -__builtin_inff() : all.m + log_z;
+  if (p.entropy) p.entropy[row] = none ? 0.0f : log_z - all.t / all.z;
+  if (p.logprob) {
+    const int token = p.tokens[row];
+    float x = token < 0 ? 0.0f : __builtin_nanf("");
+    if (token >= 0 && token < p.V) x = none ? -__builtin_inff() : (r.value(token) - all.m) - log_z;
+    p.logprob[row] = x;
+  }
+}
+
+// One thread's part of blocks [from, to): every T-th, and one of the lead's and tail's values where `odd` says so.
+template <bool F32, int T, bool PAST>
+__device__ __forceinline__ Sums stream(const Row<F32>& r, int from, int to, bool odd) {
+  Sums s;
+  const int tid = threadIdx.x;
+  auto request = [&](int b0, uint4* v) {
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      const int b = b0 + tid + T * u;
+      v[u] = Row<F32>::masked_block();
+      if (b < to) v[u] = r.template block<PAST>(b);
+    }
+  };
+  auto take = [&](const uint4* v) {
+    s.raise(Row<F32>::largest(v));
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      float x[Row<F32>::kVec];
+      Row<F32>::unpack(v[u], x);
+#pragma unroll
+      for (int i = 0; i < Row<F32>::kVec; ++i) s.add(x[i]);
+    }
+  };
+  uint4 a[kUnroll], b[kUnroll];
+  request(from, a);
+  if (odd && tid < r.lead + r.tail) {
+    const float x = r.value(r.place_of_odd(tid));
+    s.raise(x);
+    s.add(x);
+  }
+  for (int b0 = from; b0 < to; b0 += 2 * T * kUnroll) {
+    request(b0 + T * kUnroll, b);
+    take(a);
+    if (b0 + T * kUnroll >= to) break;
+    request(b0 + 2 * T * kUnroll, a);
+    take(b);
+  }
+  return s;
+}
+
+// ---- many rows: a workgroup a row
+template <bool F32, int T, bool PAST>
+__global__ __launch_bounds__(T) void logprobs_kernel(const LogprobArgs p) {
+  __shared__ float of_wave[T / 64][3], of_group[kGroups];
+  __shared__ uint2 entries[T];
+  __shared__ int count;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int64_t row = blockIdx.x;
+  const Row<F32> r(p, row);
+  const Sums mine = stream<F32, T, PAST>(r, 0, r.blocks, true);
+  if (p.top) {
+    const float g = group_max<T / kGroups>(mine.m);
+    if (tid % (T / kGroups) == 0) of_group[tid / (T / kGroups)] = g;
+    if (tid == 0) count = 0;
+  }
+  const Sums w = wave_sums(mine);
+  if (lane == 0) {
+    of_wave[wave][0] = w.m;
+    of_wave[wave][1] = w.z;
+    of_wave[wave][2] = w.t;
+  }
+  __syncthreads();
+  if (!p.top && wave > 0) return;
+  const Sums all = join_waves<T / 64>(of_wave);
+  const float log_z = logf(all.z);
+  if (tid == 0) write_numbers<F32>(p, row, r, all, log_z);
+  if (!p.top) return;
+
+  float bound = bound_of(of_group[lane], p.top);
+  List list;
+  const bool again = mine.m >= bound || mine.z != mine.z;
+  if (__ballot(again)) {
+    for (int b0 = 0; b0 < r.blocks; b0 += T * kUnroll) {
+      uint4 v[kUnroll];
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) {
+        const int b = b0 + tid + T * u;
+        v[u] = Row<F32>::masked_block();
+        if (again && b < r.blocks) v[u] = r.template block<false>(b);
+      }
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) {
+        const int b = b0 + tid + T * u;
+        float x[Row<F32>::kVec];
+        Row<F32>::unpack(v[u], x);
+#pragma unroll
+        for (int i = 0; i < Row<F32>::kVec; ++i) list.offer(again && b < r.blocks, x[i], r.place_of_block(b) + i, p.top, bound);
+      }
+    }
+    const bool odd = again && tid < r.lead + r.tail;
+    const int place = odd ? r.place_of_odd(tid) : 0;
+    list.offer(odd, odd ? r.value(place) : 0.0f, place, p.top, bound);
+  }
+  write_top<T>(p, row, list, all, log_z, entries, &count);
+}
+
+// ---- few rows: parts of them
+template <bool F32>
+__global__ __launch_bounds__(kSplitThreads) void logprobs_part_kernel(const LogprobArgs p) {
+  __shared__ float of_wave[kSplitThreads / 64][3];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, part = blockIdx.x;
+  const int64_t row = blockIdx.y;
+  const Row<F32> r(p, row);
+  const int from = min((int64_t)part * p.blocks_per_part, (int64_t)r.blocks), to = min((int64_t)from + p.blocks_per_part, (int64_t)r.blocks);
+  const Sums mine = stream<F32, kSplitThreads, false>(r, from, to, part == 0);
+  float* out = p.parts + (row * p.splits + part) * kPartValues;
+  if (p.top) {
+    const float g = group_max<kSplitThreads / kGroups>(mine.z != mine.z ? __builtin_inff() : mine.m);
+    if (tid % (kSplitThreads / kGroups) == 0) out[3 + tid / (kSplitThreads / kGroups)] = g;
+  }
+  const Sums w = wave_sums(mine);
+  if (lane == 0) {
+    of_wave[wave][0] = w.m;
+    of_wave[wave][1] = w.z;
+    of_wave[wave][2] = w.t;
+  }
+  __syncthreads();
+  if (tid == 0) {
+    const Sums all = join_waves<kSplitThreads / 64>(of_wave);
+    out[0] = all.m;
+    out[1] = all.z;
+    out[2] = all.t;
+  }
+}
+
+// the most groups of all parts of a row
+constexpr int kMostParts = 256, kJoinGroups = kMostParts * kGroups / kJoinThreads;
+
+template <bool F32, bool TOP>
+__global__ __launch_bounds__(TOP ? kJoinThreads : 64) void logprobs_join_kernel(const LogprobArgs p) {
+  constexpr int T = TOP ? kJoinThreads : 64, kWaves = T / 64;
+  __shared__ float of_wave[kWaves][3], of_group[kGroups];
+  __shared__ uint2 entries[TOP ? T : 1];
+  __shared__ int count, passing;
+  __shared__ uint16_t passed[TOP ? kMostParts * kGroups : 1];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int64_t row = blockIdx.x;
+  const Row<F32> r(p, row);
+  const float* parts = p.parts + row * p.splits * kPartValues;
+  float g[kJoinGroups];
+  if constexpr (TOP) {
+    float most = -FLT_MAX;
+#pragma unroll
+    for (int i = 0; i < kJoinGroups; ++i) {  // a wave: the groups of part wave + kWaves * i
+      const int part = wave + kWaves * i;
+      g[i] = part < p.splits ? parts[part * kPartValues + 3 + lane] : -FLT_MAX;
+      most = fmaxf(most, g[i]);
+    }
+    most = group_max<T / kGroups>(most);
+    if (tid % (T / kGroups) == 0) of_group[tid / (T / kGroups)] = most;
+    if (tid == 0) count = passing = 0;
+  }
+  Sums s;
+  for (int part = tid; part < p.splits; part += T) {
+    Sums q;
+    q.m = parts[part * kPartValues];
+    q.z = parts[part * kPartValues + 1];
+    q.t = parts[part * kPartValues + 2];
+    const float m = fmaxf(s.m, q.m);
+    s.raise(m);
+    q.raise(m);
+    s.z += q.z;
+    s.t += q.t;
+  }
+  s = wave_sums(s);
+  if constexpr (!TOP) {
+    if (tid == 0) write_numbers<F32>(p, row, r, s, logf(s.z));
+  } else {
+    if (lane == 0) {
+      of_wave[wave][0] = s.m;
+      of_wave[wave][1] = s.z;
+      of_wave[wave][2] = s.t;
+    }
+    __syncthreads();
+    const Sums all = join_waves<kWaves>(of_wave);
+    const float log_z = logf(all.z);
+    if (tid == 0) write_numbers<F32>(p, row, r, all, log_z);
+    float bound = bound_of(of_group[lane], p.top);
+#pragma unroll
+    for (int i = 0; i < kJoinGroups; ++i) {
+      const int part = wave + kWaves * i;
+      if (part < p.splits && g[i] >= bound) passed[atomicAdd(&passing, 1)] = (uint16_t)(part * kGroups + lane);
+    }
+    __syncthreads();
+    // a wave a group that passed: the values of kSplitThreads / kGroups threads of its part
+    constexpr int kLanes = kSplitThreads / kGroups;
+    List list;
+    for (int i = wave; i < passing; i += kWaves) {
+      const int part = passed[i] / kGroups, thread0 = passed[i] % kGroups * kLanes;
+      const int from = min((int64_t)part * p.blocks_per_part, (int64_t)r.blocks), to = min((int64_t)from + p.blocks_per_part, (int64_t)r.blocks);
+      // lane: block lane / kLanes of thread thread0 + lane % kLanes
+      for (int b0 = from + thread0; b0 < to; b0 += kSplitThreads * (64 / kLanes)) {
+        const int b = b0 + lane % kLanes + lane / kLanes * kSplitThreads;
+        uint4 v = Row<F32>::masked_block();
+        if (b < to) v = r.template block<false>(b);
+        float x[Row<F32>::kVec];
+        Row<F32>::unpack(v, x);
+#pragma unroll
+        for (int e = 0; e < Row<F32>::kVec; ++e) list.offer(b < to, x[e], r.place_of_block(b) + e, p.top, bound);
+      }
+      const bool odd = part == 0 && lane < kLanes && thread0 + lane < r.lead + r.tail;
+      const int place = odd ? r.place_of_odd(thread0 + lane) : 0;
+      list.offer(odd, odd ? r.value(place) : 0.0f, place, p.top, bound);
+    }
+    write_top<T>(p, row, list, all, log_z, entries, &count);
+  }
+}
+
+// Parts of a row: 1 (a workgroup a row) where the rows alone keep the CUs busy.
+struct Split {
+  int parts, blocks;
+};
+Split split_of(int64_t M, int64_t V, int type) {
+  const int64_t blocks = V / (type == QQQ_LOGITS_FP32 ? 4 : 8);
+  if (M >= 2 * num_cus() || blocks <= 4 * kSplitThreads) return {1, 0};
+  // a block a thread where that leaves no more than four workgroups a CU
+  int64_t each = 1;
+  while (each < 64 && M * ((blocks + each * kSplitThreads - 1) / (each * kSplitThreads)) > 4 * num_cus()) each *= 2;
+  while ((blocks + each * kSplitThreads - 1) / (each * kSplitThreads) > kMostParts) each *= 2;
+  const int64_t parts = (blocks + each * kSplitThreads - 1) / (each * kSplitThreads);
+  if (parts < 2) return {1, 0};
+  return {(int)parts, (int)(each * kSplitThreads)};
+}
+
+template <bool F32>
+int launch_typed(LogprobArgs& p, int64_t M, const Split& s, hipStream_t st) {
+  if (s.parts == 1) {
+    const bool past = M * p.V * (F32 ? 4 : 2) > kLastCacheBytes;
+#define QQQ_LP(T, PAST) hipLaunchKernelGGL((logprobs_kernel<F32, T, PAST>), dim3((unsigned)M), dim3(T), 0, st, p)
+    if (p.V <= 16384) QQQ_LP(256, false);
+    else if (past) QQQ_LP(1024, true);
+    else QQQ_LP(1024, false);
+#undef QQQ_LP
+  } else {
+    p.splits = s.parts;
+    p.blocks_per_part = s.blocks;
+    hipLaunchKernelGGL((logprobs_part_kernel<F32>), dim3((unsigned)s.parts, (unsigned)M), dim3(kSplitThreads), 0, st, p);
+    if (p.top) hipLaunchKernelGGL((logprobs_join_kernel<F32, true>), dim3((unsigned)M), dim3(kJoinThreads), 0, st, p);
+    else hipLaunchKernelGGL((logprobs_join_kernel<F32, false>), dim3((unsigned)M), dim3(64), 0, st, p);
+  }
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return set_error(QQQ_ERR_HIP, "logprobs launch: %s", hipGetErrorString(e));
+  route_note("logprobs parts=%d", s.parts);
+  return QQQ_OK;
+}
+
+}  // namespace
+
+size_t logprobs_bytes(int64_t M, int64_t V, int type) {
+  const Split s = split_of(M, V, type);
+  return s.parts == 1 ? 0 : (size_t)M * s.parts * kPartValues * sizeof(float);
+}
+
+int launch_logprobs(const void* logits, int64_t ld, int type, int64_t M, int64_t V, const int32_t* tokens, int top, float* logprob, float* entropy,
+                    float* lse, int32_t* top_tokens, float* top_logprobs, void* workspace, hipStream_t st) {
+  LogprobArgs p = {};
+  p.logits = static_cast<const char*>(logits);
+  p.row_bytes = ld * (type == QQQ_LOGITS_FP32 ? 4 : 2);
+  p.tokens = tokens;
+  p.logprob = logprob;
+  p.entropy = entropy;
+  p.lse = lse;
+  p.top_tokens = top_tokens;
+  p.top_logprobs = top_logprobs;
+  p.parts = static_cast<float*>(workspace);
+  p.V = (int)V;
+  p.top = top;
+  const Split s = split_of(M, V, type);
+  return type == QQQ_LOGITS_FP32 ? launch_typed<true>(p, M, s, st) : launch_typed<false>(p, M, s, st);
+}
+
+}  // namespace qqq

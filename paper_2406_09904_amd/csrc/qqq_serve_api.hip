@@ -3,6 +3,11 @@
 #include "qqq_serve.h"
 
 namespace qqq {
+
+size_t logprobs_bytes(int64_t M, int64_t V, int type);
+int launch_logprobs(const void* logits, int64_t ld, int type, int64_t M, int64_t V, const int32_t* tokens, int top, float* logprob, float* entropy,
+                    float* lse, int32_t* top_tokens, float* top_logprobs, void* workspace, hipStream_t st);
+
 namespace {
 
 constexpr int64_t kMost = 1 << 30;  // tokens of a sequence, rows of a call, pages: places stay in 32 bits
@@ -66,6 +71,12 @@ PlanArgs plan_args(const qqq_kv8_sessions* s, const qqq_kv8_batch* b) {
   return p;
 }
 
+int check_logits(const char* name, int64_t M, int64_t V, int type) {
+  if (M < 0 || M > 0x7FFFFFFF || V < 1 || V >= kMost) return set_error(QQQ_ERR_SHAPE, "%s: unsupported %lld rows of %lld logits", name, (long long)M, (long long)V);
+  if (type != QQQ_LOGITS_FP16 && type != QQQ_LOGITS_FP32) return set_error(QQQ_ERR_SHAPE, "%s: logits of type %d", name, type);
+  return QQQ_OK;
+}
+
 }  // namespace
 }  // namespace qqq
 
@@ -119,6 +130,29 @@ int qqq_kv8_release(const qqq_kv8_sessions* sessions, const int32_t* ids, int64_
   p.sequences = (int32_t)count;
   route_reset();
   return launch_kv8_release(p, (hipStream_t)stream);
+}
+
+size_t qqq_logprobs_workspace_bytes(int64_t M, int64_t V, int type) {
+  return check_logits("qqq_logprobs_workspace_bytes", M, V, type) || M == 0 ? 0 : logprobs_bytes(M, V, type);
+}
+
+int qqq_logprobs(const void* logits, int64_t ld, int type, int64_t M, int64_t V, const int32_t* tokens, int top, float* logprob, float* entropy, float* lse,
+                 int32_t* top_tokens, float* top_logprobs, void* workspace, size_t workspace_bytes, void* stream) {
+  const char* name = "qqq_logprobs";
+  if (int rc = check_logits(name, M, V, type)) return rc;
+  if (ld < V) return set_error(QQQ_ERR_SHAPE, "%s: row stride %lld for %lld logits", name, (long long)ld, (long long)V);
+  if (top < 0 || top > QQQ_MAX_TOP) return set_error(QQQ_ERR_SHAPE, "%s: the largest %d logits, %d at most", name, top, QQQ_MAX_TOP);
+  if (M == 0) return QQQ_OK;
+  if (!logits || (top > 0 && (!top_tokens || !top_logprobs)) || (logprob && !tokens)) return set_error(QQQ_ERR_NULL, "%s: NULL pointer", name);
+  if (tokens && !logprob) return set_error(QQQ_ERR_NULL, "%s: tokens without their log probabilities", name);
+  if (!aligned(logits, type == QQQ_LOGITS_FP32 ? 4 : 2) || !aligned(tokens, 4) || !aligned(logprob, 4) || !aligned(entropy, 4) || !aligned(lse, 4) ||
+      !aligned(top_tokens, 4) || !aligned(top_logprobs, 4) || !aligned(workspace, 16))
+    return set_error(QQQ_ERR_SHAPE, "%s: misaligned pointer", name);
+  const size_t need = logprobs_bytes(M, V, type);
+  if (need && (!workspace || workspace_bytes < need))
+    return set_error(QQQ_ERR_WORKSPACE, "%s: workspace %zu bytes < %zu needed", name, workspace ? workspace_bytes : 0, need);
+  route_reset();
+  return launch_logprobs(logits, ld, type, M, V, tokens, top, logprob, entropy, lse, top_tokens, top_logprobs, workspace, (hipStream_t)stream);
 }
 
 }  // extern "C"

@@ -92,3 +92,27 @@ def test_binding_refuses_cpu_tensors_and_shapes_that_disagree():
     for call in (lambda: binding.qqq_kv8_plan(sessions, batch, i32(2), 16), lambda: binding.qqq_kv8_release(sessions, 16), lambda: binding.qqq_kv8_plan_workspace_bytes(sessions, batch, 16)):
         with pytest.raises(ValueError):
             call()
+
+
+def test_logprobs_refusals(L):
+    def call(x=BAD, ld=100, kind=0, M=3, V=100, tokens=BAD, top=5, logprob=BAD, entropy=BAD, lse=BAD, top_tokens=BAD, top_logprobs=BAD, work=BAD, nbytes=1 << 20):
+        return L.qqq_logprobs(x, ld, kind, M, V, tokens, top, logprob, entropy, lse, top_tokens, top_logprobs, work, nbytes, None)
+    odd = ctypes.c_void_p(0x1002)
+    assert call(M=0) == 0
+    for bad in (dict(M=-1), dict(V=0), dict(V=1 << 30, ld=1 << 30), dict(ld=99), dict(kind=2), dict(kind=-1), dict(top=-1), dict(top=65), dict(x=ctypes.c_void_p(0x1001)),
+                dict(x=odd, kind=1), dict(tokens=odd), dict(logprob=odd), dict(entropy=odd), dict(lse=odd), dict(top_tokens=odd), dict(top_logprobs=odd), dict(work=ctypes.c_void_p(0x1008))):
+        assert call(**bad) == SHAPE, bad
+    for missing in ("x", "tokens", "logprob", "top_tokens", "top_logprobs"):
+        assert call(**{missing: None}) == NULL, missing
+    need = L.qqq_logprobs_workspace_bytes(1, 100000, 0)
+    assert need > 0 and need % 4 == 0
+    assert call(M=1, V=100000, ld=100000, nbytes=need - 1) == WORKSPACE and call(M=1, V=100000, ld=100000, work=None) == WORKSPACE
+    assert b"workspace" in L.qqq_last_error()
+    assert L.qqq_logprobs_workspace_bytes(5000, 100000, 0) == 0 and L.qqq_logprobs_workspace_bytes(1, 100, 0) == 0 and L.qqq_logprobs_workspace_bytes(1, 0, 0) == 0
+
+
+def test_logprobs_binding_refusals():
+    x = torch.zeros(2, 30, dtype=torch.float16)
+    for call in (lambda: binding.qqq_logprobs(x), lambda: binding.qqq_logprobs(x.double()), lambda: binding.qqq_logprobs(x[0]), lambda: binding.qqq_logprobs(x.t())):
+        with pytest.raises(ValueError):
+            call()
