@@ -2,7 +2,7 @@
  * qqq_serve.h — C ABI of the two ends of a serving step, before the first decoder layer and behind the last, MI355X (gfx950):
  *
  *   what sessions hold and bring --qqq_kv8_plan--> page tables, lengths, places of the rows (the qqq_kv8_batch of qqq_layer.h); --qqq_kv8_release--> pages free again
- *   logits --qqq_logprobs--> log probabilities, entropies, likeliest tokens
+ *   int8 codes of the last norm (qqq_add_rmsnorm_quant) --qqq_gemm_w8a8--> logits --qqq_logprobs--> log probabilities, entropies, likeliest tokens
  *
  * Conventions as in qqq.h: every pointer inside is a DEVICE pointer owned by the caller, `stream` is a hipStream_t passed as void*, a call only enqueues
  * kernels, never allocates, synchronises or throws; return QQQ_OK or an error code with nothing enqueued.  Forward only: the path serves quantised
@@ -62,6 +62,31 @@ int qqq_kv8_plan(const qqq_kv8_sessions* sessions, const qqq_kv8_batch* batch, c
  * is skipped, one that is there twice is released once.
  */
 int qqq_kv8_release(const qqq_kv8_sessions* sessions, const int32_t* ids, int64_t count, void* stream);
+
+/*
+ * Weights in 8 bits.  Codes and scales of fp16 weights [N,K] are what qqq_quant_act gives for them, a row for an output channel: symmetric, codes in
+ * [-127,127], one fp32 scale a channel.
+ *   w_codes [N,ldw] int8, 16-byte aligned, ldw >= K, ldw % 16 == 0.  N >= 1, K % 128 == 0, 128 <= K <= 131072.
+ *   w_packed: qqq_packed_w8_bytes(N,K) = K * (N rounded up to 16) bytes, opaque device tile layout, 16-byte aligned: 2 KiB chunks of 16 channels x 128 k in the order of
+ *   the matrix instruction's operands; channels past N are zeros.  qqq_unpack_w8 is the exact inverse ([N,K], dense).
+ */
+size_t qqq_packed_w8_bytes(int64_t N, int64_t K); /* 0 for unsupported shapes */
+int qqq_pack_w8(const int8_t* w_codes, int64_t N, int64_t K, int64_t ldw, void* w_packed, void* stream);
+int qqq_unpack_w8(const void* w_packed, int64_t N, int64_t K, int8_t* w_codes, void* stream);
+
+/*
+ * W8A8 GEMM:  acc[m,n] = sum_k a_q[m,k] * w[n,k]  (int32, exact),  t = fp32_rne(float(acc) * s_a[m]),
+ *   y[m,n] = fp16_rne(t * s_w[n])  or  fp32_rne(t * s_w[n])  by y_type.
+ *   a_q [M,K] int8, dense, 16-byte aligned, codes in [-127,127]; s_a [M] fp32; w_packed as above; s_w [N] fp32; y [M,ldy] of the type, ldy >= N, aligned to its type
+ *   (aligned to 16 bytes with rows of whole 16 bytes it is written faster); acc_out [M,N] int32 dense or NULL (parity/debug).  1 <= N <= 2^24, K as above, M == 0 is a no-op.
+ *   workspace: qqq_gemm_w8a8_workspace_bytes() bytes, 16-byte aligned (partial sums of calls that split K; 0 where none is needed), contents irrelevant on entry;
+ *   not shared by calls that may run concurrently.
+ */
+#define QQQ_OUT_FP16 0
+#define QQQ_OUT_FP32 1
+size_t qqq_gemm_w8a8_workspace_bytes(int64_t M, int64_t N, int64_t K);
+int qqq_gemm_w8a8(const int8_t* a_q, const float* s_a, const void* w_packed, const float* s_w, void* y, int y_type, int64_t ldy,
+                  int32_t* acc_out, int64_t M, int64_t N, int64_t K, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * What is asked of the logits x[m, 0 .. V-1] of M rows:

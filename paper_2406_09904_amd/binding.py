@@ -33,7 +33,7 @@ SYMBOLS = [
     "qqq_debug_count_sg_violations", "qqq_probe_stream_read", "qqq_probe_mfma_i8", "qqq_probe_prefill_loop",
     "qqq_smoothing_workspace_bytes", "qqq_adaptive_smoothing", "qqq_channel_absmax", "qqq_smooth_apply",
     "qqq_fp16_gemm_nt", "qqq_hessian", "qqq_gptq_workspace_bytes", "qqq_gptq_quantize_w4_perchannel",
-    "qqq_gptq_quantize_w4_pergroup", "qqq_set_factor_workgroups",
+    "qqq_gptq_quantize_w4_pergroup", "qqq_set_factor_workgroups", "qqq_set_w8a8_tuning",
 ]
 
 # the entry points of include/qqq_layer.h
@@ -45,6 +45,7 @@ LAYER_SYMBOLS = [
 # the entry points of include/qqq_serve.h
 SERVE_SYMBOLS = [
     "qqq_kv8_plan_workspace_bytes", "qqq_kv8_plan", "qqq_kv8_release", "qqq_logprobs_workspace_bytes", "qqq_logprobs",
+    "qqq_packed_w8_bytes", "qqq_pack_w8", "qqq_unpack_w8", "qqq_gemm_w8a8_workspace_bytes", "qqq_gemm_w8a8",
 ]
 
 _lib = None
@@ -145,6 +146,7 @@ def lib():
         L.qqq_set_prefill_tuning.argtypes = [ci]
         L.qqq_set_prefill_ksplit.argtypes = [ci]
         L.qqq_set_factor_workgroups.argtypes = [ci]
+        L.qqq_set_w8a8_tuning.argtypes = [ci, ci]
         cf = ctypes.c_float
         L.qqq_add_rmsnorm.argtypes = [vp, i64, vp, i64, ci, vp, cf, i64, i64, vp, i64, vp, vp]
         L.qqq_add_rmsnorm_quant.argtypes = [vp, i64, vp, i64, ci, vp, cf, i64, i64, vp, i64, vp, vp, vp]
@@ -158,6 +160,13 @@ def lib():
         L.qqq_kv8_plan_workspace_bytes.restype = sz
         L.qqq_kv8_plan.argtypes = [vp, vp, vp, i64, vp, vp, vp, vp, sz, vp]
         L.qqq_kv8_release.argtypes = [vp, vp, i64, vp]
+        L.qqq_packed_w8_bytes.argtypes = [i64, i64]
+        L.qqq_packed_w8_bytes.restype = sz
+        L.qqq_pack_w8.argtypes = [vp, i64, i64, i64, vp, vp]
+        L.qqq_unpack_w8.argtypes = [vp, i64, i64, vp, vp]
+        L.qqq_gemm_w8a8_workspace_bytes.argtypes = [i64, i64, i64]
+        L.qqq_gemm_w8a8_workspace_bytes.restype = sz
+        L.qqq_gemm_w8a8.argtypes = [vp, vp, vp, vp, vp, ci, i64, vp, i64, i64, i64, vp, sz, vp]
         L.qqq_logprobs_workspace_bytes.argtypes = [i64, i64, ci]
         L.qqq_logprobs_workspace_bytes.restype = sz
         L.qqq_logprobs.argtypes = [vp, i64, ci, i64, i64, vp, ci, vp, vp, vp, vp, vp, vp, sz, vp]
@@ -826,6 +835,70 @@ def qqq_kv8_release(sessions: KV8Sessions, page_tokens, ids=None):
     _check(lib().qqq_kv8_release(ctypes.byref(s), _ptr(ids, _I32), sessions.held.numel() if ids is None else ids.numel(), _stream()))
 
 
+def qqq_packed_w8_bytes(N: int, K: int) -> int:
+    return int(lib().qqq_packed_w8_bytes(N, K))
+
+
+def qqq_pack_w8(w_codes: torch.Tensor, out: torch.Tensor = None) -> torch.Tensor:
+    """w_codes [N,K] int8 (row stride allowed; qqq_quant_act gives them and their scales for fp16 weights) -> opaque packed uint8."""
+    if w_codes.dtype != _I8 or w_codes.dim() != 2 or w_codes.stride(1) != 1:
+        raise ValueError("w_codes must be a 2-D int8 device tensor with unit inner stride")
+    _here(w_codes, out)
+    N, K = w_codes.shape
+    nbytes = qqq_packed_w8_bytes(N, K)
+    if nbytes == 0:
+        raise QQQError(2, "pack: unsupported N=%d K=%d" % (N, K))
+    if out is None:
+        out = torch.empty((nbytes,), dtype=_U8, device=w_codes.device)
+    elif out.numel() != nbytes:
+        raise ValueError("out must have %d bytes" % nbytes)
+    _check(lib().qqq_pack_w8(w_codes.data_ptr(), N, K, _row_stride(w_codes), _ptr(out, _U8), _stream()))
+    return out
+
+
+def qqq_unpack_w8(w_packed: torch.Tensor, N: int, K: int) -> torch.Tensor:
+    _here(w_packed)
+    if w_packed.numel() != qqq_packed_w8_bytes(N, K):
+        raise ValueError("w_packed must have %d bytes" % qqq_packed_w8_bytes(N, K))
+    out = torch.empty((N, K), dtype=_I8, device=w_packed.device)
+    _check(lib().qqq_unpack_w8(_ptr(w_packed, _U8), N, K, _ptr(out, _I8), _stream()))
+    return out
+
+
+def qqq_gemm_w8a8_workspace_bytes(M: int, N: int, K: int) -> int:
+    return int(lib().qqq_gemm_w8a8_workspace_bytes(M, N, K))
+
+
+def new_w8a8_workspace(M: int, N: int, K: int, device="cuda") -> torch.Tensor:
+    """For a program that keeps it over calls of one size (its contents do not matter)."""
+    return torch.empty((max(qqq_gemm_w8a8_workspace_bytes(M, N, K), 16),), dtype=_U8, device=device)
+
+
+def qqq_gemm_w8a8(a_q, s_a, w_packed, s_w, workspace=None, y=None, acc_out=None, dtype=torch.float16):
+    """a_q int8 [M,K] and s_a fp32 [M] (qqq_add_rmsnorm_quant, qqq_quant_act) times packed int8 weights with s_w fp32 [N] -> y [M,N] fp16 or fp32: that of y (row stride allowed), or
+    dtype where none is given.  Any N.  workspace: a uint8 tensor of qqq_gemm_w8a8_workspace_bytes(); without one torch's allocator lends it."""
+    _here(a_q, s_a, w_packed, s_w, workspace, y, acc_out)
+    if a_q.dim() != 2 or s_w.dim() != 1 or s_a.numel() != a_q.shape[0]:
+        raise ValueError("a_q must be 2-D with a scale for each row, s_w 1-D")
+    M, K = a_q.shape
+    N = s_w.shape[0]
+    L = lib()
+    if w_packed.numel() != L.qqq_packed_w8_bytes(N, K):
+        raise ValueError("w_packed must have the %d bytes of N=%d K=%d" % (L.qqq_packed_w8_bytes(N, K), N, K))
+    if y is None:
+        y = torch.empty((M, N), dtype=dtype, device=a_q.device)
+    if y.dtype not in _LOGITS or y.shape != (M, N) or (y.numel() and y.stride(1) != 1):
+        raise ValueError("y must be [%d, %d] fp16 or fp32 with unit inner stride" % (M, N))
+    if acc_out is not None and acc_out.shape != (M, N):
+        raise ValueError("acc_out must be [%d, %d]" % (M, N))
+    if workspace is None:
+        nbytes = L.qqq_gemm_w8a8_workspace_bytes(M, N, K)
+        workspace = torch.empty((nbytes,), dtype=_U8, device=a_q.device) if nbytes else None
+    _check(L.qqq_gemm_w8a8(_ptr(a_q, _I8), _ptr(s_a, torch.float32), _ptr(w_packed, _U8), _ptr(s_w, torch.float32), y.data_ptr(), _LOGITS[y.dtype], _row_stride(y),
+                           _ptr(acc_out, _I32), M, N, K, _ptr(workspace, _U8), 0 if workspace is None else workspace.numel(), _stream()))
+    return y
+
+
 class LogProbs(typing.NamedTuple):
     """Of M rows of logits."""
     logprob: typing.Optional[torch.Tensor]       # fp32 [M], of the given tokens
@@ -941,3 +1014,8 @@ def set_prefill_ksplit(k_splits: int) -> int:
 def set_factor_workgroups(most: int) -> int:
     """Diagnostic: the most workgroups of the compensation's factorisation (0 = automatic)."""
     return lib().qqq_set_factor_workgroups(most)
+
+
+def set_w8a8_tuning(shape: int, k_splits: int = 0) -> int:
+    """Diagnostic: kernel and parts of K of qqq_gemm_w8a8 (include/qqq_tuning.h; 0 = automatic)."""
+    return lib().qqq_set_w8a8_tuning(shape, k_splits)

@@ -13,7 +13,8 @@ LIB = os.path.join(HERE, "libqqq.so")
 SOURCES = ["qqq_api.hip", "qqq_pack.hip", "qqq_quant_act.hip", "qqq_gemm_skinny.hip",
            "qqq_gemm_prefill_dma.hip", "qqq_gemm_prefill_ring.hip", "qqq_group_bias.hip", "qqq_quant_weight.hip", "qqq_probes.hip", "qqq_calib.hip",
            "qqq_hessian.hip", "qqq_compensate.hip", "qqq_layer_api.hip", "qqq_layer_rows.hip", "qqq_kv8_cache.hip", "qqq_attention_kv8.hip",
-           "qqq_serve_api.hip", "qqq_kv8_plan.hip", "qqq_logprobs.hip"]
+           "qqq_serve_api.hip", "qqq_kv8_plan.hip", "qqq_logprobs.hip",
+           "qqq_gemm_w8a8_few.hip", "qqq_gemm_w8a8_tiles.hip"]
 # The last flag but the include paths: by default the compiler leaves out the restoring of the execution mask at the end of a branch that ends together with the
 # one around it.  Where registers are short it then puts a copy of a live value into that place, for the lanes of the inner branch only: attention with 32
 # rows of heads of 256 in equal shares lost a zero in the other lanes so, and stored to an address made with what was there instead.  No other kernel's assembly

@@ -1,6 +1,7 @@
 // C-ABI entry points of qqq_serve.h: argument validation (host code only).
 #include "qqq_plan.h"
 #include "qqq_serve.h"
+#include "qqq_w8a8.h"
 
 namespace qqq {
 
@@ -71,6 +72,14 @@ PlanArgs plan_args(const qqq_kv8_sessions* s, const qqq_kv8_batch* b) {
   return p;
 }
 
+constexpr int64_t kMostK = 131072, kMostN = 1 << 24;  // 127 * 127 * K stays below 2^31
+
+int check_product(const char* name, int64_t N, int64_t K) {
+  if (N < 1 || N > kMostN || K < 128 || K % 128 != 0 || K > kMostK)
+    return set_error(QQQ_ERR_SHAPE, "%s: unsupported N=%lld K=%lld (need 1 <= N <= 2^24, K%%128==0, 128 <= K <= 131072)", name, (long long)N, (long long)K);
+  return QQQ_OK;
+}
+
 int check_logits(const char* name, int64_t M, int64_t V, int type) {
   if (M < 0 || M > 0x7FFFFFFF || V < 1 || V >= kMost) return set_error(QQQ_ERR_SHAPE, "%s: unsupported %lld rows of %lld logits", name, (long long)M, (long long)V);
   if (type != QQQ_LOGITS_FP16 && type != QQQ_LOGITS_FP32) return set_error(QQQ_ERR_SHAPE, "%s: logits of type %d", name, type);
@@ -130,6 +139,69 @@ int qqq_kv8_release(const qqq_kv8_sessions* sessions, const int32_t* ids, int64_
   p.sequences = (int32_t)count;
   route_reset();
   return launch_kv8_release(p, (hipStream_t)stream);
+}
+
+size_t qqq_packed_w8_bytes(int64_t N, int64_t K) { return check_product("qqq_packed_w8_bytes", N, K) ? 0 : (size_t)((N + 15) / 16 * 16 * K); }
+
+int qqq_pack_w8(const int8_t* w_codes, int64_t N, int64_t K, int64_t ldw, void* w_packed, void* stream) {
+  const char* name = "qqq_pack_w8";
+  if (int rc = check_product(name, N, K)) return rc;
+  if (ldw < K || ldw % 16) return set_error(QQQ_ERR_SHAPE, "%s: row stride %lld for %lld codes", name, (long long)ldw, (long long)K);
+  if (!w_codes || !w_packed) return set_error(QQQ_ERR_NULL, "%s: NULL pointer", name);
+  if (!aligned(w_codes, 16) || !aligned(w_packed, 16) || w_codes == w_packed) return set_error(QQQ_ERR_SHAPE, "%s: misaligned pointer, or in place", name);
+  route_reset();
+  return launch_pack_w8(w_codes, N, K, ldw, static_cast<int8_t*>(w_packed), (hipStream_t)stream);
+}
+
+int qqq_unpack_w8(const void* w_packed, int64_t N, int64_t K, int8_t* w_codes, void* stream) {
+  const char* name = "qqq_unpack_w8";
+  if (int rc = check_product(name, N, K)) return rc;
+  if (!w_codes || !w_packed) return set_error(QQQ_ERR_NULL, "%s: NULL pointer", name);
+  if (!aligned(w_codes, 16) || !aligned(w_packed, 16) || w_codes == w_packed) return set_error(QQQ_ERR_SHAPE, "%s: misaligned pointer, or in place", name);
+  route_reset();
+  return launch_unpack_w8(static_cast<const int8_t*>(w_packed), N, K, w_codes, (hipStream_t)stream);
+}
+
+size_t qqq_gemm_w8a8_workspace_bytes(int64_t M, int64_t N, int64_t K) {
+  if (check_product("qqq_gemm_w8a8_workspace_bytes", N, K) || M < 1 || M > 0x7FFFFFFF) return 0;
+  const W8Plan plan = w8_plan(M, N, K);
+  return plan.k_splits > 1 ? (size_t)plan.k_splits * M * N * sizeof(int32_t) : 0;
+}
+
+int qqq_gemm_w8a8(const int8_t* a_q, const float* s_a, const void* w_packed, const float* s_w, void* y, int y_type, int64_t ldy, int32_t* acc_out, int64_t M,
+                  int64_t N, int64_t K, void* workspace, size_t workspace_bytes, void* stream) {
+  const char* name = "qqq_gemm_w8a8";
+  if (int rc = check_product(name, N, K)) return rc;
+  if (M < 0 || M > 0x7FFFFFFF) return set_error(QQQ_ERR_SHAPE, "%s: M=%lld", name, (long long)M);
+  if (y_type != QQQ_OUT_FP16 && y_type != QQQ_OUT_FP32) return set_error(QQQ_ERR_SHAPE, "%s: outputs of type %d", name, y_type);
+  if (ldy < N) return set_error(QQQ_ERR_SHAPE, "%s: row stride %lld for %lld outputs", name, (long long)ldy, (long long)N);
+  if (M == 0) return QQQ_OK;
+  if (!a_q || !s_a || !w_packed || !s_w || !y) return set_error(QQQ_ERR_NULL, "%s: NULL pointer", name);
+  const int size = y_type == QQQ_OUT_FP32 ? 4 : 2;
+  if (!aligned(a_q, 16) || !aligned(w_packed, 16) || !aligned(workspace, 16) || !aligned(s_a, 4) || !aligned(s_w, 4) || !aligned(acc_out, 4) || !aligned(y, size))
+    return set_error(QQQ_ERR_SHAPE, "%s: misaligned pointer", name);
+  const W8Plan plan = w8_plan(M, N, K);
+  const size_t need = plan.k_splits > 1 ? (size_t)plan.k_splits * M * N * sizeof(int32_t) : 0;
+  if (need && (!workspace || workspace_bytes < need))
+    return set_error(QQQ_ERR_WORKSPACE, "%s: workspace %zu bytes < %zu needed", name, workspace ? workspace_bytes : 0, need);
+  W8Params p = {};
+  p.a_q = a_q;
+  p.s_a = s_a;
+  p.w = static_cast<const int8_t*>(w_packed);
+  p.s_w = s_w;
+  p.y = y;
+  p.ldy = ldy;
+  p.acc_out = acc_out;
+  p.part = static_cast<int32_t*>(workspace);
+  p.M = (int)M;
+  p.N = (int)N;
+  p.K = (int)K;
+  p.k_splits = plan.k_splits;
+  p.f32 = y_type == QQQ_OUT_FP32;
+  p.wide = aligned(y, 16) && ldy * size % 16 == 0;
+  route_reset();
+  if (int rc = plan.shape == kW8Few ? launch_w8_few(p, (hipStream_t)stream) : launch_w8_tiles(p, plan.shape, (hipStream_t)stream)) return rc;
+  return plan.k_splits > 1 ? launch_w8_sum(p, (hipStream_t)stream) : QQQ_OK;
 }
 
 size_t qqq_logprobs_workspace_bytes(int64_t M, int64_t V, int type) {

@@ -116,3 +116,41 @@ def test_logprobs_binding_refusals():
     for call in (lambda: binding.qqq_logprobs(x), lambda: binding.qqq_logprobs(x.double()), lambda: binding.qqq_logprobs(x[0]), lambda: binding.qqq_logprobs(x.t())):
         with pytest.raises(ValueError):
             call()
+
+
+def test_product_refusals(L):
+    def call(a=BAD, s_a=BAD, w=BAD, s_w=BAD, y=BAD, kind=0, ldy=100, acc=None, M=3, N=100, K=256, work=BAD, nbytes=1 << 30):
+        return L.qqq_gemm_w8a8(a, s_a, w, s_w, y, kind, ldy, acc, M, N, K, work, nbytes, None)
+    odd = ctypes.c_void_p(0x1002)
+    assert call(M=0) == 0
+    for bad in (dict(M=-1), dict(N=0), dict(N=(1 << 24) + 1, ldy=1 << 25), dict(K=200), dict(K=0), dict(K=131072 + 128), dict(kind=2), dict(kind=-1), dict(ldy=99), dict(a=ctypes.c_void_p(0x1008)),
+                dict(w=ctypes.c_void_p(0x1008)), dict(s_a=odd), dict(s_w=odd), dict(y=ctypes.c_void_p(0x1001)), dict(y=odd, kind=1), dict(acc=odd), dict(work=ctypes.c_void_p(0x1008))):
+        assert call(**bad) == SHAPE, bad
+    for missing in ("a", "s_a", "w", "s_w", "y"):
+        assert call(**{missing: None}) == NULL, missing
+    assert L.qqq_set_w8a8_tuning(9, 0) == -1 and L.qqq_set_w8a8_tuning(0, -1) == -1
+    assert L.qqq_set_w8a8_tuning(0, 2) == 0
+    try:
+        need = L.qqq_gemm_w8a8_workspace_bytes(3, 100, 256)
+        assert need == 2 * 3 * 100 * 4 and call(nbytes=need - 1) == WORKSPACE and call(work=None) == WORKSPACE
+    finally:
+        L.qqq_set_w8a8_tuning(0, 0)
+    assert L.qqq_gemm_w8a8_workspace_bytes(3, 100, 200) == 0 and L.qqq_gemm_w8a8_workspace_bytes(0, 100, 256) == 0
+
+
+def test_packing_refusals(L):
+    assert L.qqq_packed_w8_bytes(17, 256) == 32 * 256 and L.qqq_packed_w8_bytes(0, 256) == 0 and L.qqq_packed_w8_bytes(16, 200) == 0
+    other = ctypes.c_void_p(0x2000)
+    assert L.qqq_pack_w8(BAD, 16, 256, 255, other, None) == SHAPE and L.qqq_pack_w8(BAD, 16, 256, 264, other, None) == SHAPE and L.qqq_pack_w8(BAD, 16, 256, 256, BAD, None) == SHAPE
+    assert L.qqq_pack_w8(None, 16, 256, 256, other, None) == NULL and L.qqq_pack_w8(BAD, 16, 256, 256, None, None) == NULL
+    assert L.qqq_pack_w8(ctypes.c_void_p(0x1008), 16, 256, 256, other, None) == SHAPE and L.qqq_pack_w8(BAD, 16, 100, 112, other, None) == SHAPE
+    assert L.qqq_unpack_w8(None, 16, 256, other, None) == NULL and L.qqq_unpack_w8(BAD, 16, 256, BAD, None) == SHAPE and L.qqq_unpack_w8(BAD, 16, 100, other, None) == SHAPE
+
+
+def test_product_binding_refusals():
+    i8 = lambda *s: torch.zeros(s, dtype=torch.int8)  # noqa: E731
+    f32 = lambda *s: torch.zeros(s)  # noqa: E731
+    for call in (lambda: binding.qqq_pack_w8(i8(16, 128)), lambda: binding.qqq_pack_w8(f32(16, 128)), lambda: binding.qqq_unpack_w8(torch.zeros(2048, dtype=torch.uint8), 16, 128),
+                 lambda: binding.qqq_gemm_w8a8(i8(2, 128), f32(2), torch.zeros(2048, dtype=torch.uint8), f32(16))):
+        with pytest.raises(ValueError):
+            call()
