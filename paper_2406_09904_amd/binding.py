@@ -63,6 +63,7 @@ def _no_native(*args):
 
 
 _native_linear = _native_rmsnorm = _native_gated = _native_append = _native_read = _native_attention = _no_native
+_native_plan = _native_w8a8 = _native_logprobs = _no_native
 
 
 def _call_path():
@@ -71,9 +72,9 @@ def _call_path():
 
 
 def _load_native(library):
-    """The extension that takes the linear calls and those of include/qqq_layer.h from tensors to the library (csrc/qqq_torch_call.cpp).  Without
+    """The extension that takes the linear calls and those of include/qqq_layer.h and include/qqq_serve.h from tensors to the library (csrc/qqq_torch_call.cpp).  Without
     it they are marshalled here."""
-    global _native_linear, _native_rmsnorm, _native_gated, _native_append, _native_read, _native_attention
+    global _native_linear, _native_rmsnorm, _native_gated, _native_append, _native_read, _native_attention, _native_plan, _native_w8a8, _native_logprobs
     path = _call_path()
     try:
         spec = importlib.util.spec_from_file_location("_qqq_call", path)
@@ -86,7 +87,10 @@ def _load_native(library):
     module.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (library.qqq_linear_w4a8_perchannel, library.qqq_linear_w4a8_pergroup)))
     module.bind_layer(*(ctypes.cast(getattr(library, n), ctypes.c_void_p).value for n in LAYER_SYMBOLS))
     _native_linear, _native_rmsnorm, _native_gated = module.linear, module.rmsnorm, module.gated
+    module.bind_serve(*(ctypes.cast(getattr(library, n), ctypes.c_void_p).value for n in (
+        "qqq_kv8_plan_workspace_bytes", "qqq_kv8_plan", "qqq_packed_w8_bytes", "qqq_gemm_w8a8_workspace_bytes", "qqq_gemm_w8a8", "qqq_logprobs_workspace_bytes", "qqq_logprobs")))
     _native_append, _native_read, _native_attention = module.append, module.read, module.attention
+    _native_plan, _native_w8a8, _native_logprobs = module.plan, module.w8a8, module.logprobs
 
 
 def lib():
@@ -795,6 +799,13 @@ def qqq_kv8_plan(sessions: KV8Sessions, batch: KV8Batch, new, page_tokens, seque
     sequence, positions: int32 [tokens], of each row its sequence and its position; lacking: int32 [1], pages that were not there.  tokens: rows of the
     step's tensors, where neither is given (none: as many as come).  after: (held, free_count) of after the step in tensors of their own; without it in place.  workspace: a
     uint8 tensor of qqq_kv8_plan_workspace_bytes(); without one torch's allocator lends it."""
+    if _lib and new.is_cuda:
+        d = _device()
+        rc = _native_plan(sessions, batch, new, page_tokens, sequence, positions, lacking, after, tokens, workspace, d, _raw_stream(d))
+        if rc is not None:
+            if rc:
+                _check(rc)
+            return batch
     s = _sessions_struct(sessions, page_tokens, after)
     table, kv_len, cu, slots, max_new, max_len = batch
     _here(table, kv_len, cu, slots, new, sequence, positions, lacking, workspace)
@@ -877,6 +888,11 @@ def new_w8a8_workspace(M: int, N: int, K: int, device="cuda") -> torch.Tensor:
 def qqq_gemm_w8a8(a_q, s_a, w_packed, s_w, workspace=None, y=None, acc_out=None, dtype=torch.float16):
     """a_q int8 [M,K] and s_a fp32 [M] (qqq_add_rmsnorm_quant, qqq_quant_act) times packed int8 weights with s_w fp32 [N] -> y [M,N] fp16 or fp32: that of y (row stride allowed), or
     dtype where none is given.  Any N.  workspace: a uint8 tensor of qqq_gemm_w8a8_workspace_bytes(); without one torch's allocator lends it."""
+    if _lib and a_q.is_cuda and (y is not None or dtype in _LOGITS):
+        d = _device()
+        out = _native_w8a8(a_q, s_a, w_packed, s_w, workspace, y, acc_out, dtype is torch.float32, d, _raw_stream(d))
+        if out is not None:
+            return _checked(out)
     _here(a_q, s_a, w_packed, s_w, workspace, y, acc_out)
     if a_q.dim() != 2 or s_w.dim() != 1 or s_a.numel() != a_q.shape[0]:
         raise ValueError("a_q must be 2-D with a scale for each row, s_w 1-D")
@@ -920,6 +936,11 @@ def qqq_logprobs(logits, tokens=None, top=0, out: LogProbs = None, workspace=Non
     """logits [M,V] fp16 or fp32 (row stride allowed) -> log probabilities of tokens (int32 [M]; below 0: none, 0), entropies, the logarithms of the sums and the `top` likeliest
     tokens (up to MAX_TOP).  out: what to write into, None where a number is not wanted.  workspace: a uint8 tensor of qqq_logprobs_workspace_bytes(); without one
     torch's allocator lends it."""
+    if _lib and logits.is_cuda:
+        d = _device()
+        given = _native_logprobs(logits, tokens, top, out, workspace, d, _raw_stream(d))
+        if given is not None:
+            return out if given is out else LogProbs(*_checked(given))
     if logits.dtype not in _LOGITS or logits.dim() != 2 or (logits.numel() and logits.stride(1) != 1):
         raise ValueError("logits must be a 2-D fp16 or fp32 device tensor with unit inner stride")
     _here(logits, tokens, workspace)

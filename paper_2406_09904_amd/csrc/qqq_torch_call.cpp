@@ -1,4 +1,4 @@
-// The two linear calls of binding.py, and those of qqq_layer.h, from tensors to the C ABI in one step of native code.  A one-row call takes the GPU 4.8 us and
+// The two linear calls of binding.py, and those of qqq_layer.h and qqq_serve.h, from tensors to the C ABI in one step of native code.  A one-row call takes the GPU 4.8 us and
 // took Python 6.3 to marshal (a method call per data pointer, contiguity, type and size, ctypes' conversions): calls in a row 6.34 us each, 5.35 so.
 // Only the plain case is handled: dense tensors that are exactly torch.Tensor, on the GPU, as the call wants them.  Anything else (a subclass, a
 // wrapper without storage, a function mode, a wrong type or stride, a failed allocation) returns None, and binding.py's own path, which decides what is
@@ -14,6 +14,7 @@
 #include <type_traits>
 
 #include "qqq_layer.h"
+#include "qqq_serve.h"
 
 namespace {
 
@@ -402,13 +403,235 @@ PyObject* bind_layer(PyObject*, PyObject* args) {
   Py_RETURN_NONE;
 }
 
+// ---- qqq_serve.h, in the same way
+
+struct {
+  decltype(&qqq_kv8_plan_workspace_bytes) plan_bytes;
+  decltype(&qqq_kv8_plan) plan;
+  decltype(&qqq_packed_w8_bytes) packed_bytes;
+  decltype(&qqq_gemm_w8a8_workspace_bytes) w8a8_bytes;
+  decltype(&qqq_gemm_w8a8) w8a8;
+  decltype(&qqq_logprobs_workspace_bytes) logprobs_bytes;
+  decltype(&qqq_logprobs) logprobs;
+} serve = {};
+
+// None, or a dense tensor of that type and device; `ok` is cleared for anything else
+const at::Tensor* maybe(PyObject* o, at::ScalarType type, long device, bool& ok) {
+  if (o == Py_None) return nullptr;
+  const at::Tensor* t = dense(o, type);
+  if (!t || t->get_device() != device) ok = false;
+  return t;
+}
+template <typename T>
+T* pointer(const at::Tensor* t) {
+  return t ? static_cast<T*>(t->data_ptr()) : nullptr;
+}
+// the workspace that is given, or one of `bytes` that the allocator lends
+struct Work {
+  at::Tensor lent;
+  void* at = nullptr;
+  size_t bytes = 0;
+  void take(const at::Tensor* given, size_t need, const at::Tensor& like) {
+    if (given) {
+      at = given->data_ptr();
+      bytes = (size_t)given->numel();
+    } else if (need) {
+      lent = at::empty({(int64_t)need}, like.options().dtype(at::kByte));
+      at = lent.data_ptr();
+      bytes = need;
+    }
+  }
+};
+
+// plan(sessions, batch, new, page_tokens, sequence or None, positions or None, lacking or None, after or None, tokens or None, workspace or None, device, stream)
+// -> an error code (0 too), or None
+PyObject* plan(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (n != 12 || !serve.plan || !serve.plan_bytes) Py_RETURN_NONE;
+  try {
+    PyObject *const so = args[0], *const bo = args[1], *const ao = args[7];
+    if (!plain_world() || !PyTuple_Check(so) || PyTuple_GET_SIZE(so) != 4 || !PyTuple_Check(bo) || PyTuple_GET_SIZE(bo) != 6 ||
+        !(ao == Py_None || (PyTuple_Check(ao) && PyTuple_GET_SIZE(ao) == 2)) || args[8] != Py_None)
+      Py_RETURN_NONE;
+    const long page_tokens = PyLong_AsLong(args[3]), device = PyLong_AsLong(args[10]);
+    void* const stream = PyLong_AsVoidPtr(args[11]);
+    const long max_new = PyLong_AsLong(PyTuple_GET_ITEM(bo, 4)), max_len = PyLong_AsLong(PyTuple_GET_ITEM(bo, 5));
+    if (PyErr_Occurred() || page_tokens != (int32_t)page_tokens || max_new != (int32_t)max_new || max_len != (int32_t)max_len) {
+      PyErr_Clear();
+      Py_RETURN_NONE;
+    }
+    bool ok = true;
+    const at::Tensor *pages = rows(PyTuple_GET_ITEM(so, 0), at::kInt), *table = rows(PyTuple_GET_ITEM(bo, 0), at::kInt);
+    const at::Tensor *held = maybe(PyTuple_GET_ITEM(so, 1), at::kInt, device, ok), *free_pages = maybe(PyTuple_GET_ITEM(so, 2), at::kInt, device, ok);
+    const at::Tensor *count = maybe(PyTuple_GET_ITEM(so, 3), at::kInt, device, ok), *kv_len = maybe(PyTuple_GET_ITEM(bo, 1), at::kInt, device, ok);
+    const at::Tensor *cu = maybe(PyTuple_GET_ITEM(bo, 2), at::kInt, device, ok), *slots = maybe(PyTuple_GET_ITEM(bo, 3), at::kInt, device, ok);
+    const at::Tensor *fresh = maybe(args[2], at::kInt, device, ok), *sequence = maybe(args[4], at::kInt, device, ok), *positions = maybe(args[5], at::kInt, device, ok);
+    const at::Tensor *lacking = maybe(args[6], at::kInt, device, ok), *work = maybe(args[9], at::kByte, device, ok);
+    const at::Tensor *held_after = ao == Py_None ? held : maybe(PyTuple_GET_ITEM(ao, 0), at::kInt, device, ok);
+    const at::Tensor *count_after = ao == Py_None ? count : maybe(PyTuple_GET_ITEM(ao, 1), at::kInt, device, ok);
+    if (!ok || !pages || !table || !held || !free_pages || !count || !kv_len || !cu || !fresh || !held_after || !count_after || pages->get_device() != device ||
+        table->get_device() != device)
+      Py_RETURN_NONE;
+    const int64_t S = pages->size(0), B = table->size(0);
+    if (S > 0x7FFFFFFF || B > 0x7FFFFFFF || pages->size(1) > 0x7FFFFFFF || table->size(1) > 0x7FFFFFFF || !is_shape(*held, {S}) || !is_shape(*held_after, {S}) ||
+        free_pages->dim() != 1 || count->numel() != 1 || count_after->numel() != 1 || !is_shape(*kv_len, {B}) || !is_shape(*cu, {B + 1}) || !is_shape(*fresh, {B}) ||
+        (slots && !is_shape(*slots, {B})) || (sequence && sequence->dim() != 1) || (positions && positions->dim() != 1) || (lacking && lacking->numel() != 1) ||
+        (sequence && positions && sequence->numel() != positions->numel()))
+      Py_RETURN_NONE;
+    const int64_t tokens = sequence ? sequence->numel() : positions ? positions->numel() : (int64_t)1 << 30;
+    const qqq_kv8_sessions s = {pointer<int32_t>(pages), row_stride(*pages), pointer<int32_t>(held), pointer<int32_t>(held_after), pointer<int32_t>(free_pages),
+                                pointer<int32_t>(count), pointer<int32_t>(count_after), free_pages->numel(), (int32_t)S, (int32_t)pages->size(1), (int32_t)page_tokens};
+    const qqq_kv8_batch b = {pointer<int32_t>(table), row_stride(*table), pointer<int32_t>(kv_len), pointer<int32_t>(cu), pointer<int32_t>(slots), (int32_t)table->size(1),
+                             (int32_t)B, (int32_t)max_new, (int32_t)max_len};
+    Work w;
+    w.take(work, work ? 0 : serve.plan_bytes(&s, &b), *table);
+    int32_t *p0 = pointer<int32_t>(fresh), *p1 = pointer<int32_t>(sequence), *p2 = pointer<int32_t>(positions), *p3 = pointer<int32_t>(lacking);
+    int rc;
+    Py_BEGIN_ALLOW_THREADS;
+    rc = serve.plan(&s, &b, p0, tokens, p1, p2, p3, w.at, w.bytes, stream);
+    Py_END_ALLOW_THREADS;
+    return PyLong_FromLong(rc);
+  } catch (const std::exception&) {
+    PyErr_Clear();
+    Py_RETURN_NONE;
+  }
+}
+
+// w8a8(a_q, s_a, w_packed, s_w, workspace or None, y or None, acc_out or None, f32 (of a new y), device, stream) -> y, an error code, or None
+PyObject* w8a8(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (n != 10 || !serve.w8a8 || !serve.w8a8_bytes || !serve.packed_bytes) Py_RETURN_NONE;
+  try {
+    if (!plain_world() || !PyBool_Check(args[7])) Py_RETURN_NONE;
+    const long device = PyLong_AsLong(args[8]);
+    void* const stream = PyLong_AsVoidPtr(args[9]);
+    if (PyErr_Occurred()) {
+      PyErr_Clear();
+      Py_RETURN_NONE;
+    }
+    bool ok = true;
+    const at::Tensor *a = maybe(args[0], at::kChar, device, ok), *s_a = maybe(args[1], at::kFloat, device, ok), *w = maybe(args[2], at::kByte, device, ok);
+    const at::Tensor *s_w = maybe(args[3], at::kFloat, device, ok), *work = maybe(args[4], at::kByte, device, ok), *acc = maybe(args[6], at::kInt, device, ok);
+    if (!ok || !a || !s_a || !w || !s_w || a->dim() != 2 || s_w->dim() != 1 || s_a->numel() != a->size(0)) Py_RETURN_NONE;
+    const int64_t M = a->size(0), K = a->size(1), N = s_w->size(0);
+    if (w->numel() != (int64_t)serve.packed_bytes(N, K) || w->numel() == 0 || (acc && !is_shape(*acc, {M, N}))) Py_RETURN_NONE;
+    at::Tensor made;
+    const at::Tensor* y;
+    if (args[5] == Py_None) {
+      made = at::empty({M, N}, a->options().dtype(args[7] == Py_True ? at::kFloat : at::kHalf));
+      y = &made;
+    } else {
+      y = rows(args[5], at::kHalf);
+      if (!y) y = rows(args[5], at::kFloat);
+      if (!y || y->get_device() != device || !is_shape(*y, {M, N})) Py_RETURN_NONE;
+    }
+    Work lent;
+    lent.take(work, work ? 0 : serve.w8a8_bytes(M, N, K), *a);
+    const int type = y->scalar_type() == at::kFloat ? QQQ_OUT_FP32 : QQQ_OUT_FP16;
+    const int64_t ldy = row_stride(*y);
+    const int8_t* pa = pointer<int8_t>(a);
+    const float *psa = pointer<float>(s_a), *psw = pointer<float>(s_w);
+    void *pw = w->data_ptr(), *py = y->data_ptr();
+    int32_t* pacc = pointer<int32_t>(acc);
+    int rc;
+    Py_BEGIN_ALLOW_THREADS;
+    rc = serve.w8a8(pa, psa, pw, psw, py, type, ldy, pacc, M, N, K, lent.at, lent.bytes, stream);
+    Py_END_ALLOW_THREADS;
+    return rc != 0 ? PyLong_FromLong(rc) : given_or(args[5], made);
+  } catch (const std::exception&) {
+    PyErr_Clear();
+    Py_RETURN_NONE;
+  }
+}
+
+// logprobs(logits, tokens or None, top, out or None, workspace or None, device, stream) -> the five outputs (out where it is given), an error code, or None
+PyObject* logprobs(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (n != 7 || !serve.logprobs || !serve.logprobs_bytes) Py_RETURN_NONE;
+  try {
+    const long top = PyLong_AsLong(args[2]), device = PyLong_AsLong(args[5]);
+    void* const stream = PyLong_AsVoidPtr(args[6]);
+    if (PyErr_Occurred()) {
+      PyErr_Clear();
+      Py_RETURN_NONE;
+    }
+    if (!plain_world() || top < 0 || top > QQQ_MAX_TOP || !(args[3] == Py_None || (PyTuple_Check(args[3]) && PyTuple_GET_SIZE(args[3]) == 5))) Py_RETURN_NONE;
+    bool ok = true;
+    const at::Tensor* x = rows(args[0], at::kHalf);
+    if (!x) x = rows(args[0], at::kFloat);
+    const at::Tensor *tokens = maybe(args[1], at::kInt, device, ok), *work = maybe(args[4], at::kByte, device, ok);
+    if (!ok || !x || x->get_device() != device) Py_RETURN_NONE;
+    const int64_t M = x->size(0), V = x->size(1);
+    if (tokens && !is_shape(*tokens, {M})) Py_RETURN_NONE;
+    at::Tensor made[5];
+    const at::Tensor* out[5] = {};
+    const bool wanted[5] = {tokens != nullptr, true, true, top > 0, top > 0};
+    for (int i = 0; i < 5; ++i) {
+      const at::ScalarType type = i == 3 ? at::kInt : at::kFloat;
+      if (args[3] == Py_None) {
+        if (!wanted[i]) continue;
+        made[i] = i < 3 ? at::empty({M}, x->options().dtype(type)) : at::empty({M, top}, x->options().dtype(type));
+        out[i] = &made[i];
+      } else {
+        out[i] = maybe(PyTuple_GET_ITEM(args[3], i), type, device, ok);
+        if (!ok || (out[i] && !(i < 3 ? is_shape(*out[i], {M}) : is_shape(*out[i], {M, top})))) Py_RETURN_NONE;
+      }
+    }
+    const int type = x->scalar_type() == at::kFloat ? QQQ_LOGITS_FP32 : QQQ_LOGITS_FP16;
+    Work lent;
+    lent.take(work, work ? 0 : serve.logprobs_bytes(M, V, type), *x);
+    const void* px = x->data_ptr();
+    const int64_t ld = row_stride(*x);
+    const int32_t* pt = pointer<int32_t>(tokens);
+    float *p0 = pointer<float>(out[0]), *p1 = pointer<float>(out[1]), *p2 = pointer<float>(out[2]), *p4 = pointer<float>(out[4]);
+    int32_t* p3 = pointer<int32_t>(out[3]);
+    int rc;
+    Py_BEGIN_ALLOW_THREADS;
+    rc = serve.logprobs(px, ld, type, M, V, pt, (int)top, p0, p1, p2, p3, p4, lent.at, lent.bytes, stream);
+    Py_END_ALLOW_THREADS;
+    if (rc != 0) return PyLong_FromLong(rc);
+    if (args[3] != Py_None) {
+      Py_INCREF(args[3]);
+      return args[3];
+    }
+    PyObject* t = PyTuple_New(5);
+    if (!t) return nullptr;
+    for (int i = 0; i < 5; ++i) {
+      PyObject* o = out[i] ? THPVariable_Wrap(made[i]) : none();
+      if (!o) {
+        Py_DECREF(t);
+        return nullptr;
+      }
+      PyTuple_SET_ITEM(t, i, o);
+    }
+    return t;
+  } catch (const std::exception&) {
+    PyErr_Clear();
+    Py_RETURN_NONE;
+  }
+}
+
+// bind_serve(addresses of the seven entry points, in the order of `serve`)
+PyObject* bind_serve(PyObject*, PyObject* args) {
+  unsigned long long a[7] = {};
+  if (!PyArg_ParseTuple(args, "KKKKKKK", a, a + 1, a + 2, a + 3, a + 4, a + 5, a + 6)) return nullptr;
+  auto set = [&](auto& f, int i) { f = reinterpret_cast<std::decay_t<decltype(f)>>(static_cast<uintptr_t>(a[i])); };
+  set(serve.plan_bytes, 0);
+  set(serve.plan, 1);
+  set(serve.packed_bytes, 2);
+  set(serve.w8a8_bytes, 3);
+  set(serve.w8a8, 4);
+  set(serve.logprobs_bytes, 5);
+  set(serve.logprobs, 6);
+  Py_RETURN_NONE;
+}
+
 template <typename F>
 PyMethodDef fast(const char* name, F f) {
   return {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(f)), METH_FASTCALL, nullptr};
 }
 
 PyMethodDef methods[] = {fast("rmsnorm", rmsnorm), fast("gated", gated), fast("append", append), fast("read", read), fast("attention", attention),
+                         fast("plan", plan), fast("w8a8", w8a8), fast("logprobs", logprobs),
                          {"bind_layer", bind_layer, METH_VARARGS, nullptr},
+                         {"bind_serve", bind_serve, METH_VARARGS, nullptr},
                          {"linear", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(linear)), METH_FASTCALL, nullptr},
                          {"bind", bind, METH_VARARGS, nullptr},
                          {nullptr, nullptr, 0, nullptr}};

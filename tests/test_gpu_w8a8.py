@@ -155,3 +155,30 @@ def test_captured(M, shape, k_splits):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(y, _want(a_q, s_a, w_q, s_w, torch.float32)[1])
+
+
+def test_refusals_on_the_device():
+    """What neither path of the binding takes."""
+    a_q, s_a, w, s_w = torch.zeros(2, 128, dtype=torch.int8, device="cuda"), torch.zeros(2, device="cuda"), torch.zeros(2048, dtype=torch.uint8, device="cuda"), torch.zeros(16, device="cuda")
+    for call in (lambda: qqq.qqq_gemm_w8a8(a_q, s_a, w, s_w, dtype=torch.bfloat16), lambda: qqq.qqq_gemm_w8a8(a_q, s_a, w[:1024], s_w), lambda: qqq.qqq_gemm_w8a8(a_q, s_a[:1], w, s_w),
+                 lambda: qqq.qqq_gemm_w8a8(a_q, s_a, w, s_w.half()), lambda: qqq.qqq_gemm_w8a8(a_q, s_a, w, s_w, y=torch.zeros(2, 15, device="cuda")),
+                 lambda: qqq.qqq_gemm_w8a8(a_q, s_a, w, s_w, acc_out=torch.zeros(16, 2, dtype=torch.int32, device="cuda").t()), lambda: qqq.qqq_gemm_w8a8(a_q.cpu(), s_a, w, s_w),
+                 lambda: qqq.qqq_gemm_w8a8(a_q, s_a, w.cpu(), s_w)):
+        with pytest.raises(ValueError):
+            call()
+    with pytest.raises(qqq.QQQError):
+        qqq.qqq_pack_w8(a_q[:, :112])
+
+
+def test_tensors_of_another_device_than_the_current_one(monkeypatch):
+    """As if the current device were another: refused, by the native marshalling's fall-back too."""
+    a_q, s_a, w, s_w = torch.zeros(2, 128, dtype=torch.int8, device="cuda"), torch.zeros(2, device="cuda"), torch.zeros(2048, dtype=torch.uint8, device="cuda"), torch.zeros(16, device="cuda")
+    stream = torch.cuda.current_stream().cuda_stream
+    monkeypatch.setattr(qqq, "_device", lambda: 1)
+    monkeypatch.setattr(qqq, "_raw_stream", lambda device: stream)
+    logits = torch.zeros(3, 40, device="cuda")
+    sessions, batch = qqq.new_kv8_sessions(2, 3, 9), qqq.new_kv8_batch(2, 3, 1, 20)
+    for call in (lambda: qqq.qqq_gemm_w8a8(a_q, s_a, w, s_w), lambda: qqq.qqq_logprobs(logits), lambda: qqq.qqq_kv8_plan(sessions, batch, batch.kv_len, 16),
+                 lambda: qqq.qqq_kv8_release(sessions, 16), lambda: qqq.qqq_pack_w8(a_q)):
+        with pytest.raises(ValueError, match="current device"):
+            call()
