@@ -77,8 +77,8 @@ int qqq_unpack_w8(const void* w_packed, int64_t N, int64_t K, int8_t* w_codes, v
 /*
  * W8A8 GEMM:  acc[m,n] = sum_k a_q[m,k] * w[n,k]  (int32, exact),  t = fp32_rne(float(acc) * s_a[m]),
  *   y[m,n] = fp16_rne(t * s_w[n])  or  fp32_rne(t * s_w[n])  by y_type.
- *   a_q [M,K] int8, dense, 16-byte aligned, codes in [-127,127]; s_a [M] fp32; w_packed as above; s_w [N] fp32; y [M,ldy] of the type, ldy >= N, aligned to its type
- *   (aligned to 16 bytes with rows of whole 16 bytes it is written faster); acc_out [M,N] int32 dense or NULL (parity/debug).  1 <= N <= 2^24, K as above, M == 0 is a no-op.
+ *   a_q [M,K] int8, dense, 16-byte aligned, codes in [-127,127]; s_a [M] fp32; w_packed as above; s_w [N] fp32; y [M,ldy] of the type, ldy >= N, aligned to its type;
+ *   acc_out [M,N] int32 dense or NULL (parity/debug).  1 <= N <= 2^24, K as above, M == 0 is a no-op.
  *   workspace: qqq_gemm_w8a8_workspace_bytes() bytes, 16-byte aligned (partial sums of calls that split K; 0 where none is needed), contents irrelevant on entry;
  *   not shared by calls that may run concurrently.
  */

@@ -198,7 +198,6 @@ int qqq_gemm_w8a8(const int8_t* a_q, const float* s_a, const void* w_packed, con
   p.K = (int)K;
   p.k_splits = plan.k_splits;
   p.f32 = y_type == QQQ_OUT_FP32;
-  p.wide = aligned(y, 16) && ldy * size % 16 == 0;
   route_reset();
   if (int rc = plan.shape == kW8Few ? launch_w8_few(p, (hipStream_t)stream) : launch_w8_tiles(p, plan.shape, (hipStream_t)stream)) return rc;
   return plan.k_splits > 1 ? launch_w8_sum(p, (hipStream_t)stream) : QQQ_OK;

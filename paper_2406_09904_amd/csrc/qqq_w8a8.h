@@ -17,7 +17,6 @@ struct W8Params {
   int32_t* part;       // k_splits > 1: [k_splits][M][N] partial sums
   int M, N, K, k_splits;
   bool f32;            // the output's type
-  bool wide;           // rows of y are whole 16 bytes, aligned so
 };
 
 // One product rounded once to the output's type
@@ -36,11 +35,12 @@ int launch_pack_w8(const int8_t* w, int64_t N, int64_t K, int64_t ldw, int8_t* p
 int launch_unpack_w8(const int8_t* packed, int64_t N, int64_t K, int8_t* w, hipStream_t st);
 
 // How a call is launched: a rule on the sizes (w8_plan in qqq_gemm_w8a8_tiles.hip)
-enum W8ShapeId : int { kW8Few = 1, kW8Tile256x256, kW8Tile128x256, kW8Tile128x128, kW8Tile64x128 };  // (numbered as in qqq_tuning.h)
+enum W8ShapeId : int { kW8Few = 1, kW8Tile256x256, kW8Tile192x256, kW8Tile128x256, kW8Tile128x128, kW8Tile64x128 };  // (numbered as in qqq_tuning.h)
 struct W8Plan {
   int shape, k_splits;
 };
 W8Plan w8_plan(int64_t M, int64_t N, int64_t K);
+int w8_few_tiles(int64_t N, int mt);  // 16-channel tiles of its workgroups for mt row tiles
 int launch_w8_few(const W8Params& p, hipStream_t st);
 int launch_w8_tiles(const W8Params& p, int shape, hipStream_t st);
 int launch_w8_sum(const W8Params& p, hipStream_t st);
