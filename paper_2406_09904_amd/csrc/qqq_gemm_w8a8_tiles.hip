@@ -346,21 +346,22 @@ int launch_w8_sum(const W8Params& p, hipStream_t st) {
 }
 
 // ---- which kernel, and into how many parts K is cut: the least time of a cost model, in us.  Its constants are fitted to 6600 calls (N 512 .. 50001, K 512 .. 11008, M 1 .. 2048, each
-// with every kernel and up to 16 parts; rms 6 to 10 %); what it picks is 1.9 % behind the best of them on average and 33 % at most (N = 13824, K = 11008, M = 64 unsplit).
+// with every kernel and up to 16 parts; rms 6 to 10 %); what it picks is 1.6 % behind the best of them on average and 33 % at most (N = 13824, K = 11008, M = 64 unsplit).
 // Tiles: start + rounds * (fixed + blocks * per_block), a round being a workgroup a CU (two for the small tiles, whose blocks then take per_block_full); a last round of a share
-// x of the places takes alone + rising * x a block (small tiles with more than one workgroup on some CU: from shared to per_block_full).  Never less than the weights' bytes.
+// x of the places takes alone + rising * x a block (small tiles with more than one workgroup on some CU: from shared to per_block_full).  Never less than the weights'
+// bytes at the rate that such a launch streams them, a lower one where CUs have different numbers of workgroups.
 struct W8Cost {
   int bm, bn, per_cu;
-  double start, fixed, alone, rising, shared, per_block_full, per_byte;
+  double start, fixed, alone, rising, shared, per_block_full, per_byte, per_byte_uneven;
 };
 constexpr W8Cost kW8Cost[] = {
-    {256, 256, 1, 0.5, 7.4, 0.863, 0.425, 0, 1.481, 0.274e-6},
-    {192, 256, 1, 0.73, 6.19, 0.83, 0.278, 0, 1.18, 0.255e-6},
-    {128, 256, 1, 1.91, 3.81, 0.529, 0.359, 0, 0.975, 0.186e-6},
-    {128, 128, 2, 2.84, 2.04, 0.307, 0.424, 0.83, 1.09, 0.173e-6},
-    {64, 128, 2, 2.5, 1.7, 0.217, 0.248, 0.587, 0.731, 0.172e-6},
+    {256, 256, 1, 0.5, 7.59, 0.853, 0.465, 0, 1.458, 0.245e-6, 0.296e-6},
+    {192, 256, 1, 1.72, 5.41, 0.821, 0.301, 0, 1.203, 0.235e-6, 0.29e-6},
+    {128, 256, 1, 2.48, 3.41, 0.523, 0.384, 0, 0.998, 0.18e-6, 0.183e-6},
+    {128, 128, 2, 2.83, 2.16, 0.304, 0.425, 0.874, 1.09, 0.177e-6, 0.182e-6},
+    {64, 128, 2, 2.88, 1.39, 0.217, 0.264, 0.636, 0.746, 0.157e-6, 0.181e-6},
 };
-constexpr double kW8SumStart = 2.7, kW8SumPerValue = 1.7e-6;  // of the second launch that a split needs
+constexpr double kW8SumStart = 2.6, kW8SumPerValue = 1.7e-6;  // of the second launch that a split needs
 
 static double w8_tile_cost(const W8Cost& c, int64_t M, int64_t N, int64_t K, int splits) {
   const double blocks = (double)((K / 128 + splits - 1) / splits), places = (double)num_cus() * c.per_cu;
@@ -368,7 +369,8 @@ static double w8_tile_cost(const W8Cost& c, int64_t M, int64_t N, int64_t K, int
   const double full = floor(tiles / places), x = tiles / places - full;
   double t = c.start + full * (c.fixed + blocks * c.per_block_full);
   if (x > 0) t += c.fixed + blocks * (c.per_cu == 1 || x <= 0.5 ? c.alone + c.rising * x : c.shared + (c.per_block_full - c.shared) * (2 * x - 1));
-  const double bytes = c.start + c.per_byte * (double)N * (double)K;
+  const bool uneven = full > 0 || (c.per_cu == 2 && x > 0.5);
+  const double bytes = c.start + (uneven ? c.per_byte_uneven : c.per_byte) * (double)N * (double)K;
   return t > bytes ? t : bytes;
 }
 // Few rows: the weights' bytes, or what a workgroup computes where there are several a CU; every workgroup reads the activations

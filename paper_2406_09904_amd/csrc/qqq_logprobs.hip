@@ -2,6 +2,8 @@
 //
 // One pass keeps, per thread and relative to the largest logit m it has met,  z = sum e^(x-m)  and  t = sum (x-m) e^(x-m);  a larger m' turns them into
 // z f  and  (t + (m-m') z) f,  f = e^(m-m').  Then  lse = m + log z,  H = log z - t / z: no difference of large numbers is left in either.
+// For fp16 logits all of it is in powers of two and the reference is c, the integer above m log2 e: x log2 e - c is one mixed multiply-add, rounded once, and a change of c scales by
+// a power of two, exactly.  fp32 logits reach where x log2 e overflows, so x - m comes first.
 //
 // The largest `top` logits need nothing in that pass but the threads' maxima.  64 groups of threads hold disjoint parts of the row, so the top-th largest of the groups' maxima is
 // a lower bound of the row's top-th largest value, and only threads with a maximum of at least that look at their values again: 24 of them are expected for the
@@ -55,7 +57,7 @@ struct Row {
   // the i-th of the lead's and the tail's values, and its place
   __device__ __forceinline__ int place_of_odd(int i) const { return i < lead ? i : i + blocks * kVec; }
   template <bool PAST>
-  __device__ __forceinline__ uint4 block(int b) const { return load16<PAST>(at + lead * kSize + (int64_t)b * 16); }
+  __device__ __forceinline__ uint4 block(int b) const { return load16<PAST>(at + lead * kSize + (uint32_t)b * 16u); }
   __device__ __forceinline__ int place_of_block(int b) const { return lead + b * kVec; }
   static __device__ __forceinline__ uint4 masked_block() {
     constexpr uint32_t w = F32 ? 0xFF800000u : 0xFC00FC00u;  // -infinity
@@ -78,30 +80,72 @@ struct Row {
       }
       return m;
     } else {
-      h2 m = as_h2(v[0].x);
+      // (the instruction itself, which takes three operands and gives a NaN where there is one: the compiler would quiet every operand first)
+      uint32_t m = v[0].x;
 #pragma unroll
-      for (int u = 0; u < kUnroll; ++u) {
-        const uint32_t w[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) m = __builtin_elementwise_max(m, as_h2(w[i]));
-      }
-      return fmaxf((float)m[0], (float)m[1]);
+      for (int u = 0; u < kUnroll; ++u)
+        asm("v_pk_maximum3_f16 %0, %0, %1, %2\n\tv_pk_maximum3_f16 %0, %0, %3, %4" : "+v"(m) : "v"(v[u].x), "v"(v[u].y), "v"(v[u].z), "v"(v[u].w));
+      const h2 pair = as_h2(m);
+      return fmaxf((float)pair[0], (float)pair[1]);
     }
   }
 };
 
+template <bool F32>
 struct Sums {
-  float m = -FLT_MAX, z = 0.0f, t = 0.0f;
-  __device__ __forceinline__ void raise(float to) {  // m becomes the larger of the two; a NaN leaves it
-    const float larger = fmaxf(m, to), d = fmaxf(m - larger, kFar), f = __builtin_amdgcn_exp2f(d * kLog2e);
+  static constexpr float kUnit = F32 ? 1.0f : 0.6931471805599453f;   // of m and t, in natural logarithms
+  static constexpr float kToTwo = F32 ? kLog2e : 1.0f;               // and in powers of two
+  float largest = -FLT_MAX;                      // value met (a NaN is not one)
+  float m = F32 ? -FLT_MAX : -94505.0f;          // reference: of fp32 the largest value, of fp16 the integer above its log2 e times
+  float z = 0.0f, t = 0.0f;
+  __device__ __forceinline__ void refer_to(float to) {
+    const float higher = fmaxf(m, to), d = fmaxf(m - higher, kFar), f = __builtin_amdgcn_exp2f(d * kToTwo);
     t = (t + d * z) * f;
     z *= f;
-    m = larger;
+    m = higher;
   }
-  __device__ __forceinline__ void add(float x) {  // x <= m, or a NaN or infinity, which makes z a NaN
-    const float d = x - m, e = __builtin_amdgcn_exp2f(d * kLog2e);
+  __device__ __forceinline__ void meet(float x) {
+    largest = fmaxf(largest, x);
+    refer_to(F32 ? largest : ceilf(largest * kLog2e));
+  }
+  // of a value no larger than the largest; a NaN or infinity gives a NaN
+  __device__ __forceinline__ float below(float x) const { return F32 ? x - m : __builtin_fmaf(x, kLog2e, -m); }
+  static __device__ __forceinline__ float power(float d) { return __builtin_amdgcn_exp2f(d * kToTwo); }
+  __device__ __forceinline__ void add(float x) {
+    const float d = below(x), e = power(d);
     z += e;
     t = __builtin_fmaf(fmaxf(d, kFar), e, t);
+  }
+  __device__ __forceinline__ void add_blocks(const uint4* v) {
+    meet(Row<F32>::largest(v));
+    const float t_before = t;
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      float x[Row<F32>::kVec];
+      Row<F32>::unpack(v[u], x);
+#pragma unroll
+      for (int i = 0; i < Row<F32>::kVec; ++i) {
+        const float d = below(x[i]), e = power(d);
+        z += e;
+        t = __builtin_fmaf(d, e, t);
+      }
+    }
+    asm volatile("" : "+v"(z));  // (here: else every power is kept until behind the branch)
+    if (__builtin_expect(__ballot(t != t), 0)) {  // -infinity times 0: a masked value, whose part is 0 (or there is a NaN, which z has too)
+      t = t_before;
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) {
+        uint4 again = v[u];
+        asm("" : "+v"(again.x), "+v"(again.y), "+v"(again.z), "+v"(again.w));  // (else every difference and power is kept for this branch: 64 registers)
+        float x[Row<F32>::kVec];
+        Row<F32>::unpack(again, x);
+#pragma unroll
+        for (int i = 0; i < Row<F32>::kVec; ++i) {
+          const float d = below(x[i]);
+          t = __builtin_fmaf(fmaxf(d, kFar), power(d), t);
+        }
+      }
+    }
   }
 };
 
@@ -131,28 +175,23 @@ __device__ __forceinline__ float wave_sum(float v) {
   return (lane_value(v, 0) + lane_value(v, 16)) + (lane_value(v, 32) + lane_value(v, 48));
 }
 // of all lanes, in each of them; the order is fixed
-__device__ __forceinline__ Sums wave_sums(Sums s) {
-  s.raise(wave_max(s.m));
+template <bool F32>
+__device__ __forceinline__ Sums<F32> wave_sums(Sums<F32> s) {
+  s.refer_to(wave_max(s.m));
   s.z = wave_sum(s.z);
   s.t = wave_sum(s.t);
   return s;
 }
-template <int WAVES>
-__device__ __forceinline__ Sums join_waves(const float (*of_wave)[3]) {
-  Sums all;
-#pragma unroll
-  for (int w = 0; w < WAVES; ++w) all.m = fmaxf(all.m, of_wave[w][0]);
-#pragma unroll
-  for (int w = 0; w < WAVES; ++w) {
-    Sums s;
-    s.m = of_wave[w][0];
-    s.z = of_wave[w][1];
-    s.t = of_wave[w][2];
-    s.raise(all.m);
-    all.z += s.z;
-    all.t += s.t;
+template <bool F32, int WAVES>
+__device__ __forceinline__ Sums<F32> join_waves(const float (*of_wave)[3]) {  // a wave's sums a lane
+  Sums<F32> s;
+  const int lane = threadIdx.x & 63;
+  if (lane < WAVES) {
+    s.m = of_wave[lane][0];
+    s.z = of_wave[lane][1];
+    s.t = of_wave[lane][2];
   }
-  return all;
+  return wave_sums(s);
 }
 
 // ---- order.  Values by 32 bits that order as they do: a NaN above everything, -0 as 0
@@ -205,8 +244,8 @@ struct List {
 };
 
 // The waves' lists as one: entries to LDS, each one's rank counted, the first `top` written.
-template <int T>
-__device__ __forceinline__ void write_top(const LogprobArgs& p, int64_t row, const List& list, const Sums& all, float log_z, uint2* entries, int* count) {
+template <bool F32, int T>
+__device__ __forceinline__ void write_top(const LogprobArgs& p, int64_t row, const List& list, const Sums<F32>& all, float log_z, uint2* entries, int* count) {
   const int lane = threadIdx.x & 63;
   const bool has = lane < p.top && (list.order | list.place) != 0;
   const uint64_t some = __ballot(has);
@@ -226,7 +265,7 @@ __device__ __forceinline__ void write_top(const LogprobArgs& p, int64_t row, con
       }
       if (rank < p.top) {
         p.top_tokens[row * p.top + rank] = (int32_t)~mine.y;
-        p.top_logprobs[row * p.top + rank] = all.z == 0.0f ? -__builtin_inff() : (value_of(mine.x) - all.m) - log_z;
+        p.top_logprobs[row * p.top + rank] = all.z == 0.0f ? -__builtin_inff() : all.below(value_of(mine.x)) * all.kUnit - log_z;
       }
     } else {  // fewer values than that
       p.top_tokens[row * p.top + i] = -1;
@@ -235,75 +274,72 @@ __device__ __forceinline__ void write_top(const LogprobArgs& p, int64_t row, con
   }
 }
 
+// The row's given token and its logit, requested long before they are used
+struct Given {
+  int token = -1;
+  float x = 0.0f;
+  template <bool F32>
+  __device__ __forceinline__ void request(const LogprobArgs& p, int64_t row, const Row<F32>& r) {
+    if (!p.tokens) return;
+    token = p.tokens[row];
+    if (token >= 0 && token < p.V) x = r.value(token);
+  }
+};
+
 template <bool F32>
-__device__ __forceinline__ void write_numbers(const LogprobArgs& p, int64_t row, const Row<F32>& r, const Sums& all, float log_z) {
+__device__ __forceinline__ void write_numbers(const LogprobArgs& p, int64_t row, const Given& given, const Sums<F32>& all, float log_z) {
   const bool none = all.z == 0.0f;  // everything masked
-  if (p.lse) p.lse[row] = none ? -__builtin_inff() : all.m + log_z;
-  if (p.entropy) p.entropy[row] = none ? 0.0f : log_z - all.t / all.z;
+  if (p.lse) p.lse[row] = none ? -__builtin_inff() : (float)((double)all.m * (F32 ? 1.0 : 0.69314718055994531) + (double)log_z);
+  if (p.entropy) p.entropy[row] = none ? 0.0f : log_z - all.t / all.z * all.kUnit;
   if (p.logprob) {
-    const int token = p.tokens[row];
-    float x = token < 0 ? 0.0f : __builtin_nanf("");
-    if (token >= 0 && token < p.V) x = none ? -__builtin_inff() : (r.value(token) - all.m) - log_z;
-    p.logprob[row] = x;
+    float y = given.token < 0 ? 0.0f : __builtin_nanf("");
+    if (given.token >= 0 && given.token < p.V) y = none ? -__builtin_inff() : all.below(given.x) * all.kUnit - log_z;
+    p.logprob[row] = y;
   }
 }
 
 // One thread's part of blocks [from, to): every T-th, and one of the lead's and tail's values where `odd` says so.
 template <bool F32, int T, bool PAST>
-__device__ __forceinline__ Sums stream(const Row<F32>& r, int from, int to, bool odd) {
-  Sums s;
+__device__ __forceinline__ Sums<F32> stream(const Row<F32>& r, int from, int to, bool odd) {
+  Sums<F32> s;
   const int tid = threadIdx.x;
-  auto request = [&](int b0, uint4* v) {
+  const bool has_odd = odd && tid < r.lead + r.tail;
+  const float x = has_odd ? r.value(r.place_of_odd(tid)) : 0.0f;
+  for (int b0 = from; b0 < to; b0 += T * kUnroll) {
+    uint4 v[kUnroll];
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
       const int b = b0 + tid + T * u;
       v[u] = Row<F32>::masked_block();
       if (b < to) v[u] = r.template block<PAST>(b);
     }
-  };
-  auto take = [&](const uint4* v) {
-    s.raise(Row<F32>::largest(v));
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      float x[Row<F32>::kVec];
-      Row<F32>::unpack(v[u], x);
-#pragma unroll
-      for (int i = 0; i < Row<F32>::kVec; ++i) s.add(x[i]);
-    }
-  };
-  uint4 a[kUnroll], b[kUnroll];
-  request(from, a);
-  if (odd && tid < r.lead + r.tail) {
-    const float x = r.value(r.place_of_odd(tid));
-    s.raise(x);
-    s.add(x);
+    s.add_blocks(v);
   }
-  for (int b0 = from; b0 < to; b0 += 2 * T * kUnroll) {
-    request(b0 + T * kUnroll, b);
-    take(a);
-    if (b0 + T * kUnroll >= to) break;
-    request(b0 + 2 * T * kUnroll, a);
-    take(b);
+  if (has_odd) {
+    s.meet(x);
+    s.add(x);
   }
   return s;
 }
 
 // ---- many rows: a workgroup a row
 template <bool F32, int T, bool PAST>
-__global__ __launch_bounds__(T) void logprobs_kernel(const LogprobArgs p) {
+__global__ __launch_bounds__(T, 8) void logprobs_kernel(const LogprobArgs p) {
   __shared__ float of_wave[T / 64][3], of_group[kGroups];
   __shared__ uint2 entries[T];
   __shared__ int count;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t row = blockIdx.x;
   const Row<F32> r(p, row);
-  const Sums mine = stream<F32, T, PAST>(r, 0, r.blocks, true);
+  Given given;
+  given.request(p, row, r);
+  const Sums<F32> mine = stream<F32, T, PAST>(r, 0, r.blocks, true);
   if (p.top) {
-    const float g = group_max<T / kGroups>(mine.m);
+    const float g = group_max<T / kGroups>(mine.largest);
     if (tid % (T / kGroups) == 0) of_group[tid / (T / kGroups)] = g;
     if (tid == 0) count = 0;
   }
-  const Sums w = wave_sums(mine);
+  const Sums<F32> w = wave_sums(mine);
   if (lane == 0) {
     of_wave[wave][0] = w.m;
     of_wave[wave][1] = w.z;
@@ -311,14 +347,14 @@ __global__ __launch_bounds__(T) void logprobs_kernel(const LogprobArgs p) {
   }
   __syncthreads();
   if (!p.top && wave > 0) return;
-  const Sums all = join_waves<T / 64>(of_wave);
+  const Sums<F32> all = join_waves<F32, T / 64>(of_wave);
   const float log_z = logf(all.z);
-  if (tid == 0) write_numbers<F32>(p, row, r, all, log_z);
+  if (tid == 0) write_numbers<F32>(p, row, given, all, log_z);
   if (!p.top) return;
 
   float bound = bound_of(of_group[lane], p.top);
   List list;
-  const bool again = mine.m >= bound || mine.z != mine.z;
+  const bool again = mine.largest >= bound || mine.z != mine.z;
   if (__ballot(again)) {
     for (int b0 = 0; b0 < r.blocks; b0 += T * kUnroll) {
       uint4 v[kUnroll];
@@ -341,7 +377,7 @@ __global__ __launch_bounds__(T) void logprobs_kernel(const LogprobArgs p) {
     const int place = odd ? r.place_of_odd(tid) : 0;
     list.offer(odd, odd ? r.value(place) : 0.0f, place, p.top, bound);
   }
-  write_top<T>(p, row, list, all, log_z, entries, &count);
+  write_top<F32, T>(p, row, list, all, log_z, entries, &count);
 }
 
 // ---- few rows: parts of them
@@ -352,21 +388,22 @@ __global__ __launch_bounds__(kSplitThreads) void logprobs_part_kernel(const Logp
   const int64_t row = blockIdx.y;
   const Row<F32> r(p, row);
   const int from = min((int64_t)part * p.blocks_per_part, (int64_t)r.blocks), to = min((int64_t)from + p.blocks_per_part, (int64_t)r.blocks);
-  const Sums mine = stream<F32, kSplitThreads, false>(r, from, to, part == 0);
+  const Sums<F32> mine = stream<F32, kSplitThreads, false>(r, from, to, part == 0);
   float* out = p.parts + (row * p.splits + part) * kPartValues;
   if (p.top) {
-    const float g = group_max<kSplitThreads / kGroups>(mine.z != mine.z ? __builtin_inff() : mine.m);
+    const float g = group_max<kSplitThreads / kGroups>(mine.z != mine.z ? __builtin_inff() : mine.largest);
     if (tid % (kSplitThreads / kGroups) == 0) out[3 + tid / (kSplitThreads / kGroups)] = g;
   }
-  const Sums w = wave_sums(mine);
+  const Sums<F32> w = wave_sums(mine);
   if (lane == 0) {
     of_wave[wave][0] = w.m;
     of_wave[wave][1] = w.z;
     of_wave[wave][2] = w.t;
   }
   __syncthreads();
-  if (tid == 0) {
-    const Sums all = join_waves<kSplitThreads / 64>(of_wave);
+  if (wave > 0) return;
+  const Sums<F32> all = join_waves<F32, kSplitThreads / 64>(of_wave);
+  if (lane == 0) {
     out[0] = all.m;
     out[1] = all.z;
     out[2] = all.t;
@@ -400,21 +437,23 @@ __global__ __launch_bounds__(TOP ? kJoinThreads : 64) void logprobs_join_kernel(
     if (tid % (T / kGroups) == 0) of_group[tid / (T / kGroups)] = most;
     if (tid == 0) count = passing = 0;
   }
-  Sums s;
+  Given given;
+  given.request(p, row, r);
+  Sums<F32> s;
   for (int part = tid; part < p.splits; part += T) {
-    Sums q;
+    Sums<F32> q;
     q.m = parts[part * kPartValues];
     q.z = parts[part * kPartValues + 1];
     q.t = parts[part * kPartValues + 2];
     const float m = fmaxf(s.m, q.m);
-    s.raise(m);
-    q.raise(m);
+    s.refer_to(m);
+    q.refer_to(m);
     s.z += q.z;
     s.t += q.t;
   }
   s = wave_sums(s);
   if constexpr (!TOP) {
-    if (tid == 0) write_numbers<F32>(p, row, r, s, logf(s.z));
+    if (tid == 0) write_numbers<F32>(p, row, given, s, logf(s.z));
   } else {
     if (lane == 0) {
       of_wave[wave][0] = s.m;
@@ -422,9 +461,6 @@ __global__ __launch_bounds__(TOP ? kJoinThreads : 64) void logprobs_join_kernel(
       of_wave[wave][2] = s.t;
     }
     __syncthreads();
-    const Sums all = join_waves<kWaves>(of_wave);
-    const float log_z = logf(all.z);
-    if (tid == 0) write_numbers<F32>(p, row, r, all, log_z);
     float bound = bound_of(of_group[lane], p.top);
 #pragma unroll
     for (int i = 0; i < kJoinGroups; ++i) {
@@ -432,27 +468,32 @@ __global__ __launch_bounds__(TOP ? kJoinThreads : 64) void logprobs_join_kernel(
       if (part < p.splits && g[i] >= bound) passed[atomicAdd(&passing, 1)] = (uint16_t)(part * kGroups + lane);
     }
     __syncthreads();
-    // a wave a group that passed: the values of kSplitThreads / kGroups threads of its part
+    // the values of each group that passed, kLanes threads of its part, by as many lanes: a wave takes 64 / kLanes groups at a time, neighbours of the list going to different waves
     constexpr int kLanes = kSplitThreads / kGroups;
     List list;
-    for (int i = wave; i < passing; i += kWaves) {
-      const int part = passed[i] / kGroups, thread0 = passed[i] % kGroups * kLanes;
-      const int from = min((int64_t)part * p.blocks_per_part, (int64_t)r.blocks), to = min((int64_t)from + p.blocks_per_part, (int64_t)r.blocks);
-      // lane: block lane / kLanes of thread thread0 + lane % kLanes
-      for (int b0 = from + thread0; b0 < to; b0 += kSplitThreads * (64 / kLanes)) {
-        const int b = b0 + lane % kLanes + lane / kLanes * kSplitThreads;
+    const int n = passing;
+    for (int e0 = wave; e0 < n; e0 += kWaves * (64 / kLanes)) {
+      const int e = e0 + lane / kLanes * kWaves;
+      const int id = e < n ? passed[e] : 0, part = id / kGroups, thread = id % kGroups * kLanes + lane % kLanes;
+      const int from = min((int64_t)part * p.blocks_per_part, (int64_t)r.blocks), to = e < n ? min((int64_t)from + p.blocks_per_part, (int64_t)r.blocks) : 0;
+      const bool odd = e < n && part == 0 && thread < r.lead + r.tail;
+      const int place = odd ? r.place_of_odd(thread) : 0;
+      const float x_odd = odd ? r.value(place) : 0.0f;
+      for (int j = thread; j < p.blocks_per_part; j += kSplitThreads) {  // (blocks_per_part is a multiple of kSplitThreads: every lane turns as often)
+        const int b = from + j;
         uint4 v = Row<F32>::masked_block();
         if (b < to) v = r.template block<false>(b);
         float x[Row<F32>::kVec];
         Row<F32>::unpack(v, x);
 #pragma unroll
-        for (int e = 0; e < Row<F32>::kVec; ++e) list.offer(b < to, x[e], r.place_of_block(b) + e, p.top, bound);
+        for (int i = 0; i < Row<F32>::kVec; ++i) list.offer(b < to, x[i], r.place_of_block(b) + i, p.top, bound);
       }
-      const bool odd = part == 0 && lane < kLanes && thread0 + lane < r.lead + r.tail;
-      const int place = odd ? r.place_of_odd(thread0 + lane) : 0;
-      list.offer(odd, odd ? r.value(place) : 0.0f, place, p.top, bound);
+      list.offer(odd, x_odd, place, p.top, bound);
     }
-    write_top<T>(p, row, list, all, log_z, entries, &count);
+    const Sums<F32> all = join_waves<F32, kWaves>(of_wave);
+    const float log_z = logf(all.z);
+    write_top<F32, T>(p, row, list, all, log_z, entries, &count);
+    if (tid == T - 1) write_numbers<F32>(p, row, given, all, log_z);
   }
 }
 
