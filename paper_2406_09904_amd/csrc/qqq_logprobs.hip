@@ -22,7 +22,7 @@ namespace qqq {
 
 namespace {
 
-constexpr int kSplitThreads = 256, kJoinThreads = 1024, kUnroll = 4;
+constexpr int kSplitThreads = 256, kJoinThreads = 512, kUnroll = 2;
 constexpr int kGroups = 64;              // of a workgroup's threads
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kFar = -1000.0f;         // e^kFar is 0: further than that is as far, and stays finite
@@ -241,6 +241,21 @@ struct List {
     const uint32_t last = (uint32_t)__builtin_amdgcn_readlane((int)order, top - 1);
     if (last != 0 && last != 0xFFFFFFFFu) bound = fmaxf(bound, value_of(last));
   }
+  // and a block of values each, where one of them has something
+  template <bool F32>
+  __device__ __forceinline__ void offer_block(const Row<F32>& r, int b, bool has, int top, float& bound) {
+    uint4 v = Row<F32>::masked_block();
+    if (has) v = r.template block<false>(b);
+    float x[Row<F32>::kVec];
+    Row<F32>::unpack(v, x);
+    bool some = false;
+#pragma unroll
+    for (int i = 0; i < Row<F32>::kVec; ++i) some |= !(x[i] < bound);
+    some &= has;
+    if (!__ballot(some)) return;
+#pragma unroll
+    for (int i = 0; i < Row<F32>::kVec; ++i) offer(some, x[i], r.place_of_block(b) + i, top, bound);
+  }
 };
 
 // The waves' lists as one: entries to LDS, each one's rank counted, the first `top` written.
@@ -282,7 +297,7 @@ struct Given {
   __device__ __forceinline__ void request(const LogprobArgs& p, int64_t row, const Row<F32>& r) {
     if (!p.tokens) return;
     token = p.tokens[row];
-    if (token >= 0 && token < p.V) x = r.value(token);
+    x = r.value(min(max(token, 0), p.V - 1));  // (no branch, which would wait for the token here)
   }
 };
 
@@ -305,15 +320,22 @@ __device__ __forceinline__ Sums<F32> stream(const Row<F32>& r, int from, int to,
   const int tid = threadIdx.x;
   const bool has_odd = odd && tid < r.lead + r.tail;
   const float x = has_odd ? r.value(r.place_of_odd(tid)) : 0.0f;
-  for (int b0 = from; b0 < to; b0 += T * kUnroll) {
-    uint4 v[kUnroll];
+  auto request = [&](int b0, uint4* v) {
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
       const int b = b0 + tid + T * u;
       v[u] = Row<F32>::masked_block();
       if (b < to) v[u] = r.template block<PAST>(b);
     }
+  };
+  uint4 v[kUnroll], w[kUnroll];
+  request(from, v);
+  for (int b0 = from; b0 < to; b0 += 2 * T * kUnroll) {
+    request(b0 + T * kUnroll, w);
     s.add_blocks(v);
+    if (b0 + T * kUnroll >= to) break;
+    request(b0 + 2 * T * kUnroll, v);
+    s.add_blocks(w);
   }
   if (has_odd) {
     s.meet(x);
@@ -327,7 +349,8 @@ template <bool F32, int T, bool PAST>
 __global__ __launch_bounds__(T, 8) void logprobs_kernel(const LogprobArgs p) {
   __shared__ float of_wave[T / 64][3], of_group[kGroups];
   __shared__ uint2 entries[T];
-  __shared__ int count;
+  __shared__ uint16_t passed[T];
+  __shared__ int count, passing;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t row = blockIdx.x;
   const Row<F32> r(p, row);
@@ -337,7 +360,7 @@ __global__ __launch_bounds__(T, 8) void logprobs_kernel(const LogprobArgs p) {
   if (p.top) {
     const float g = group_max<T / kGroups>(mine.largest);
     if (tid % (T / kGroups) == 0) of_group[tid / (T / kGroups)] = g;
-    if (tid == 0) count = 0;
+    if (tid == 0) count = passing = 0;
   }
   const Sums<F32> w = wave_sums(mine);
   if (lane == 0) {
@@ -347,37 +370,29 @@ __global__ __launch_bounds__(T, 8) void logprobs_kernel(const LogprobArgs p) {
   }
   __syncthreads();
   if (!p.top && wave > 0) return;
-  const Sums<F32> all = join_waves<F32, T / 64>(of_wave);
-  const float log_z = logf(all.z);
-  if (tid == 0) write_numbers<F32>(p, row, given, all, log_z);
-  if (!p.top) return;
+  if (!p.top) {
+    const Sums<F32> all = join_waves<F32, T / 64>(of_wave);
+    if (tid == 0) write_numbers<F32>(p, row, given, all, logf(all.z));
+    return;
+  }
 
   float bound = bound_of(of_group[lane], p.top);
+  // threads with such a value, and then their blocks spread over all threads: a thread's own, one after the other, would be as many memory latencies
+  if (mine.largest >= bound || mine.z != mine.z) passed[atomicAdd(&passing, 1)] = (uint16_t)tid;
+  __syncthreads();
   List list;
-  const bool again = mine.largest >= bound || mine.z != mine.z;
-  if (__ballot(again)) {
-    for (int b0 = 0; b0 < r.blocks; b0 += T * kUnroll) {
-      uint4 v[kUnroll];
-#pragma unroll
-      for (int u = 0; u < kUnroll; ++u) {
-        const int b = b0 + tid + T * u;
-        v[u] = Row<F32>::masked_block();
-        if (again && b < r.blocks) v[u] = r.template block<false>(b);
-      }
-#pragma unroll
-      for (int u = 0; u < kUnroll; ++u) {
-        const int b = b0 + tid + T * u;
-        float x[Row<F32>::kVec];
-        Row<F32>::unpack(v[u], x);
-#pragma unroll
-        for (int i = 0; i < Row<F32>::kVec; ++i) list.offer(again && b < r.blocks, x[i], r.place_of_block(b) + i, p.top, bound);
-      }
-    }
-    const bool odd = again && tid < r.lead + r.tail;
-    const int place = odd ? r.place_of_odd(tid) : 0;
-    list.offer(odd, odd ? r.value(place) : 0.0f, place, p.top, bound);
+  const int each = (r.blocks + T - 1) / T, items = passing * each;
+  for (int i0 = wave * 64; i0 < items; i0 += T) {
+    const int i = i0 + lane, b = i < items ? passed[i / each] + i % each * T : r.blocks;
+    list.offer_block<F32>(r, b, b < r.blocks, p.top, bound);
   }
+  const bool odd = tid < r.lead + r.tail;
+  const int place = odd ? r.place_of_odd(tid) : 0;
+  list.offer(odd, odd ? r.value(place) : 0.0f, place, p.top, bound);
+  const Sums<F32> all = join_waves<F32, T / 64>(of_wave);
+  const float log_z = logf(all.z);
   write_top<F32, T>(p, row, list, all, log_z, entries, &count);
+  if (tid == T - 1) write_numbers<F32>(p, row, given, all, log_z);
 }
 
 // ---- few rows: parts of them
@@ -411,7 +426,7 @@ __global__ __launch_bounds__(kSplitThreads) void logprobs_part_kernel(const Logp
 }
 
 // the most groups of all parts of a row
-constexpr int kMostParts = 256, kJoinGroups = kMostParts * kGroups / kJoinThreads;
+constexpr int kMostParts = 128, kJoinGroups = kMostParts * kGroups / kJoinThreads;
 
 template <bool F32, bool TOP>
 __global__ __launch_bounds__(TOP ? kJoinThreads : 64) void logprobs_join_kernel(const LogprobArgs p) {
@@ -480,13 +495,7 @@ __global__ __launch_bounds__(TOP ? kJoinThreads : 64) void logprobs_join_kernel(
       const int place = odd ? r.place_of_odd(thread) : 0;
       const float x_odd = odd ? r.value(place) : 0.0f;
       for (int j = thread; j < p.blocks_per_part; j += kSplitThreads) {  // (blocks_per_part is a multiple of kSplitThreads: every lane turns as often)
-        const int b = from + j;
-        uint4 v = Row<F32>::masked_block();
-        if (b < to) v = r.template block<false>(b);
-        float x[Row<F32>::kVec];
-        Row<F32>::unpack(v, x);
-#pragma unroll
-        for (int i = 0; i < Row<F32>::kVec; ++i) list.offer(b < to, x[i], r.place_of_block(b) + i, p.top, bound);
+        list.offer_block<F32>(r, from + j, from + j < to, p.top, bound);
       }
       list.offer(odd, x_odd, place, p.top, bound);
     }
@@ -503,7 +512,8 @@ struct Split {
 };
 Split split_of(int64_t M, int64_t V, int type) {
   const int64_t blocks = V / (type == QQQ_LOGITS_FP32 ? 4 : 8);
-  if (M >= 2 * num_cus() || blocks <= 4 * kSplitThreads) return {1, 0};
+  // us, split / whole: 2 rows of 64 KB 8.8 / 7.9, of 130 KB 8.6 / 9.6, of 256 KB 8.9 / 12.9; 48 rows of 130 KB 10.4 / 10.2, of 256 KB 12.8 / 14.4; 100 rows of 256 KB 17.4 / 14.7 (top 5)
+  if (M > 64 || blocks * 16 * 48 <= (128 << 10) * (48 + M)) return {1, 0};
   // a block a thread where that leaves no more than four workgroups a CU
   int64_t each = 1;
   while (each < 64 && M * ((blocks + each * kSplitThreads - 1) / (each * kSplitThreads)) > 4 * num_cus()) each *= 2;
@@ -518,9 +528,15 @@ int launch_typed(LogprobArgs& p, int64_t M, const Split& s, hipStream_t st) {
   if (s.parts == 1) {
     const bool past = M * p.V * (F32 ? 4 : 2) > kLastCacheBytes;
 #define QQQ_LP(T, PAST) hipLaunchKernelGGL((logprobs_kernel<F32, T, PAST>), dim3((unsigned)M), dim3(T), 0, st, p)
-    if (p.V <= 16384) QQQ_LP(256, false);
-    else if (past) QQQ_LP(1024, true);
-    else QQQ_LP(1024, false);
+    // Threads a row, us (256 / 512 / 1024): a row a CU or less 400 KB 35.9 / 20.9 / 17.5 (100 rows, top 20), 130 KB 12.7 / 10.8 / 11.5, 32 KB 7.8 / 7.5 / 8.1; many rows 40 KB 62 / 87 / 180
+    // (8000 rows, top 5), 256 KB 248 / 203 / 190 (4096 rows, top 20), 166 / 161 / 167 (top 1); 777 rows of 131 KB, sums only, 24.8 / 26.6 / 31.0
+    const int64_t bytes = (int64_t)p.V * (F32 ? 4 : 2);
+    if (M <= num_cus() && bytes >= 384 << 10) QQQ_LP(1024, false);
+    else if (M <= num_cus() || (bytes > 64 << 10 && (p.top > 0 || M >= 8 * num_cus())))
+      if (past) QQQ_LP(512, true);
+      else QQQ_LP(512, false);
+    else if (past) QQQ_LP(256, true);
+    else QQQ_LP(256, false);
 #undef QQQ_LP
   } else {
     p.splits = s.parts;
