@@ -6,14 +6,16 @@
 // a power of two, exactly.  fp32 logits reach where x log2 e overflows, so x - m comes first.
 //
 // The largest `top` logits need nothing in that pass but the threads' maxima.  64 groups of threads hold disjoint parts of the row, so the top-th largest of the groups' maxima is
-// a lower bound of the row's top-th largest value, and only threads with a maximum of at least that look at their values again: 24 of them are expected for the
-// largest 20 of 64 groups, whatever V is.  What passes the bound goes into a list of up to 64 entries held in a wave's lanes in falling order; the waves' lists are
-// joined by counting, for each entry, how many are larger.  Entries are ordered by (value, lower place first), so equal values have one order and no result depends on
-// which wave came first.
+// a lower bound of the row's top-th largest value, and only the blocks of threads with a maximum of at least that are looked at again: 24 threads are expected for the
+// largest 20 of 64 groups, whatever V is.  Values that reach the bound are gathered in LDS, and each one's rank is the number of larger ones.  Where they are too many (a row of equal
+// values, say) they go through lists instead, of up to 64 entries in a wave's lanes in falling order.  Entries are ordered by (value, lower place first), so equal values have
+// one order and no result depends on which wave came first.
 //
 // Many rows: a workgroup a row.  Few rows: a row is split, the parts leave their sums and their groups' maxima in the workspace, and a second kernel joins
 // them and looks again at the groups that pass.
 #include <float.h>
+
+#include <type_traits>
 
 #include "qqq_past.h"
 #include "qqq_serve.h"
@@ -22,7 +24,7 @@ namespace qqq {
 
 namespace {
 
-constexpr int kSplitThreads = 256, kJoinThreads = 512, kUnroll = 2;
+constexpr int kSplitThreads = 256, kJoinThreads = 512;
 constexpr int kGroups = 64;              // of a workgroup's threads
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kFar = -1000.0f;         // e^kFar is 0: further than that is as far, and stays finite
@@ -69,11 +71,12 @@ struct Row {
     for (int i = 0; i < kVec; ++i)
       x[i] = F32 ? __builtin_bit_cast(float, w[i]) : half_bits_to_float(i & 1 ? w[i >> 1] >> 16 : w[i >> 1] & 0xFFFFu);
   }
-  static __device__ __forceinline__ float largest(const uint4* v) {  // of kUnroll blocks; not a NaN unless all are
+  template <int U>
+  static __device__ __forceinline__ float largest(const uint4* v) {  // of U blocks; not a NaN unless all are
     if constexpr (F32) {
       float m = __builtin_bit_cast(float, v[0].x);
 #pragma unroll
-      for (int u = 0; u < kUnroll; ++u) {
+      for (int u = 0; u < U; ++u) {
         const uint32_t w[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
 #pragma unroll
         for (int i = 0; i < 4; ++i) m = fmaxf(m, __builtin_bit_cast(float, w[i]));
@@ -83,7 +86,7 @@ struct Row {
       // (the instruction itself, which takes three operands and gives a NaN where there is one: the compiler would quiet every operand first)
       uint32_t m = v[0].x;
 #pragma unroll
-      for (int u = 0; u < kUnroll; ++u)
+      for (int u = 0; u < U; ++u)
         asm("v_pk_maximum3_f16 %0, %0, %1, %2\n\tv_pk_maximum3_f16 %0, %0, %3, %4" : "+v"(m) : "v"(v[u].x), "v"(v[u].y), "v"(v[u].z), "v"(v[u].w));
       const h2 pair = as_h2(m);
       return fmaxf((float)pair[0], (float)pair[1]);
@@ -116,11 +119,12 @@ struct Sums {
     z += e;
     t = __builtin_fmaf(fmaxf(d, kFar), e, t);
   }
+  template <int U>
   __device__ __forceinline__ void add_blocks(const uint4* v) {
-    meet(Row<F32>::largest(v));
+    meet(Row<F32>::template largest<U>(v));
     const float t_before = t;
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
+    for (int u = 0; u < U; ++u) {
       float x[Row<F32>::kVec];
       Row<F32>::unpack(v[u], x);
 #pragma unroll
@@ -134,7 +138,7 @@ struct Sums {
     if (__builtin_expect(__ballot(t != t), 0)) {  // -infinity times 0: a masked value, whose part is 0 (or there is a NaN, which z has too)
       t = t_before;
 #pragma unroll
-      for (int u = 0; u < kUnroll; ++u) {
+      for (int u = 0; u < U; ++u) {
         uint4 again = v[u];
         asm("" : "+v"(again.x), "+v"(again.y), "+v"(again.z), "+v"(again.w));  // (else every difference and power is kept for this branch: 64 registers)
         float x[Row<F32>::kVec];
@@ -203,17 +207,23 @@ __device__ __forceinline__ float value_of(uint32_t order) {
   return __builtin_bit_cast(float, order & 0x80000000u ? order ^ 0x80000000u : ~order);
 }
 
-// A lower bound of the top-th largest of the lanes' values (none of them a NaN): the largest number of 20 leading bits that `top` lanes reach.
+// The top-th largest of the workgroup's kGroups values (none of them a NaN), in all its threads.  Each wave counts, for every value, the larger ones among its share of them.
 // Where it is no more than the value that threads start from, everything passes, -infinity too.
-__device__ __forceinline__ float bound_of(float v, int top) {
-  const uint32_t order = order_of(v);
-  uint32_t bound = 0;
+template <int T>
+__device__ __forceinline__ float bound_of(const float* of_group, int (*larger)[kGroups], int top) {
+  constexpr int W = T / 64, kShare = kGroups / W;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const float v = of_group[lane];
+  int n = 0;
 #pragma unroll
-  for (int bit = 31; bit >= 12; --bit) {
-    const uint32_t raised = bound | 1u << bit;
-    if (__popcll(__ballot(order >= raised)) >= top) bound = raised;
-  }
-  return bound <= 0x00800000u ? -__builtin_inff() : value_of(bound);
+  for (int i = 0; i < kShare; ++i) n += of_group[wave * kShare + i] > v;
+  larger[wave][lane] = n;
+  __syncthreads();
+  n = 0;
+#pragma unroll
+  for (int w = 0; w < W; ++w) n += larger[w][lane];
+  const float bound = -wave_max(n < top ? -v : -__builtin_inff());
+  return bound <= -FLT_MAX ? -__builtin_inff() : bound;
 }
 
 // The largest entries so far, in the wave's lanes in falling order: (order of the value, bits of the place inverted); 0, 0: none
@@ -241,51 +251,80 @@ struct List {
     const uint32_t last = (uint32_t)__builtin_amdgcn_readlane((int)order, top - 1);
     if (last != 0 && last != 0xFFFFFFFFu) bound = fmaxf(bound, value_of(last));
   }
-  // and a block of values each, where one of them has something
-  template <bool F32>
-  __device__ __forceinline__ void offer_block(const Row<F32>& r, int b, bool has, int top, float& bound) {
-    uint4 v = Row<F32>::masked_block();
-    if (has) v = r.template block<false>(b);
-    float x[Row<F32>::kVec];
-    Row<F32>::unpack(v, x);
-    bool some = false;
-#pragma unroll
-    for (int i = 0; i < Row<F32>::kVec; ++i) some |= !(x[i] < bound);
-    some &= has;
-    if (!__ballot(some)) return;
-#pragma unroll
-    for (int i = 0; i < Row<F32>::kVec; ++i) offer(some, x[i], r.place_of_block(b) + i, top, bound);
-  }
 };
 
-// The waves' lists as one: entries to LDS, each one's rank counted, the first `top` written.
+// What a workgroup has found of the largest values
+template <int T>
+struct Found {
+  uint2 entries[T];  // (order of the value, bits of the place inverted)
+  int ranks[64];
+  int count;         // (also of those that found no room)
+  __device__ __forceinline__ void add(uint32_t order, uint32_t place) {
+    const int at = atomicAdd(&count, 1);  // (which entry lies where decides nothing)
+    if (at < T) entries[at] = make_uint2(order, place);
+  }
+  __device__ __forceinline__ void add_list(const List& list, int top) {
+    if ((int)(threadIdx.x & 63) < top && (list.order | list.place) != 0) add(list.order, list.place);
+  }
+};
+// Lanes with a block of values (or one of the lead's and tail's) that reach the bound: straight to what is found, or through the wave's list
+template <bool F32, int T, bool LIST>
+__device__ __forceinline__ void look_at_block(const Row<F32>& r, int b, bool has, int top, float& bound, List& list, Found<T>& found) {
+  uint4 v = Row<F32>::masked_block();
+  if (has) v = r.template block<false>(b);
+  float x[Row<F32>::kVec];
+  Row<F32>::unpack(v, x);
+  bool some = false;
+#pragma unroll
+  for (int i = 0; i < Row<F32>::kVec; ++i) some |= !(x[i] < bound);
+  some &= has;
+  if (!__ballot(some)) return;
+#pragma unroll
+  for (int i = 0; i < Row<F32>::kVec; ++i) {
+    if constexpr (LIST) list.offer(some, x[i], r.place_of_block(b) + i, top, bound);
+    else if (some && !(x[i] < bound)) found.add(order_of(x[i]), ~(uint32_t)(r.place_of_block(b) + i));
+  }
+}
+template <bool F32, int T, bool LIST>
+__device__ __forceinline__ void look_at_value(const Row<F32>& r, int place, bool has, int top, float& bound, List& list, Found<T>& found) {
+  const float x = has ? r.value(place) : 0.0f;
+  if constexpr (LIST) list.offer(has, x, place, top, bound);
+  else if (has && !(x < bound)) found.add(order_of(x), ~(uint32_t)place);
+}
+
+// Each entry's rank counted, the first `top` written.
 template <bool F32, int T>
-__device__ __forceinline__ void write_top(const LogprobArgs& p, int64_t row, const List& list, const Sums<F32>& all, float log_z, uint2* entries, int* count) {
-  const int lane = threadIdx.x & 63;
-  const bool has = lane < p.top && (list.order | list.place) != 0;
-  const uint64_t some = __ballot(has);
-  int base = 0;
-  if (lane == 0 && some) base = atomicAdd(count, __popcll(some));  // (in LDS; the entries' order decides nothing)
-  base = __builtin_amdgcn_readfirstlane(base);
-  if (has) entries[base + lane] = make_uint2(list.order, list.place);
-  __syncthreads();
-  const int n = *count;
-  for (int i = threadIdx.x; i < max(n, p.top); i += T) {
-    if (i < n) {
-      const uint2 mine = entries[i];
+__device__ __forceinline__ void write_top(const LogprobArgs& p, int64_t row, const Sums<F32>& all, float log_z, Found<T>& found) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = found.count;
+  auto write = [&](const uint2& entry, int rank) {
+    if (rank >= p.top) return;
+    p.top_tokens[row * p.top + rank] = (int32_t)~entry.y;
+    p.top_logprobs[row * p.top + rank] = all.z == 0.0f ? -__builtin_inff() : all.below(value_of(entry.x)) * all.kUnit - log_z;
+  };
+  if (n <= 64) {  // a wave compares all of them with its share
+    const uint2 mine = lane < n ? found.entries[lane] : make_uint2(0, 0);
+    int rank = 0;
+    for (int j = wave; j < n; j += T / 64) {
+      const uint2 other = found.entries[j];
+      rank += List::above(other.x, other.y, mine.x, mine.y);
+    }
+    if (rank) atomicAdd(&found.ranks[lane], rank);
+    __syncthreads();
+    if (wave == 0 && lane < n) write(mine, found.ranks[lane]);
+  } else {
+    for (int i = threadIdx.x; i < n; i += T) {
+      const uint2 mine = found.entries[i];
       int rank = 0;
       for (int j = 0; j < n; ++j) {
-        const uint2 other = entries[j];
+        const uint2 other = found.entries[j];
         rank += List::above(other.x, other.y, mine.x, mine.y);
       }
-      if (rank < p.top) {
-        p.top_tokens[row * p.top + rank] = (int32_t)~mine.y;
-        p.top_logprobs[row * p.top + rank] = all.z == 0.0f ? -__builtin_inff() : all.below(value_of(mine.x)) * all.kUnit - log_z;
-      }
-    } else {  // fewer values than that
-      p.top_tokens[row * p.top + i] = -1;
-      p.top_logprobs[row * p.top + i] = -__builtin_inff();
+      write(mine, rank);
     }
+  }
+  for (int i = n + (int)threadIdx.x; i < p.top; i += T) {  // fewer values than that
+    p.top_tokens[row * p.top + i] = -1;
+    p.top_logprobs[row * p.top + i] = -__builtin_inff();
   }
 }
 
@@ -314,7 +353,7 @@ __device__ __forceinline__ void write_numbers(const LogprobArgs& p, int64_t row,
 }
 
 // One thread's part of blocks [from, to): every T-th, and one of the lead's and tail's values where `odd` says so.
-template <bool F32, int T, bool PAST>
+template <bool F32, int T, int U, bool PAST>
 __device__ __forceinline__ Sums<F32> stream(const Row<F32>& r, int from, int to, bool odd) {
   Sums<F32> s;
   const int tid = threadIdx.x;
@@ -322,20 +361,20 @@ __device__ __forceinline__ Sums<F32> stream(const Row<F32>& r, int from, int to,
   const float x = has_odd ? r.value(r.place_of_odd(tid)) : 0.0f;
   auto request = [&](int b0, uint4* v) {
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
+    for (int u = 0; u < U; ++u) {
       const int b = b0 + tid + T * u;
       v[u] = Row<F32>::masked_block();
       if (b < to) v[u] = r.template block<PAST>(b);
     }
   };
-  uint4 v[kUnroll], w[kUnroll];
+  uint4 v[U], w[U];
   request(from, v);
-  for (int b0 = from; b0 < to; b0 += 2 * T * kUnroll) {
-    request(b0 + T * kUnroll, w);
-    s.add_blocks(v);
-    if (b0 + T * kUnroll >= to) break;
-    request(b0 + 2 * T * kUnroll, v);
-    s.add_blocks(w);
+  for (int b0 = from; b0 < to; b0 += 2 * T * U) {
+    request(b0 + T * U, w);
+    s.template add_blocks<U>(v);
+    if (b0 + T * U >= to) break;
+    request(b0 + 2 * T * U, v);
+    s.template add_blocks<U>(w);
   }
   if (has_odd) {
     s.meet(x);
@@ -344,23 +383,25 @@ __device__ __forceinline__ Sums<F32> stream(const Row<F32>& r, int from, int to,
   return s;
 }
 
-// ---- many rows: a workgroup a row
-template <bool F32, int T, bool PAST>
+// ---- a workgroup a row
+template <bool F32, int T, int U, bool PAST>
 __global__ __launch_bounds__(T, 8) void logprobs_kernel(const LogprobArgs p) {
   __shared__ float of_wave[T / 64][3], of_group[kGroups];
-  __shared__ uint2 entries[T];
+  __shared__ int larger[T / 64][kGroups];
+  __shared__ Found<T> found;
   __shared__ uint16_t passed[T];
-  __shared__ int count, passing;
+  __shared__ int passing;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t row = blockIdx.x;
   const Row<F32> r(p, row);
   Given given;
   given.request(p, row, r);
-  const Sums<F32> mine = stream<F32, T, PAST>(r, 0, r.blocks, true);
+  const Sums<F32> mine = stream<F32, T, U, PAST>(r, 0, r.blocks, true);
   if (p.top) {
     const float g = group_max<T / kGroups>(mine.largest);
     if (tid % (T / kGroups) == 0) of_group[tid / (T / kGroups)] = g;
-    if (tid == 0) count = passing = 0;
+    if (tid < 64) found.ranks[tid] = 0;
+    if (tid == 0) found.count = passing = 0;
   }
   const Sums<F32> w = wave_sums(mine);
   if (lane == 0) {
@@ -369,29 +410,42 @@ __global__ __launch_bounds__(T, 8) void logprobs_kernel(const LogprobArgs p) {
     of_wave[wave][2] = w.t;
   }
   __syncthreads();
-  if (!p.top && wave > 0) return;
   if (!p.top) {
+    if (wave > 0) return;
     const Sums<F32> all = join_waves<F32, T / 64>(of_wave);
     if (tid == 0) write_numbers<F32>(p, row, given, all, logf(all.z));
     return;
   }
 
-  float bound = bound_of(of_group[lane], p.top);
-  // threads with such a value, and then their blocks spread over all threads: a thread's own, one after the other, would be as many memory latencies
+  float bound = bound_of<T>(of_group, larger, p.top);
+  // threads with such a value, and then their blocks spread over all waves: a thread's own, one after the other, would be as many memory latencies
   if (mine.largest >= bound || mine.z != mine.z) passed[atomicAdd(&passing, 1)] = (uint16_t)tid;
   __syncthreads();
-  List list;
   const int each = (r.blocks + T - 1) / T, items = passing * each;
-  for (int i0 = wave * 64; i0 < items; i0 += T) {
-    const int i = i0 + lane, b = i < items ? passed[i / each] + i % each * T : r.blocks;
-    list.offer_block<F32>(r, b, b < r.blocks, p.top, bound);
-  }
   const bool odd = tid < r.lead + r.tail;
   const int place = odd ? r.place_of_odd(tid) : 0;
-  list.offer(odd, odd ? r.value(place) : 0.0f, place, p.top, bound);
+  List list;
+  auto look = [&](auto through_list) {
+    constexpr bool LIST = decltype(through_list)::value;
+    for (int i0 = wave; i0 < items; i0 += T) {
+      const int i = i0 + lane * (T / 64), b = i < items ? passed[i / each] + i % each * T : r.blocks;
+      look_at_block<F32, T, LIST>(r, b, b < r.blocks, p.top, bound, list, found);
+    }
+    look_at_value<F32, T, LIST>(r, place, odd, p.top, bound, list, found);
+  };
+  look(std::false_type{});
+  __syncthreads();
+  if (found.count > T) {  // the same in every thread
+    look(std::true_type{});
+    __syncthreads();
+    if (tid == 0) found.count = 0;
+    __syncthreads();
+    found.add_list(list, p.top);
+    __syncthreads();
+  }
   const Sums<F32> all = join_waves<F32, T / 64>(of_wave);
   const float log_z = logf(all.z);
-  write_top<F32, T>(p, row, list, all, log_z, entries, &count);
+  write_top<F32, T>(p, row, all, log_z, found);
   if (tid == T - 1) write_numbers<F32>(p, row, given, all, log_z);
 }
 
@@ -403,7 +457,7 @@ __global__ __launch_bounds__(kSplitThreads) void logprobs_part_kernel(const Logp
   const int64_t row = blockIdx.y;
   const Row<F32> r(p, row);
   const int from = min((int64_t)part * p.blocks_per_part, (int64_t)r.blocks), to = min((int64_t)from + p.blocks_per_part, (int64_t)r.blocks);
-  const Sums<F32> mine = stream<F32, kSplitThreads, false>(r, from, to, part == 0);
+  const Sums<F32> mine = stream<F32, kSplitThreads, 2, false>(r, from, to, part == 0);
   float* out = p.parts + (row * p.splits + part) * kPartValues;
   if (p.top) {
     const float g = group_max<kSplitThreads / kGroups>(mine.z != mine.z ? __builtin_inff() : mine.largest);
@@ -432,8 +486,9 @@ template <bool F32, bool TOP>
 __global__ __launch_bounds__(TOP ? kJoinThreads : 64) void logprobs_join_kernel(const LogprobArgs p) {
   constexpr int T = TOP ? kJoinThreads : 64, kWaves = T / 64;
   __shared__ float of_wave[kWaves][3], of_group[kGroups];
-  __shared__ uint2 entries[TOP ? T : 1];
-  __shared__ int count, passing;
+  __shared__ int larger[TOP ? kWaves : 1][kGroups];
+  __shared__ Found<T> found;
+  __shared__ int passing;
   __shared__ uint16_t passed[TOP ? kMostParts * kGroups : 1];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t row = blockIdx.x;
@@ -450,7 +505,8 @@ __global__ __launch_bounds__(TOP ? kJoinThreads : 64) void logprobs_join_kernel(
     }
     most = group_max<T / kGroups>(most);
     if (tid % (T / kGroups) == 0) of_group[tid / (T / kGroups)] = most;
-    if (tid == 0) count = passing = 0;
+    if (tid < 64) found.ranks[tid] = 0;
+    if (tid == 0) found.count = passing = 0;
   }
   Given given;
   given.request(p, row, r);
@@ -476,7 +532,7 @@ __global__ __launch_bounds__(TOP ? kJoinThreads : 64) void logprobs_join_kernel(
       of_wave[wave][2] = s.t;
     }
     __syncthreads();
-    float bound = bound_of(of_group[lane], p.top);
+    float bound = bound_of<T>(of_group, larger, p.top);
 #pragma unroll
     for (int i = 0; i < kJoinGroups; ++i) {
       const int part = wave + kWaves * i;
@@ -485,23 +541,33 @@ __global__ __launch_bounds__(TOP ? kJoinThreads : 64) void logprobs_join_kernel(
     __syncthreads();
     // the values of each group that passed, kLanes threads of its part, by as many lanes: a wave takes 64 / kLanes groups at a time, neighbours of the list going to different waves
     constexpr int kLanes = kSplitThreads / kGroups;
-    List list;
     const int n = passing;
-    for (int e0 = wave; e0 < n; e0 += kWaves * (64 / kLanes)) {
-      const int e = e0 + lane / kLanes * kWaves;
-      const int id = e < n ? passed[e] : 0, part = id / kGroups, thread = id % kGroups * kLanes + lane % kLanes;
-      const int from = min((int64_t)part * p.blocks_per_part, (int64_t)r.blocks), to = e < n ? min((int64_t)from + p.blocks_per_part, (int64_t)r.blocks) : 0;
-      const bool odd = e < n && part == 0 && thread < r.lead + r.tail;
-      const int place = odd ? r.place_of_odd(thread) : 0;
-      const float x_odd = odd ? r.value(place) : 0.0f;
-      for (int j = thread; j < p.blocks_per_part; j += kSplitThreads) {  // (blocks_per_part is a multiple of kSplitThreads: every lane turns as often)
-        list.offer_block<F32>(r, from + j, from + j < to, p.top, bound);
+    List list;
+    auto look = [&](auto through_list) {
+      constexpr bool LIST = decltype(through_list)::value;
+      for (int e0 = wave; e0 < n; e0 += kWaves * (64 / kLanes)) {
+        const int e = e0 + lane / kLanes * kWaves;
+        const int id = e < n ? passed[e] : 0, part = id / kGroups, thread = id % kGroups * kLanes + lane % kLanes;
+        const int from = min((int64_t)part * p.blocks_per_part, (int64_t)r.blocks), to = e < n ? min((int64_t)from + p.blocks_per_part, (int64_t)r.blocks) : 0;
+        for (int j = thread; j < p.blocks_per_part; j += kSplitThreads)  // (blocks_per_part is a multiple of kSplitThreads: every lane turns as often)
+          look_at_block<F32, T, LIST>(r, from + j, from + j < to, p.top, bound, list, found);
+        const bool odd = e < n && part == 0 && thread < r.lead + r.tail;
+        look_at_value<F32, T, LIST>(r, odd ? r.place_of_odd(thread) : 0, odd, p.top, bound, list, found);
       }
-      list.offer(odd, x_odd, place, p.top, bound);
+    };
+    look(std::false_type{});
+    __syncthreads();
+    if (found.count > T) {
+      look(std::true_type{});
+      __syncthreads();
+      if (tid == 0) found.count = 0;
+      __syncthreads();
+      found.add_list(list, p.top);
+      __syncthreads();
     }
     const Sums<F32> all = join_waves<F32, kWaves>(of_wave);
     const float log_z = logf(all.z);
-    write_top<F32, T>(p, row, list, all, log_z, entries, &count);
+    write_top<F32, T>(p, row, all, log_z, found);
     if (tid == T - 1) write_numbers<F32>(p, row, given, all, log_z);
   }
 }
@@ -527,16 +593,17 @@ template <bool F32>
 int launch_typed(LogprobArgs& p, int64_t M, const Split& s, hipStream_t st) {
   if (s.parts == 1) {
     const bool past = M * p.V * (F32 ? 4 : 2) > kLastCacheBytes;
-#define QQQ_LP(T, PAST) hipLaunchKernelGGL((logprobs_kernel<F32, T, PAST>), dim3((unsigned)M), dim3(T), 0, st, p)
+#define QQQ_LP(T, U, PAST) hipLaunchKernelGGL((logprobs_kernel<F32, T, U, PAST>), dim3((unsigned)M), dim3(T), 0, st, p)
     // Threads a row, us (256 / 512 / 1024): a row a CU or less 400 KB 35.9 / 20.9 / 17.5 (100 rows, top 20), 130 KB 12.7 / 10.8 / 11.5, 32 KB 7.8 / 7.5 / 8.1; many rows 40 KB 62 / 87 / 180
     // (8000 rows, top 5), 256 KB 248 / 203 / 190 (4096 rows, top 20), 166 / 161 / 167 (top 1); 777 rows of 131 KB, sums only, 24.8 / 26.6 / 31.0
     const int64_t bytes = (int64_t)p.V * (F32 ? 4 : 2);
-    if (M <= num_cus() && bytes >= 384 << 10) QQQ_LP(1024, false);
-    else if (M <= num_cus() || (bytes > 64 << 10 && (p.top > 0 || M >= 8 * num_cus())))
-      if (past) QQQ_LP(512, true);
-      else QQQ_LP(512, false);
-    else if (past) QQQ_LP(256, true);
-    else QQQ_LP(256, false);
+    if (M <= num_cus() && bytes >= 384 << 10) QQQ_LP(1024, 4, false);
+    else if (M <= num_cus()) QQQ_LP(512, 4, false);
+    else if (bytes > 64 << 10 && (p.top > 0 || M >= 8 * num_cus()))
+      if (past) QQQ_LP(512, 2, true);
+      else QQQ_LP(512, 2, false);
+    else if (past) QQQ_LP(256, 2, true);
+    else QQQ_LP(256, 2, false);
 #undef QQQ_LP
   } else {
     p.splits = s.parts;
