@@ -5,9 +5,9 @@
 // For fp16 logits all of it is in powers of two and the reference is c, the integer above m log2 e: x log2 e - c is one mixed multiply-add, rounded once, and a change of c scales by
 // a power of two, exactly.  fp32 logits reach where x log2 e overflows, so x - m comes first.
 //
-// The largest `top` logits need nothing in that pass but the threads' maxima.  64 groups of threads hold disjoint parts of the row, so the top-th largest of the groups' maxima is
-// a lower bound of the row's top-th largest value, and only the blocks of threads with a maximum of at least that are looked at again: 24 threads are expected for the
-// largest 20 of 64 groups, whatever V is.  Values that reach the bound are gathered in LDS, and each one's rank is the number of larger ones.  Where they are too many (a row of equal
+// The largest `top` logits need nothing in that pass but the threads' maxima.  128 groups of threads hold disjoint parts of the row, so the top-th largest of the groups' maxima is
+// a lower bound of the row's top-th largest value, and only the blocks of threads with a maximum of at least that are looked at again: in a row without order the bound lets
+// 128 log(128 / (128 - top)) values pass, 22 for the largest 20, 89 for 64, whatever V is.  Values that reach the bound are gathered in LDS, and each one's rank is the number of larger ones.  Where they are too many (a row of equal
 // values, say) they go through lists instead, of up to 64 entries in a wave's lanes in falling order.  Entries are ordered by (value, lower place first), so equal values have
 // one order and no result depends on which wave came first.
 //
@@ -25,7 +25,9 @@ namespace qqq {
 namespace {
 
 constexpr int kSplitThreads = 256, kJoinThreads = 512;
-constexpr int kGroups = 64;              // of a workgroup's threads
+constexpr int kBound = 128;              // groups of a workgroup's threads, whose maxima give the bound
+constexpr int kGroups = 64;              // of the threads of a part of a row
+constexpr int kOddEach = 4;              // values a thread takes one by one, at most: a row of no more than that is spread over all threads, or its blocks would be in too few groups
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kFar = -1000.0f;         // e^kFar is 0: further than that is as far, and stays finite
 
@@ -46,9 +48,10 @@ struct Row {
   static constexpr int kVec = F32 ? 4 : 8, kSize = F32 ? 4 : 2;
   const char* at;
   int lead, blocks, tail;  // values before the first whole 16 aligned bytes, those 16 bytes, values behind the last
-  __device__ __forceinline__ Row(const LogprobArgs& p, int64_t row) {
+  // one_by_one: a short row, all of whose values are taken as the lead's
+  __device__ __forceinline__ Row(const LogprobArgs& p, int64_t row, bool one_by_one = false) {
     at = p.logits + row * p.row_bytes;
-    lead = min((int)((16 - (reinterpret_cast<uintptr_t>(at) & 15)) & 15) / kSize, p.V);
+    lead = one_by_one ? p.V : min((int)((16 - (reinterpret_cast<uintptr_t>(at) & 15)) & 15) / kSize, p.V);
     blocks = (p.V - lead) / kVec;
     tail = p.V - lead - blocks * kVec;
   }
@@ -207,22 +210,34 @@ __device__ __forceinline__ float value_of(uint32_t order) {
   return __builtin_bit_cast(float, order & 0x80000000u ? order ^ 0x80000000u : ~order);
 }
 
-// The top-th largest of the workgroup's kGroups values (none of them a NaN), in all its threads.  Each wave counts, for every value, the larger ones among its share of them.
+// The top-th largest of the workgroup's kBound values (none of them a NaN), in all its threads.  Each wave counts, for every value, the larger ones among its share of them.
 // Where it is no more than the value that threads start from, everything passes, -infinity too.
 template <int T>
-__device__ __forceinline__ float bound_of(const float* of_group, int (*larger)[kGroups], int top) {
-  constexpr int W = T / 64, kShare = kGroups / W;
+__device__ __forceinline__ float bound_of(const float* of_group, int (*larger)[kBound], int top) {
+  constexpr int W = T / 64, kShare = kBound / W;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const float v = of_group[lane];
-  int n = 0;
+  const float v[2] = {of_group[lane], of_group[64 + lane]};
+  if (top == 1) {  // the largest of all
+    const float largest = wave_max(fmaxf(v[0], v[1]));
+    return largest <= -FLT_MAX ? -__builtin_inff() : largest;
+  }
+  int n[2] = {0, 0};
 #pragma unroll
-  for (int i = 0; i < kShare; ++i) n += of_group[wave * kShare + i] > v;
-  larger[wave][lane] = n;
+  for (int i = 0; i < kShare; ++i)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) n[h] += of_group[wave * kShare + i] > v[h];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) larger[wave][64 * h + lane] = n[h];
   __syncthreads();
-  n = 0;
+  float least = __builtin_inff();
 #pragma unroll
-  for (int w = 0; w < W; ++w) n += larger[w][lane];
-  const float bound = -wave_max(n < top ? -v : -__builtin_inff());
+  for (int h = 0; h < 2; ++h) {
+    n[h] = 0;
+#pragma unroll
+    for (int w = 0; w < W; ++w) n[h] += larger[w][64 * h + lane];
+    if (n[h] < top) least = fminf(least, v[h]);
+  }
+  const float bound = -wave_max(-least);
   return bound <= -FLT_MAX ? -__builtin_inff() : bound;
 }
 
@@ -256,12 +271,12 @@ struct List {
 // What a workgroup has found of the largest values
 template <int T>
 struct Found {
-  uint2 entries[T];  // (order of the value, bits of the place inverted)
+  uint64_t entries[T];  // order of the value, then bits of the place inverted
   int ranks[64];
   int count;         // (also of those that found no room)
   __device__ __forceinline__ void add(uint32_t order, uint32_t place) {
     const int at = atomicAdd(&count, 1);  // (which entry lies where decides nothing)
-    if (at < T) entries[at] = make_uint2(order, place);
+    if (at < T) entries[at] = (uint64_t)order << 32 | place;
   }
   __device__ __forceinline__ void add_list(const List& list, int top) {
     if ((int)(threadIdx.x & 63) < top && (list.order | list.place) != 0) add(list.order, list.place);
@@ -296,29 +311,24 @@ __device__ __forceinline__ void look_at_value(const Row<F32>& r, int place, bool
 template <bool F32, int T>
 __device__ __forceinline__ void write_top(const LogprobArgs& p, int64_t row, const Sums<F32>& all, float log_z, Found<T>& found) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = found.count;
-  auto write = [&](const uint2& entry, int rank) {
+  auto write = [&](uint64_t entry, int rank) {
     if (rank >= p.top) return;
-    p.top_tokens[row * p.top + rank] = (int32_t)~entry.y;
-    p.top_logprobs[row * p.top + rank] = all.z == 0.0f ? -__builtin_inff() : all.below(value_of(entry.x)) * all.kUnit - log_z;
+    p.top_tokens[row * p.top + rank] = (int32_t)~(uint32_t)entry;
+    p.top_logprobs[row * p.top + rank] = all.z == 0.0f ? -__builtin_inff() : all.below(value_of((uint32_t)(entry >> 32))) * all.kUnit - log_z;
   };
   if (n <= 64) {  // a wave compares all of them with its share
-    const uint2 mine = lane < n ? found.entries[lane] : make_uint2(0, 0);
+    const uint64_t mine = lane < n ? found.entries[lane] : 0;
     int rank = 0;
-    for (int j = wave; j < n; j += T / 64) {
-      const uint2 other = found.entries[j];
-      rank += List::above(other.x, other.y, mine.x, mine.y);
-    }
+    for (int j = wave; j < n; j += T / 64) rank += found.entries[j] > mine;
     if (rank) atomicAdd(&found.ranks[lane], rank);
     __syncthreads();
     if (wave == 0 && lane < n) write(mine, found.ranks[lane]);
   } else {
     for (int i = threadIdx.x; i < n; i += T) {
-      const uint2 mine = found.entries[i];
+      const uint64_t mine = found.entries[i];
       int rank = 0;
-      for (int j = 0; j < n; ++j) {
-        const uint2 other = found.entries[j];
-        rank += List::above(other.x, other.y, mine.x, mine.y);
-      }
+#pragma unroll 8
+      for (int j = 0; j < n; ++j) rank += found.entries[j] > mine;
       write(mine, rank);
     }
   }
@@ -357,8 +367,12 @@ template <bool F32, int T, int U, bool PAST>
 __device__ __forceinline__ Sums<F32> stream(const Row<F32>& r, int from, int to, bool odd) {
   Sums<F32> s;
   const int tid = threadIdx.x;
-  const bool has_odd = odd && tid < r.lead + r.tail;
-  const float x = has_odd ? r.value(r.place_of_odd(tid)) : 0.0f;
+  float x[kOddEach];
+#pragma unroll
+  for (int i = 0; i < kOddEach; ++i) {
+    const int at = tid + T * i;
+    x[i] = odd && at < r.lead + r.tail ? r.value(r.place_of_odd(at)) : -__builtin_inff();
+  }
   auto request = [&](int b0, uint4* v) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -376,30 +390,32 @@ __device__ __forceinline__ Sums<F32> stream(const Row<F32>& r, int from, int to,
     request(b0 + 2 * T * U, v);
     s.template add_blocks<U>(w);
   }
-  if (has_odd) {
-    s.meet(x);
-    s.add(x);
-  }
+#pragma unroll
+  for (int i = 0; i < kOddEach; ++i)
+    if (odd && tid + T * i < r.lead + r.tail) {
+      s.meet(x[i]);
+      s.add(x[i]);
+    }
   return s;
 }
 
 // ---- a workgroup a row
 template <bool F32, int T, int U, bool PAST>
 __global__ __launch_bounds__(T, 8) void logprobs_kernel(const LogprobArgs p) {
-  __shared__ float of_wave[T / 64][3], of_group[kGroups];
-  __shared__ int larger[T / 64][kGroups];
+  __shared__ float of_wave[T / 64][3], of_group[kBound];
+  __shared__ int larger[T / 64][kBound];
   __shared__ Found<T> found;
   __shared__ uint16_t passed[T];
   __shared__ int passing;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t row = blockIdx.x;
-  const Row<F32> r(p, row);
+  const Row<F32> r(p, row, p.V <= kOddEach * T);
   Given given;
   given.request(p, row, r);
   const Sums<F32> mine = stream<F32, T, U, PAST>(r, 0, r.blocks, true);
   if (p.top) {
-    const float g = group_max<T / kGroups>(mine.largest);
-    if (tid % (T / kGroups) == 0) of_group[tid / (T / kGroups)] = g;
+    const float g = group_max<T / kBound>(mine.largest);
+    if (tid % (T / kBound) == 0) of_group[tid / (T / kBound)] = g;
     if (tid < 64) found.ranks[tid] = 0;
     if (tid == 0) found.count = passing = 0;
   }
@@ -422,8 +438,6 @@ __global__ __launch_bounds__(T, 8) void logprobs_kernel(const LogprobArgs p) {
   if (mine.largest >= bound || mine.z != mine.z) passed[atomicAdd(&passing, 1)] = (uint16_t)tid;
   __syncthreads();
   const int each = (r.blocks + T - 1) / T, items = passing * each;
-  const bool odd = tid < r.lead + r.tail;
-  const int place = odd ? r.place_of_odd(tid) : 0;
   List list;
   auto look = [&](auto through_list) {
     constexpr bool LIST = decltype(through_list)::value;
@@ -431,7 +445,11 @@ __global__ __launch_bounds__(T, 8) void logprobs_kernel(const LogprobArgs p) {
       const int i = i0 + lane * (T / 64), b = i < items ? passed[i / each] + i % each * T : r.blocks;
       look_at_block<F32, T, LIST>(r, b, b < r.blocks, p.top, bound, list, found);
     }
-    look_at_value<F32, T, LIST>(r, place, odd, p.top, bound, list, found);
+    for (int i0 = wave * 64; i0 < r.lead + r.tail; i0 += T) {
+      const int i = i0 + lane;
+      const bool odd = i < r.lead + r.tail;
+      look_at_value<F32, T, LIST>(r, odd ? r.place_of_odd(i) : 0, odd, p.top, bound, list, found);
+    }
   };
   look(std::false_type{});
   __syncthreads();
@@ -485,8 +503,8 @@ constexpr int kMostParts = 128, kJoinGroups = kMostParts * kGroups / kJoinThread
 template <bool F32, bool TOP>
 __global__ __launch_bounds__(TOP ? kJoinThreads : 64) void logprobs_join_kernel(const LogprobArgs p) {
   constexpr int T = TOP ? kJoinThreads : 64, kWaves = T / 64;
-  __shared__ float of_wave[kWaves][3], of_group[kGroups];
-  __shared__ int larger[TOP ? kWaves : 1][kGroups];
+  __shared__ float of_wave[kWaves][3], of_group[kBound];
+  __shared__ int larger[TOP ? kWaves : 1][kBound];
   __shared__ Found<T> found;
   __shared__ int passing;
   __shared__ uint16_t passed[TOP ? kMostParts * kGroups : 1];
@@ -503,8 +521,8 @@ __global__ __launch_bounds__(TOP ? kJoinThreads : 64) void logprobs_join_kernel(
       g[i] = part < p.splits ? parts[part * kPartValues + 3 + lane] : -FLT_MAX;
       most = fmaxf(most, g[i]);
     }
-    most = group_max<T / kGroups>(most);
-    if (tid % (T / kGroups) == 0) of_group[tid / (T / kGroups)] = most;
+    most = group_max<T / kBound>(most);
+    if (tid % (T / kBound) == 0) of_group[tid / (T / kBound)] = most;
     if (tid < 64) found.ranks[tid] = 0;
     if (tid == 0) found.count = passing = 0;
   }
