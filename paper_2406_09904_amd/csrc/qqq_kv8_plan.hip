@@ -2,7 +2,9 @@
 //
 // Sequence b brings n_b tokens: cu is the sequences' prefix sum of n_b, and the places of its fresh pages in the stack are a prefix sum of
 // fresh_b = len_b / P - held_b / P.  Both sums saturate at 2^30 (no count that is used passes it), so they stay in 32 bits whatever the tensors hold.
-// One workgroup makes the sums, a sequence a thread; the tables' entries and the rows' places are then copies, 8 bytes moved for each.
+// One workgroup makes the sums, in registers by lane moves; the tables' entries and the rows' places are then copies, 8 bytes moved for each.  What
+// bounds it: for few sequences the time that a launch and three dependent reads take (ids, held, entries: 2.4 us for one sequence, 4.2 for 64 of 125
+// entries); for many the sums' one workgroup (2048 sequences: 5.7 us) and the copies (2048 tables of about 1000 entries, 17 MB: 6.1 us).
 #include <algorithm>
 
 #include "qqq_plan.h"
@@ -16,52 +18,65 @@ constexpr int kMost = 1 << 30;
 
 __device__ __forceinline__ int add_saturating(int a, int b) { return (int)min((uint32_t)a + (uint32_t)b, (uint32_t)kMost); }
 
-// Sum of the values of the threads before this one, and of all (0 <= v <= kMost), saturating.  smem: one value a wave.
+// Sum of the lanes up to this one, saturating (0 <= v <= kMost)
+__device__ __forceinline__ int wave_inclusive_sum(int v) {
+  auto add = [&](int moved) { v = add_saturating(v, moved); };
+  add(__builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false));  // row_shr:1, 2, 4, 8 in rows of 16 lanes (none: 0)
+  add(__builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false));
+  add(__builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false));
+  add(__builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false));
+  add(__builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false));  // row_bcast:15: a row's last to the next, rows 1 and 3
+  add(__builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false));  // row_bcast:31: the second row's last to rows 2 and 3
+  return v;
+}
+
+// Sum of the values of the threads before this one, and of all, saturating.  ONE_WAVE: only the first wave has any, and only it has the results.
+template <bool ONE_WAVE>
 __device__ __forceinline__ int block_exclusive_sum(int v, int* smem, int& total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int sum = v;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int below = __shfl_up(sum, d);
-    if (lane >= d) sum = add_saturating(sum, below);
+  const int sum = wave_inclusive_sum(v);
+  int before = __builtin_amdgcn_update_dpp(0, sum, 0x138, 0xF, 0xF, false);  // wave_shr:1
+  if constexpr (ONE_WAVE) {
+    total = __builtin_amdgcn_readlane(sum, 63);
+    return before;
   }
   if (lane == 63) smem[wave] = sum;
-  int before = __shfl_up(sum, 1);
-  if (lane == 0) before = 0;
   __syncthreads();
-  int waves = 0, all = 0;
-#pragma unroll
-  for (int w = 0; w < kScanThreads / 64; ++w) {
-    const int x = smem[w];
-    if (w < wave) waves = add_saturating(waves, x);
-    all = add_saturating(all, x);
-  }
+  // the waves' sums the same way, in each of them
+  const int waves = wave_inclusive_sum(lane < kScanThreads / 64 ? smem[lane] : 0);
+  total = __builtin_amdgcn_readlane(waves, 63);
+  if (wave > 0) before = add_saturating(before, __builtin_amdgcn_readlane(waves, wave - 1));
   __syncthreads();
-  total = all;
-  return add_saturating(waves, before);
+  return before;
 }
 
 struct Sequence {
   int session, held, len, row, top;  // top: entries of the stack that are left when its turn comes (below 0: lacking)
 };
 
-// One sequence's entries and rows, every `step`-th from `from` on.
-__device__ __forceinline__ void fill(const PlanArgs& p, int b, const Sequence& s, int64_t from, int64_t step) {
+// One sequence's entries and rows, every `step`-th from `from` on.  early: what the session's entries from, from + step, .. hold, as far as it was read before.
+template <int EARLY = 0>
+__device__ __forceinline__ void fill(const PlanArgs& p, int b, const Sequence& s, int64_t from, int64_t step, const int* early = nullptr) {
   const int closed = s.len >> p.shift, had = s.held >> p.shift, n = s.len - s.held;
   if (closed > 0) {
     int32_t* own = p.pages + (int64_t)s.session * p.pages_stride;
     int32_t* table = p.table + (int64_t)b * p.table_stride;
-    for (int64_t j = (p.same_table ? had : 0) + from; j < closed; j += step) {
-      int page;
-      if (j < had) {
-        page = own[j];
-      } else {
+    auto entry = [&](int64_t j, int held_page) {
+      int page = held_page;
+      if (j >= had) {
         const int64_t place = s.top - 1 - (j - had);
         page = place >= 0 ? p.free_pages[place] : -1;
         own[j] = page;
       }
       table[j] = page;
+    };
+    int64_t j = (p.same_table ? had : 0) + from;
+    if (!p.same_table) {
+#pragma unroll
+      for (int e = 0; e < EARLY; ++e, j += step)
+        if (j < closed) entry(j, early[e]);
     }
+    for (; j < closed; j += step) entry(j, j < had ? own[j] : 0);
   }
   if (p.sequence)
     for (int64_t i = from; i < n; i += step) p.sequence[s.row + i] = b;
@@ -69,51 +84,94 @@ __device__ __forceinline__ void fill(const PlanArgs& p, int b, const Sequence& s
     for (int64_t i = from; i < n; i += step) p.positions[s.row + i] = s.held + (int)i;
 }
 
-// The sums; FILL (up to kScanThreads sequences, a thread each): the tables and rows too.
-template <bool FILL>
+// The sums, kEach consecutive sequences a thread.  ONE_WAVE: up to 64 sequences, one a lane of the first wave, so without a barrier.  FILL (with
+// ONE_WAVE): the tables and rows too, by all waves.
+template <bool FILL, bool ONE_WAVE>
 __global__ __launch_bounds__(kScanThreads) void kv8_plan_kernel(const PlanArgs p) {
+  constexpr int kEach = ONE_WAVE ? 1 : 4;
   __shared__ int smem[kScanThreads / 64];
-  __shared__ Sequence seqs[FILL ? kScanThreads : 1];
+  __shared__ Sequence seqs[FILL ? 64 : 1];
   const int tid = threadIdx.x;
+  // as many threads for a sequence's tables as there are, a wave at least
+  const int lanes = !FILL ? 0 : p.sequences <= 1 ? kScanThreads : max(64, kScanThreads >> (32 - __clz(p.sequences - 1)));
+  // One wave's sequences: a group of threads has up to four of them, and their first entries are on their way before the sums are known
+  constexpr int kMine = FILL ? 4 : 1, kEarly = 2;
+  int early[kMine][kEarly];
+  if constexpr (FILL) {
+    int session[kMine];
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) {
+      const int b = tid / lanes + kScanThreads / lanes * i;
+      session[i] = b >= p.sequences ? -1 : p.ids ? p.ids[b] : b;
+    }
+#pragma unroll
+    for (int i = 0; i < kMine; ++i)
+#pragma unroll
+      for (int e = 0; e < kEarly; ++e) {
+        const int j = tid % lanes + lanes * e;
+        early[i][e] = 0;
+        if ((uint32_t)session[i] < (uint32_t)p.sessions && j < p.columns && !p.same_table) early[i][e] = p.pages[(int64_t)session[i] * p.pages_stride + j];
+      }
+  }
   const int count = min(max(*p.free_count, 0), p.pool);
   int rows = 0, taken = 0;  // of the sequences before this turn's
-  for (int first = 0; first < p.sequences; first += kScanThreads) {
-    const int b = first + tid;
-    int session = -1, held = 0, n = 0;
-    if (b < p.sequences) {
-      session = p.ids ? p.ids[b] : b;
-      if ((uint32_t)session < (uint32_t)p.sessions) {
-        held = min(max(p.held[session], 0), p.max_len);
-        n = min(min(max(p.new_tokens[b], 0), p.max_new), p.max_len - held);
-      } else {
-        session = -1;
+  if (!ONE_WAVE || tid < 64) {
+    for (int64_t first = 0; first < p.sequences; first += kScanThreads * kEach) {
+      int session[kEach], held[kEach], n[kEach], all_n = 0;
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) {
+        const int64_t b = first + (int64_t)tid * kEach + e;
+        session[e] = b >= p.sequences ? -1 : p.ids ? p.ids[b] : (int)b;
+        n[e] = b >= p.sequences ? 0 : p.new_tokens[b];
+        if ((uint32_t)session[e] >= (uint32_t)p.sessions) session[e] = -1;
+      }
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) {
+        held[e] = session[e] >= 0 ? min(max(p.held[session[e]], 0), p.max_len) : 0;
+        n[e] = session[e] >= 0 ? min(min(max(n[e], 0), p.max_new), p.max_len - held[e]) : 0;
+        all_n = add_saturating(all_n, n[e]);
+      }
+      int all;
+      int row = add_saturating(rows, block_exclusive_sum<ONE_WAVE>(all_n, smem, all));
+      rows = add_saturating(rows, all);
+      int row_of[kEach], fresh[kEach], all_fresh = 0;
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) {
+        row_of[e] = min(row, p.tokens);
+        row = add_saturating(row, n[e]);
+        n[e] = min(n[e], p.tokens - row_of[e]);  // rows that the step's tensors do not have are not taken
+        fresh[e] = (held[e] + n[e] >> p.shift) - (held[e] >> p.shift);
+        all_fresh = add_saturating(all_fresh, fresh[e]);
+      }
+      int before = add_saturating(taken, block_exclusive_sum<ONE_WAVE>(all_fresh, smem, all));
+      taken = add_saturating(taken, all);
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) {
+        const int64_t b = first + (int64_t)tid * kEach + e;
+        if (b < p.sequences) {
+          const int len = held[e] + n[e];
+          p.kv_len[b] = len;
+          p.cu[b] = row_of[e];
+          if (session[e] >= 0) p.held_after[session[e]] = len;
+          if constexpr (FILL) seqs[tid] = Sequence{session[e], held[e], len, row_of[e], count - before};
+          else p.top[b] = count - before;
+        }
+        before = add_saturating(before, fresh[e]);
       }
     }
-    int all;
-    const int row = min(add_saturating(rows, block_exclusive_sum(n, smem, all)), p.tokens);
-    n = min(n, p.tokens - row);  // rows that the step's tensors do not have are not taken
-    rows = add_saturating(rows, all);
-    const int len = held + n, fresh = (len >> p.shift) - (held >> p.shift);
-    const int before = add_saturating(taken, block_exclusive_sum(fresh, smem, all));
-    taken = add_saturating(taken, all);
-    if (b < p.sequences) {
-      p.kv_len[b] = len;
-      p.cu[b] = row;
-      if (session >= 0) p.held_after[session] = len;
-      if constexpr (FILL) seqs[tid] = Sequence{session, held, len, row, count - before};
-      else p.top[b] = count - before;
+    if (tid == 0) {
+      p.cu[p.sequences] = min(rows, p.tokens);
+      *p.free_count_after = max(count - taken, 0);
+      if (p.lacking) *p.lacking = max(taken - count, 0);
     }
-  }
-  if (tid == 0) {
-    p.cu[p.sequences] = min(rows, p.tokens);
-    *p.free_count_after = max(count - taken, 0);
-    if (p.lacking) *p.lacking = max(taken - count, 0);
   }
   if constexpr (FILL) {
     __syncthreads();
-    // as many threads for a sequence as there are, a wave at least
-    const int lanes = p.sequences <= 1 ? kScanThreads : max(64, kScanThreads >> (32 - __clz(p.sequences - 1)));
-    for (int b = tid / lanes; b < p.sequences; b += kScanThreads / lanes) fill(p, b, seqs[b], tid % lanes, lanes);
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) {
+      const int b = tid / lanes + kScanThreads / lanes * i;
+      if (b < p.sequences) fill<kEarly>(p, b, seqs[b], tid % lanes, lanes, early[i]);
+    }
   }
 }
 
@@ -161,7 +219,7 @@ __global__ __launch_bounds__(kScanThreads) void kv8_release_kernel(const PlanArg
     }
     __syncthreads();
     int all;
-    const int before = block_exclusive_sum(tid < here ? pages_of[tid] : 0, smem, all);
+    const int before = block_exclusive_sum<false>(tid < here ? pages_of[tid] : 0, smem, all);
     if (tid < here) pages_of[tid] = add_saturating(count, before);
     __syncthreads();
     for (int i = wave; i < here; i += kWaves) {
@@ -181,9 +239,12 @@ __global__ __launch_bounds__(kScanThreads) void kv8_release_kernel(const PlanArg
   if (tid == 0) *p.free_count_after = count;
 }
 
-// One launch while a single workgroup moves the entries and rows sooner than a second launch starts
+// One launch while a single workgroup moves the entries and rows about as soon as a second launch would.  Measured in a graph, us with one launch and
+// with two: one sequence of 1 entry 2.4 and 3.4, of 4096 3.1 and 4.2, of 16384 5.8 and 4.3; 37 of 256 4.9 and 4.2; 64 of 16 4.2 and 4.2, of 1024 16.7
+// and 4.5.  Outside a graph a second launch also costs the host 2 us.  More than 64 sequences, whose sums take barriers, are behind in one launch at
+// every length (200 of one entry 6.0 and 5.4, 1024 of one 21 and 6.2).
 bool in_one_launch(const PlanArgs& p) {
-  return p.sequences <= kScanThreads && (int64_t)p.sequences * ((p.max_len >> p.shift) + (int64_t)p.max_new) <= kPlanOneLaunch;
+  return p.sequences <= 64 && (int64_t)p.sequences * ((p.max_len >> p.shift) + (int64_t)p.max_new) <= kPlanOneLaunch;
 }
 
 int launched(const char* what, const char* name) {
@@ -199,10 +260,11 @@ size_t kv8_plan_bytes(const PlanArgs& p) { return in_one_launch(p) ? 0 : (size_t
 
 int launch_kv8_plan(const PlanArgs& p, hipStream_t st) {
   if (in_one_launch(p)) {
-    hipLaunchKernelGGL((kv8_plan_kernel<true>), dim3(1), dim3(kScanThreads), 0, st, p);
+    hipLaunchKernelGGL((kv8_plan_kernel<true, true>), dim3(1), dim3(kScanThreads), 0, st, p);
     return launched("plan", "plan one launch");
   }
-  hipLaunchKernelGGL((kv8_plan_kernel<false>), dim3(1), dim3(kScanThreads), 0, st, p);
+  if (p.sequences <= 64) hipLaunchKernelGGL((kv8_plan_kernel<false, true>), dim3(1), dim3(64), 0, st, p);
+  else hipLaunchKernelGGL((kv8_plan_kernel<false, false>), dim3(1), dim3(kScanThreads), 0, st, p);
   if (int rc = launched("plan", "plan sums")) return rc;
   const int64_t most = std::max(p.max_len >> p.shift, std::min(p.max_new, p.tokens));  // entries or rows of a sequence
   const int64_t parts = std::min<int64_t>(std::max<int64_t>((most + 4 * kFillThreads - 1) / (4 * kFillThreads), 1), std::max(8 * num_cus() / p.sequences, 1));
