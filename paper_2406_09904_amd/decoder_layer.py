@@ -113,28 +113,34 @@ def pages_in_order(sequences, max_len, page_tokens, device="cuda"):
 
 def main():
     sessions, prompt, steps, page = 8, 500, 20, 64
+    max_len = prompt + steps
     layer = random_layer()
-    table, pages = pages_in_order(sessions, prompt + steps, page)
-    cache = qqq.new_kv8_cache(pages, layer.kv_heads, layer.head_dim, page, sessions)
+    columns = max_len // page
+    held = qqq.new_kv8_sessions(sessions, columns, sessions * columns)
+    cache = qqq.new_kv8_cache(sessions * columns, layer.kv_heads, layer.head_dim, page, sessions)
+    new = torch.zeros(sessions, dtype=torch.int32, device="cuda")
     # prompts, in two pieces
-    at = 0
     for n in (300, prompt - 300):
-        cu = torch.arange(sessions + 1, dtype=torch.int32, device="cuda") * n
-        kv_len = torch.full((sessions,), at + n, dtype=torch.int32, device="cuda")
-        positions = at + torch.arange(n, device="cuda").repeat(sessions)
-        x, residual = layer(torch.randn(sessions * n, 4096, device="cuda").half(), None, cache, qqq.KV8Batch(table, kv_len, cu, None, n, prompt + steps), positions)
-        at += n
+        batch = qqq.new_kv8_batch(sessions, columns, n, max_len)
+        positions = torch.zeros(sessions * n, dtype=torch.int32, device="cuda")
+        qqq.qqq_kv8_plan(held, batch, new.fill_(n), page, positions=positions)
+        x, residual = layer(torch.randn(sessions * n, 4096, device="cuda").half(), None, cache, batch, positions)
     # single tokens: one captured step, replayed
     x, residual = torch.randn(sessions, 4096, device="cuda").half(), torch.zeros(sessions, 4096, device="cuda").half()
-    batch = qqq.KV8Batch(table, kv_len, torch.arange(sessions + 1, dtype=torch.int32, device="cuda"), None, 1, prompt + steps)
+    batch, positions = qqq.new_kv8_batch(sessions, columns, 1, max_len), torch.zeros(sessions, dtype=torch.int32, device="cuda")
     work = layer.new_workspaces(sessions)   # (the graph's own)
-    layer(x, residual.clone(), cache, batch._replace(kv_len=kv_len + 1), kv_len, work)   # (once outside of the capture; the step below writes the same token again)
+
+    def step(residual):
+        qqq.qqq_kv8_plan(held, batch, new, page, positions=positions)
+        return layer(x, residual, cache, batch, positions, work)
+
+    new.zero_()
+    step(residual.clone())   # (once outside of the capture; it brings no token)
     torch.cuda.synchronize()
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
-        kv_len += 1
-        y, stream = layer(x, residual, cache, batch, kv_len - 1, work)
-    kv_len.fill_(prompt)
+        y, stream = step(residual)
+    new.fill_(1)
     start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
     start.record()
     for _ in range(steps):

@@ -1,0 +1,217 @@
+"""The serving step's calls together (paper_2406_09904_amd/serving.py): the plan, the layers over the cache, the vocabulary's product and the log probabilities.
+
+What the pages are called and in which rows sequences lie is of no weight to any number, so a step that the plan laid out gives bit for bit what the same calls
+give on tables made on the host.  Products are checked as integers; of the log probabilities' tolerance see test_gpu_logprobs.py: sums of V terms in 32 bits of
+logits up to 16 here, (2 * 16 + V / 64 + 16) * 2^-24 < 1e-5.
+"""
+import numpy as np
+import pytest
+import torch
+
+from paper_2406_09904_amd import binding as qqq
+from paper_2406_09904_amd import decoder_layer as dl
+from paper_2406_09904_amd import serving
+
+pytestmark = pytest.mark.gpu
+
+SHAPE = dict(layers=2, vocabulary=1003, hidden=512, q_heads=8, kv_heads=2, head_dim=64, ffn=1024)
+
+
+def _server(sessions, max_len, seed=0, **more):
+    return serving.random_server(sessions=sessions, max_len=max_len, seed=seed, **SHAPE, **more)
+
+
+def _i32(v):
+    return torch.tensor(np.asarray(v), dtype=torch.int32, device="cuda")
+
+
+class ByHand:
+    """The same model with tables, lengths and positions from the host."""
+
+    def __init__(self, server, sessions, max_len, page):
+        self.server, self.page, self.max_len = server, page, max_len
+        self.table, pages = dl.pages_in_order(sessions, max_len, page)
+        self.caches = [qqq.new_kv8_cache(pages, m.kv_heads, m.head_dim, page, sessions) for m in server.layers]
+        self.held = np.zeros(sessions, int)
+
+    def logits(self, ids, new, slots, max_new, rows=None):
+        """Of every row; rows: of how many the step's tensors are."""
+        before = self.held[slots].copy()
+        self.held[slots] += new
+        batch = qqq.KV8Batch(self.table[torch.tensor(slots).cuda()].contiguous(), _i32(self.held[slots]), _i32(np.concatenate([[0], np.cumsum(new)])), _i32(slots), max_new,
+                             self.max_len)
+        positions = np.zeros(rows or len(ids), int)
+        positions[:len(ids)] = np.concatenate([b + np.arange(n) for b, n in zip(before, new)])
+        ids = np.concatenate([ids, np.zeros(len(positions) - len(ids), int)])
+        x, residual = self.server.embedding[_i32(ids)], None
+        for m, cache in zip(self.server.layers, self.caches):
+            x, residual = m(x, residual, cache, batch, _i32(positions))
+        _, a_q, s_a = qqq.qqq_add_rmsnorm_quant(x, self.server.gain, residual, m.eps)
+        return a_q, s_a, self.server.head(a_q, s_a)
+
+
+def _steps(rng, sessions, max_len, turns):
+    """Which sessions bring how many tokens: prompts, pieces of them, single tokens, none."""
+    held = np.zeros(sessions, int)
+    for turn in range(turns):
+        slots = rng.permutation(sessions)[:rng.integers(1, sessions + 1)]
+        new = rng.choice([0, 1, 1, 1, 7, 16, 33, 60], len(slots))
+        new = np.minimum(new, max_len - held[slots])
+        if not new.sum():
+            new[0] = min(1, max_len - held[slots[0]])
+        held[slots] += new
+        yield slots, new
+
+
+def _check_logprobs(out, logits, targets, at):
+    l = logits.double().cpu().numpy()
+    lse = np.log(np.exp(l - l.max(-1, keepdims=True)).sum(-1)) + l.max(-1)
+    assert np.abs(l).max() < 16
+    if targets is not None:
+        want = np.where(targets < 0, 0, np.take_along_axis(l, np.maximum(targets, 0)[:, None], 1)[:, 0] - lse)
+        assert np.abs(out.logprob[at].cpu().numpy() - want).max() <= 1e-5
+    assert np.abs(out.lse[at].cpu().numpy() - lse).max() <= 1e-5
+    order = np.argsort(-l, axis=-1, kind="stable")[:, :out.top_tokens.shape[1]]
+    assert np.array_equal(out.top_tokens[at].cpu().numpy(), order)
+    assert np.abs(out.top_logprobs[at].cpu().numpy() - (np.take_along_axis(l, order, 1) - lse[:, None])).max() <= 1e-5
+
+
+@pytest.mark.parametrize("page", [16, 64])
+@pytest.mark.parametrize("scored", [False, True])
+def test_steps_against_tables_made_on_the_host(page, scored):
+    sessions, max_len = 5, 192
+    server = _server(sessions, max_len, page_tokens=page)
+    hand = ByHand(server, sessions, max_len, page)
+    rng = np.random.default_rng(page + scored)
+    codes, scale = qqq.qqq_unpack_w8(server.head.packed, server.head.V, server.head.K).double(), server.head.scale.double()
+    for slots, new in _steps(rng, sessions, max_len, 12):
+        n = int(new.sum())
+        ids = rng.integers(0, SHAPE["vocabulary"], n)
+        step = server.new_step(n, int(new.max()), _i32(slots))
+        step.ids.copy_(_i32(ids))
+        step.new.copy_(_i32(new))
+        targets = rng.integers(-1, SHAPE["vocabulary"], n) if scored else None
+        out = server(step, _i32(targets) if scored else None, top=5)
+        a_q, s_a, logits = hand.logits(ids, new, slots, int(new.max()))
+        assert torch.equal(step.batch.kv_len, _i32(hand.held[slots])) and step.lacking.item() == 0
+        # a sum of 512 products, the scales' product rounded in fp32, the whole in fp32 and to fp16: half steps of 2^-11, 2^-24, 2^-24
+        exact = (a_q.double() @ codes.t()) * s_a.double().view(-1, 1) * scale
+        assert ((logits.double() - exact).abs() <= (2.0 ** -11 + 2.0 ** -22) * exact.abs() + 2.0 ** -25).all()
+        if scored:
+            _check_logprobs(out, logits, targets, slice(None))
+        else:
+            b = np.flatnonzero(new)     # (a sequence without a token has no row)
+            # the same row in a product of fewer rows: integer sums, so the same logits
+            _check_logprobs(out, logits[torch.from_numpy(np.cumsum(new)[b] - 1).cuda()], None, torch.from_numpy(b).cuda())
+
+
+def test_captured_steps_with_sessions_that_come_and_go():
+    """A graph of single tokens, replayed while sessions rest, end and begin in others' pages; each as if it were alone, eager and in order."""
+    sessions, max_len, page = 6, 96, 16
+    server = _server(sessions, max_len, seed=4, page_tokens=page, pages=16)
+    step = server.new_step(sessions, 1, keep=True)
+    server(step)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = server(step, top=3)
+    rng = np.random.default_rng(5)
+    alone = _server(sessions, max_len, seed=4, page_tokens=page)     # the same weights, pages enough
+    eager = alone.new_step(sessions, 1)
+    for turn in range(40):
+        if turn % 8 == 0:     # two end, and begin with prompts, in any order
+            ends = rng.permutation(sessions)[:2]
+            lengths = rng.integers(1, 50, 2)
+            ids = rng.integers(0, SHAPE["vocabulary"], lengths.sum())
+            for s in (server, alone):
+                s.release(_i32(np.concatenate([ends, ends[:1]])))     # (one twice: once)
+                prompt = s.new_step(int(lengths.sum()), 49, _i32(ends))
+                prompt.ids.copy_(_i32(ids))
+                prompt.new.copy_(_i32(lengths))
+                s(prompt)
+        new = (rng.random(sessions) < 0.8).astype(int)
+        new = np.minimum(new, max_len - alone.sessions.held.cpu().numpy())
+        ids = rng.integers(0, SHAPE["vocabulary"], sessions)
+        for s in (step, eager):
+            s.ids.copy_(_i32(ids))
+            s.new.copy_(_i32(new))
+        graph.replay()
+        want = alone(eager, top=3)
+        torch.cuda.synchronize()
+        assert step.lacking.item() == 0 and torch.equal(server.sessions.held, alone.sessions.held)
+        b = torch.from_numpy(np.flatnonzero(new)).cuda()
+        for name in ("entropy", "lse", "top_tokens", "top_logprobs"):
+            assert torch.equal(getattr(out, name)[b], getattr(want, name)[b]), (turn, name)
+    server.release()
+    assert server.sessions.free_count.item() == 16 and sorted(server.sessions.free.tolist()) == list(range(16)) and not server.sessions.held.any()
+
+
+def test_generated_tokens_are_those_of_the_whole_text():
+    """Greedy tokens from a graph that feeds itself; then the same text scored in one step: the cache holds the same keys and values, so attention sees the same,
+    and only its own roundings of another split of the work part the two."""
+    server = _server(3, 128, seed=9, page_tokens=16)
+    rng = np.random.default_rng(10)
+    prompt = rng.integers(0, SHAPE["vocabulary"], 12)
+    start = server.new_step(12, 12, _i32([1]))
+    start.ids.copy_(_i32(prompt))
+    start.new.fill_(12)
+    first = server(start)
+    step = server.new_step(1, 1, _i32([1]), keep=True)
+    server(step)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    text, scores = [], []
+    with torch.cuda.graph(graph):
+        out = server(step)
+        step.ids.copy_(out.top_tokens[:, 0])
+    step.ids.copy_(first.top_tokens[:, 0])
+    step.new.fill_(1)
+    text.append(first.top_tokens.item())
+    for _ in range(40):
+        graph.replay()
+        text.append(step.ids.item())
+        scores.append(out.top_logprobs.item())
+    ids = np.concatenate([prompt, text[:-1]])
+    whole = server.new_step(len(ids), len(ids), _i32([2]))
+    whole.ids.copy_(_i32(ids))
+    whole.new.fill_(len(ids))
+    out = server(whole, _i32(np.concatenate([ids[1:], text[-1:]])))
+    # Where two values differ by fp16's half step (2^-11), a code falls to its neighbour with probability 127 / 4 * 2^-11 = 1.5 % (the largest of a row is
+    # about 4 deviations): 8 of 512, each by 4 / 127 of a deviation, sqrt(8 / 512) * 4 / 127 = 0.4 % of the row; of eight quantisations 1.1 %, and of a
+    # logit, deviation 2, 0.023.  The largest of 40 stays within 4 deviations of that, 0.1; 0.25 is asked.
+    assert np.abs(out.logprob[12:].cpu().numpy() - np.array(scores)).max() < 0.25
+
+
+def test_two_servers_on_two_streams():
+    servers = [_server(4, 64, seed=s, page_tokens=16) for s in (1, 2)]
+    rng = np.random.default_rng(3)
+    ids = [[rng.integers(0, SHAPE["vocabulary"], 4 * n) for n in (9, 1, 1, 1)] for _ in servers]
+
+    def run(server, ids):
+        outs = []
+        for row in ids:
+            step = server.new_step(len(row), len(row) // 4)
+            step.ids.copy_(_i32(row))
+            step.new.fill_(len(row) // 4)
+            outs.append(server(step, top=4).top_logprobs)
+        return outs
+
+    want = [run(s, i) for s, i in zip(servers, ids)]
+    for s in servers:
+        s.release()
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in servers]
+    got = []
+    for s, i, stream in zip(servers, ids, streams):
+        with torch.cuda.stream(stream):
+            got.append(run(s, i))
+    torch.cuda.synchronize()
+    for a, b in zip(want, got):
+        for x, y in zip(a, b):
+            assert torch.equal(x, y)
+
+
+def test_the_program_runs(capsys):
+    serving.main()
+    said = capsys.readouterr().out
+    assert "us a step" in said and "held now: [84, 57, 41, 52, 104, 169, 290, 490] tokens" in said
