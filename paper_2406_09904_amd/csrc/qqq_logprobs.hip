@@ -7,8 +7,9 @@
 //
 // The largest `top` logits need nothing in that pass but the threads' maxima.  128 groups of threads hold disjoint parts of the row, so the top-th largest of the groups' maxima is
 // a lower bound of the row's top-th largest value, and only the blocks of threads with a maximum of at least that are looked at again: in a row without order the bound lets
-// 128 log(128 / (128 - top)) values pass, 22 for the largest 20, 89 for 64, whatever V is.  Values that reach the bound are gathered in LDS, and each one's rank is the number of larger ones.  Where they are too many (a row of equal
-// values, say) they go through lists instead, of up to 64 entries in a wave's lanes in falling order.  Entries are ordered by (value, lower place first), so equal values have
+// 128 log(128 / (128 - top)) values pass, 22 for the largest 20, 89 for 64, whatever V is.  Values that reach the bound are gathered in LDS, and each one's rank is the number of larger ones.  Where they are too many, because
+// most of the row is masked or equal, those above the bound are gathered, and then the row's first values that are the bound.  Where these are too many as well (rising values) they go
+// through lists, of up to 64 entries in a wave's lanes in falling order.  Entries are ordered by (value, lower place first), so equal values have
 // one order and no result depends on which wave came first.
 //
 // Many rows: a workgroup a row.  Few rows: a row is split, the parts leave their sums and their groups' maxima in the workspace, and a second kernel joins
@@ -114,6 +115,8 @@ struct Sums {
     largest = fmaxf(largest, x);
     refer_to(F32 ? largest : ceilf(largest * kLog2e));
   }
+  // for the bound: the largest value, or infinity where there may be a NaN
+  __device__ __forceinline__ float reached() const { return z != z ? __builtin_inff() : z == 0.0f ? -__builtin_inff() : largest; }
   // of a value no larger than the largest; a NaN or infinity gives a NaN
   __device__ __forceinline__ float below(float x) const { return F32 ? x - m : __builtin_fmaf(x, kLog2e, -m); }
   static __device__ __forceinline__ float power(float d) { return __builtin_amdgcn_exp2f(d * kToTwo); }
@@ -211,16 +214,12 @@ __device__ __forceinline__ float value_of(uint32_t order) {
 }
 
 // The top-th largest of the workgroup's kBound values (none of them a NaN), in all its threads.  Each wave counts, for every value, the larger ones among its share of them.
-// Where it is no more than the value that threads start from, everything passes, -infinity too.
 template <int T>
 __device__ __forceinline__ float bound_of(const float* of_group, int (*larger)[kBound], int top) {
   constexpr int W = T / 64, kShare = kBound / W;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const float v[2] = {of_group[lane], of_group[64 + lane]};
-  if (top == 1) {  // the largest of all
-    const float largest = wave_max(fmaxf(v[0], v[1]));
-    return largest <= -FLT_MAX ? -__builtin_inff() : largest;
-  }
+  if (top == 1) return wave_max(fmaxf(v[0], v[1]));  // the largest of all
   int n[2] = {0, 0};
 #pragma unroll
   for (int i = 0; i < kShare; ++i)
@@ -237,8 +236,7 @@ __device__ __forceinline__ float bound_of(const float* of_group, int (*larger)[k
     for (int w = 0; w < W; ++w) n[h] += larger[w][64 * h + lane];
     if (n[h] < top) least = fminf(least, v[h]);
   }
-  const float bound = -wave_max(-least);
-  return bound <= -FLT_MAX ? -__builtin_inff() : bound;
+  return -wave_max(-least);
 }
 
 // The largest entries so far, in the wave's lanes in falling order: (order of the value, bits of the place inverted); 0, 0: none
@@ -278,12 +276,18 @@ struct Found {
     const int at = atomicAdd(&count, 1);  // (which entry lies where decides nothing)
     if (at < T) entries[at] = (uint64_t)order << 32 | place;
   }
+  __device__ __forceinline__ bool is_full() const { return *const_cast<const volatile int*>(&count) > T; }  // (then nothing more need be added)
   __device__ __forceinline__ void add_list(const List& list, int top) {
     if ((int)(threadIdx.x & 63) < top && (list.order | list.place) != 0) add(list.order, list.place);
   }
 };
-// Lanes with a block of values (or one of the lead's and tail's) that reach the bound: straight to what is found, or through the wave's list
-template <bool F32, int T, bool LIST>
+// What lanes do with the values that they look at: gather those that reach the bound, or those above it, or offer them to the wave's list
+enum { kReach, kAbove, kList };
+template <int MODE>
+__device__ __forceinline__ bool wanted(float x, float bound) {
+  return MODE == kAbove ? !(x <= bound) : !(x < bound);  // (and a NaN)
+}
+template <bool F32, int T, int MODE>
 __device__ __forceinline__ void look_at_block(const Row<F32>& r, int b, bool has, int top, float& bound, List& list, Found<T>& found) {
   uint4 v = Row<F32>::masked_block();
   if (has) v = r.template block<false>(b);
@@ -291,20 +295,94 @@ __device__ __forceinline__ void look_at_block(const Row<F32>& r, int b, bool has
   Row<F32>::unpack(v, x);
   bool some = false;
 #pragma unroll
-  for (int i = 0; i < Row<F32>::kVec; ++i) some |= !(x[i] < bound);
+  for (int i = 0; i < Row<F32>::kVec; ++i) some |= wanted<MODE>(x[i], bound);
   some &= has;
   if (!__ballot(some)) return;
 #pragma unroll
   for (int i = 0; i < Row<F32>::kVec; ++i) {
-    if constexpr (LIST) list.offer(some, x[i], r.place_of_block(b) + i, top, bound);
-    else if (some && !(x[i] < bound)) found.add(order_of(x[i]), ~(uint32_t)(r.place_of_block(b) + i));
+    if constexpr (MODE == kList) list.offer(some, x[i], r.place_of_block(b) + i, top, bound);
+    else if (some && wanted<MODE>(x[i], bound)) found.add(order_of(x[i]), ~(uint32_t)(r.place_of_block(b) + i));
   }
 }
-template <bool F32, int T, bool LIST>
+template <bool F32, int T, int MODE>
 __device__ __forceinline__ void look_at_value(const Row<F32>& r, int place, bool has, int top, float& bound, List& list, Found<T>& found) {
   const float x = has ? r.value(place) : 0.0f;
-  if constexpr (LIST) list.offer(has, x, place, top, bound);
-  else if (has && !(x < bound)) found.add(order_of(x), ~(uint32_t)place);
+  if constexpr (MODE == kList) list.offer(has, x, place, top, bound);
+  else if (has && wanted<MODE>(x, bound)) found.add(order_of(x), ~(uint32_t)place);
+}
+
+// Whether a thread that reached that much has values to look at
+__device__ __forceinline__ bool passes(float reached, float level, bool above) { return (above ? reached > level : reached >= level) || reached == __builtin_inff(); }
+
+// The first `want` of the row's values that equal `value`: T blocks at a time, from the row's begin on
+template <bool F32, int T>
+__device__ __forceinline__ void find_equal(const Row<F32>& r, float value, int want, Found<T>& found) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  int got = 0;
+  auto turn = [&](uint32_t hits, int place) {
+    int sum = __popc(hits);
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      const int other = __shfl_up(sum, d);
+      if (lane >= d) sum += other;
+    }
+    if (lane == 63) found.ranks[wave] = sum;
+    __syncthreads();
+    int at = got + sum - __popc(hits);
+    for (int w = 0; w < T / 64; ++w) {
+      at += w < wave ? found.ranks[w] : 0;
+      got += found.ranks[w];
+    }
+    for (; hits && at < want; hits &= hits - 1, ++at) found.add(order_of(value), ~(uint32_t)(place + __builtin_ctz(hits)));
+    __syncthreads();
+  };
+  for (int i = 0; i < r.lead && got < want; i += T) turn(i + tid < r.lead && r.value(i + tid) == value, i + tid);
+  for (int b0 = 0; b0 < r.blocks && got < want; b0 += T) {
+    uint32_t hits = 0;
+    if (b0 + tid < r.blocks) {
+      float x[Row<F32>::kVec];
+      Row<F32>::unpack(r.template block<false>(b0 + tid), x);
+#pragma unroll
+      for (int i = 0; i < Row<F32>::kVec; ++i) hits |= (uint32_t)(x[i] == value) << i;
+    }
+    turn(hits, r.place_of_block(b0 + tid));
+  }
+  if (got < want) turn(tid < r.tail && r.value(r.place_of_odd(r.lead + tid)) == value, r.place_of_odd(r.lead + tid));
+  if (tid < 64) found.ranks[tid] = 0;
+}
+
+// The row's largest.  pass(level, above): the threads (or groups of them) that met a value of the level, or above it, are listed; look(mode, level, list): what they met is.
+template <bool F32, int T, class Pass, class Look>
+__device__ __forceinline__ void find_top(const Row<F32>& r, int top, float bound, int& passing, Found<T>& found, Pass pass, Look look) {
+  auto again = [&] {
+    __syncthreads();
+    if (threadIdx.x == 0) found.count = passing = 0;
+    __syncthreads();
+  };
+  List list;
+  pass(bound, false);
+  __syncthreads();
+  look(std::integral_constant<int, kReach>{}, bound, list);
+  __syncthreads();
+  if (found.count <= T) return;  // (the same in every thread)
+  // Too many: of those that are the bound itself only the first few can be wanted, and few are above it
+  again();
+  pass(bound, true);
+  __syncthreads();
+  look(std::integral_constant<int, kAbove>{}, bound, list);
+  __syncthreads();
+  if (found.count <= T) {
+    const int want = top - found.count;
+    if (want > 0) find_equal<F32, T>(r, bound, want, found);
+  } else {
+    again();
+    pass(bound, false);
+    __syncthreads();
+    look(std::integral_constant<int, kList>{}, bound, list);
+    again();
+    found.add_list(list, top);
+  }
+  __syncthreads();
 }
 
 // Each entry's rank counted, the first `top` written.
@@ -414,7 +492,7 @@ __global__ __launch_bounds__(T, 8) void logprobs_kernel(const LogprobArgs p) {
   given.request(p, row, r);
   const Sums<F32> mine = stream<F32, T, U, PAST>(r, 0, r.blocks, true);
   if (p.top) {
-    const float g = group_max<T / kBound>(mine.largest);
+    const float g = group_max<T / kBound>(mine.reached());
     if (tid % (T / kBound) == 0) of_group[tid / (T / kBound)] = g;
     if (tid < 64) found.ranks[tid] = 0;
     if (tid == 0) found.count = passing = 0;
@@ -433,34 +511,26 @@ __global__ __launch_bounds__(T, 8) void logprobs_kernel(const LogprobArgs p) {
     return;
   }
 
-  float bound = bound_of<T>(of_group, larger, p.top);
   // threads with such a value, and then their blocks spread over all waves: a thread's own, one after the other, would be as many memory latencies
-  if (mine.largest >= bound || mine.z != mine.z) passed[atomicAdd(&passing, 1)] = (uint16_t)tid;
-  __syncthreads();
-  const int each = (r.blocks + T - 1) / T, items = passing * each;
-  List list;
-  auto look = [&](auto through_list) {
-    constexpr bool LIST = decltype(through_list)::value;
+  auto pass = [&](float level, bool above) {
+    if (passes(mine.reached(), level, above)) passed[atomicAdd(&passing, 1)] = (uint16_t)tid;
+  };
+  const int each = (r.blocks + T - 1) / T;
+  auto look = [&](auto mode, float level, List& list) {
+    constexpr int MODE = decltype(mode)::value;
+    const int items = passing * each;
     for (int i0 = wave; i0 < items; i0 += T) {
+      if (MODE != kList && found.is_full()) return;
       const int i = i0 + lane * (T / 64), b = i < items ? passed[i / each] + i % each * T : r.blocks;
-      look_at_block<F32, T, LIST>(r, b, b < r.blocks, p.top, bound, list, found);
+      look_at_block<F32, T, MODE>(r, b, b < r.blocks, p.top, level, list, found);
     }
     for (int i0 = wave * 64; i0 < r.lead + r.tail; i0 += T) {
       const int i = i0 + lane;
       const bool odd = i < r.lead + r.tail;
-      look_at_value<F32, T, LIST>(r, odd ? r.place_of_odd(i) : 0, odd, p.top, bound, list, found);
+      look_at_value<F32, T, MODE>(r, odd ? r.place_of_odd(i) : 0, odd, p.top, level, list, found);
     }
   };
-  look(std::false_type{});
-  __syncthreads();
-  if (found.count > T) {  // the same in every thread
-    look(std::true_type{});
-    __syncthreads();
-    if (tid == 0) found.count = 0;
-    __syncthreads();
-    found.add_list(list, p.top);
-    __syncthreads();
-  }
+  find_top<F32, T>(r, p.top, bound_of<T>(of_group, larger, p.top), passing, found, pass, look);
   const Sums<F32> all = join_waves<F32, T / 64>(of_wave);
   const float log_z = logf(all.z);
   write_top<F32, T>(p, row, all, log_z, found);
@@ -478,7 +548,7 @@ __global__ __launch_bounds__(kSplitThreads) void logprobs_part_kernel(const Logp
   const Sums<F32> mine = stream<F32, kSplitThreads, 2, false>(r, from, to, part == 0);
   float* out = p.parts + (row * p.splits + part) * kPartValues;
   if (p.top) {
-    const float g = group_max<kSplitThreads / kGroups>(mine.z != mine.z ? __builtin_inff() : mine.largest);
+    const float g = group_max<kSplitThreads / kGroups>(mine.reached());
     if (tid % (kSplitThreads / kGroups) == 0) out[3 + tid / (kSplitThreads / kGroups)] = g;
   }
   const Sums<F32> w = wave_sums(mine);
@@ -514,11 +584,11 @@ __global__ __launch_bounds__(TOP ? kJoinThreads : 64) void logprobs_join_kernel(
   const float* parts = p.parts + row * p.splits * kPartValues;
   float g[kJoinGroups];
   if constexpr (TOP) {
-    float most = -FLT_MAX;
+    float most = -__builtin_inff();
 #pragma unroll
     for (int i = 0; i < kJoinGroups; ++i) {  // a wave: the groups of part wave + kWaves * i
       const int part = wave + kWaves * i;
-      g[i] = part < p.splits ? parts[part * kPartValues + 3 + lane] : -FLT_MAX;
+      g[i] = part < p.splits ? parts[part * kPartValues + 3 + lane] : -__builtin_inff();
       most = fmaxf(most, g[i]);
     }
     most = group_max<T / kBound>(most);
@@ -550,39 +620,30 @@ __global__ __launch_bounds__(TOP ? kJoinThreads : 64) void logprobs_join_kernel(
       of_wave[wave][2] = s.t;
     }
     __syncthreads();
-    float bound = bound_of<T>(of_group, larger, p.top);
+    auto pass = [&](float level, bool above) {
 #pragma unroll
-    for (int i = 0; i < kJoinGroups; ++i) {
-      const int part = wave + kWaves * i;
-      if (part < p.splits && g[i] >= bound) passed[atomicAdd(&passing, 1)] = (uint16_t)(part * kGroups + lane);
-    }
-    __syncthreads();
+      for (int i = 0; i < kJoinGroups; ++i) {
+        const int part = wave + kWaves * i;
+        if (part < p.splits && passes(g[i], level, above)) passed[atomicAdd(&passing, 1)] = (uint16_t)(part * kGroups + lane);
+      }
+    };
     // the values of each group that passed, kLanes threads of its part, by as many lanes: a wave takes 64 / kLanes groups at a time, neighbours of the list going to different waves
     constexpr int kLanes = kSplitThreads / kGroups;
-    const int n = passing;
-    List list;
-    auto look = [&](auto through_list) {
-      constexpr bool LIST = decltype(through_list)::value;
+    auto look = [&](auto mode, float level, List& list) {
+      constexpr int MODE = decltype(mode)::value;
+      const int n = passing;
       for (int e0 = wave; e0 < n; e0 += kWaves * (64 / kLanes)) {
+        if (MODE != kList && found.is_full()) return;
         const int e = e0 + lane / kLanes * kWaves;
         const int id = e < n ? passed[e] : 0, part = id / kGroups, thread = id % kGroups * kLanes + lane % kLanes;
         const int from = min((int64_t)part * p.blocks_per_part, (int64_t)r.blocks), to = e < n ? min((int64_t)from + p.blocks_per_part, (int64_t)r.blocks) : 0;
         for (int j = thread; j < p.blocks_per_part; j += kSplitThreads)  // (blocks_per_part is a multiple of kSplitThreads: every lane turns as often)
-          look_at_block<F32, T, LIST>(r, from + j, from + j < to, p.top, bound, list, found);
+          look_at_block<F32, T, MODE>(r, from + j, from + j < to, p.top, level, list, found);
         const bool odd = e < n && part == 0 && thread < r.lead + r.tail;
-        look_at_value<F32, T, LIST>(r, odd ? r.place_of_odd(thread) : 0, odd, p.top, bound, list, found);
+        look_at_value<F32, T, MODE>(r, odd ? r.place_of_odd(thread) : 0, odd, p.top, level, list, found);
       }
     };
-    look(std::false_type{});
-    __syncthreads();
-    if (found.count > T) {
-      look(std::true_type{});
-      __syncthreads();
-      if (tid == 0) found.count = 0;
-      __syncthreads();
-      found.add_list(list, p.top);
-      __syncthreads();
-    }
+    find_top<F32, T>(r, p.top, bound_of<T>(of_group, larger, p.top), passing, found, pass, look);
     const Sums<F32> all = join_waves<F32, kWaves>(of_wave);
     const float log_z = logf(all.z);
     write_top<F32, T>(p, row, all, log_z, found);

@@ -142,6 +142,71 @@ def _check_some(x, top):
     _close(out.lse[some], want[2], r + 2 * U * (np.abs(want[2]) + np.abs(x[some]).max(1) + np.log(x.shape[1])), "lse")
 
 
+# rows of 256 threads value by value and by blocks, of 512, of 1024, split ones
+@pytest.mark.parametrize("M,V", [(300, 700), (600, 30011), (100, 9001), (70, 200003), (2100, 40013), (2, 70000), (1, 12000)])
+@pytest.mark.parametrize("dtype", [np.float16, np.float32])
+def test_more_candidates_than_there_is_room_for(M, V, dtype):
+    """Values in great number that are the last of the largest, or are more than that: only the first of them count, wherever in the row they lie."""
+    rng = np.random.default_rng(M + V)
+    lowest, inf = np.finfo(dtype).min, np.inf
+    rows = []
+    for masked in (-inf, lowest):                                           # few allowed
+        for allowed in (1, 5, 63):
+            r = np.full(V, masked)
+            r[rng.permutation(V)[:allowed]] = 3 * rng.standard_normal(allowed)
+            rows.append(r)
+    r = np.full(V, -inf)                                                    # few allowed, some at the type's end, nothing else
+    r[rng.permutation(V)[:13]] = lowest
+    r[rng.permutation(V)[:3]] = [1, 2, 1]
+    rows.append(r)
+    for value in (2.0, 0.0, inf, np.nan):                                   # the last quarter, and the same with three above and a tail that is not
+        r = rng.uniform(-5, -1, V)
+        r[V - V // 4:] = value
+        if value == 0:
+            r[V - V // 4:][rng.random(V // 4) < 0.5] = -0.0
+        rows.append(r)
+        rows.append(np.where(np.arange(V) > V - 9, -7.0, r))
+        rows[-1][[V // 2, 1, V - 1]] = 4.0
+    r = np.floor(rng.uniform(0, 3, V))                                      # three values, the largest rare at first
+    r[:V // 2] = np.minimum(r[:V // 2], 1)
+    rows.append(r)
+    rows.append(np.sort(rng.uniform(-8, 8, V)))                             # rising
+    rows.append(np.where(np.arange(V) % 2, np.nan, inf))
+    rows = np.stack(rows).astype(dtype)
+    for top in (1, 2, 20, 64):
+        for offset in (0, 1):
+            want = ref.logprobs(rows, None, top)
+            for begin in range(0, len(rows), M):                            # (few rows at a time where that is what is tested)
+                some = rows[begin:begin + M]
+                n = len(some)
+                out = qqq.qqq_logprobs(_device(some[np.arange(M) % n], offset=offset, pad=1), None, top)    # the rows again and again, until it is M
+                for i in {0, max(0, (M - n) // n * n)}:
+                    assert np.array_equal(out.top_tokens[i:i + n].cpu().numpy(), want[3][begin:begin + n]), (top, offset)
+                    r = (V / 256 * (1 + 6 / 16) + 100 + 3 * np.log(V)) * U
+                    with np.errstate(invalid="ignore"):
+                        _close(out.top_logprobs[i:i + n], want[4][begin:begin + n], r + 2 * U * (2 * np.abs(want[4][begin:begin + n]) + 2 * np.log(V)), "top logprobs")
+
+
+def test_rows_that_are_past_the_last_cache():
+    """Logits of more than the last level of cache holds, in both sizes of workgroup."""
+    for M, V, dtype in ((2100, 80001, np.float16), (3000, 50001, np.float32), (9000, 20001, np.float16)):
+        rng = np.random.default_rng(V)
+        some = _logits(rng, 7, V, dtype)
+        dev = torch.from_numpy(some).cuda().repeat((M + 6) // 7, 1)[:M].contiguous()
+        assert dev.numel() * dev.element_size() > 256 << 20
+        for top in (0, 7):
+            out = qqq.qqq_logprobs(dev, None, top)
+            want = ref.logprobs(some, None, top)
+            last = (M - 7) // 7 * 7
+            for i in (0, last):
+                r = (V / 256 * (1 + 6 / 16) + 100 + 3 * np.log(V)) * U
+                _close(out.lse[i:i + 7], want[2], r + 2 * U * (np.abs(want[2]) + np.abs(some).max(1) + np.log(V)), "lse")
+                if top:
+                    assert np.array_equal(out.top_tokens[i:i + 7].cpu().numpy(), want[3])
+            # equal rows, equal numbers, where they begin at as many bytes behind 16 (which threads have which values goes by that): every 56th of these odd rows
+            assert torch.equal(out.lse, out.lse[:56].repeat((M + 55) // 56)[:M])
+
+
 def test_no_token_and_a_short_vocabulary():
     x = _logits(np.random.default_rng(1), 6, 5, np.float16)
     out = _check(x, 9, np.array([-1, 0, 4, 5, -2 ** 31, 2 ** 31 - 1], np.int32))
