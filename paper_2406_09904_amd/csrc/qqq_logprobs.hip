@@ -105,13 +105,21 @@ struct Sums {
   float largest = -FLT_MAX;                      // value met (a NaN is not one)
   float m = F32 ? -FLT_MAX : -94505.0f;          // reference: of fp32 the largest value, of fp16 the integer above its log2 e times
   float z = 0.0f, t = 0.0f;
+  // TRACK: the largest value of all batches of blocks but the one that has the largest, and which that is (below 0: of none)
+  float others = -FLT_MAX;
+  int at = -1;
   __device__ __forceinline__ void refer_to(float to) {
     const float higher = fmaxf(m, to), d = fmaxf(m - higher, kFar), f = __builtin_amdgcn_exp2f(d * kToTwo);
     t = (t + d * z) * f;
     z *= f;
     m = higher;
   }
-  __device__ __forceinline__ void meet(float x) {
+  template <bool TRACK>
+  __device__ __forceinline__ void meet(float x, int batch) {
+    if constexpr (TRACK) {
+      others = __builtin_amdgcn_fmed3f(others, largest, x);
+      at = x > largest ? batch : at;
+    }
     largest = fmaxf(largest, x);
     refer_to(F32 ? largest : ceilf(largest * kLog2e));
   }
@@ -125,9 +133,9 @@ struct Sums {
     z += e;
     t = __builtin_fmaf(fmaxf(d, kFar), e, t);
   }
-  template <int U>
-  __device__ __forceinline__ void add_blocks(const uint4* v) {
-    meet(Row<F32>::template largest<U>(v));
+  template <int U, bool TRACK>
+  __device__ __forceinline__ void add_blocks(const uint4* v, int batch) {
+    meet<TRACK>(Row<F32>::template largest<U>(v), batch);
     const float t_before = t;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -353,10 +361,10 @@ __device__ __forceinline__ void find_equal(const Row<F32>& r, float value, int w
 
 // The row's largest.  pass(level, above): the threads (or groups of them) that met a value of the level, or above it, are listed; look(mode, level, list): what they met is.
 template <bool F32, int T, class Pass, class Look>
-__device__ __forceinline__ void find_top(const Row<F32>& r, int top, float bound, int& passing, Found<T>& found, Pass pass, Look look) {
+__device__ __forceinline__ void find_top(const Row<F32>& r, int top, float bound, int& passing, int& passing_once, Found<T>& found, Pass pass, Look look) {
   auto again = [&] {
     __syncthreads();
-    if (threadIdx.x == 0) found.count = passing = 0;
+    if (threadIdx.x == 0) found.count = passing = passing_once = 0;
     __syncthreads();
   };
   List list;
@@ -441,7 +449,7 @@ __device__ __forceinline__ void write_numbers(const LogprobArgs& p, int64_t row,
 }
 
 // One thread's part of blocks [from, to): every T-th, and one of the lead's and tail's values where `odd` says so.
-template <bool F32, int T, int U, bool PAST>
+template <bool F32, int T, int U, bool PAST, bool TRACK>
 __device__ __forceinline__ Sums<F32> stream(const Row<F32>& r, int from, int to, bool odd) {
   Sums<F32> s;
   const int tid = threadIdx.x;
@@ -463,39 +471,38 @@ __device__ __forceinline__ Sums<F32> stream(const Row<F32>& r, int from, int to,
   request(from, v);
   for (int b0 = from; b0 < to; b0 += 2 * T * U) {
     request(b0 + T * U, w);
-    s.template add_blocks<U>(v);
+    s.template add_blocks<U, TRACK>(v, b0);
     if (b0 + T * U >= to) break;
     request(b0 + 2 * T * U, v);
-    s.template add_blocks<U>(w);
+    s.template add_blocks<U, TRACK>(w, b0 + T * U);
   }
 #pragma unroll
   for (int i = 0; i < kOddEach; ++i)
     if (odd && tid + T * i < r.lead + r.tail) {
-      s.meet(x[i]);
+      s.template meet<TRACK>(x[i], -1);
       s.add(x[i]);
     }
   return s;
 }
 
 // ---- a workgroup a row
-template <bool F32, int T, int U, bool PAST>
+template <bool F32, int T, int U, bool PAST, bool TRACK>
 __global__ __launch_bounds__(T, 8) void logprobs_kernel(const LogprobArgs p) {
   __shared__ float of_wave[T / 64][3], of_group[kBound];
   __shared__ int larger[T / 64][kBound];
   __shared__ Found<T> found;
-  __shared__ uint16_t passed[T];
-  __shared__ int passing;
+  __shared__ int passed[T], passing, passing_once;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t row = blockIdx.x;
   const Row<F32> r(p, row, p.V <= kOddEach * T);
   Given given;
   given.request(p, row, r);
-  const Sums<F32> mine = stream<F32, T, U, PAST>(r, 0, r.blocks, true);
+  const Sums<F32> mine = stream<F32, T, U, PAST, TRACK>(r, 0, r.blocks, true);
   if (p.top) {
     const float g = group_max<T / kBound>(mine.reached());
     if (tid % (T / kBound) == 0) of_group[tid / (T / kBound)] = g;
     if (tid < 64) found.ranks[tid] = 0;
-    if (tid == 0) found.count = passing = 0;
+    if (tid == 0) found.count = passing = passing_once = 0;
   }
   const Sums<F32> w = wave_sums(mine);
   if (lane == 0) {
@@ -511,17 +518,23 @@ __global__ __launch_bounds__(T, 8) void logprobs_kernel(const LogprobArgs p) {
     return;
   }
 
-  // threads with such a value, and then their blocks spread over all waves: a thread's own, one after the other, would be as many memory latencies
+  // Threads with such a value, and then their blocks spread over all waves: a thread's own, one after the other, would be as many memory latencies.  TRACK: where one batch of a
+  // thread's blocks alone has one, as most do, no other is read again.
   auto pass = [&](float level, bool above) {
-    if (passes(mine.reached(), level, above)) passed[atomicAdd(&passing, 1)] = (uint16_t)tid;
+    if (!passes(mine.reached(), level, above)) return;
+    if (!TRACK || mine.z != mine.z || passes(mine.others, level, above)) passed[atomicAdd(&passing, 1)] = tid;
+    else if (mine.at >= 0) passed[T - 1 - atomicAdd(&passing_once, 1)] = mine.at + tid;
   };
   const int each = (r.blocks + T - 1) / T;
   auto look = [&](auto mode, float level, List& list) {
     constexpr int MODE = decltype(mode)::value;
-    const int items = passing * each;
+    const int whole = passing * each, items = TRACK ? whole + passing_once * U : whole;
     for (int i0 = wave; i0 < items; i0 += T) {
       if (MODE != kList && found.is_full()) return;
-      const int i = i0 + lane * (T / 64), b = i < items ? passed[i / each] + i % each * T : r.blocks;
+      const int i = i0 + lane * (T / 64);
+      int b = r.blocks;
+      if (i < whole) b = passed[i / each] + i % each * T;
+      else if (TRACK && i < items) b = passed[T - 1 - (i - whole) / U] + (i - whole) % U * T;
       look_at_block<F32, T, MODE>(r, b, b < r.blocks, p.top, level, list, found);
     }
     for (int i0 = wave * 64; i0 < r.lead + r.tail; i0 += T) {
@@ -530,7 +543,7 @@ __global__ __launch_bounds__(T, 8) void logprobs_kernel(const LogprobArgs p) {
       look_at_value<F32, T, MODE>(r, odd ? r.place_of_odd(i) : 0, odd, p.top, level, list, found);
     }
   };
-  find_top<F32, T>(r, p.top, bound_of<T>(of_group, larger, p.top), passing, found, pass, look);
+  find_top<F32, T>(r, p.top, bound_of<T>(of_group, larger, p.top), passing, passing_once, found, pass, look);
   const Sums<F32> all = join_waves<F32, T / 64>(of_wave);
   const float log_z = logf(all.z);
   write_top<F32, T>(p, row, all, log_z, found);
@@ -545,7 +558,7 @@ __global__ __launch_bounds__(kSplitThreads) void logprobs_part_kernel(const Logp
   const int64_t row = blockIdx.y;
   const Row<F32> r(p, row);
   const int from = min((int64_t)part * p.blocks_per_part, (int64_t)r.blocks), to = min((int64_t)from + p.blocks_per_part, (int64_t)r.blocks);
-  const Sums<F32> mine = stream<F32, kSplitThreads, 2, false>(r, from, to, part == 0);
+  const Sums<F32> mine = stream<F32, kSplitThreads, 2, false, false>(r, from, to, part == 0);
   float* out = p.parts + (row * p.splits + part) * kPartValues;
   if (p.top) {
     const float g = group_max<kSplitThreads / kGroups>(mine.reached());
@@ -643,7 +656,7 @@ __global__ __launch_bounds__(TOP ? kJoinThreads : 64) void logprobs_join_kernel(
         look_at_value<F32, T, MODE>(r, odd ? r.place_of_odd(thread) : 0, odd, p.top, level, list, found);
       }
     };
-    find_top<F32, T>(r, p.top, bound_of<T>(of_group, larger, p.top), passing, found, pass, look);
+    find_top<F32, T>(r, p.top, bound_of<T>(of_group, larger, p.top), passing, passing, found, pass, look);
     const Sums<F32> all = join_waves<F32, kWaves>(of_wave);
     const float log_z = logf(all.z);
     write_top<F32, T>(p, row, all, log_z, found);
@@ -672,17 +685,22 @@ template <bool F32>
 int launch_typed(LogprobArgs& p, int64_t M, const Split& s, hipStream_t st) {
   if (s.parts == 1) {
     const bool past = M * p.V * (F32 ? 4 : 2) > kLastCacheBytes;
-#define QQQ_LP(T, U, PAST) hipLaunchKernelGGL((logprobs_kernel<F32, T, U, PAST>), dim3((unsigned)M), dim3(T), 0, st, p)
+#define QQQ_LP(T, U, PAST, TRACK) hipLaunchKernelGGL((logprobs_kernel<F32, T, U, PAST, TRACK>), dim3((unsigned)M), dim3(T), 0, st, p)
     // Threads a row, us (256 / 512 / 1024): a row a CU or less 400 KB 35.9 / 20.9 / 17.5 (100 rows, top 20), 130 KB 12.7 / 10.8 / 11.5, 32 KB 7.8 / 7.5 / 8.1; many rows 40 KB 62 / 87 / 180
     // (8000 rows, top 5), 256 KB 248 / 203 / 190 (4096 rows, top 20), 166 / 161 / 167 (top 1); 777 rows of 131 KB, sums only, 24.8 / 26.6 / 31.0
     const int64_t bytes = (int64_t)p.V * (F32 ? 4 : 2);
-    if (M <= num_cus() && bytes >= 384 << 10) QQQ_LP(1024, 4, false);
-    else if (M <= num_cus()) QQQ_LP(512, 4, false);
+    if (M <= num_cus() && bytes >= 384 << 10) QQQ_LP(1024, 4, false, false);
+    else if (M <= num_cus()) QQQ_LP(512, 4, false, false);
+    // (TRACK, us without / with: 4096 rows of 256 KB, top 4 167 / 165, 8 172 / 166, 20 195 / 171, 64 276 / 183; of 128 KB, top 8 90 / 91, 20 99 / 93; 2100 rows of 80 KB, top 20
+    // 40 / 43, 64 49 / 48)
+    else if (bytes > 64 << 10 && p.top * bytes >= 1800 << 10)
+      if (past) QQQ_LP(512, 2, true, true);
+      else QQQ_LP(512, 2, false, true);
     else if (bytes > 64 << 10 && (p.top > 0 || M >= 8 * num_cus()))
-      if (past) QQQ_LP(512, 2, true);
-      else QQQ_LP(512, 2, false);
-    else if (past) QQQ_LP(256, 2, true);
-    else QQQ_LP(256, 2, false);
+      if (past) QQQ_LP(512, 2, true, false);
+      else QQQ_LP(512, 2, false, false);
+    else if (past) QQQ_LP(256, 2, true, false);
+    else QQQ_LP(256, 2, false, false);
 #undef QQQ_LP
   } else {
     p.splits = s.parts;
