@@ -48,7 +48,7 @@ typedef struct qqq_kv8_sessions {
  *   lacking [1] int32: pages that were wanted and not there.  Their entries are -1, which is no page: append drops what it would write to them, so a program
  *   gives up or repeats that step's last sequences.  One that admits no more than free_count covers never sees it.
  * batch is a qqq_kv8_batch as the calls of qqq_layer.h take it, its tensors written here.  page_table may be sessions->pages itself (with its stride) where slots is NULL;
- * no other outputs may overlap.  max_len / page_tokens <= columns of both tables.  A session that does not exist brings nothing; one that is there twice, or held and free_count
+ * no other outputs may overlap.  max_len / page_tokens <= columns of both tables; sequences < 2^24.  A session that does not exist brings nothing; one that is there twice, or held and free_count
  * that are out of bounds, give wrong tables, never an access outside.
  *   workspace: qqq_kv8_plan_workspace_bytes() bytes, 4-byte aligned, contents irrelevant on entry; not shared by calls that may run concurrently.
  */
@@ -66,7 +66,7 @@ int qqq_kv8_release(const qqq_kv8_sessions* sessions, const int32_t* ids, int64_
 /*
  * Weights in 8 bits.  Codes and scales of fp16 weights [N,K] are what qqq_quant_act gives for them, a row for an output channel: symmetric, codes in
  * [-127,127], one fp32 scale a channel.
- *   w_codes [N,ldw] int8, 16-byte aligned, ldw >= K, ldw % 16 == 0.  N >= 1, K % 128 == 0, 128 <= K <= 131072.
+ *   w_codes [N,ldw] int8, 16-byte aligned, ldw >= K, ldw % 16 == 0.  1 <= N <= 2^24, K % 128 == 0, 128 <= K <= 131072, N K <= 2^35.
  *   w_packed: qqq_packed_w8_bytes(N,K) = K * (N rounded up to 16) bytes, opaque device tile layout, 16-byte aligned: 2 KiB chunks of 16 channels x 128 k in the order of
  *   the matrix instruction's operands; channels past N are zeros.  qqq_unpack_w8 is the exact inverse ([N,K], dense).
  */
@@ -78,7 +78,7 @@ int qqq_unpack_w8(const void* w_packed, int64_t N, int64_t K, int8_t* w_codes, v
  * W8A8 GEMM:  acc[m,n] = sum_k a_q[m,k] * w[n,k]  (int32, exact),  t = fp32_rne(float(acc) * s_a[m]),
  *   y[m,n] = fp16_rne(t * s_w[n])  or  fp32_rne(t * s_w[n])  by y_type.
  *   a_q [M,K] int8, dense, 16-byte aligned, codes in [-127,127]; s_a [M] fp32; w_packed as above; s_w [N] fp32; y [M,ldy] of the type, ldy >= N, aligned to its type;
- *   acc_out [M,N] int32 dense or NULL (parity/debug).  1 <= N <= 2^24, K as above, M == 0 is a no-op.
+ *   acc_out [M,N] int32 dense or NULL (parity/debug).  N and K as above, M <= 2^30, M == 0 is a no-op.
  *   workspace: qqq_gemm_w8a8_workspace_bytes() bytes, 16-byte aligned (partial sums of calls that split K; 0 where none is needed), contents irrelevant on entry;
  *   not shared by calls that may run concurrently.
  */
@@ -96,7 +96,7 @@ int qqq_gemm_w8a8(const int8_t* a_q, const float* s_a, const void* w_packed, con
  * A logit of -infinity is masked: its probability is 0 and it adds nothing to the entropy.  A row of nothing else gives lse = -infinity, entropy 0 and log probabilities of
  * -infinity.  A row with a NaN or +infinity gives NaN in all its numbers; among the top tokens NaN counts as larger than everything.  A token below 0 is none: its logprob is 0,
  * whatever the row holds; one past V - 1 gives NaN.  All sums are fp32, relative to the largest logit.
- *   logits [M,ld] fp16 or fp32 by type, aligned to it, ld >= V; 1 <= V < 2^30; tokens [M] int32 or NULL (then logprob is NULL); 0 <= top <= QQQ_MAX_TOP, top_tokens [M,top] int32
+ *   logits [M,ld] fp16 or fp32 by type, aligned to it, ld >= V; 1 <= V < 2^30, M < 2^24; tokens [M] int32 or NULL (then logprob is NULL); 0 <= top <= QQQ_MAX_TOP, top_tokens [M,top] int32
  *   and top_logprobs [M,top] fp32 where top > 0; logprob, entropy, lse [M] fp32, each may be NULL.
  *   workspace: qqq_logprobs_workspace_bytes() bytes, 16-byte aligned (0 where rows are not split over workgroups), contents irrelevant on entry; not shared by calls
  *   that may run concurrently.

@@ -300,7 +300,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void w8_tile_kernel(const W8Params
   w8_write<TM, TN, OUT>(p, acc, m0 + wm * TM * 16, tn * S::kBN + wn * TN * 16, split, lds + wave * S::kOutWave);
 }
 
-// Second launch of a call that splits K: the parts' sums, four channels a thread
+// Second launch of a call that splits K: the parts' sums, an output a thread
 __global__ __launch_bounds__(256) void w8_sum_kernel(const W8Params p) {
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, slab = (int64_t)p.M * p.N;
   if (i >= slab) return;
@@ -314,7 +314,7 @@ template <int WM, int WN, int TM, int TN, int NB, bool FULL>
 int launch_tile(const W8Params& p, hipStream_t st) {
   using S = W8Shape<WM, WN, TM, TN, NB, FULL>;
   const int tiles_m = (p.M + S::kBM - 1) / S::kBM, tiles_n = (p.N + S::kBN - 1) / S::kBN;
-  if ((int64_t)tiles_m * tiles_n > 0x7FFFFFFF) return set_error(QQQ_ERR_SHAPE, "w8a8: too many output tiles for one launch");
+  if ((int64_t)tiles_m * tiles_n * (S::kWaves * 64) > 0xFFFFFFFFll) return set_error(QQQ_ERR_SHAPE, "w8a8: too many output tiles for one launch");
   const dim3 grid((unsigned)(tiles_m * tiles_n), (unsigned)p.k_splits), block(S::kWaves * 64);
   if (p.k_splits > 1) hipLaunchKernelGGL((w8_tile_kernel<WM, WN, TM, TN, NB, FULL, kPart>), grid, block, 0, st, p, tiles_m, tiles_n);
   else if (p.f32) hipLaunchKernelGGL((w8_tile_kernel<WM, WN, TM, TN, NB, FULL, kF32>), grid, block, 0, st, p, tiles_m, tiles_n);
@@ -404,7 +404,7 @@ W8Plan w8_plan(int64_t M, int64_t N, int64_t K) {
   }
   if (g_shape > 0 && (g_shape != kW8Few || M <= kW8FewRows)) best.shape = g_shape;
   if (g_shape > 0) best.k_splits = 1;
-  if (g_k_splits > 0) best.k_splits = (int)(g_k_splits < K / 128 ? g_k_splits : K / 128);
+  if (g_k_splits > 0 && M * N <= 1 << 30) best.k_splits = (int)(g_k_splits < K / 128 ? g_k_splits : K / 128);
   return best;
 }
 

@@ -11,7 +11,8 @@ int launch_logprobs(const void* logits, int64_t ld, int type, int64_t M, int64_t
 
 namespace {
 
-constexpr int64_t kMost = 1 << 30;  // tokens of a sequence, rows of a call, pages: places stay in 32 bits
+constexpr int64_t kMost = 1 << 30;      // tokens of a sequence, rows of a call, pages: places stay in 32 bits
+constexpr int64_t kMostGroups = (1 << 24) - 1;  // workgroups of 256 threads: a launch takes fewer than 2^32 threads
 
 bool aligned(const void* p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 
@@ -34,7 +35,7 @@ int check_session_pointers(const char* name, const qqq_kv8_sessions* s) {
 int check_plan(const char* name, const qqq_kv8_sessions* s, const qqq_kv8_batch* b) {
   if (int rc = check_sessions(name, s)) return rc;
   if (!b) return set_error(QQQ_ERR_NULL, "%s: NULL struct", name);
-  if (b->sequences < 0 || b->max_new < 0 || b->max_new > kMost || b->max_len < 0 || b->max_len > kMost || b->columns < 0 || b->table_stride < b->columns ||
+  if (b->sequences < 0 || b->sequences > kMostGroups || b->max_new < 0 || b->max_new > kMost || b->max_len < 0 || b->max_len > kMost || b->columns < 0 || b->table_stride < b->columns ||
       b->max_len / s->page_tokens > b->columns || b->max_len / s->page_tokens > s->columns)
     return set_error(QQQ_ERR_SHAPE, "%s: unsupported batch: %d sequences, at most %d new of %d tokens, %d page columns of stride %lld (the sessions' table: %d)", name,
                      b->sequences, b->max_new, b->max_len, b->columns, (long long)b->table_stride, s->columns);
@@ -75,13 +76,13 @@ PlanArgs plan_args(const qqq_kv8_sessions* s, const qqq_kv8_batch* b) {
 constexpr int64_t kMostK = 131072, kMostN = 1 << 24;  // 127 * 127 * K stays below 2^31
 
 int check_product(const char* name, int64_t N, int64_t K) {
-  if (N < 1 || N > kMostN || K < 128 || K % 128 != 0 || K > kMostK)
-    return set_error(QQQ_ERR_SHAPE, "%s: unsupported N=%lld K=%lld (need 1 <= N <= 2^24, K%%128==0, 128 <= K <= 131072)", name, (long long)N, (long long)K);
+  if (N < 1 || N > kMostN || K < 128 || K % 128 != 0 || K > kMostK || N * K > 1ll << 35)
+    return set_error(QQQ_ERR_SHAPE, "%s: unsupported N=%lld K=%lld (need 1 <= N <= 2^24, K%%128==0, 128 <= K <= 131072, N K <= 2^35)", name, (long long)N, (long long)K);
   return QQQ_OK;
 }
 
 int check_logits(const char* name, int64_t M, int64_t V, int type) {
-  if (M < 0 || M > 0x7FFFFFFF || V < 1 || V >= kMost) return set_error(QQQ_ERR_SHAPE, "%s: unsupported %lld rows of %lld logits", name, (long long)M, (long long)V);
+  if (M < 0 || M > kMostGroups || V < 1 || V >= kMost) return set_error(QQQ_ERR_SHAPE, "%s: unsupported %lld rows of %lld logits", name, (long long)M, (long long)V);
   if (type != QQQ_LOGITS_FP16 && type != QQQ_LOGITS_FP32) return set_error(QQQ_ERR_SHAPE, "%s: logits of type %d", name, type);
   return QQQ_OK;
 }
@@ -163,7 +164,7 @@ int qqq_unpack_w8(const void* w_packed, int64_t N, int64_t K, int8_t* w_codes, v
 }
 
 size_t qqq_gemm_w8a8_workspace_bytes(int64_t M, int64_t N, int64_t K) {
-  if (check_product("qqq_gemm_w8a8_workspace_bytes", N, K) || M < 1 || M > 0x7FFFFFFF) return 0;
+  if (check_product("qqq_gemm_w8a8_workspace_bytes", N, K) || M < 1 || M > kMost) return 0;
   const W8Plan plan = w8_plan(M, N, K);
   return plan.k_splits > 1 ? (size_t)plan.k_splits * M * N * sizeof(int32_t) : 0;
 }
@@ -172,7 +173,7 @@ int qqq_gemm_w8a8(const int8_t* a_q, const float* s_a, const void* w_packed, con
                   int64_t N, int64_t K, void* workspace, size_t workspace_bytes, void* stream) {
   const char* name = "qqq_gemm_w8a8";
   if (int rc = check_product(name, N, K)) return rc;
-  if (M < 0 || M > 0x7FFFFFFF) return set_error(QQQ_ERR_SHAPE, "%s: M=%lld", name, (long long)M);
+  if (M < 0 || M > kMost) return set_error(QQQ_ERR_SHAPE, "%s: M=%lld", name, (long long)M);
   if (y_type != QQQ_OUT_FP16 && y_type != QQQ_OUT_FP32) return set_error(QQQ_ERR_SHAPE, "%s: outputs of type %d", name, y_type);
   if (ldy < N) return set_error(QQQ_ERR_SHAPE, "%s: row stride %lld for %lld outputs", name, (long long)ldy, (long long)N);
   if (M == 0) return QQQ_OK;

@@ -211,6 +211,31 @@ def test_two_servers_on_two_streams():
             assert torch.equal(x, y)
 
 
+def test_calls_without_the_native_marshalling(monkeypatch):
+    """The same through ctypes, as tensors that the native marshalling leaves to Python go."""
+    ids = _i32(np.random.default_rng(8).integers(0, SHAPE["vocabulary"], 40))
+    new, targets = _i32([20, 3, 17]), ids.roll(-1)
+
+    def run():
+        server = _server(3, 64, seed=6, page_tokens=16)
+        step = server.new_step(40, 20, _i32([2, 0, 1]))
+        step.ids.copy_(ids)
+        step.new.copy_(new)
+        out = server(step, targets, top=6)
+        sequence = torch.full((40,), -1, dtype=torch.int32, device="cuda")
+        before = server.sessions.held.clone()
+        after = (before.clone(), server.sessions.free_count.clone())
+        qqq.qqq_kv8_plan(server.sessions, step.batch, new, 16, sequence, after=after)     # (again, to other places)
+        assert torch.equal(server.sessions.held, before)
+        return [*out, *after, sequence, *step.batch[:3], server.sessions.pages, server.sessions.free]
+
+    native = run()
+    for name in ("_native_plan", "_native_w8a8", "_native_logprobs"):
+        monkeypatch.setattr(qqq, name, lambda *a: None)
+    for i, (a, b) in enumerate(zip(native, run())):
+        assert torch.equal(a, b), i
+
+
 def test_the_program_runs(capsys):
     serving.main()
     said = capsys.readouterr().out

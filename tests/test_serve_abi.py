@@ -56,7 +56,7 @@ def test_plan_refusals(L):
     for missing in ("pages", "held", "held_after", "free_pages", "free_count", "free_count_after"):
         assert _plan(L, _sessions(**{missing: None}), _batch()) == NULL, missing
     for bad in (dict(sequences=-1), dict(max_new=-1), dict(max_new=(1 << 30) + 1), dict(max_len=-1), dict(max_len=5 * 32), dict(columns=-1), dict(table_stride=3), dict(columns=3),
-                dict(sequences=4), dict(page_table=0x2002), dict(kv_len=0x1001), dict(cu=0x1002), dict(slots=0x1002),
+                dict(sequences=4), dict(sequences=1 << 24, slots=0x1000), dict(page_table=0x2002), dict(kv_len=0x1001), dict(cu=0x1002), dict(slots=0x1002),
                 dict(page_table=0x1000, slots=0x1000), dict(page_table=0x1000, table_stride=5)):    # the last two: the sessions' own table with slots, with another stride
         assert _plan(L, _sessions(), _batch(**bad)) == SHAPE, bad
     for missing in ("page_table", "kv_len", "cu"):
@@ -99,7 +99,7 @@ def test_logprobs_refusals(L):
         return L.qqq_logprobs(x, ld, kind, M, V, tokens, top, logprob, entropy, lse, top_tokens, top_logprobs, work, nbytes, None)
     odd = ctypes.c_void_p(0x1002)
     assert call(M=0) == 0
-    for bad in (dict(M=-1), dict(V=0), dict(V=1 << 30, ld=1 << 30), dict(ld=99), dict(kind=2), dict(kind=-1), dict(top=-1), dict(top=65), dict(x=ctypes.c_void_p(0x1001)),
+    for bad in (dict(M=-1), dict(M=1 << 24), dict(V=0), dict(V=1 << 30, ld=1 << 30), dict(ld=99), dict(kind=2), dict(kind=-1), dict(top=-1), dict(top=65), dict(x=ctypes.c_void_p(0x1001)),
                 dict(x=odd, kind=1), dict(tokens=odd), dict(logprob=odd), dict(entropy=odd), dict(lse=odd), dict(top_tokens=odd), dict(top_logprobs=odd), dict(work=ctypes.c_void_p(0x1008))):
         assert call(**bad) == SHAPE, bad
     for missing in ("x", "tokens", "logprob", "top_tokens", "top_logprobs"):
@@ -123,7 +123,7 @@ def test_product_refusals(L):
         return L.qqq_gemm_w8a8(a, s_a, w, s_w, y, kind, ldy, acc, M, N, K, work, nbytes, None)
     odd = ctypes.c_void_p(0x1002)
     assert call(M=0) == 0
-    for bad in (dict(M=-1), dict(N=0), dict(N=(1 << 24) + 1, ldy=1 << 25), dict(K=200), dict(K=0), dict(K=131072 + 128), dict(kind=2), dict(kind=-1), dict(ldy=99), dict(a=ctypes.c_void_p(0x1008)),
+    for bad in (dict(M=-1), dict(M=(1 << 30) + 1), dict(N=0), dict(N=1 << 24, K=2176, ldy=1 << 25), dict(N=(1 << 24) + 1, ldy=1 << 25), dict(K=200), dict(K=0), dict(K=131072 + 128), dict(kind=2), dict(kind=-1), dict(ldy=99), dict(a=ctypes.c_void_p(0x1008)),
                 dict(w=ctypes.c_void_p(0x1008)), dict(s_a=odd), dict(s_w=odd), dict(y=ctypes.c_void_p(0x1001)), dict(y=odd, kind=1), dict(acc=odd), dict(work=ctypes.c_void_p(0x1008))):
         assert call(**bad) == SHAPE, bad
     for missing in ("a", "s_a", "w", "s_w", "y"):
@@ -139,7 +139,7 @@ def test_product_refusals(L):
 
 
 def test_packing_refusals(L):
-    assert L.qqq_packed_w8_bytes(17, 256) == 32 * 256 and L.qqq_packed_w8_bytes(0, 256) == 0 and L.qqq_packed_w8_bytes(16, 200) == 0
+    assert L.qqq_packed_w8_bytes(17, 256) == 32 * 256 and L.qqq_packed_w8_bytes(0, 256) == 0 and L.qqq_packed_w8_bytes(1 << 24, 2176) == 0 and L.qqq_packed_w8_bytes(16, 200) == 0
     other = ctypes.c_void_p(0x2000)
     assert L.qqq_pack_w8(BAD, 16, 256, 255, other, None) == SHAPE and L.qqq_pack_w8(BAD, 16, 256, 264, other, None) == SHAPE and L.qqq_pack_w8(BAD, 16, 256, 256, BAD, None) == SHAPE
     assert L.qqq_pack_w8(None, 16, 256, 256, other, None) == NULL and L.qqq_pack_w8(BAD, 16, 256, 256, None, None) == NULL
