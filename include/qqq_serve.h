@@ -50,7 +50,7 @@ typedef struct qqq_kv8_sessions {
  * batch is a qqq_kv8_batch as the calls of qqq_layer.h take it, its tensors written here.  page_table may be sessions->pages itself (with its stride) where slots is NULL;
  * no other outputs may overlap.  max_len / page_tokens <= columns of both tables; sequences < 2^24.  A session that does not exist brings nothing; one that is there twice, or held and free_count
  * that are out of bounds, give wrong tables, never an access outside.
- *   workspace: qqq_kv8_plan_workspace_bytes() bytes, 4-byte aligned, contents irrelevant on entry; not shared by calls that may run concurrently.
+ *   workspace: qqq_kv8_plan_workspace_bytes() bytes (of the call with these pointers: most calls with held_after and free_count_after of their own need none), 4-byte aligned, contents irrelevant on entry; not shared by calls that may run concurrently.
  */
 size_t qqq_kv8_plan_workspace_bytes(const qqq_kv8_sessions* sessions, const qqq_kv8_batch* batch);
 int qqq_kv8_plan(const qqq_kv8_sessions* sessions, const qqq_kv8_batch* batch, const int32_t* new_tokens, int64_t tokens,

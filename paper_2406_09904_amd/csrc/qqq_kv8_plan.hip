@@ -2,9 +2,10 @@
 //
 // Sequence b brings n_b tokens: cu is the sequences' prefix sum of n_b, and the places of its fresh pages in the stack are a prefix sum of
 // fresh_b = len_b / P - held_b / P.  Both sums saturate at 2^30 (no count that is used passes it), so they stay in 32 bits whatever the tensors hold.
-// One workgroup makes the sums, in registers by lane moves; the tables' entries and the rows' places are then copies, 8 bytes moved for each.  What
-// bounds it: for few sequences the time that a launch and three dependent reads take (ids, held, entries: 2.4 us for one sequence, 4.2 for 64 of 125
-// entries); for many the sums' one workgroup (2048 sequences: 5.7 us) and the copies (2048 tables of about 1000 entries, 17 MB: 6.1 us).
+// The sums are made in registers by lane moves; the tables' entries and the rows' places are then copies, 8 bytes moved for each.  A workgroup may fill what its sums tell only where
+// no other still reads what it writes: held_after in place asks for one workgroup, or for a launch of its own for the sums.
+// What bounds it: up to 1024 sequences the time that a launch and four dependent reads take (ids, held, entries, the stack: 2.1 us for one sequence, 2.7 for 64 of 125 entries, 4.2
+// for 200 of 1000); for more the sums' one workgroup (2048 sequences: 5.7 us) and the copies (2048 tables of about 1000 entries, 17 MB: 6.1 us).
 #include <algorithm>
 
 #include "qqq_plan.h"
@@ -30,20 +31,20 @@ __device__ __forceinline__ int wave_inclusive_sum(int v) {
   return v;
 }
 
-// Sum of the values of the threads before this one, and of all, saturating.  ONE_WAVE: only the first wave has any, and only it has the results.
-template <bool ONE_WAVE>
+// Sum of the values of the T threads before this one, and of all, saturating.  T of 64: of a wave, without a barrier.
+template <int T>
 __device__ __forceinline__ int block_exclusive_sum(int v, int* smem, int& total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int sum = wave_inclusive_sum(v);
   int before = __builtin_amdgcn_update_dpp(0, sum, 0x138, 0xF, 0xF, false);  // wave_shr:1
-  if constexpr (ONE_WAVE) {
+  if constexpr (T == 64) {
     total = __builtin_amdgcn_readlane(sum, 63);
     return before;
   }
   if (lane == 63) smem[wave] = sum;
   __syncthreads();
   // the waves' sums the same way, in each of them
-  const int waves = wave_inclusive_sum(lane < kScanThreads / 64 ? smem[lane] : 0);
+  const int waves = wave_inclusive_sum(lane < T / 64 ? smem[lane] : 0);
   total = __builtin_amdgcn_readlane(waves, 63);
   if (wave > 0) before = add_saturating(before, __builtin_amdgcn_readlane(waves, wave - 1));
   __syncthreads();
@@ -84,95 +85,129 @@ __device__ __forceinline__ void fill(const PlanArgs& p, int b, const Sequence& s
     for (int64_t i = from; i < n; i += step) p.positions[s.row + i] = s.held + (int)i;
 }
 
-// The sums, kEach consecutive sequences a thread.  ONE_WAVE: up to 64 sequences, one a lane of the first wave, so without a barrier.  FILL (with
-// ONE_WAVE): the tables and rows too, by all waves.
-template <bool FILL, bool ONE_WAVE>
-__global__ __launch_bounds__(kScanThreads) void kv8_plan_kernel(const PlanArgs p) {
-  constexpr int kEach = ONE_WAVE ? 1 : 4;
-  __shared__ int smem[kScanThreads / 64];
-  __shared__ Sequence seqs[FILL ? 64 : 1];
+// The sums over sequences 0 .. until - 1 by T threads, kEach consecutive sequences each: met(b, its numbers) for all of them, in the thread that has it.
+struct Totals {
+  int rows = 0, taken = 0;
+};
+template <int T, int kEach, class Met>
+__device__ __forceinline__ Totals make_sums(const PlanArgs& p, int64_t until, int* smem, Met met) {
+  const int tid = threadIdx.x, count = min(max(*p.free_count, 0), p.pool);
+  Totals sum;  // of the sequences before this turn's
+  for (int64_t first = 0; first < until; first += T * kEach) {
+    int session[kEach], held[kEach], n[kEach], all_n = 0;
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+      const int64_t b = first + (int64_t)tid * kEach + e;
+      session[e] = b >= until ? -1 : p.ids ? p.ids[b] : (int)b;
+      n[e] = b >= until ? 0 : p.new_tokens[b];
+      if ((uint32_t)session[e] >= (uint32_t)p.sessions) session[e] = -1;
+    }
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+      held[e] = session[e] >= 0 ? min(max(p.held[session[e]], 0), p.max_len) : 0;
+      n[e] = session[e] >= 0 ? min(min(max(n[e], 0), p.max_new), p.max_len - held[e]) : 0;
+      all_n = add_saturating(all_n, n[e]);
+    }
+    int all;
+    int row = add_saturating(sum.rows, block_exclusive_sum<T>(all_n, smem, all));
+    sum.rows = add_saturating(sum.rows, all);
+    int row_of[kEach], fresh[kEach], all_fresh = 0;
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+      row_of[e] = min(row, p.tokens);
+      row = add_saturating(row, n[e]);
+      n[e] = min(n[e], p.tokens - row_of[e]);  // rows that the step's tensors do not have are not taken
+      fresh[e] = (held[e] + n[e] >> p.shift) - (held[e] >> p.shift);
+      all_fresh = add_saturating(all_fresh, fresh[e]);
+    }
+    int before = add_saturating(sum.taken, block_exclusive_sum<T>(all_fresh, smem, all));
+    sum.taken = add_saturating(sum.taken, all);
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+      const int64_t b = first + (int64_t)tid * kEach + e;
+      if (b < until) met(b, Sequence{session[e], held[e], held[e] + n[e], row_of[e], count - before});
+      before = add_saturating(before, fresh[e]);
+    }
+  }
+  return sum;
+}
+__device__ __forceinline__ void write_sequence(const PlanArgs& p, int64_t b, const Sequence& s) {
+  p.kv_len[b] = s.len;
+  p.cu[b] = s.row;
+  if (s.session >= 0) p.held_after[s.session] = s.len;
+}
+__device__ __forceinline__ void write_totals(const PlanArgs& p, const Totals& sum) {
+  const int count = min(max(*p.free_count, 0), p.pool);
+  p.cu[p.sequences] = min(sum.rows, p.tokens);
+  *p.free_count_after = max(count - sum.taken, 0);
+  if (p.lacking) *p.lacking = max(sum.taken - count, 0);
+}
+
+// Few sequences and entries: all by one workgroup, the sums by its first wave
+__global__ __launch_bounds__(kScanThreads) void kv8_plan_small_kernel(const PlanArgs p) {
+  __shared__ Sequence seqs[64];
   const int tid = threadIdx.x;
   // as many threads for a sequence's tables as there are, a wave at least
-  const int lanes = !FILL ? 0 : p.sequences <= 1 ? kScanThreads : max(64, kScanThreads >> (32 - __clz(p.sequences - 1)));
-  // One wave's sequences: a group of threads has up to four of them, and their first entries are on their way before the sums are known
-  constexpr int kMine = FILL ? 4 : 1, kEarly = 2;
-  int early[kMine][kEarly];
-  if constexpr (FILL) {
-    int session[kMine];
+  const int lanes = p.sequences <= 1 ? kScanThreads : max(64, kScanThreads >> (32 - __clz(p.sequences - 1)));
+  // A group of threads has up to four sequences, and their first entries are on their way before the sums are known
+  constexpr int kMine = 4, kEarly = 2;
+  int early[kMine][kEarly], session[kMine];
 #pragma unroll
-    for (int i = 0; i < kMine; ++i) {
-      const int b = tid / lanes + kScanThreads / lanes * i;
-      session[i] = b >= p.sequences ? -1 : p.ids ? p.ids[b] : b;
-    }
-#pragma unroll
-    for (int i = 0; i < kMine; ++i)
-#pragma unroll
-      for (int e = 0; e < kEarly; ++e) {
-        const int j = tid % lanes + lanes * e;
-        early[i][e] = 0;
-        if ((uint32_t)session[i] < (uint32_t)p.sessions && j < p.columns && !p.same_table) early[i][e] = p.pages[(int64_t)session[i] * p.pages_stride + j];
-      }
+  for (int i = 0; i < kMine; ++i) {
+    const int b = tid / lanes + kScanThreads / lanes * i;
+    session[i] = b >= p.sequences ? -1 : p.ids ? p.ids[b] : b;
   }
-  const int count = min(max(*p.free_count, 0), p.pool);
-  int rows = 0, taken = 0;  // of the sequences before this turn's
-  if (!ONE_WAVE || tid < 64) {
-    for (int64_t first = 0; first < p.sequences; first += kScanThreads * kEach) {
-      int session[kEach], held[kEach], n[kEach], all_n = 0;
 #pragma unroll
-      for (int e = 0; e < kEach; ++e) {
-        const int64_t b = first + (int64_t)tid * kEach + e;
-        session[e] = b >= p.sequences ? -1 : p.ids ? p.ids[b] : (int)b;
-        n[e] = b >= p.sequences ? 0 : p.new_tokens[b];
-        if ((uint32_t)session[e] >= (uint32_t)p.sessions) session[e] = -1;
-      }
+  for (int i = 0; i < kMine; ++i)
 #pragma unroll
-      for (int e = 0; e < kEach; ++e) {
-        held[e] = session[e] >= 0 ? min(max(p.held[session[e]], 0), p.max_len) : 0;
-        n[e] = session[e] >= 0 ? min(min(max(n[e], 0), p.max_new), p.max_len - held[e]) : 0;
-        all_n = add_saturating(all_n, n[e]);
-      }
-      int all;
-      int row = add_saturating(rows, block_exclusive_sum<ONE_WAVE>(all_n, smem, all));
-      rows = add_saturating(rows, all);
-      int row_of[kEach], fresh[kEach], all_fresh = 0;
-#pragma unroll
-      for (int e = 0; e < kEach; ++e) {
-        row_of[e] = min(row, p.tokens);
-        row = add_saturating(row, n[e]);
-        n[e] = min(n[e], p.tokens - row_of[e]);  // rows that the step's tensors do not have are not taken
-        fresh[e] = (held[e] + n[e] >> p.shift) - (held[e] >> p.shift);
-        all_fresh = add_saturating(all_fresh, fresh[e]);
-      }
-      int before = add_saturating(taken, block_exclusive_sum<ONE_WAVE>(all_fresh, smem, all));
-      taken = add_saturating(taken, all);
-#pragma unroll
-      for (int e = 0; e < kEach; ++e) {
-        const int64_t b = first + (int64_t)tid * kEach + e;
-        if (b < p.sequences) {
-          const int len = held[e] + n[e];
-          p.kv_len[b] = len;
-          p.cu[b] = row_of[e];
-          if (session[e] >= 0) p.held_after[session[e]] = len;
-          if constexpr (FILL) seqs[tid] = Sequence{session[e], held[e], len, row_of[e], count - before};
-          else p.top[b] = count - before;
-        }
-        before = add_saturating(before, fresh[e]);
-      }
+    for (int e = 0; e < kEarly; ++e) {
+      const int j = tid % lanes + lanes * e;
+      early[i][e] = 0;
+      if ((uint32_t)session[i] < (uint32_t)p.sessions && j < p.columns && !p.same_table) early[i][e] = p.pages[(int64_t)session[i] * p.pages_stride + j];
     }
-    if (tid == 0) {
-      p.cu[p.sequences] = min(rows, p.tokens);
-      *p.free_count_after = max(count - taken, 0);
-      if (p.lacking) *p.lacking = max(taken - count, 0);
-    }
+  if (tid < 64) {
+    const Totals sum = make_sums<64, 1>(p, p.sequences, nullptr, [&](int64_t b, const Sequence& s) {
+      write_sequence(p, b, s);
+      seqs[b] = s;
+    });
+    if (tid == 0) write_totals(p, sum);
   }
-  if constexpr (FILL) {
-    __syncthreads();
+  __syncthreads();
 #pragma unroll
-    for (int i = 0; i < kMine; ++i) {
-      const int b = tid / lanes + kScanThreads / lanes * i;
-      if (b < p.sequences) fill<kEarly>(p, b, seqs[b], tid % lanes, lanes, early[i]);
-    }
+  for (int i = 0; i < kMine; ++i) {
+    const int b = tid / lanes + kScanThreads / lanes * i;
+    if (b < p.sequences) fill<kEarly>(p, b, seqs[b], tid % lanes, lanes, early[i]);
   }
+}
+
+// More: the sums by one workgroup of T threads, then the fill kernel
+template <int T>
+__global__ __launch_bounds__(T) void kv8_plan_sums_kernel(const PlanArgs p) {
+  __shared__ int smem[T / 64];
+  const Totals sum = make_sums<T, T == 64 ? 1 : 4>(p, p.sequences, smem, [&](int64_t b, const Sequence& s) {
+    write_sequence(p, b, s);
+    p.top[b] = s.top;
+  });
+  if (threadIdx.x == 0) write_totals(p, sum);
+}
+
+// Where what holds after the step goes to other memory, so that held and the stack's height stay as they are: one launch, in which each workgroup makes the sums up to its
+// sequence by itself (T of its threads do)
+template <int T>
+__global__ __launch_bounds__(kFillThreads) void kv8_plan_each_kernel(const PlanArgs p) {
+  __shared__ int smem[T / 64];
+  __shared__ Sequence mine;
+  const int64_t b = blockIdx.x;
+  if (T == kFillThreads || threadIdx.x < T) {
+    const Totals sum = make_sums<T, T == 64 ? 1 : 4>(p, b + 1, smem, [&](int64_t i, const Sequence& s) {
+      if (i < b) return;
+      mine = s;
+      if (blockIdx.y == 0) write_sequence(p, b, s);
+    });
+    if (blockIdx.y == 0 && b == p.sequences - 1 && threadIdx.x == 0) write_totals(p, sum);
+  }
+  __syncthreads();
+  fill(p, (int)b, mine, (int64_t)blockIdx.y * kFillThreads + threadIdx.x, (int64_t)gridDim.y * kFillThreads);
 }
 
 // The tables and rows of many sequences, gridDim.y workgroups for each
@@ -219,7 +254,7 @@ __global__ __launch_bounds__(kScanThreads) void kv8_release_kernel(const PlanArg
     }
     __syncthreads();
     int all;
-    const int before = block_exclusive_sum<false>(tid < here ? pages_of[tid] : 0, smem, all);
+    const int before = block_exclusive_sum<kScanThreads>(tid < here ? pages_of[tid] : 0, smem, all);
     if (tid < here) pages_of[tid] = add_saturating(count, before);
     __syncthreads();
     for (int i = wave; i < here; i += kWaves) {
@@ -239,12 +274,18 @@ __global__ __launch_bounds__(kScanThreads) void kv8_release_kernel(const PlanArg
   if (tid == 0) *p.free_count_after = count;
 }
 
-// One launch while a single workgroup moves the entries and rows about as soon as a second launch would.  Measured in a graph, us with one launch and
-// with two: one sequence of 1 entry 2.4 and 3.4, of 4096 3.1 and 4.2, of 16384 5.8 and 4.3; 37 of 256 4.9 and 4.2; 64 of 16 4.2 and 4.2, of 1024 16.7
-// and 4.5.  Outside a graph a second launch also costs the host 2 us.  More than 64 sequences, whose sums take barriers, are behind in one launch at
-// every length (200 of one entry 6.0 and 5.4, 1024 of one 21 and 6.2).
-bool in_one_launch(const PlanArgs& p) {
-  return p.sequences <= 64 && (int64_t)p.sequences * ((p.max_len >> p.shift) + (int64_t)p.max_new) <= kPlanOneLaunch;
+// What holds afterwards in other memory: a workgroup a sequence, up to 1024 of them (a turn of 256 threads; each reads what all before it hold).  us in a graph, this and two
+// launches: one sequence of one entry 2.1 and 3.4, of 16384 2.8 and 4.4; 64 of 128 2.7 and 4.2, of 4096 3.1 and 4.7; 200 of 1024 4.2 and 6.4; 1000 of 128 4.9 and 6.9, of 4096 11.1 and
+// 11.0; 1500 of 128 7.8 and 7.5; 2500 of 128 13 and 9.
+bool each_by_itself(const PlanArgs& p) {
+  return p.sequences > 0 && p.sequences <= 4 * kFillThreads && p.held_after != p.held && p.free_count_after != p.free_count;
+}
+// In place, where a workgroup's sums must be there before another's are written: one workgroup while it moves the entries and rows about as soon as a second launch would.  Measured in
+// a graph, us with one launch and with two: one sequence of 1 entry 2.4 and 3.4, of 4096 3.1 and 4.2, of 16384 5.8 and 4.3; 37 of 256 4.9 and 4.2; 64 of 16 4.2 and 4.2, of 1024 16.7
+// and 4.5.  Outside a graph a second launch also costs the host 2 us.  More than 64 sequences, whose sums take barriers, are behind in one workgroup at every length (200 of one
+// entry 6.0 and 5.4, 1024 of one 21 and 6.2).
+bool in_one_workgroup(const PlanArgs& p) {
+  return p.sequences <= 64 && (int64_t)p.sequences * ((p.max_len >> p.shift) + (int64_t)p.max_new) <= kPlanSmall;
 }
 
 int launched(const char* what, const char* name) {
@@ -256,19 +297,25 @@ int launched(const char* what, const char* name) {
 
 }  // namespace
 
-size_t kv8_plan_bytes(const PlanArgs& p) { return in_one_launch(p) ? 0 : (size_t)p.sequences * sizeof(int32_t); }
+size_t kv8_plan_bytes(const PlanArgs& p) { return in_one_workgroup(p) || each_by_itself(p) ? 0 : (size_t)p.sequences * sizeof(int32_t); }
 
 int launch_kv8_plan(const PlanArgs& p, hipStream_t st) {
-  if (in_one_launch(p)) {
-    hipLaunchKernelGGL((kv8_plan_kernel<true, true>), dim3(1), dim3(kScanThreads), 0, st, p);
-    return launched("plan", "plan one launch");
+  if (!each_by_itself(p) && in_one_workgroup(p)) {
+    hipLaunchKernelGGL(kv8_plan_small_kernel, dim3(1), dim3(kScanThreads), 0, st, p);
+    return launched("plan", "plan one workgroup");
   }
-  if (p.sequences <= 64) hipLaunchKernelGGL((kv8_plan_kernel<false, true>), dim3(1), dim3(64), 0, st, p);
-  else hipLaunchKernelGGL((kv8_plan_kernel<false, false>), dim3(1), dim3(kScanThreads), 0, st, p);
-  if (int rc = launched("plan", "plan sums")) return rc;
   const int64_t most = std::max(p.max_len >> p.shift, std::min(p.max_new, p.tokens));  // entries or rows of a sequence
   const int64_t parts = std::min<int64_t>(std::max<int64_t>((most + 4 * kFillThreads - 1) / (4 * kFillThreads), 1), std::max(8 * num_cus() / p.sequences, 1));
-  hipLaunchKernelGGL(kv8_plan_fill_kernel, dim3((unsigned)p.sequences, (unsigned)parts), dim3(kFillThreads), 0, st, p);
+  const dim3 grid((unsigned)p.sequences, (unsigned)parts);
+  if (each_by_itself(p)) {
+    if (p.sequences <= 64) hipLaunchKernelGGL(kv8_plan_each_kernel<64>, grid, dim3(kFillThreads), 0, st, p);
+    else hipLaunchKernelGGL(kv8_plan_each_kernel<kFillThreads>, grid, dim3(kFillThreads), 0, st, p);
+    return launched("plan", "plan one launch");
+  }
+  if (p.sequences <= 64) hipLaunchKernelGGL(kv8_plan_sums_kernel<64>, dim3(1), dim3(64), 0, st, p);
+  else hipLaunchKernelGGL(kv8_plan_sums_kernel<kScanThreads>, dim3(1), dim3(kScanThreads), 0, st, p);
+  if (int rc = launched("plan", "plan sums")) return rc;
+  hipLaunchKernelGGL(kv8_plan_fill_kernel, grid, dim3(kFillThreads), 0, st, p);
   return launched("plan", "fill");
 }
 

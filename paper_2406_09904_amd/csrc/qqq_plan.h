@@ -18,7 +18,7 @@ struct PlanArgs {
   bool same_table;  // the batch's table is the sessions' own
 };
 
-constexpr int64_t kPlanOneLaunch = 8192;
+constexpr int64_t kPlanSmall = 8192;
 
 size_t kv8_plan_bytes(const PlanArgs& p);
 int launch_kv8_plan(const PlanArgs& p, hipStream_t st);

@@ -74,25 +74,27 @@ class Both:
 @pytest.mark.parametrize("B,new_hi,held_hi,page", [(1, 1, 0, 16), (1, 1, 63, 64), (1, 1000, 5000, 16), (2, 3, 100, 32), (63, 1, 500, 64), (64, 5, 300, 16), (65, 90, 40, 16),
                                                    (300, 2, 700, 64), (1023, 1, 90, 32), (1024, 3, 33, 16), (1025, 2, 50, 16), (2500, 4, 200, 16), (4096, 1, 40, 16),
                                                    (4097, 2, 40, 16), (9001, 3, 60, 16), (5, 4000, 9000, 16), (20, 1, 5000, 16), (1, 1, 90000, 16)])
+@pytest.mark.parametrize("apart", [False, True])
 @pytest.mark.parametrize("slots", [False, True])
-def test_plan(B, new_hi, held_hi, page, slots):
+def test_plan(B, new_hi, held_hi, page, slots, apart):
     rng = np.random.default_rng(B * 7 + new_hi)
     sessions = B + (B // 3 + 1 if slots else 0)
     both = Both(B, sessions, (held_hi + new_hi) // page + 2, sessions * ((held_hi + new_hi) // page + 1) + 3, page, stride=3)
     both.hold(rng.integers(0, held_hi + 1, sessions))
     ids = rng.permutation(sessions)[:B] if slots else None
-    both.step(rng.integers(0, new_hi + 1, B), ids, max_new=new_hi, spare=5, apart=slots, pad=B % 3)
+    both.step(rng.integers(0, new_hi + 1, B), ids, max_new=new_hi, spare=5, apart=apart, pad=B % 3)
 
 
 @pytest.mark.parametrize("B,columns", [(40, 30), (40, 150), (300, 200)])   # in one launch and in two
 @pytest.mark.parametrize("page", [16, 64])
-def test_steps_and_releases_in_turn(B, columns, page):
+@pytest.mark.parametrize("apart", [False, True])
+def test_steps_and_releases_in_turn(B, columns, page, apart):
     both = Both(B + page, B + 9, columns, (B + 9) * columns // 2, page)
     rng = both.rng
     for turn in range(8):
         ids = rng.permutation(B + 9)[:B]
         new = np.minimum(rng.integers(0, 3 * page, B) * (rng.random(B) < 0.7), both.max_len - both.host.held[ids])
-        both.step(new, ids, max_new=3 * page)
+        both.step(new, ids, max_new=3 * page, apart=apart)
         ends = np.concatenate([rng.permutation(B + 9)[:B // 3], [-1, B + 9]])     # (two that do not exist)
         qqq.qqq_kv8_release(both.dev, page, _dev(ends.astype(np.int32)))
         both.host.release(ends)
@@ -103,39 +105,41 @@ def test_steps_and_releases_in_turn(B, columns, page):
     assert both.host.count == (B + 9) * columns // 2 and sorted(both.host.free) == list(range(both.host.count))    # every page is back, once
 
 
-@pytest.mark.parametrize("B", [7, 1500])
-def test_pages_that_are_lacking(B):
+@pytest.mark.parametrize("B", [7, 500, 1500])
+@pytest.mark.parametrize("apart", [False, True])
+def test_pages_that_are_lacking(B, apart):
     """Entries without a page are -1, the stack stays at its bottom, and a release gives back only what is one."""
     both = Both(B, B, 12, 3 * B, 16)
-    both.step(np.full(B, 16 * 8 + 3))
+    both.step(np.full(B, 16 * 8 + 3), apart=apart)
     assert both.host.count == 0 and (both.host.pages == -1).any()
-    both.step(np.full(B, 40))
+    both.step(np.full(B, 40), apart=apart)
     both.host.release(range(B))
     qqq.qqq_kv8_release(both.dev, 16)
     both.check()
     assert both.host.count == 3 * B
 
 
-@pytest.mark.parametrize("B", [50, 1300])
-def test_what_is_out_of_bounds_is_cut(B):
+@pytest.mark.parametrize("B", [50, 700, 1300])
+@pytest.mark.parametrize("apart", [False, True])
+def test_what_is_out_of_bounds_is_cut(B, apart):
     """More tokens than the bounds, the rows or the cache allow, fewer than none, sessions that do not exist, numbers that no program writes."""
     both = Both(B, B, 6, 4 * B, 16)
     both.hold(np.arange(B) % 90)
     rng = both.rng
-    both.step(rng.integers(-5, 60, B), max_new=31, max_len=100)
-    both.step(rng.integers(0, 60, B), tokens=10 * B, max_new=1 << 30)
+    both.step(rng.integers(-5, 60, B), max_new=31, max_len=100, apart=apart)
+    both.step(rng.integers(0, 60, B), tokens=10 * B, max_new=1 << 30, apart=apart)
     ids = rng.permutation(B)
     ids[::5], ids[1::11] = -3, B
-    both.step(rng.integers(0, 4, B), ids, tokens=0)
-    both.step(rng.integers(0, 4, B), ids, max_len=0)
+    both.step(rng.integers(0, 4, B), ids, tokens=0, apart=apart)
+    both.step(rng.integers(0, 4, B), ids, max_len=0, apart=apart)
     for held, count in ((np.full(B, -2 ** 31), -5), (np.full(B, 2 ** 31 - 1), 2 ** 31 - 1)):
         both.host.held[:], both.host.count = held.astype(np.int32), count
         both.dev.held.copy_(_dev(both.host.held))
         both.dev.free_count.fill_(count)
         if count < 0:
-            both.step(rng.integers(0, 40, B))
+            both.step(rng.integers(0, 40, B), apart=apart)
         else:
-            both.step(np.full(B, 2 ** 31 - 1, np.int64).astype(np.int32), tokens=3, max_new=1 << 30)
+            both.step(np.full(B, 2 ** 31 - 1, np.int64).astype(np.int32), tokens=3, max_new=1 << 30, apart=apart)
 
 
 def test_no_sequence_and_no_page():
@@ -147,13 +151,18 @@ def test_no_sequence_and_no_page():
     short.step([62, 5, 63, 1], max_new=63)
 
 
-def test_the_sessions_own_table():
+@pytest.mark.parametrize("apart", [False, True])
+def test_the_sessions_own_table(apart):
     """Without slots the step's table can be the sessions' own: only fresh pages are written."""
     both = Both(4, 30, 20, 400, 16, stride=4)
     both.hold(both.rng.integers(0, 200, 30))
     new = both.rng.integers(0, 50, 30).astype(np.int32)
     batch = qqq.new_kv8_batch(30, 20, 50, both.max_len)._replace(page_table=both.dev.pages)
-    qqq.qqq_kv8_plan(both.dev, batch, _dev(new), 16)
+    after = (both.dev.held.clone(), both.dev.free_count.clone()) if apart else None
+    qqq.qqq_kv8_plan(both.dev, batch, _dev(new), 16, after=after)
+    if apart:
+        both.dev.held.copy_(after[0])
+        both.dev.free_count.copy_(after[1])
     kv_len, cu, _ = both.host.plan(None, new, 50, both.max_len, np.zeros((30, 20), np.int32), np.zeros(9999, np.int32), np.zeros(9999, np.int32))
     assert np.array_equal(batch.kv_len.cpu(), kv_len) and np.array_equal(batch.cu.cpu(), cu)
     both.check()
