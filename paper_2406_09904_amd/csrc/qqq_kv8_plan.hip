@@ -4,8 +4,8 @@
 // fresh_b = len_b / P - held_b / P.  Both sums saturate at 2^30 (no count that is used passes it), so they stay in 32 bits whatever the tensors hold.
 // The sums are made in registers by lane moves; the tables' entries and the rows' places are then copies, 8 bytes moved for each.  A workgroup may fill what its sums tell only where
 // no other still reads what it writes: held_after in place asks for one workgroup, or for a launch of its own for the sums.
-// What bounds it: up to 1024 sequences the time that a launch and four dependent reads take (ids, held, entries, the stack: 2.1 us for one sequence, 2.7 for 64 of 125 entries, 4.2
-// for 200 of 1000); for more the sums' one workgroup (2048 sequences: 5.7 us) and the copies (2048 tables of about 1000 entries, 17 MB: 6.1 us).
+// What bounds it: up to 1024 sequences the time that a launch and four dependent reads take (ids, held, entries, the stack: 2.1 us for one sequence, 2.7 for 64 of 125 entries, 3.5
+// for 200 of 1000); for more the sums' one workgroup (2048 sequences: 4.3 us) and the copies (2048 tables of about 1000 entries, 17 MB: 6.1 us).
 #include <algorithm>
 
 #include "qqq_plan.h"
@@ -181,10 +181,10 @@ __global__ __launch_bounds__(kScanThreads) void kv8_plan_small_kernel(const Plan
 }
 
 // More: the sums by one workgroup of T threads, then the fill kernel
-template <int T>
+template <int T, int E>
 __global__ __launch_bounds__(T) void kv8_plan_sums_kernel(const PlanArgs p) {
   __shared__ int smem[T / 64];
-  const Totals sum = make_sums<T, T == 64 ? 1 : 4>(p, p.sequences, smem, [&](int64_t b, const Sequence& s) {
+  const Totals sum = make_sums<T, E>(p, p.sequences, smem, [&](int64_t b, const Sequence& s) {
     write_sequence(p, b, s);
     p.top[b] = s.top;
   });
@@ -193,13 +193,13 @@ __global__ __launch_bounds__(T) void kv8_plan_sums_kernel(const PlanArgs p) {
 
 // Where what holds after the step goes to other memory, so that held and the stack's height stay as they are: one launch, in which each workgroup makes the sums up to its
 // sequence by itself (T of its threads do)
-template <int T>
+template <int T, int E>
 __global__ __launch_bounds__(kFillThreads) void kv8_plan_each_kernel(const PlanArgs p) {
   __shared__ int smem[T / 64];
   __shared__ Sequence mine;
   const int64_t b = blockIdx.x;
   if (T == kFillThreads || threadIdx.x < T) {
-    const Totals sum = make_sums<T, T == 64 ? 1 : 4>(p, b + 1, smem, [&](int64_t i, const Sequence& s) {
+    const Totals sum = make_sums<T, E>(p, b + 1, smem, [&](int64_t i, const Sequence& s) {
       if (i < b) return;
       mine = s;
       if (blockIdx.y == 0) write_sequence(p, b, s);
@@ -275,15 +275,15 @@ __global__ __launch_bounds__(kScanThreads) void kv8_release_kernel(const PlanArg
 }
 
 // What holds afterwards in other memory: a workgroup a sequence, up to 1024 of them (a turn of 256 threads; each reads what all before it hold).  us in a graph, this and two
-// launches: one sequence of one entry 2.1 and 3.4, of 16384 2.8 and 4.4; 64 of 128 2.7 and 4.2, of 4096 3.1 and 4.7; 200 of 1024 4.2 and 6.4; 1000 of 128 4.9 and 6.9, of 4096 11.1 and
-// 11.0; 1500 of 128 7.8 and 7.5; 2500 of 128 13 and 9.
+// launches: one sequence of one entry 2.1 and 3.4, of 16384 2.8 and 4.4; 64 of 128 2.7 and 4.2, of 4096 3.1 and 4.7; 200 of 1024 3.5 and 5.2; 1000 of 128 4.9 and 5.2, of 1024 5.7 and
+// 6.1; 1500 of 128 7.8 and 6.3; 2500 of 128 13 and 8.6.
 bool each_by_itself(const PlanArgs& p) {
   return p.sequences > 0 && p.sequences <= 4 * kFillThreads && p.held_after != p.held && p.free_count_after != p.free_count;
 }
 // In place, where a workgroup's sums must be there before another's are written: one workgroup while it moves the entries and rows about as soon as a second launch would.  Measured in
 // a graph, us with one launch and with two: one sequence of 1 entry 2.4 and 3.4, of 4096 3.1 and 4.2, of 16384 5.8 and 4.3; 37 of 256 4.9 and 4.2; 64 of 16 4.2 and 4.2, of 1024 16.7
 // and 4.5.  Outside a graph a second launch also costs the host 2 us.  More than 64 sequences, whose sums take barriers, are behind in one workgroup at every length (200 of one
-// entry 6.0 and 5.4, 1024 of one 21 and 6.2).
+// entry 6.0 and 4.2, 1024 of one 21 and 4.4).
 bool in_one_workgroup(const PlanArgs& p) {
   return p.sequences <= 64 && (int64_t)p.sequences * ((p.max_len >> p.shift) + (int64_t)p.max_new) <= kPlanSmall;
 }
@@ -308,12 +308,17 @@ int launch_kv8_plan(const PlanArgs& p, hipStream_t st) {
   const int64_t parts = std::min<int64_t>(std::max<int64_t>((most + 4 * kFillThreads - 1) / (4 * kFillThreads), 1), std::max(8 * num_cus() / p.sequences, 1));
   const dim3 grid((unsigned)p.sequences, (unsigned)parts);
   if (each_by_itself(p)) {
-    if (p.sequences <= 64) hipLaunchKernelGGL(kv8_plan_each_kernel<64>, grid, dim3(kFillThreads), 0, st, p);
-    else hipLaunchKernelGGL(kv8_plan_each_kernel<kFillThreads>, grid, dim3(kFillThreads), 0, st, p);
+    // (a sequence a thread where that covers them, us in a graph with 1, 2 and 4: 200 of one entry 2.9, 3.1, 3.6; 512 of one 3.8, 3.3, 3.8; 1000 of one 5.7, 4.9, 4.5)
+    if (p.sequences <= 64) hipLaunchKernelGGL((kv8_plan_each_kernel<64, 1>), grid, dim3(kFillThreads), 0, st, p);
+    else if (p.sequences <= kFillThreads) hipLaunchKernelGGL((kv8_plan_each_kernel<kFillThreads, 1>), grid, dim3(kFillThreads), 0, st, p);
+    else if (p.sequences <= 2 * kFillThreads) hipLaunchKernelGGL((kv8_plan_each_kernel<kFillThreads, 2>), grid, dim3(kFillThreads), 0, st, p);
+    else hipLaunchKernelGGL((kv8_plan_each_kernel<kFillThreads, 4>), grid, dim3(kFillThreads), 0, st, p);
     return launched("plan", "plan one launch");
   }
-  if (p.sequences <= 64) hipLaunchKernelGGL(kv8_plan_sums_kernel<64>, dim3(1), dim3(64), 0, st, p);
-  else hipLaunchKernelGGL(kv8_plan_sums_kernel<kScanThreads>, dim3(1), dim3(kScanThreads), 0, st, p);
+  // (1000 of one entry, fill kernel too, 4.4, 4.8, 6.0; 2048 of one 6.4, 6.1, 7.5; 4000 of one 9.4, 9.1, 10.5)
+  if (p.sequences <= 64) hipLaunchKernelGGL((kv8_plan_sums_kernel<64, 1>), dim3(1), dim3(64), 0, st, p);
+  else if (p.sequences <= kScanThreads) hipLaunchKernelGGL((kv8_plan_sums_kernel<kScanThreads, 1>), dim3(1), dim3(kScanThreads), 0, st, p);
+  else hipLaunchKernelGGL((kv8_plan_sums_kernel<kScanThreads, 2>), dim3(1), dim3(kScanThreads), 0, st, p);
   if (int rc = launched("plan", "plan sums")) return rc;
   hipLaunchKernelGGL(kv8_plan_fill_kernel, grid, dim3(kFillThreads), 0, st, p);
   return launched("plan", "fill");
