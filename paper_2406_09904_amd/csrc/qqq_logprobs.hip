@@ -133,6 +133,30 @@ struct Sums {
     z += e;
     t = __builtin_fmaf(fmaxf(d, kFar), e, t);
   }
+  // One block's values, none of them larger than the largest.  whole: all lanes have one (a lane without one has masked values)
+  __device__ __forceinline__ void add_block(const uint4& v, bool whole) {
+    float x[Row<F32>::kVec];
+    Row<F32>::unpack(v, x);
+    const float t_before = t;
+    if (whole) {
+#pragma unroll
+      for (int i = 0; i < Row<F32>::kVec; ++i) {
+        const float d = below(x[i]), e = power(d);
+        z += e;
+        t = __builtin_fmaf(d, e, t);
+      }
+      if (__builtin_expect(!__ballot(t != t), 1)) return;
+      t = t_before;
+#pragma unroll
+      for (int i = 0; i < Row<F32>::kVec; ++i) {
+        const float d = below(x[i]);
+        t = __builtin_fmaf(fmaxf(d, kFar), power(d), t);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < Row<F32>::kVec; ++i) add(x[i]);
+    }
+  }
   template <int U, bool TRACK>
   __device__ __forceinline__ void add_blocks(const uint4* v, int batch) {
     meet<TRACK>(Row<F32>::template largest<U>(v), batch);
@@ -278,7 +302,7 @@ struct List {
 template <int T>
 struct Found {
   uint64_t entries[T];  // order of the value, then bits of the place inverted
-  int ranks[64];
+  int ranks[128];
   int count;         // (also of those that found no room)
   __device__ __forceinline__ void add(uint32_t order, uint32_t place) {
     const int at = atomicAdd(&count, 1);  // (which entry lies where decides nothing)
@@ -356,27 +380,31 @@ __device__ __forceinline__ void find_equal(const Row<F32>& r, float value, int w
     turn(hits, r.place_of_block(b0 + tid));
   }
   if (got < want) turn(tid < r.tail && r.value(r.place_of_odd(r.lead + tid)) == value, r.place_of_odd(r.lead + tid));
-  if (tid < 64) found.ranks[tid] = 0;
+  if (tid < 128) found.ranks[tid] = 0;
 }
 
-// The row's largest.  pass(level, above): the threads (or groups of them) that met a value of the level, or above it, are listed; look(mode, level, list): what they met is.
-template <bool F32, int T, class Pass, class Look>
+// The row's largest.  pass(level, above): the threads (or groups of them) that met a value of the level, or above it, are listed (LISTED); look(mode, level, list): what they met is.
+template <bool F32, int T, bool LISTED, class Pass, class Look>
 __device__ __forceinline__ void find_top(const Row<F32>& r, int top, float bound, int& passing, int& passing_once, Found<T>& found, Pass pass, Look look) {
   auto again = [&] {
     __syncthreads();
     if (threadIdx.x == 0) found.count = passing = passing_once = 0;
     __syncthreads();
   };
+  auto start = [&](bool above) {
+    if constexpr (LISTED) {
+      pass(bound, above);
+      __syncthreads();
+    }
+  };
   List list;
-  pass(bound, false);
-  __syncthreads();
+  start(false);
   look(std::integral_constant<int, kReach>{}, bound, list);
   __syncthreads();
   if (found.count <= T) return;  // (the same in every thread)
   // Too many: of those that are the bound itself only the first few can be wanted, and few are above it
   again();
-  pass(bound, true);
-  __syncthreads();
+  start(true);
   look(std::integral_constant<int, kAbove>{}, bound, list);
   __syncthreads();
   if (found.count <= T) {
@@ -384,8 +412,7 @@ __device__ __forceinline__ void find_top(const Row<F32>& r, int top, float bound
     if (want > 0) find_equal<F32, T>(r, bound, want, found);
   } else {
     again();
-    pass(bound, false);
-    __syncthreads();
+    start(false);
     look(std::integral_constant<int, kList>{}, bound, list);
     again();
     found.add_list(list, top);
@@ -402,13 +429,18 @@ __device__ __forceinline__ void write_top(const LogprobArgs& p, int64_t row, con
     p.top_tokens[row * p.top + rank] = (int32_t)~(uint32_t)entry;
     p.top_logprobs[row * p.top + rank] = all.z == 0.0f ? -__builtin_inff() : all.below(value_of((uint32_t)(entry >> 32))) * all.kUnit - log_z;
   };
-  if (n <= 64) {  // a wave compares all of them with its share
-    const uint64_t mine = lane < n ? found.entries[lane] : 0;
-    int rank = 0;
-    for (int j = wave; j < n; j += T / 64) rank += found.entries[j] > mine;
-    if (rank) atomicAdd(&found.ranks[lane], rank);
+  if (n <= 128) {  // a wave compares all of them with its share
+    const uint64_t mine[2] = {lane < n ? found.entries[lane] : 0, 64 + lane < n ? found.entries[64 + lane] : 0};
+    int rank[2] = {0, 0};
+    for (int j = wave; j < n; j += T / 64) {
+      const uint64_t other = found.entries[j];
+      rank[0] += other > mine[0];
+      rank[1] += other > mine[1];
+    }
+    if (rank[0]) atomicAdd(&found.ranks[lane], rank[0]);
+    if (rank[1] && n > 64) atomicAdd(&found.ranks[64 + lane], rank[1]);
     __syncthreads();
-    if (wave == 0 && lane < n) write(mine, found.ranks[lane]);
+    if (wave < 2 && 64 * wave + lane < n) write(mine[wave], found.ranks[64 * wave + lane]);
   } else {
     for (int i = threadIdx.x; i < n; i += T) {
       const uint64_t mine = found.entries[i];
@@ -501,7 +533,7 @@ __global__ __launch_bounds__(T, 8) void logprobs_kernel(const LogprobArgs p) {
   if (p.top) {
     const float g = group_max<T / kBound>(mine.reached());
     if (tid % (T / kBound) == 0) of_group[tid / (T / kBound)] = g;
-    if (tid < 64) found.ranks[tid] = 0;
+    if (tid < 128) found.ranks[tid] = 0;
     if (tid == 0) found.count = passing = passing_once = 0;
   }
   const Sums<F32> w = wave_sums(mine);
@@ -543,7 +575,99 @@ __global__ __launch_bounds__(T, 8) void logprobs_kernel(const LogprobArgs p) {
       look_at_value<F32, T, MODE>(r, odd ? r.place_of_odd(i) : 0, odd, p.top, level, list, found);
     }
   };
-  find_top<F32, T>(r, p.top, bound_of<T>(of_group, larger, p.top), passing, passing_once, found, pass, look);
+  find_top<F32, T, true>(r, p.top, bound_of<T>(of_group, larger, p.top), passing, passing_once, found, pass, look);
+  const Sums<F32> all = join_waves<F32, T / 64>(of_wave);
+  const float log_z = logf(all.z);
+  write_top<F32, T>(p, row, all, log_z, found);
+  if (tid == T - 1) write_numbers<F32>(p, row, given, all, log_z);
+}
+
+// ---- a workgroup a row that its registers hold: U blocks a thread (and its share of the lead and tail), so nothing is read twice
+constexpr int kShortThreads = 512;
+template <bool F32, int U>
+__global__ __launch_bounds__(kShortThreads) void logprobs_short_kernel(const LogprobArgs p) {
+  constexpr int T = kShortThreads;
+  __shared__ float of_wave[T / 64][3], of_group[kBound];
+  __shared__ int larger[T / 64][kBound];
+  __shared__ Found<T> found;
+  __shared__ int passed[T], passing;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int64_t row = blockIdx.x;
+  const Row<F32> r(p, row, p.V <= kOddEach * T);
+  const int odd = r.lead + r.tail;
+  uint4 kept[U];
+  float kept_odd[kOddEach];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    kept[u] = Row<F32>::masked_block();
+    if (tid + T * u < r.blocks) kept[u] = r.template block<false>(tid + T * u);
+  }
+#pragma unroll
+  for (int i = 0; i < kOddEach; ++i) kept_odd[i] = tid + T * i < odd ? r.value(r.place_of_odd(tid + T * i)) : -__builtin_inff();
+  Given given;
+  given.request(p, row, r);
+
+  Sums<F32> mine;
+  mine.template meet<false>(Row<F32>::template largest<U>(kept), 0);
+#pragma unroll
+  for (int i = 0; i < kOddEach; ++i)
+    if (64 * wave + T * i < odd) mine.template meet<false>(kept_odd[i], 0);
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+    if (64 * wave + T * u < r.blocks) mine.add_block(kept[u], 64 * wave + T * u + 64 <= r.blocks);
+#pragma unroll
+  for (int i = 0; i < kOddEach; ++i)
+    if (64 * wave + T * i < odd) mine.add(kept_odd[i]);
+  const float reached = mine.reached();
+  if (p.top) {
+    const float g = group_max<T / kBound>(reached);
+    if (tid % (T / kBound) == 0) of_group[tid / (T / kBound)] = g;
+    if (tid < 128) found.ranks[tid] = 0;
+    if (tid == 0) found.count = passing = 0;
+  }
+  const Sums<F32> w = wave_sums(mine);
+  if (lane == 0) {
+    of_wave[wave][0] = w.m;
+    of_wave[wave][1] = w.z;
+    of_wave[wave][2] = w.t;
+  }
+  __syncthreads();
+  if (!p.top) {
+    if (wave > 0) return;
+    const Sums<F32> all = join_waves<F32, T / 64>(of_wave);
+    if (tid == 0) write_numbers<F32>(p, row, given, all, logf(all.z));
+    return;
+  }
+  // More than one block a thread: as in the kernel above.  Looked for in these registers they took 1 to 2 us longer, since a wave's threads have theirs in different blocks.
+  auto pass = [&](float level, bool above) {
+    if (passes(reached, level, above)) passed[atomicAdd(&passing, 1)] = tid;
+  };
+  auto look = [&](auto mode, float level, List& list) {
+    constexpr int MODE = decltype(mode)::value;
+    auto see = [&](bool has, float x, int place) {
+      if constexpr (MODE == kList) list.offer(has, x, place, p.top, level);
+      else if (has && wanted<MODE>(x, level)) found.add(order_of(x), ~(uint32_t)place);
+    };
+    if constexpr (U == 1) {
+      if (MODE == kList || passes(reached, level, MODE == kAbove)) {
+        float x[Row<F32>::kVec];
+        Row<F32>::unpack(kept[0], x);
+#pragma unroll
+        for (int i = 0; i < Row<F32>::kVec; ++i) see(tid < r.blocks, x[i], r.place_of_block(tid) + i);
+      }
+    } else {
+      const int items = passing * U;
+      for (int i0 = wave; i0 < items; i0 += T) {
+        if (MODE != kList && found.is_full()) return;
+        const int i = i0 + lane * (T / 64), b = i < items ? passed[i / U] + i % U * T : r.blocks;
+        look_at_block<F32, T, MODE>(r, b, b < r.blocks, p.top, level, list, found);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kOddEach; ++i)
+      if (64 * wave + T * i < odd) see(tid + T * i < odd, kept_odd[i], r.place_of_odd(tid + T * i));
+  };
+  find_top<F32, T, (U > 1)>(r, p.top, bound_of<T>(of_group, larger, p.top), passing, passing, found, pass, look);
   const Sums<F32> all = join_waves<F32, T / 64>(of_wave);
   const float log_z = logf(all.z);
   write_top<F32, T>(p, row, all, log_z, found);
@@ -606,7 +730,7 @@ __global__ __launch_bounds__(TOP ? kJoinThreads : 64) void logprobs_join_kernel(
     }
     most = group_max<T / kBound>(most);
     if (tid % (T / kBound) == 0) of_group[tid / (T / kBound)] = most;
-    if (tid < 64) found.ranks[tid] = 0;
+    if (tid < 128) found.ranks[tid] = 0;
     if (tid == 0) found.count = passing = 0;
   }
   Given given;
@@ -656,7 +780,7 @@ __global__ __launch_bounds__(TOP ? kJoinThreads : 64) void logprobs_join_kernel(
         look_at_value<F32, T, MODE>(r, odd ? r.place_of_odd(thread) : 0, odd, p.top, level, list, found);
       }
     };
-    find_top<F32, T>(r, p.top, bound_of<T>(of_group, larger, p.top), passing, passing, found, pass, look);
+    find_top<F32, T, true>(r, p.top, bound_of<T>(of_group, larger, p.top), passing, passing, found, pass, look);
     const Sums<F32> all = join_waves<F32, kWaves>(of_wave);
     const float log_z = logf(all.z);
     write_top<F32, T>(p, row, all, log_z, found);
@@ -689,7 +813,15 @@ int launch_typed(LogprobArgs& p, int64_t M, const Split& s, hipStream_t st) {
     // Threads a row, us (256 / 512 / 1024): a row a CU or less 400 KB 35.9 / 20.9 / 17.5 (100 rows, top 20), 130 KB 12.7 / 10.8 / 11.5, 32 KB 7.8 / 7.5 / 8.1; many rows 40 KB 62 / 87 / 180
     // (8000 rows, top 5), 256 KB 248 / 203 / 190 (4096 rows, top 20), 166 / 161 / 167 (top 1); 777 rows of 131 KB, sums only, 24.8 / 26.6 / 31.0
     const int64_t bytes = (int64_t)p.V * (F32 ? 4 : 2);
-    if (M <= num_cus() && bytes >= 384 << 10) QQQ_LP(1024, 4, false, false);
+    const int64_t a_thread = ((int64_t)p.V / (F32 ? 4 : 8) + kShortThreads - 1) / kShortThreads;
+    if (M <= num_cus() && a_thread <= 8) {
+#define QQQ_LP_SHORT(U) hipLaunchKernelGGL((logprobs_short_kernel<F32, U>), dim3((unsigned)M), dim3(kShortThreads), 0, st, p)
+      if (a_thread <= 1) QQQ_LP_SHORT(1);
+      else if (a_thread <= 2) QQQ_LP_SHORT(2);
+      else if (a_thread <= 4) QQQ_LP_SHORT(4);
+      else QQQ_LP_SHORT(8);
+#undef QQQ_LP_SHORT
+    } else if (M <= num_cus() && bytes >= 384 << 10) QQQ_LP(1024, 4, false, false);
     else if (M <= num_cus()) QQQ_LP(512, 4, false, false);
     // (TRACK, us without / with: 4096 rows of 256 KB, top 4 167 / 165, 8 172 / 166, 20 195 / 171, 64 276 / 183; of 128 KB, top 8 90 / 91, 20 99 / 93; 2100 rows of 80 KB, top 20
     // 40 / 43, 64 49 / 48)
