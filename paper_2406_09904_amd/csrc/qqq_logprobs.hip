@@ -583,10 +583,8 @@ __global__ __launch_bounds__(T, 8) void logprobs_kernel(const LogprobArgs p) {
 }
 
 // ---- a workgroup a row that its registers hold: U blocks a thread (and its share of the lead and tail), so nothing is read twice
-constexpr int kShortThreads = 512;
-template <bool F32, int U>
-__global__ __launch_bounds__(kShortThreads) void logprobs_short_kernel(const LogprobArgs p) {
-  constexpr int T = kShortThreads;
+template <bool F32, int T, int U>
+__global__ __launch_bounds__(T) void logprobs_short_kernel(const LogprobArgs p) {
   __shared__ float of_wave[T / 64][3], of_group[kBound];
   __shared__ int larger[T / 64][kBound];
   __shared__ Found<T> found;
@@ -794,8 +792,9 @@ struct Split {
 };
 Split split_of(int64_t M, int64_t V, int type) {
   const int64_t blocks = V / (type == QQQ_LOGITS_FP32 ? 4 : 8);
-  // us, split / whole: 2 rows of 64 KB 8.8 / 7.9, of 130 KB 8.6 / 9.6, of 256 KB 8.9 / 12.9; 48 rows of 130 KB 10.4 / 10.2, of 256 KB 12.8 / 14.4; 100 rows of 256 KB 17.4 / 14.7 (top 5)
-  if (M > 64 || blocks * 16 * 48 <= (128 << 10) * (48 + M)) return {1, 0};
+  // us in a graph, split / whole, the largest 5 asked for.  fp16: one row of 48000 7.9 / 7.4, of 64000 7.8 / 8.3; 16 of 64000 8.7 / 8.8, of 100000 9.8 / 11.0; 32 of 64000 9.6 / 8.8, of 100000 9.5 / 11.0;
+  // 64 of 100000 10.7 / 11.1.  fp32: one of 32000 7.4 / 6.6, of 42000 7.4 / 7.7; 16 of 50000 8.7 / 8.4; 32 of 64000 8.8 / 9.0; 64 of 64000 10.3 / 9.1.  (An fp32 value counts for 1.4.)
+  if (M > 64 || V * (type == QQQ_LOGITS_FP32 ? 7 : 5) * 64 <= 5 * 56000 * (64 + M)) return {1, 0};
   // a block a thread where that leaves no more than four workgroups a CU
   int64_t each = 1;
   while (each < 64 && M * ((blocks + each * kSplitThreads - 1) / (each * kSplitThreads)) > 4 * num_cus()) each *= 2;
@@ -810,19 +809,23 @@ int launch_typed(LogprobArgs& p, int64_t M, const Split& s, hipStream_t st) {
   if (s.parts == 1) {
     const bool past = M * p.V * (F32 ? 4 : 2) > kLastCacheBytes;
 #define QQQ_LP(T, U, PAST, TRACK) hipLaunchKernelGGL((logprobs_kernel<F32, T, U, PAST, TRACK>), dim3((unsigned)M), dim3(T), 0, st, p)
-    // Threads a row, us (256 / 512 / 1024): a row a CU or less 400 KB 35.9 / 20.9 / 17.5 (100 rows, top 20), 130 KB 12.7 / 10.8 / 11.5, 32 KB 7.8 / 7.5 / 8.1; many rows 40 KB 62 / 87 / 180
+    // Threads a row, us (256 / 512 / 1024): a row a CU or less 400 KB 35.9 / 20.9 / 17.5 (100 rows, top 20); many rows 40 KB 62 / 87 / 180
     // (8000 rows, top 5), 256 KB 248 / 203 / 190 (4096 rows, top 20), 166 / 161 / 167 (top 1); 777 rows of 131 KB, sums only, 24.8 / 26.6 / 31.0
     const int64_t bytes = (int64_t)p.V * (F32 ? 4 : 2);
-    const int64_t a_thread = ((int64_t)p.V / (F32 ? 4 : 8) + kShortThreads - 1) / kShortThreads;
-    if (M <= num_cus() && a_thread <= 8) {
-#define QQQ_LP_SHORT(U) hipLaunchKernelGGL((logprobs_short_kernel<F32, U>), dim3((unsigned)M), dim3(kShortThreads), 0, st, p)
-      if (a_thread <= 1) QQQ_LP_SHORT(1);
-      else if (a_thread <= 2) QQQ_LP_SHORT(2);
-      else if (a_thread <= 4) QQQ_LP_SHORT(4);
-      else QQQ_LP_SHORT(8);
+    // Rows of up to 256 KB, no more of them than CUs, in registers.  us in a graph with 512 / 1024 threads: one of 64 KB, the largest 20 6.9 / 7.3, the largest 64 8.4 / 8.1; of 120 KB, sums
+    // 6.0 / 5.6, 5 8.2 / 8.4, 64 11.0 / 9.6; 48 of 200 KB, 5 8.7 / 8.5, 64 12.4 / 10.0; read in turns (the kernel above) 4.7, 7.2, 9.6 for 64 KB, 9.0, 12.3 for the last
+    const int64_t row_blocks = p.V / (F32 ? 4 : 8), a_thread = (row_blocks + 511) / 512;
+    if (M <= num_cus() && a_thread <= 32) {
+#define QQQ_LP_SHORT(T, U) hipLaunchKernelGGL((logprobs_short_kernel<F32, T, U>), dim3((unsigned)M), dim3(T), 0, st, p)
+      if (a_thread <= 1) QQQ_LP_SHORT(512, 1);
+      else if (a_thread <= 2) QQQ_LP_SHORT(512, 2);
+      else if (a_thread <= 4) QQQ_LP_SHORT(512, 4);
+      else if (a_thread <= 8) QQQ_LP_SHORT(512, 8);
+      else if (a_thread <= 16 && p.top <= 32) QQQ_LP_SHORT(512, 16);
+      else if (a_thread <= 16) QQQ_LP_SHORT(1024, 8);
+      else QQQ_LP_SHORT(1024, 16);
 #undef QQQ_LP_SHORT
-    } else if (M <= num_cus() && bytes >= 384 << 10) QQQ_LP(1024, 4, false, false);
-    else if (M <= num_cus()) QQQ_LP(512, 4, false, false);
+    } else if (M <= num_cus()) QQQ_LP(1024, 4, false, false);
     // (TRACK, us without / with: 4096 rows of 256 KB, top 4 167 / 165, 8 172 / 166, 20 195 / 171, 64 276 / 183; of 128 KB, top 8 90 / 91, 20 99 / 93; 2100 rows of 80 KB, top 20
     // 40 / 43, 64 49 / 48)
     else if (bytes > 64 << 10 && p.top * bytes >= 1800 << 10)

@@ -64,7 +64,7 @@ def _logits(rng, M, V, dtype):
 
 # one value, less and more than 16 bytes, a thread's, a wave's, both workgroup sizes, split rows and whole ones, several turns of a thread
 SIZES = [(1, 1), (3, 2), (2, 7), (5, 9), (4, 63), (600, 65), (3, 511), (7, 1000), (1, 8192), (2, 8193), (513, 4099), (1, 16385), (30, 16391), (1, 32000), (3, 50001), (2, 131071),
-         (520, 20011), (1, 600011)]
+         (520, 20011), (100, 700), (90, 40013), (70, 70001), (1, 600011)]
 
 
 @pytest.mark.parametrize("dtype", [np.float16, np.float32])
@@ -142,8 +142,8 @@ def _check_some(x, top):
     _close(out.lse[some], want[2], r + 2 * U * (np.abs(want[2]) + np.abs(x[some]).max(1) + np.log(x.shape[1])), "lse")
 
 
-# rows of 256 threads value by value and by blocks, of 512, of 1024, split ones
-@pytest.mark.parametrize("M,V", [(300, 700), (600, 30011), (100, 9001), (70, 200003), (2100, 40013), (2, 70000), (1, 12000)])
+# rows of 256 threads value by value and by blocks, of 512, of 1024, in registers or not, split ones
+@pytest.mark.parametrize("M,V", [(300, 700), (600, 30011), (100, 700), (100, 3001), (100, 9001), (100, 40013), (70, 70001), (70, 200003), (2100, 40013), (2, 70000), (1, 12000)])
 @pytest.mark.parametrize("dtype", [np.float16, np.float32])
 def test_more_candidates_than_there_is_room_for(M, V, dtype):
     """Values in great number that are the last of the largest, or are more than that: only the first of them count, wherever in the row they lie."""
