@@ -12,10 +12,15 @@
 // through lists, of up to 64 entries in a wave's lanes in falling order.  Entries are ordered by (value, lower place first), so equal values have
 // one order and no result depends on which wave came first.
 //
-// Many rows: a workgroup a row.  Few rows: a row is split, the parts leave their sums and their groups' maxima in the workspace, and a second kernel joins
-// them and looks again at the groups that pass.
+// Many rows: a workgroup a row, read in turns.  Up to as many as CUs, of up to 256 KB: the same with the row in registers, its largest known before the first exponential.  Few long
+// rows: each is split, the parts leave their sums and their groups' maxima in the workspace, and a second kernel joins them and looks again at the groups that pass.
+//
+// What bounds it: many rows the bytes (4096 rows of 256 KB, log probabilities and the likeliest token, 164 us, 6.4 TB/s; 777 of 131 KB 23 us, 4.4 TB/s, three rows a CU); few the launch, one
+// CU's exponentials (16 cycles for 64 of them, 1.6 us for 32000 values) and the chain of steps from the maxima to the ranks (one row of 64 KB, the largest 20, 6.8 us in a graph, 4.2 of them for
+// the sums; 48 of 200 KB, the largest 5, 8.5).
 #include <float.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "qqq_past.h"
@@ -814,8 +819,9 @@ int launch_typed(LogprobArgs& p, int64_t M, const Split& s, hipStream_t st) {
     const int64_t bytes = (int64_t)p.V * (F32 ? 4 : 2);
     // Rows of up to 256 KB, no more of them than CUs, in registers.  us in a graph with 512 / 1024 threads: one of 64 KB, the largest 20 6.9 / 7.3, the largest 64 8.4 / 8.1; of 120 KB, sums
     // 6.0 / 5.6, 5 8.2 / 8.4, 64 11.0 / 9.6; 48 of 200 KB, 5 8.7 / 8.5, 64 12.4 / 10.0; read in turns (the kernel above) 4.7, 7.2, 9.6 for 64 KB, 9.0, 12.3 for the last
-    const int64_t row_blocks = p.V / (F32 ? 4 : 8), a_thread = (row_blocks + 511) / 512;
-    if (M <= num_cus() && a_thread <= 32) {
+    const int64_t row_blocks = p.V / (F32 ? 4 : 8), a_thread = std::max<int64_t>((row_blocks + 511) / 512, 1);
+    // Twice as many of up to 64 KB: 400 of 64 KB, the largest 20 10.2, in turns 11.6; more of them, or longer ones, are sooner in turns (777 of 64 KB 16.6 and 16.4, 400 of 131 KB 22.0 and 17.2)
+    if (a_thread <= (M <= num_cus() ? 32 : M <= 2 * num_cus() ? 8 : 0)) {
 #define QQQ_LP_SHORT(T, U) hipLaunchKernelGGL((logprobs_short_kernel<F32, T, U>), dim3((unsigned)M), dim3(T), 0, st, p)
       if (a_thread <= 1) QQQ_LP_SHORT(512, 1);
       else if (a_thread <= 2) QQQ_LP_SHORT(512, 2);
