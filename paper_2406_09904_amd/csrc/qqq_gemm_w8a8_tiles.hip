@@ -1,12 +1,20 @@
 // W8A8 GEMM, tiles: WM x WN waves of 16 TM x 16 TN outputs each, v_mfma_i32_16x16x64_i8.
 //
 // Both operands come through LDS, filled by DMA (global_load_lds_dwordx4) ahead of the products.  A step is 64 k.  Activations are fetched 128 k at a time (whole
-// 128-byte lines of their rows) into three slots, weights 64 k at a time (the packed layout's 1 KiB halves of chunks, lane by lane as the operand is) into four.  Every
-// step requests the weights of the third step after it and half of the activations' rows of the second 128 k after its own: the same number of requests each step, so
-// "all but the newest two steps' requests have landed" is one wait count.  The wait and the workgroup's barrier stand kAhead row tiles before the step's end: the
-// products still to come have their operands in registers, and the fragments read after the barrier are the next step's.
+// 128-byte lines of their rows) into (NB + 2) / 2 slots, weights 64 k at a time (the packed layout's 1 KiB halves of chunks, lane by lane as the operand is) into NB.  Every
+// step requests the weights of a later step and half of the activations' rows of a later 128 k, into slots that are free: the same number of requests each step, so
+// "all but the newest NB - 2 steps' requests have landed" is one wait count.
+//   256 x 256: the wait and the workgroup's barrier stand kAhead row tiles before the step's end.  The products still to come have their operands in registers, and the
+//   fragments read after the barrier are the next step's.  2 waves a SIMD of 128 accumulators each leave no room for more.
+//   FULL, the smaller tiles: the wait and the barrier stand at the step's start, and every fragment of the next step is read in this one, so a slot is free a step sooner and LDS's
+//   latency is covered where there is little else to cover it.  On 256 x 256 it is 1 to 2 % slower.
 // Activations lie in rows of 128 bytes, 16-byte chunk c of row r in slot c ^ ((r/2)%8), so that the 16 rows of a fragment read fall into different banks (as in
 // the W4A8 tiles); the exchange is made on the global side of the DMA.
+//
+// What bounds it: long prompts the board's power (4096 x 28672 x 8192 in 680 to 690 us, 2.8 POP/s: matrix units busy 75 % of the cycles at some 1.72 GHz; the library's int8 product with 32-bit
+// output takes 848); 64 to 600 rows the shares of CUs that tiles fill, and the step's barrier (333 x 13824 x 5120 in 30 us from the last-level cache, 37 from memory, 162 tiles on 256 CUs; at the
+// long prompts' rate 17); 33 to 64 rows over a wide N the weights' bytes (48 x 50001 x 5120 in 41 us, 6.3 TB/s).  Not kept: an outer ring of 2, 4 or 5 row tiles ahead (level to 2 % slower),
+// 16 row tiles to a group (2 %), wave priorities (2 %), weights straight to registers without LDS (slower everywhere), tiles of 96, 160 and 224 rows.
 #include <math.h>
 
 #include "qqq_prefill_common.h"
