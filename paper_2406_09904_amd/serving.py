@@ -30,7 +30,7 @@ class Head:
 
 class Step(typing.NamedTuple):
     """A step's tensors (Server.new_step).  The program writes ids and new (and batch.slots); the rest is filled by the step.  A graph's are its own."""
-    ids: torch.Tensor        # int32 [rows]: the sequences' tokens, one sequence after the other; rows behind the last one's hold any ids
+    ids: torch.Tensor        # int32 [rows]: the sequences' tokens, one sequence after the other (one outside of the vocabulary is its nearest end); rows behind the last one's hold any
     new: torch.Tensor        # int32 [sequences]: tokens that each brings, none for one that rests
     batch: qqq.KV8Batch
     positions: torch.Tensor  # int32 [rows]
@@ -43,6 +43,8 @@ class Server:
     up to max_len tokens share (pages: as many as all need at their longest)."""
 
     def __init__(self, embedding, layers: typing.Sequence[DecoderLayer], gain, head, sessions, max_len, page_tokens=64, pages=None):
+        if not layers or embedding.shape != head.shape:
+            raise ValueError("a server takes layers, and a head of the embedding's shape")
         self.embedding, self.layers, self.gain, self.head = embedding, list(layers), gain, Head(head)
         self.max_len, self.page_tokens = max_len, page_tokens
         columns = max(1, max_len // page_tokens)
@@ -53,6 +55,8 @@ class Server:
     def new_step(self, rows, max_new, slots=None, keep=False) -> Step:
         """Of up to `rows` rows, at most max_new of a sequence, of the sessions slots (int32 [sequences]; None: all in order).  keep: with workspaces of its own,
         for a graph."""
+        if rows < 1:
+            raise ValueError("a step of %d rows" % rows)
         sequences, device = self.sessions.held.numel() if slots is None else slots.numel(), self.embedding.device
         i32 = lambda n: torch.zeros((n,), dtype=torch.int32, device=device)  # noqa: E731
         batch = qqq.new_kv8_batch(sequences, self.sessions.pages.shape[1], max_new, self.max_len, slots, device)
@@ -62,7 +66,7 @@ class Server:
         """The step -> the `top` likeliest tokens behind each sequence's last row [sequences, top] and their log probabilities, or, given targets (int32 [rows]; below 0: none),
         those of every row and of its target.  Those of a sequence that brings no token are without meaning."""
         qqq.qqq_kv8_plan(self.sessions, step.batch, step.new, self.page_tokens, positions=step.positions, lacking=step.lacking)
-        x, residual = self.embedding[step.ids], None
+        x, residual = self.embedding[step.ids.clamp(0, self.embedding.shape[0] - 1)], None
         for i, layer in enumerate(self.layers):
             x, residual = layer(x, residual, self.caches[i], step.batch, step.positions, step.workspaces and step.workspaces[i])
         if targets is None:

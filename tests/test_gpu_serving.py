@@ -211,6 +211,24 @@ def test_two_servers_on_two_streams():
             assert torch.equal(x, y)
 
 
+def test_tokens_outside_of_the_vocabulary_and_steps_of_nothing():
+    server, V = _server(2, 64, seed=7, page_tokens=16), SHAPE["vocabulary"]
+    outs = []
+    for ids in ([5, -3, V, 2 ** 31 - 1, -2 ** 31], [5, 0, V - 1, V - 1, 0]):
+        step = server.new_step(5, 4)
+        step.ids.copy_(_i32(ids))
+        step.new.copy_(_i32([3, 2]))
+        outs.append(server(step, top=7).top_logprobs)
+        server.release()
+    assert torch.equal(*outs)
+    with pytest.raises(ValueError):
+        server.new_step(0, 1)
+    with pytest.raises(ValueError):
+        serving.Server(server.embedding, [], server.gain, server.embedding, 2, 64)
+    with pytest.raises(ValueError):
+        serving.Server(server.embedding, server.layers, server.gain, server.embedding[:-1], 2, 64)
+
+
 def test_calls_without_the_native_marshalling(monkeypatch):
     """The same through ctypes, as tensors that the native marshalling leaves to Python go."""
     ids = _i32(np.random.default_rng(8).integers(0, SHAPE["vocabulary"], 40))
