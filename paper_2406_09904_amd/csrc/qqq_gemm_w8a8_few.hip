@@ -1,4 +1,5 @@
-// W8A8 GEMM, few rows (M <= 64): the packed weights are streamed once, so it is bound by their bytes.
+// W8A8 GEMM, few rows (up to 64 a workgroup): the packed weights are streamed once, so up to 64 rows it is bound by their bytes.  More rows are taken while they and the channels
+// are few: with eight waves that share K it ends sooner than a tile does (128 x 1500 x 2048 5.6 us, by tiles 8.4; 300 x 600 x 896 4.7 and 6.6).
 //
 // A workgroup of W waves owns 16 NT channels (and one of k_splits parts of K); its waves take the k-steps (128 k) in turn and their int32 sums meet in LDS.  A lane's 16 bytes of a
 // chunk are its operand of v_mfma_i32_16x16x64_i8 as they are: no conversion, so nothing but loads stands between memory and the matrix units.  Two batches of
@@ -20,7 +21,7 @@ struct W8Batch {
 
 // Every call issues the same loads: k-steps past the end repeat the last one's (their products are skipped).
 template <int NT, int MT, int U>
-__device__ __forceinline__ void w8_load(W8Batch<NT, MT, U>& b, const W8Params& p, int ntiles, int tb, int stride, int t1, const uint32_t (&wtile)[NT], uint32_t lane,
+__device__ __forceinline__ void w8_load(W8Batch<NT, MT, U>& b, const W8Params& p, const int8_t* a_q, int ntiles, int tb, int stride, int t1, const uint32_t (&wtile)[NT], uint32_t lane,
                                         const uint32_t (&aoff)[MT][2]) {
 #pragma unroll
   for (int u = 0; u < U; ++u) {
@@ -31,7 +32,7 @@ __device__ __forceinline__ void w8_load(W8Batch<NT, MT, U>& b, const W8Params& p
 #pragma unroll
       for (int s = 0; s < 2; ++s)  // (streamed once: non-temporal, so that they do not drive the activations from L2)
         b.w[u][i][s] = __builtin_nontemporal_load(reinterpret_cast<const v4i*>(wt + wtile[i] + s * 1024u + lane * 16u));
-    const int8_t* at = p.a_q + (int64_t)t * 128;
+    const int8_t* at = a_q + (int64_t)t * 128;
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
@@ -70,7 +71,8 @@ __global__ __launch_bounds__(W * 64) void w8_few_kernel(const W8Params p, const 
   __shared__ __attribute__((aligned(16))) int8_t turns[W * 2048];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int nl = lane & 15, kc = lane >> 4;
-  const int T = p.K >> 7, ntiles = (p.N + 15) >> 4, M = p.M, N = p.N;
+  const int row0 = blockIdx.y * 16 * MT;
+  const int T = p.K >> 7, ntiles = (p.N + 15) >> 4, M = min(p.M - row0, 16 * MT), N = p.N;  // this workgroup's rows
   const int group = blockIdx.x % groups, split = blockIdx.x / groups;  // neighbours sweep one window of the weights
   const int t0 = (int)((int64_t)split * T / p.k_splits), t1 = (int)((int64_t)(split + 1) * T / p.k_splits);
 
@@ -96,20 +98,21 @@ __global__ __launch_bounds__(W * 64) void w8_few_kernel(const W8Params p, const 
                                 : (uint32_t)min(mt * 16 + nl, M - 1) * (uint32_t)p.K + 64u * s + 16u * kc;
     }
     int8_t* const turn = row_major ? turns + wave * 2048 : nullptr;
+    const int8_t* const a_q = p.a_q + (int64_t)row0 * p.K;
     constexpr int kStep = W * U;
     W8Batch<NT, MT, U> b0, b1;
     int tb = t0 + wave;
     int more = (t1 - tb - 1) / kStep;  // batches after the first
-    w8_load(b0, p, ntiles, tb, W, t1, wtile, lane, aoff);
+    w8_load(b0, p, a_q, ntiles, tb, W, t1, wtile, lane, aoff);
     for (; more >= 2; more -= 2) {
-      w8_load(b1, p, ntiles, tb + kStep, W, t1, wtile, lane, aoff);
+      w8_load(b1, p, a_q, ntiles, tb + kStep, W, t1, wtile, lane, aoff);
       w8_multiply(b0, acc, tb, W, t1, turn, woff, roff);
-      w8_load(b0, p, ntiles, tb + 2 * kStep, W, t1, wtile, lane, aoff);
+      w8_load(b0, p, a_q, ntiles, tb + 2 * kStep, W, t1, wtile, lane, aoff);
       w8_multiply(b1, acc, tb + kStep, W, t1, turn, woff, roff);
       tb += 2 * kStep;
     }
     if (more == 1) {
-      w8_load(b1, p, ntiles, tb + kStep, W, t1, wtile, lane, aoff);
+      w8_load(b1, p, a_q, ntiles, tb + kStep, W, t1, wtile, lane, aoff);
       w8_multiply(b0, acc, tb, W, t1, turn, woff, roff);
       w8_multiply(b1, acc, tb + kStep, W, t1, turn, woff, roff);
     } else {
@@ -133,32 +136,42 @@ __global__ __launch_bounds__(W * 64) void w8_few_kernel(const W8Params p, const 
     int x = 0;
 #pragma unroll
     for (int w = 0; w < W; ++w) x += sums[w * kElems + at];
-    if (p.k_splits > 1) p.part[((int64_t)split * M + m) * N + n] = x;
-    else w8_store(p, m, n, x, p.s_a[m], p.s_w[n]);
+    if (p.k_splits > 1) p.part[((int64_t)split * p.M + row0 + m) * N + n] = x;
+    else w8_store(p, row0 + m, n, x, p.s_a[row0 + m], p.s_w[n]);
   }
 }
 
 template <int NT, int MT, int W, int U>
 int launch_few(const W8Params& p, hipStream_t st) {
   const int groups = (p.N + 16 * NT - 1) / (16 * NT);
-  hipLaunchKernelGGL((w8_few_kernel<NT, MT, W, U>), dim3((unsigned)(groups * p.k_splits)), dim3(W * 64), 0, st, p, groups);
+  hipLaunchKernelGGL((w8_few_kernel<NT, MT, W, U>), dim3((unsigned)(groups * p.k_splits), (unsigned)((p.M + 16 * MT - 1) / (16 * MT))), dim3(W * 64), 0, st, p, groups);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return set_error(QQQ_ERR_HIP, "w8a8 launch: %s", hipGetErrorString(e));
-  route_note("w8a8 few rows channels=%d rows=%d waves=%d ksplit=%d", 16 * NT, 16 * MT, W, p.k_splits);
+  route_note("w8a8 few rows channels=%d rows=%dx%d waves=%d ksplit=%d", 16 * NT, (p.M + 16 * MT - 1) / (16 * MT), 16 * MT, W, p.k_splits);
   return QQQ_OK;
 }
 
 }  // namespace
 
-// 16-channel tiles of a workgroup: as many as leave two workgroups for three CUs
-int w8_few_tiles(int64_t N, int mt) {
-  int nt = mt <= 2 ? 4 : 2;
-  while (nt > 1 && (N + 16 * nt - 1) / (16 * nt) * 3 < 2 * (int64_t)num_cus()) nt >>= 1;
-  return nt;
+// Rows in workgroups of up to 64, as even as 16-row tiles allow (fewer rows in more workgroups, where CUs are free, take as long); channel tiles: as many as leave two workgroups for
+// three CUs
+W8FewShape w8_few_shape(int64_t M, int64_t N) {
+  W8FewShape s;
+  s.row_groups = (int)((M + 63) / 64);
+  s.mt = (int)((M + 16 * s.row_groups - 1) / (16 * s.row_groups));
+  s.row_groups = (int)((M + 16 * s.mt - 1) / (16 * s.mt));
+  s.nt = s.mt <= 2 ? 4 : 2;
+  while (s.nt > 1 && (N + 16 * s.nt - 1) / (16 * s.nt) * s.row_groups * 3 < 2 * (int64_t)num_cus()) s.nt >>= 1;
+  // Two instead of four where the CU with most channels then has fewer.  us, four / two, one row: 17616 x 10752 39.5 / 34.5, 24000 x 4096 17.6 / 16.2, 40000 x 4096 27.0 / 25.6; where it
+  // has as many, 16384 x 4096 11.6 / 12.4, 28672 x 8192 35.9 / 39.4
+  auto share = [&](int nt) { return ((N + 16 * nt - 1) / (16 * nt) * s.row_groups + num_cus() - 1) / num_cus() * nt; };
+  if (s.nt == 4 && share(2) < share(4)) s.nt = 2;
+  return s;
 }
 
 int launch_w8_few(const W8Params& p, hipStream_t st) {
-  const int mt = (p.M + 15) / 16, nt = w8_few_tiles(p.N, mt);
+  const W8FewShape shape = w8_few_shape(p.M, p.N);
+  const int mt = shape.mt, nt = shape.nt;
   if (mt == 1) return nt == 4 ? launch_few<4, 1, 8, 1>(p, st) : nt == 2 ? launch_few<2, 1, 8, 2>(p, st) : launch_few<1, 1, 8, 2>(p, st);
   if (mt == 2) return nt == 4 ? launch_few<4, 2, 8, 1>(p, st) : nt == 2 ? launch_few<2, 2, 8, 1>(p, st) : launch_few<1, 2, 8, 2>(p, st);
   if (mt == 3) return nt == 2 ? launch_few<2, 3, 8, 1>(p, st) : launch_few<1, 3, 8, 1>(p, st);

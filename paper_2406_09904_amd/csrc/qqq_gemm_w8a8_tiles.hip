@@ -354,7 +354,8 @@ int launch_w8_sum(const W8Params& p, hipStream_t st) {
 }
 
 // ---- which kernel, and into how many parts K is cut: the least time of a cost model, in us.  Its constants are fitted to 6600 calls (N 512 .. 50001, K 512 .. 11008, M 1 .. 2048, each
-// with every kernel and up to 16 parts; rms 6 to 10 %); what it picks is 1.6 % behind the best of them on average and 33 % at most (N = 13824, K = 11008, M = 64 unsplit).
+// with every kernel and up to 16 parts; rms 6 to 10 %).  Of 320 other calls of random sizes what it picks is up to 7 % behind the best of them in nine of ten, 36 % at most (M = 33, N = 128,
+// K = 7168: 16 parts instead of none).
 // Tiles: start + rounds * (fixed + blocks * per_block), a round being a workgroup a CU (two for the small tiles, whose blocks then take per_block_full); a last round of a share
 // x of the places takes alone + rising * x a block (small tiles with more than one workgroup on some CU: from shared to per_block_full).  Never less than the weights'
 // bytes at the rate that such a launch streams them, a lower one where CUs have different numbers of workgroups.
@@ -369,7 +370,7 @@ constexpr W8Cost kW8Cost[] = {
     {128, 128, 2, 2.83, 2.16, 0.304, 0.425, 0.874, 1.09, 0.177e-6, 0.182e-6},
     {64, 128, 2, 2.88, 1.39, 0.217, 0.264, 0.636, 0.746, 0.157e-6, 0.181e-6},
 };
-constexpr double kW8SumStart = 2.6, kW8SumPerValue = 1.7e-6;  // of the second launch that a split needs
+constexpr double kW8SumStart = 4.1, kW8SumPerValue = 1.7e-6;  // of the second launch that a split needs
 
 static double w8_tile_cost(const W8Cost& c, int64_t M, int64_t N, int64_t K, int splits) {
   const double blocks = (double)((K / 128 + splits - 1) / splits), places = (double)num_cus() * c.per_cu;
@@ -381,12 +382,14 @@ static double w8_tile_cost(const W8Cost& c, int64_t M, int64_t N, int64_t K, int
   const double bytes = c.start + (uneven ? c.per_byte_uneven : c.per_byte) * (double)N * (double)K;
   return t > bytes ? t : bytes;
 }
-// Few rows: the weights' bytes, or what a workgroup computes where there are several a CU; every workgroup reads the activations
+// Few rows, or more of them for few channels: the weights' bytes, or what a workgroup computes where there are several a CU; every workgroup reads its rows' activations
 static double w8_few_cost(int64_t M, int64_t N, int64_t K, int splits) {
-  const int mt = (int)((M + 15) / 16), nt = w8_few_tiles(N, mt);
-  const double groups = (double)((N + 16 * nt - 1) / (16 * nt)) * splits, k = (double)K / splits;
+  const W8FewShape s = w8_few_shape(M, N);
+  const int mt = s.mt, nt = s.nt;
+  const double groups = (double)((N + 16 * nt - 1) / (16 * nt)) * s.row_groups * splits, k = (double)K / splits;
   const double rounds = groups > num_cus() ? groups / num_cus() : 1;
-  const double bytes = 0.129e-6 * (double)N * (double)K, work = k / 1024 * (0.043 + 0.244 * mt * nt) * rounds;
+  // (the CUs with most workgroups are last)
+  const double bytes = 0.129e-6 * (double)N * (double)K, work = k / 1024 * (0.043 + 0.244 * mt * nt) * ceil(rounds);
   return 2.65 + (bytes > work ? bytes : work) + 0.656 * rounds + 0.191e-6 * groups * mt * k;
 }
 
@@ -397,7 +400,8 @@ W8Plan w8_plan(int64_t M, int64_t N, int64_t K) {
   double least = 1e300;
   for (int shape = kW8Few; shape <= kW8Tile64x128; ++shape) {
     if (shape == kW8Few && M > kW8FewRows) continue;
-    const int64_t rows = shape == kW8Few ? M : kW8Cost[shape - kW8Tile256x256].bm, cols = shape == kW8Few ? 16 * w8_few_tiles(N, (int)((M + 15) / 16)) : kW8Cost[shape - kW8Tile256x256].bn;
+    const W8FewShape few = w8_few_shape(M, N);
+    const int64_t rows = shape == kW8Few ? 16 * few.mt : kW8Cost[shape - kW8Tile256x256].bm, cols = shape == kW8Few ? 16 * few.nt : kW8Cost[shape - kW8Tile256x256].bn;
     const bool crowded = ((M + rows - 1) / rows) * ((N + cols - 1) / cols) * 2 > num_cus() * (shape >= kW8Tile128x128 ? 2 : 1);
     for (int splits : {1, 2, 3, 4, 6, 8, 12, 16}) {
       // (parts of two blocks of 128 at least; slabs of 256 MB at most; none where half the places are taken without)

@@ -29,7 +29,7 @@ __device__ __forceinline__ void w8_store(const W8Params& p, int m, int n, int ac
   if (p.acc_out) p.acc_out[(int64_t)m * p.N + n] = acc;
 }
 
-constexpr int kW8FewRows = 64;  // rows that the few-rows kernel takes
+constexpr int kW8FewRows = 4096;  // rows that the few-rows kernel is considered for (64 a workgroup)
 
 int launch_pack_w8(const int8_t* w, int64_t N, int64_t K, int64_t ldw, int8_t* packed, hipStream_t st);
 int launch_unpack_w8(const int8_t* packed, int64_t N, int64_t K, int8_t* w, hipStream_t st);
@@ -40,7 +40,10 @@ struct W8Plan {
   int shape, k_splits;
 };
 W8Plan w8_plan(int64_t M, int64_t N, int64_t K);
-int w8_few_tiles(int64_t N, int mt);  // 16-channel tiles of its workgroups for mt row tiles
+struct W8FewShape {
+  int row_groups, mt, nt;  // workgroups over the rows; row tiles and channel tiles of 16 each
+};
+W8FewShape w8_few_shape(int64_t M, int64_t N);
 int launch_w8_few(const W8Params& p, hipStream_t st);
 int launch_w8_tiles(const W8Params& p, int shape, hipStream_t st);
 int launch_w8_sum(const W8Params& p, hipStream_t st);
