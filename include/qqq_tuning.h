@@ -139,7 +139,7 @@ int qqq_set_prefill_ksplit(int k_splits);
 int qqq_set_factor_workgroups(int most);
 
 /*
- * Tuning/diagnostic knob (host state, not thread-safe) of qqq_gemm_w8a8.  shape: 0 = automatic, 1 = the few-rows kernel (where M <= 64, else automatic), tiles of 2 = 256 x 256,
+ * Tuning/diagnostic knob (host state, not thread-safe) of qqq_gemm_w8a8.  shape: 0 = automatic, 1 = the few-rows kernel (where M <= 4096, else automatic), tiles of 2 = 256 x 256,
  * 3 = 192 x 256, 4 = 128 x 256, 5 = 128 x 128, 6 = 64 x 128.  k_splits: 0 = automatic (1 with a forced shape), else that many parts of K (no more than K / 128).  The workspace query follows.  Returns the
  * previous shape, -1 for one that does not exist.
  */

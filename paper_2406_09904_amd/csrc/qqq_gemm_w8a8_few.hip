@@ -1,5 +1,5 @@
 // W8A8 GEMM, few rows (up to 64 a workgroup): the packed weights are streamed once, so up to 64 rows it is bound by their bytes.  More rows are taken while they and the channels
-// are few: with eight waves that share K it ends sooner than a tile does (128 x 1500 x 2048 5.6 us, by tiles 8.4; 300 x 600 x 896 4.7 and 6.6).
+// are few: with eight waves that share K it ends sooner than a tile does (us in a graph: 100 x 600 x 4096 5.9, by tiles 11.8; 670 x 141 x 2944 4.4 and 10.0).
 //
 // A workgroup of W waves owns 16 NT channels (and one of k_splits parts of K); its waves take the k-steps (128 k) in turn and their int32 sums meet in LDS.  A lane's 16 bytes of a
 // chunk are its operand of v_mfma_i32_16x16x64_i8 as they are: no conversion, so nothing but loads stands between memory and the matrix units.  Two batches of
@@ -153,11 +153,12 @@ int launch_few(const W8Params& p, hipStream_t st) {
 
 }  // namespace
 
-// Rows in workgroups of up to 64, as even as 16-row tiles allow (fewer rows in more workgroups, where CUs are free, take as long); channel tiles: as many as leave two workgroups for
-// three CUs
+// Rows in workgroups of up to 64, and of fewer while that fills CUs, as even as 16-row tiles allow (us in a graph, by 64 / by fewer: 200 x 128 x 8192 9.8 / 5.6, 50 x 222 x 5120 7.7 / 5.3,
+// 64 x 1500 x 2048 5.0 / 4.0); channel tiles: as many as leave two workgroups for three CUs
 W8FewShape w8_few_shape(int64_t M, int64_t N) {
   W8FewShape s;
-  s.row_groups = (int)((M + 63) / 64);
+  const int64_t fill = num_cus() / ((N + 15) / 16), most = (M + 15) / 16, least = (M + 63) / 64;
+  s.row_groups = (int)(fill > most ? most : fill > least ? fill : least);
   s.mt = (int)((M + 16 * s.row_groups - 1) / (16 * s.row_groups));
   s.row_groups = (int)((M + 16 * s.mt - 1) / (16 * s.mt));
   s.nt = s.mt <= 2 ? 4 : 2;

@@ -354,8 +354,8 @@ int launch_w8_sum(const W8Params& p, hipStream_t st) {
 }
 
 // ---- which kernel, and into how many parts K is cut: the least time of a cost model, in us.  Its constants are fitted to 6600 calls (N 512 .. 50001, K 512 .. 11008, M 1 .. 2048, each
-// with every kernel and up to 16 parts; rms 6 to 10 %).  Of 320 other calls of random sizes what it picks is up to 7 % behind the best of them in nine of ten, 36 % at most (M = 33, N = 128,
-// K = 7168: 16 parts instead of none).
+// with every kernel and up to 16 parts; rms 6 to 10 %).  Of 190 other calls of random sizes what it picks is up to 7 % behind the best of them in nine of ten, 14 % at most (M = 15, N = 55407,
+// K = 1152: tiles of 128 x 256 instead of 64 x 128).
 // Tiles: start + rounds * (fixed + blocks * per_block), a round being a workgroup a CU (two for the small tiles, whose blocks then take per_block_full); a last round of a share
 // x of the places takes alone + rising * x a block (small tiles with more than one workgroup on some CU: from shared to per_block_full).  Never less than the weights'
 // bytes at the rate that such a launch streams them, a lower one where CUs have different numbers of workgroups.
