@@ -155,23 +155,23 @@ int launch_few(const W8Params& p, hipStream_t st) {
 
 // Rows in workgroups of up to 64, and of fewer while that fills CUs, as even as 16-row tiles allow (us in a graph, by 64 / by fewer: 200 x 128 x 8192 9.8 / 5.6, 50 x 222 x 5120 7.7 / 5.3,
 // 64 x 1500 x 2048 5.0 / 4.0); channel tiles: as many as leave two workgroups for three CUs
-W8FewShape w8_few_shape(int64_t M, int64_t N) {
+W8FewShape w8_few_shape(int64_t M, int64_t N, int cus) {
   W8FewShape s;
-  const int64_t fill = num_cus() / ((N + 15) / 16), most = (M + 15) / 16, least = (M + 63) / 64;
+  const int64_t fill = cus / ((N + 15) / 16), most = (M + 15) / 16, least = (M + 63) / 64;
   s.row_groups = (int)(fill > most ? most : fill > least ? fill : least);
   s.mt = (int)((M + 16 * s.row_groups - 1) / (16 * s.row_groups));
   s.row_groups = (int)((M + 16 * s.mt - 1) / (16 * s.mt));
   s.nt = s.mt <= 2 ? 4 : 2;
-  while (s.nt > 1 && (N + 16 * s.nt - 1) / (16 * s.nt) * s.row_groups * 3 < 2 * (int64_t)num_cus()) s.nt >>= 1;
+  while (s.nt > 1 && (N + 16 * s.nt - 1) / (16 * s.nt) * s.row_groups * 3 < 2 * (int64_t)cus) s.nt >>= 1;
   // Two instead of four where the CU with most channels then has fewer.  us, four / two, one row: 17616 x 10752 39.5 / 34.5, 24000 x 4096 17.6 / 16.2, 40000 x 4096 27.0 / 25.6; where it
   // has as many, 16384 x 4096 11.6 / 12.4, 28672 x 8192 35.9 / 39.4
-  auto share = [&](int nt) { return ((N + 16 * nt - 1) / (16 * nt) * s.row_groups + num_cus() - 1) / num_cus() * nt; };
+  auto share = [&](int nt) { return ((N + 16 * nt - 1) / (16 * nt) * s.row_groups + cus - 1) / cus * nt; };
   if (s.nt == 4 && share(2) < share(4)) s.nt = 2;
   return s;
 }
 
 int launch_w8_few(const W8Params& p, hipStream_t st) {
-  const W8FewShape shape = w8_few_shape(p.M, p.N);
+  const W8FewShape shape = w8_few_shape(p.M, p.N, num_cus());
   const int mt = shape.mt, nt = shape.nt;
   if (mt == 1) return nt == 4 ? launch_few<4, 1, 8, 1>(p, st) : nt == 2 ? launch_few<2, 1, 8, 2>(p, st) : launch_few<1, 1, 8, 2>(p, st);
   if (mt == 2) return nt == 4 ? launch_few<4, 2, 8, 1>(p, st) : nt == 2 ? launch_few<2, 2, 8, 1>(p, st) : launch_few<1, 2, 8, 2>(p, st);

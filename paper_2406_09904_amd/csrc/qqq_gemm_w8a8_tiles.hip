@@ -372,8 +372,8 @@ constexpr W8Cost kW8Cost[] = {
 };
 constexpr double kW8SumStart = 4.1, kW8SumPerValue = 1.7e-6;  // of the second launch that a split needs
 
-static double w8_tile_cost(const W8Cost& c, int64_t M, int64_t N, int64_t K, int splits) {
-  const double blocks = (double)((K / 128 + splits - 1) / splits), places = (double)num_cus() * c.per_cu;
+static double w8_tile_cost(const W8Cost& c, int64_t M, int64_t N, int64_t K, int splits, int cus) {
+  const double blocks = (double)((K / 128 + splits - 1) / splits), places = (double)cus * c.per_cu;
   const double tiles = (double)((M + c.bm - 1) / c.bm) * (double)((N + c.bn - 1) / c.bn) * splits;
   const double full = floor(tiles / places), x = tiles / places - full;
   double t = c.start + full * (c.fixed + blocks * c.per_block_full);
@@ -383,11 +383,10 @@ static double w8_tile_cost(const W8Cost& c, int64_t M, int64_t N, int64_t K, int
   return t > bytes ? t : bytes;
 }
 // Few rows, or more of them for few channels: the weights' bytes, or what a workgroup computes where there are several a CU; every workgroup reads its rows' activations
-static double w8_few_cost(int64_t M, int64_t N, int64_t K, int splits) {
-  const W8FewShape s = w8_few_shape(M, N);
+static double w8_few_cost(const W8FewShape& s, int64_t N, int64_t K, int splits, int cus) {
   const int mt = s.mt, nt = s.nt;
   const double groups = (double)((N + 16 * nt - 1) / (16 * nt)) * s.row_groups * splits, k = (double)K / splits;
-  const double rounds = groups > num_cus() ? groups / num_cus() : 1;
+  const double rounds = groups > cus ? groups / cus : 1;
   // (the CUs with most workgroups are last)
   const double bytes = 0.129e-6 * (double)N * (double)K, work = k / 1024 * (0.043 + 0.244 * mt * nt) * ceil(rounds);
   return 2.65 + (bytes > work ? bytes : work) + 0.656 * rounds + 0.191e-6 * groups * mt * k;
@@ -396,17 +395,18 @@ static double w8_few_cost(int64_t M, int64_t N, int64_t K, int splits) {
 static int g_shape = 0, g_k_splits = 0;  // qqq_set_w8a8_tuning
 
 W8Plan w8_plan(int64_t M, int64_t N, int64_t K) {
+  const int cus = num_cus();
+  const W8FewShape few = w8_few_shape(M, N, cus);
   W8Plan best = {kW8Tile64x128, 1};
   double least = 1e300;
   for (int shape = kW8Few; shape <= kW8Tile64x128; ++shape) {
     if (shape == kW8Few && M > kW8FewRows) continue;
-    const W8FewShape few = w8_few_shape(M, N);
     const int64_t rows = shape == kW8Few ? 16 * few.mt : kW8Cost[shape - kW8Tile256x256].bm, cols = shape == kW8Few ? 16 * few.nt : kW8Cost[shape - kW8Tile256x256].bn;
-    const bool crowded = ((M + rows - 1) / rows) * ((N + cols - 1) / cols) * 2 > num_cus() * (shape >= kW8Tile128x128 ? 2 : 1);
+    const bool crowded = ((M + rows - 1) / rows) * ((N + cols - 1) / cols) * 2 > cus * (shape >= kW8Tile128x128 ? 2 : 1);
     for (int splits : {1, 2, 3, 4, 6, 8, 12, 16}) {
       // (parts of two blocks of 128 at least; slabs of 256 MB at most; none where half the places are taken without)
       if (splits > 1 && (K / 128 / splits < 2 || M * N * splits > 64000000 || crowded)) break;
-      double t = shape == kW8Few ? w8_few_cost(M, N, K, splits) : w8_tile_cost(kW8Cost[shape - kW8Tile256x256], M, N, K, splits);
+      double t = shape == kW8Few ? w8_few_cost(few, N, K, splits, cus) : w8_tile_cost(kW8Cost[shape - kW8Tile256x256], M, N, K, splits, cus);
       if (splits > 1) t += kW8SumStart + kW8SumPerValue * (double)M * (double)N * splits;
       if (t < least) {
         least = t;

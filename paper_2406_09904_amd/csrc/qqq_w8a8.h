@@ -43,7 +43,7 @@ W8Plan w8_plan(int64_t M, int64_t N, int64_t K);
 struct W8FewShape {
   int row_groups, mt, nt;  // workgroups over the rows; row tiles and channel tiles of 16 each
 };
-W8FewShape w8_few_shape(int64_t M, int64_t N);
+W8FewShape w8_few_shape(int64_t M, int64_t N, int cus);
 int launch_w8_few(const W8Params& p, hipStream_t st);
 int launch_w8_tiles(const W8Params& p, int shape, hipStream_t st);
 int launch_w8_sum(const W8Params& p, hipStream_t st);
