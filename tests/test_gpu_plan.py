@@ -72,7 +72,7 @@ class Both:
 
 # one sequence, one wave's and a wave and one, a workgroup's and one more, several turns of the scan; single tokens, ragged, none
 @pytest.mark.parametrize("B,new_hi,held_hi,page", [(1, 1, 0, 16), (1, 1, 63, 64), (1, 1000, 5000, 16), (2, 3, 100, 32), (63, 1, 500, 64), (64, 5, 300, 16), (65, 90, 40, 16),
-                                                   (300, 2, 700, 64), (1023, 1, 90, 32), (1024, 3, 33, 16), (1025, 2, 50, 16), (2500, 4, 200, 16), (4096, 1, 40, 16),
+                                                   (256, 1, 300, 64), (257, 2, 300, 16), (300, 2, 700, 64), (512, 1, 90, 16), (513, 40, 90, 16), (1023, 1, 90, 32), (1024, 3, 33, 16), (1025, 2, 50, 16), (2500, 4, 200, 16), (4096, 1, 40, 16),
                                                    (4097, 2, 40, 16), (9001, 3, 60, 16), (5, 4000, 9000, 16), (20, 1, 5000, 16), (1, 1, 90000, 16)])
 @pytest.mark.parametrize("apart", [False, True])
 @pytest.mark.parametrize("slots", [False, True])

@@ -51,6 +51,14 @@ def test_sizes(M, N, K):
     _check(M, N, K)
 
 
+# many rows of few channels: the few-rows kernel by 16, 32, 48 and 64 rows, and where it is not considered any more
+@pytest.mark.parametrize("M,N,K", [(70, 40, 1024), (500, 100, 640), (1000, 33, 2048), (1333, 70, 256), (4096, 17, 384), (4097, 16, 384), (3000, 300, 128)])
+def test_many_rows_of_few_channels(M, N, K):
+    for shape in (0, 1):
+        qqq.set_w8a8_tuning(shape, 0)
+        _check(M, N, K)
+
+
 @pytest.mark.parametrize("shape", range(1, 7))
 @pytest.mark.parametrize("M", [1, 63, 64, 65, 300, 513])
 def test_every_kernel(shape, M):
