@@ -125,14 +125,15 @@ __global__ __launch_bounds__(NW * 64, 1) void gemm_prefill_dma_kernel(const Gemm
   // The DMA loads are issued through inline assembly so that the compiler's wait-count pass does
   // not know they write LDS (it would otherwise drain every outstanding load before the first LDS
   // read of each k-step); the waits are placed by hand below.  M0 carries the wave-uniform LDS
-  // destination; lane l writes its 16 (or 4) bytes at M0 + 16*l (4*l).
+  // destination; lane l writes its 16 (or 4) bytes at M0 + 16*l (4*l).  A load into LDS comes one wait state after a write of M0 at the earliest, and the
+  // compiler puts none into inline assembly.
   const uint32_t lds_base = (uint32_t)(uintptr_t)(lds_ptr_t)lds;
   auto dma16s = [&](const int8_t* base, uint32_t voff, uint32_t dst) {  // scalar base + lane offset
-    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(dst), "v"(voff), "s"(base)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(dst), "v"(voff), "s"(base)
                  : "memory", "m0");
   };
   auto dma4 = [&](const int8_t* src, uint32_t dst) {
-    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, off" ::"s"(dst), "v"(src)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(dst), "v"(src)
                  : "memory", "m0");
   };
   // One DMA instruction of k-step t into `stage` (piece 0 .. kDmaPerStep-1): the k-loop spreads a

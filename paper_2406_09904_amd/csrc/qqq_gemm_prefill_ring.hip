@@ -88,16 +88,17 @@ __global__ __launch_bounds__(512, 1) void gemm_prefill_ring_kernel(const GemmPar
   // DMA loads are issued through inline assembly so that the compiler's wait-count pass does not
   // know they write LDS (it would drain every outstanding load before the first LDS read of each
   // k-step); the waits are placed by hand.  M0 carries the wave-uniform LDS destination; lane l
-  // writes its 16 (or 4) bytes at M0 + 16*l (4*l).
+  // writes its 16 (or 4) bytes at M0 + 16*l (4*l).  A load into LDS comes one wait state after a write of M0 at the earliest, and
+  // the compiler puts none into inline assembly.
   const uint32_t lds_base = (uint32_t)(uintptr_t)(lds_ptr_t)lds;
   const uint32_t side_base = (uint32_t)(uintptr_t)(lds_ptr_t)side;
   const uint32_t wave_u = (uint32_t)__builtin_amdgcn_readfirstlane(wave);
   auto dma16s = [&](const int8_t* base, uint32_t voff, uint32_t dst) {  // scalar base + lane offset
-    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(dst), "v"(voff), "s"(base)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(dst), "v"(voff), "s"(base)
                  : "memory", "m0");
   };
   auto dma4 = [&](const int8_t* src, uint32_t dst) {
-    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, off" ::"s"(dst), "v"(src)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(dst), "v"(src)
                  : "memory", "m0");
   };
   // (the tile order's integer divisions run on the vector unit; this brings a wave-uniform address

@@ -178,9 +178,10 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void w8_tile_kernel(const W8Params
   auto a_on = [&](int t) { a_from += t < T - 1 ? 128 : 0; };
   auto b_on = [&](int t) { b_from += t < T - 1 ? w_step : 0; };
   const uint32_t lds_base = (uint32_t)(uintptr_t)(lds_ptr_t)lds;
-  // Through inline assembly, so that the compiler does not wait for all of them before an LDS read; M0 holds the LDS place, lane l writes at M0 + 16 l.
+  // Through inline assembly, so that the compiler does not wait for all of them before an LDS read; M0 holds the LDS place, lane l writes at M0 + 16 l;
+  // such a load comes one wait state after a write of M0 at the earliest, and the compiler puts none into inline assembly.
   auto dma = [&](const int8_t* base, uint32_t voff, uint32_t to) {
-    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(voff), "s"(base) : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(voff), "s"(base) : "memory", "m0");
   };
   constexpr uint32_t kB0 = S::kASlots * S::kASlot;
   // this wave's request of round r: activations' rows into the slot at a_slot (bytes), or weights into the one at b_slot

@@ -101,7 +101,8 @@ __global__ __launch_bounds__(512, 1) void probe_prefill_loop_kernel(int steps, c
                            (piece < 2 ? (2 * wave_u + piece) * 1024 : kLoopAStage + wave_u * kLoopWWave + (piece - 2) * 1024);
       const int8_t* b = base + soff + (piece < 2 ? piece : piece - 2) * 1024;
       const uint32_t voff = piece < 2 ? a_voff : w_voff;
-      asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(dst), "v"(voff), "s"(b) : "memory", "m0");
+      // (one wait state between a write of M0 and a load into LDS)
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(dst), "v"(voff), "s"(b) : "memory", "m0");
     }
   };
   auto advance = [&]() {
