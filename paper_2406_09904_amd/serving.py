@@ -29,13 +29,19 @@ class Head:
 
 
 class Step(typing.NamedTuple):
-    """A step's tensors (Server.new_step).  The program writes ids and new (and batch.slots); the rest is filled by the step.  A graph's are its own."""
+    """A step's tensors (Server.new_step).  The program writes ids and new (and batch.slots); the rest is filled by the step.  A graph's are its own.
+
+    A sequence brings fewer tokens than new says where max_new, max_len or the rows end: batch.cu and batch.kv_len say what it brought and holds then.  The others are none the
+    worse for it: ids, targets and the results of rows stay where new puts them."""
     ids: torch.Tensor        # int32 [rows]: the sequences' tokens, one sequence after the other (one outside of the vocabulary is its nearest end); rows behind the last one's hold any
-    new: torch.Tensor        # int32 [sequences]: tokens that each brings, none for one that rests
+    new: torch.Tensor        # int32 [sequences]: tokens that each has there, none for one that rests (written in place: it lies in starts)
     batch: qqq.KV8Batch
-    positions: torch.Tensor  # int32 [rows]
+    positions: torch.Tensor  # int32 [rows], of the rows that are brought, one sequence after the other
     lacking: torch.Tensor    # int32 [1]: pages that were not there; the tokens behind them are not kept
     workspaces: typing.Optional[typing.List[Workspaces]]
+    starts: torch.Tensor     # int32 [1 + sequences]: 0, then new
+    sequence: torch.Tensor   # int32 [rows]: of the rows that are brought
+    places: torch.Tensor     # int32 [rows]: 0, 1, 2, ..
 
 
 class Server:
@@ -60,19 +66,32 @@ class Server:
         sequences, device = self.sessions.held.numel() if slots is None else slots.numel(), self.embedding.device
         i32 = lambda n: torch.zeros((n,), dtype=torch.int32, device=device)  # noqa: E731
         batch = qqq.new_kv8_batch(sequences, self.sessions.pages.shape[1], max_new, self.max_len, slots, device)
-        return Step(i32(rows), i32(sequences), batch, i32(rows), i32(1), [m.new_workspaces(rows) for m in self.layers] if keep else None)
+        starts = i32(1 + sequences)
+        return Step(i32(rows), starts[1:], batch, i32(rows), i32(1), [m.new_workspaces(rows) for m in self.layers] if keep else None, starts, i32(rows),
+                    torch.arange(rows, dtype=torch.int32, device=device))
 
     def __call__(self, step: Step, targets=None, top=1) -> qqq.LogProbs:
         """The step -> the `top` likeliest tokens behind each sequence's last row [sequences, top] and their log probabilities, or, given targets (int32 [rows]; below 0: none),
-        those of every row and of its target.  Those of a sequence that brings no token are without meaning."""
-        qqq.qqq_kv8_plan(self.sessions, step.batch, step.new, self.page_tokens, positions=step.positions, lacking=step.lacking)
-        x, residual = self.embedding[step.ids.clamp(0, self.embedding.shape[0] - 1)], None
+        those of every row and of its target.  A sequence that brings no token has every token equally likely (nothing of another's is in its results), a row that is not brought NaN."""
+        rows, sequences, cu = step.ids.numel(), step.new.numel(), step.batch.cu
+        starts = step.starts.clamp(0, rows).cumsum(0, dtype=torch.int32)
+        new = torch.minimum(step.new, rows - starts[:-1])     # (what has no row brings nothing)
+        qqq.qqq_kv8_plan(self.sessions, step.batch, new, self.page_tokens, step.sequence, step.positions, step.lacking)
+        # The rows that are brought lie one after the other; in ids those that are not stand between them
+        of_row = ((starts - cu).index_select(0, step.sequence) + step.places).clamp_(0, rows - 1)
+        x, residual = self.embedding.index_select(0, step.ids.index_select(0, of_row).clamp_(0, self.embedding.shape[0] - 1)), None
         for i, layer in enumerate(self.layers):
             x, residual = layer(x, residual, self.caches[i], step.batch, step.positions, step.workspaces and step.workspaces[i])
         if targets is None:
-            last = (step.batch.cu[1:] - 1).clamp_(min=0)
-            x, residual = x[last], residual[last]
+            at, none = (cu[1:] - 1).clamp_(min=0), cu[1:] == cu[:-1]
+        else:
+            sequence = torch.searchsorted(starts[1:], step.places, right=True, out_int32=True)
+            at = (cu - starts).index_select(0, sequence) + step.places
+            none = at >= cu.index_select(0, (sequence + 1).clamp_(max=sequences))
+            at.clamp_(0, rows - 1)
+        x, residual = x.index_select(0, at), residual.index_select(0, at)
         _, a_q, s_a = qqq.qqq_add_rmsnorm_quant(x, self.gain, residual, self.layers[-1].eps, sum_out=residual)
+        s_a.masked_fill_(none, 0.0 if targets is None else float("nan"))
         return qqq.qqq_logprobs(self.head(a_q, s_a), targets, top)
 
     def release(self, ids=None):

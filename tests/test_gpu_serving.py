@@ -258,3 +258,81 @@ def test_the_program_runs(capsys):
     serving.main()
     said = capsys.readouterr().out
     assert "us a step" in said and "held now: [84, 57, 41, 52, 104, 169, 290, 490] tokens" in said
+
+
+def _bring(server, slots, ids, new, max_new=None, targets=None, rows=None, top=3):
+    """One eager step -> (its results, the step)."""
+    step = server.new_step(rows or max(len(ids), 1), max(new) if max_new is None else max_new, _i32(slots))
+    step.ids[:len(ids)] = _i32(ids)
+    step.new.copy_(_i32(new))
+    return server(step, targets, top), step
+
+
+def _same(got, want, at, where):
+    for name in ("entropy", "lse", "top_tokens", "top_logprobs"):
+        assert torch.equal(getattr(got, name)[at], getattr(want, name)[at]), (where, name)
+
+
+def _nothing(out, at):
+    """Of sequences without a token: V logits of 0."""
+    log_v = np.log(SHAPE["vocabulary"])
+    for t, want in ((out.lse[at], log_v), (out.entropy[at], log_v), (out.top_logprobs[at], -log_v)):
+        assert (t - want).abs().max().item() <= 1e-5 if t.numel() else True
+    assert (out.top_tokens[at] == torch.arange(out.top_tokens.shape[1], device="cuda")).all()
+
+
+def test_sessions_that_are_full_leave_the_others_rows_where_they_are():
+    """A captured loop over sessions of which the first is full after a few tokens: the others go on with their own tokens."""
+    max_len = 32
+    server, alone = (_server(3, max_len, seed=15, page_tokens=16) for _ in range(2))
+    rng = np.random.default_rng(16)
+    lengths = np.array([29, 3, 9])
+    ids = rng.integers(0, SHAPE["vocabulary"], lengths.sum())
+    for s in (server, alone):
+        _bring(s, range(3), ids, lengths)
+    step = server.new_step(3, 1, keep=True)
+    server(step)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = server(step, top=3)
+    step.new.fill_(1)
+    held = lengths.copy()
+    for turn in range(28):
+        token = rng.integers(0, SHAPE["vocabulary"], 3)
+        step.ids.copy_(_i32(token))
+        graph.replay()
+        torch.cuda.synchronize()
+        brings = held < max_len
+        held += brings
+        assert np.array_equal(server.sessions.held.cpu().numpy(), held)
+        if brings.any():
+            want, _ = _bring(alone, range(3), token[brings], brings.astype(int), max_new=1)
+            _same(out, want, torch.from_numpy(np.flatnonzero(brings)).cuda(), turn)
+        _nothing(out, torch.from_numpy(np.flatnonzero(~brings)).cuda())
+    assert held.tolist() == [32, 31, 32]
+
+
+def test_tokens_that_are_cut_leave_the_others_rows_where_they_are():
+    """More tokens than max_new, than the cache and than the rows allow, and numbers below none, in one step."""
+    server, alone = (_server(5, 32, seed=17, page_tokens=16) for _ in range(2))
+    rng = np.random.default_rng(18)
+    first = rng.integers(0, SHAPE["vocabulary"], 28)
+    for s in (server, alone):
+        _bring(s, [1], first, [28])
+    new, rows = [9, 6, -3, 5, 7], 24           # 9 of which max_new 6; 6 of which 4 still fit; none; 5; 7 of which 4 have rows
+    ids, targets = rng.integers(0, SHAPE["vocabulary"], rows), rng.integers(0, SHAPE["vocabulary"], rows)
+    brought = np.r_[0:6, 9:13, 15:20, 20:24]
+    for scored in (True, False):
+        out, step = _bring(server, range(5), ids, new, max_new=6, targets=_i32(targets) if scored else None, rows=rows)
+        assert np.diff(step.batch.cu.cpu().numpy()).tolist() == [6, 4, 0, 5, 4]
+        want, _ = _bring(alone, range(5), ids[brought], [6, 4, 0, 5, 4], targets=_i32(targets[brought]) if scored else None)
+        if scored:
+            for got, w in zip(out, want):
+                assert torch.equal(got[torch.from_numpy(brought).cuda()], w)
+            assert out.lse.isnan().sum().item() == rows - len(brought)
+        else:
+            _same(out, want, torch.tensor([0, 1, 3, 4], device="cuda"), "last")
+        for s in (server, alone):
+            s.release()
+            _bring(s, [1], first, [28])
