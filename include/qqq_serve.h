@@ -45,8 +45,10 @@ typedef struct qqq_kv8_sessions {
  * Written: batch->kv_len [sequences], batch->cu [sequences + 1], batch->page_table (of row b the first len_b / page_tokens entries: the session's pages, then the
  * fresh ones), the fresh ones in sessions->pages too, held_after, free_count_after, and, where they are not NULL,
  *   sequence [tokens], positions [tokens] int32: of each row its sequence in the step and its place in it, held .. len_b - 1; rows behind cu[sequences] are left as they are
- *   lacking [1] int32: pages that were wanted and not there.  Their entries are -1, which is no page: append drops what it would write to them, so a program
- *   gives up or repeats that step's last sequences.  One that admits no more than free_count covers never sees it.
+ *   lacking [1] int32: pages that were wanted and not there.  Their entries are -1, which is no page: append drops what it would write to them, and attention reads the cache's last
+ *   page in their place, whosever it is, in this step and in all that follow.  So a program either wants no more than free_count covers (the sequences in order, fresh_b each), or gives
+ *   held_after and free_count_after of their own, looks at lacking before anything is appended, and makes the plan again for fewer tokens: pages, held and free_count still say
+ *   what they said of all that the sessions hold.  After a plan in place a session with such an entry can only end.
  * batch is a qqq_kv8_batch as the calls of qqq_layer.h take it, its tensors written here.  page_table may be sessions->pages itself (with its stride) where slots is NULL;
  * no other outputs may overlap.  max_len / page_tokens <= columns of both tables; sequences < 2^24.  A session that does not exist brings nothing; one that is there twice, or held and free_count
  * that are out of bounds, give wrong tables, never an access outside.

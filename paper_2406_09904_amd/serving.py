@@ -31,13 +31,14 @@ class Head:
 class Step(typing.NamedTuple):
     """A step's tensors (Server.new_step).  The program writes ids and new (and batch.slots); the rest is filled by the step.  A graph's are its own.
 
-    A sequence brings fewer tokens than new says where max_new, max_len or the rows end: batch.cu and batch.kv_len say what it brought and holds then.  The others are none the
-    worse for it: ids, targets and the results of rows stay where new puts them."""
+    A sequence brings fewer tokens than new says where max_new, max_len or the rows end, and none where a page that it needs is not there: batch.cu and batch.kv_len
+    say what it brought and holds then.  The others are none the worse for it: ids, targets and the results of rows stay where new puts them."""
     ids: torch.Tensor        # int32 [rows]: the sequences' tokens, one sequence after the other (one outside of the vocabulary is its nearest end); rows behind the last one's hold any
     new: torch.Tensor        # int32 [sequences]: tokens that each has there, none for one that rests (written in place: it lies in starts)
     batch: qqq.KV8Batch
     positions: torch.Tensor  # int32 [rows], of the rows that are brought, one sequence after the other
-    lacking: torch.Tensor    # int32 [1]: pages that were not there; the tokens behind them are not kept
+    lacking: torch.Tensor    # int32 [1]: pages that were not there.  What is free goes to the first sequences; the first that wants more than is left, and those behind it that
+                             # want any, bring nothing and hold what they held
     workspaces: typing.Optional[typing.List[Workspaces]]
     starts: torch.Tensor     # int32 [1 + sequences]: 0, then new
     sequence: torch.Tensor   # int32 [rows]: of the rows that are brought
@@ -54,6 +55,7 @@ class Server:
         self.embedding, self.layers, self.gain, self.head = embedding, list(layers), gain, Head(head)
         self.max_len, self.page_tokens = max_len, page_tokens
         columns = max(1, max_len // page_tokens)
+        self.scarce = pages is not None and pages < sessions * (max_len // page_tokens)   # (else every session has its pages at its longest)
         pages = sessions * columns if pages is None else pages
         self.sessions = qqq.new_kv8_sessions(sessions, columns, pages, embedding.device)
         self.caches = [qqq.new_kv8_cache(pages, m.kv_heads, m.head_dim, page_tokens, sessions, embedding.device) for m in self.layers]
@@ -70,13 +72,31 @@ class Server:
         return Step(i32(rows), starts[1:], batch, i32(rows), i32(1), [m.new_workspaces(rows) for m in self.layers] if keep else None, starts, i32(rows),
                     torch.arange(rows, dtype=torch.int32, device=device))
 
+    def _affordable(self, step: Step, new):
+        """new, or none for a sequence whose pages are not all there; counts those pages.  The plan itself would give such a sequence entries without a page: what append puts
+        there is lost, and attention reads another session's page in its place."""
+        held, slots, P = self.sessions.held, step.batch.slots, self.page_tokens
+        if slots is None:
+            held = held[:new.numel()]
+        else:
+            there = (slots >= 0) & (slots < held.numel())
+            held, new = held.index_select(0, slots.clamp(0, held.numel() - 1)), new * there
+        new = torch.minimum(new.clamp(0, step.batch.max_new), self.max_len - held)
+        fresh = torch.div(held + new, P, rounding_mode="floor") - torch.div(held, P, rounding_mode="floor")
+        wanted = fresh.cumsum(0)
+        step.lacking.copy_((wanted[-1:] - self.sessions.free_count).clamp(min=0))
+        return new * ((fresh == 0) | (wanted <= self.sessions.free_count))
+
     def __call__(self, step: Step, targets=None, top=1) -> qqq.LogProbs:
         """The step -> the `top` likeliest tokens behind each sequence's last row [sequences, top] and their log probabilities, or, given targets (int32 [rows]; below 0: none),
         those of every row and of its target.  A sequence that brings no token has every token equally likely (nothing of another's is in its results), a row that is not brought NaN."""
         rows, sequences, cu = step.ids.numel(), step.new.numel(), step.batch.cu
         starts = step.starts.clamp(0, rows).cumsum(0, dtype=torch.int32)
         new = torch.minimum(step.new, rows - starts[:-1])     # (what has no row brings nothing)
-        qqq.qqq_kv8_plan(self.sessions, step.batch, new, self.page_tokens, step.sequence, step.positions, step.lacking)
+        scarce = self.scarce and sequences > 0
+        if scarce:
+            new = self._affordable(step, new)
+        qqq.qqq_kv8_plan(self.sessions, step.batch, new, self.page_tokens, step.sequence, step.positions, None if scarce else step.lacking)
         # The rows that are brought lie one after the other; in ids those that are not stand between them
         of_row = ((starts - cu).index_select(0, step.sequence) + step.places).clamp_(0, rows - 1)
         x, residual = self.embedding.index_select(0, step.ids.index_select(0, of_row).clamp_(0, self.embedding.shape[0] - 1)), None

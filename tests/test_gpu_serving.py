@@ -281,6 +281,87 @@ def _nothing(out, at):
     assert (out.top_tokens[at] == torch.arange(out.top_tokens.shape[1], device="cuda")).all()
 
 
+@pytest.mark.parametrize("captured", [False, True])
+def test_pages_that_are_not_there_touch_nobody(captured):
+    """Four sessions over five pages of 16: when one needs a page that is not there it brings nothing and holds what it held, and goes on when another has ended; each session as if
+    it were alone with pages enough, and the starved one's results hold nothing of another's."""
+    page, max_len = 16, 96
+    server, alone = (_server(4, max_len, seed=11, page_tokens=page, **more) for more in (dict(pages=5), {}))
+    rng = np.random.default_rng(12)
+    lengths = [40, 20, 30, 14]          # pages 2 + 1 + 1 + 0 of the five
+    ids = rng.integers(0, SHAPE["vocabulary"], sum(lengths))
+    for s in (server, alone):
+        _bring(s, range(4), ids, lengths)
+    step = server.new_step(4, 1, keep=captured)
+    out = [None]
+
+    def run():
+        out[0] = server(step, top=3)
+
+    if captured:
+        server(step)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            run()
+    held, starved = np.array(lengths), np.zeros(4, int)
+    for turn in range(30):
+        if turn == 20:                  # the longest ends: two pages and what it took since
+            for s in (server, alone):
+                s.release(_i32([0]))
+            held[0] = 0
+        free = int(server.sessions.free_count)
+        token = rng.integers(0, SHAPE["vocabulary"], 4)
+        new = np.ones(4, int) * (held < max_len)
+        if turn >= 20:
+            new[0] = 0
+        brings = new.copy()
+        for b in range(4):
+            fresh = (held[b] + new[b]) // page - held[b] // page
+            free -= fresh
+            if fresh and free < 0:
+                brings[b] = 0
+        step.ids[:new.sum()] = _i32(token[new > 0])
+        step.new.copy_(_i32(new))
+        graph.replay() if captured else run()
+        torch.cuda.synchronize()
+        held += brings
+        starved += new - brings
+        assert step.lacking.item() == max(-free, 0) and np.array_equal(server.sessions.held.cpu().numpy(), held), turn
+        assert (server.sessions.pages.cpu().numpy() >= 0).all() and np.array_equal(np.diff(step.batch.cu.cpu().numpy()), brings)
+        if brings.any():
+            want, _ = _bring(alone, range(4), token[brings > 0], brings, max_new=1)
+            _same(out[0], want, torch.from_numpy(np.flatnonzero(brings)).cuda(), turn)
+        without = torch.from_numpy(np.flatnonzero(brings == 0)).cuda()
+        _nothing(out[0], without)
+    assert starved[1:].all() and held[1:].max() > 40
+    server.release()
+    assert sorted(server.sessions.free.tolist()) == list(range(5)) and server.sessions.free_count.item() == 5
+
+
+def test_prompts_whose_pages_are_not_there():
+    """Pieces of several pages, scored: what is left goes to the first that it is enough for, in order; slots that do not exist want nothing."""
+    page, max_len = 16, 96
+    server, alone = (_server(5, max_len, seed=13, page_tokens=page, **more) for more in (dict(pages=6), {}))
+    rng = np.random.default_rng(14)
+    lengths, slots = [33, 50, 10, 40, 17, 5], [2, 0, 4, 9, 1, 3]      # 2 pages, 3 (5 of 6), none, no such session, 1 (6 of 6), none
+    ids = rng.integers(0, SHAPE["vocabulary"], sum(lengths))
+    _bring(server, slots, ids, lengths)
+    _bring(alone, slots, ids, lengths)
+    assert server.sessions.held.tolist() == [50, 17, 33, 5, 10] and server.sessions.free_count.item() == 0
+    lengths, slots = [20, 12, 4, 15, 11], [0, 1, 2, 3, 4]             # 50 + 20 and 33 + 4 and 17 + 12: 1, 0, 0 pages; 5 + 15: 1; 10 + 11: 1
+    ids = rng.integers(0, SHAPE["vocabulary"], sum(lengths))
+    targets = rng.integers(-1, SHAPE["vocabulary"], sum(lengths))
+    out, step = _bring(server, slots, ids, lengths, targets=_i32(targets), rows=sum(lengths))
+    assert step.lacking.item() == 3 and np.diff(step.batch.cu.cpu().numpy()).tolist() == [0, 12, 4, 0, 0]
+    brought = np.repeat([0, 1, 1, 0, 0], lengths).astype(bool)
+    want, _ = _bring(alone, [1, 2], ids[brought], [12, 4], targets=_i32(targets[brought]))
+    at, without = (torch.from_numpy(np.flatnonzero(f)).cuda() for f in (brought, ~brought))
+    for got, w in zip(out, want):
+        assert torch.equal(got[at], w)
+    assert out.lse[without].isnan().all() and (out.logprob[without].isnan() == (_i32(targets)[without] >= 0)).all()
+
+
 def test_sessions_that_are_full_leave_the_others_rows_where_they_are():
     """A captured loop over sessions of which the first is full after a few tokens: the others go on with their own tokens."""
     max_len = 32
