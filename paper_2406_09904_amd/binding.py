@@ -750,7 +750,7 @@ def _here(*tensors):
 
 
 def _row_stride(t):
-    """Of a 2-D tensor; of one row or none it may be anything."""
+    """Of a 2-D tensor; of one row or none it may be anything that is long enough."""
     return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], t.stride(0))
 
 
@@ -863,7 +863,7 @@ def qqq_pack_w8(w_codes: torch.Tensor, out: torch.Tensor = None) -> torch.Tensor
         out = torch.empty((nbytes,), dtype=_U8, device=w_codes.device)
     elif out.numel() != nbytes:
         raise ValueError("out must have %d bytes" % nbytes)
-    _check(lib().qqq_pack_w8(w_codes.data_ptr(), N, K, _row_stride(w_codes), _ptr(out, _U8), _stream()))
+    _check(lib().qqq_pack_w8(w_codes.data_ptr(), N, K, w_codes.stride(0) if N > 1 else K, _ptr(out, _U8), _stream()))
     return out
 
 

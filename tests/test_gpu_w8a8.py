@@ -190,3 +190,12 @@ def test_tensors_of_another_device_than_the_current_one(monkeypatch):
                  lambda: qqq.qqq_kv8_release(sessions, 16), lambda: qqq.qqq_pack_w8(a_q)):
         with pytest.raises(ValueError, match="current device"):
             call()
+
+
+def test_packing_one_channel_of_a_tensor_whose_rows_lie_anywhere():
+    """One row's stride is used by nobody; of more rows it has to be a multiple of 16."""
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    wide = _codes(gen, 3, 265)
+    assert torch.equal(qqq.qqq_unpack_w8(qqq.qqq_pack_w8(wide[:1, :256]), 1, 256), wide[:1, :256])
+    with pytest.raises(qqq.QQQError):
+        qqq.qqq_pack_w8(wide[:2, :256])
