@@ -61,7 +61,7 @@ int qqq_kv8_plan(const qqq_kv8_sessions* sessions, const qqq_kv8_batch* batch, c
 /*
  * Sessions ids[0 .. count-1] (NULL: 0 .. count-1) end: their pages go to the stack in that order, a session's in their own, and they hold nothing.  In place only: held_after is
  * held and free_count_after is free_count.  Entries that are no page (-1) are dropped, and so is what the stack has no room for; a session that does not exist
- * is skipped, one that is there twice is released once.
+ * is skipped, one that is there twice is released once, in the first of its places.
  */
 int qqq_kv8_release(const qqq_kv8_sessions* sessions, const int32_t* ids, int64_t count, void* stream);
 

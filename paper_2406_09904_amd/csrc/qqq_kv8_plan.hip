@@ -6,6 +6,8 @@
 // no other still reads what it writes: held_after in place asks for one workgroup, or for a launch of its own for the sums.
 // What bounds it: up to 1024 sequences the time that a launch and four dependent reads take (ids, held, entries, the stack: 2.1 us for one sequence, 2.7 for 64 of 125 entries, 3.5
 // for 200 of 1000); for more the sums' one workgroup (2048 sequences: 4.3 us) and the copies (2048 tables of about 1000 entries, 17 MB: 6.1 us).
+#include <limits.h>
+
 #include <algorithm>
 
 #include "qqq_plan.h"
@@ -234,16 +236,23 @@ __global__ __launch_bounds__(kScanThreads) void kv8_release_kernel(const PlanArg
   int count = min(max(*p.free_count, 0), p.pool);
   for (int64_t first = 0; first < p.sequences; first += kScanThreads) {
     const int here = (int)min((int64_t)kScanThreads, p.sequences - first);
+    // A session may be listed twice: the first place in the list has its pages.  Every place goes to where the session's length was, as a number below all lengths, the least stays, and
+    // who met the length itself hands it to that place.
+    int session = -1, length = 0;
     if (tid < here) {
-      int session = p.ids ? p.ids[first + tid] : (int)first + tid, closed = 0;
-      if ((uint32_t)session < (uint32_t)p.sessions)
-        closed = min(max(atomicExch(&p.held_after[session], 0), 0) >> p.shift, p.columns);  // (there twice: the second finds nothing)
-      else
-        session = 0;
-      session_of[tid] = session;
-      closed_of[tid] = closed;
+      session = p.ids ? p.ids[first + tid] : (int)first + tid;
+      if ((uint32_t)session >= (uint32_t)p.sessions) session = -1;
+      session_of[tid] = max(session, 0);
+      closed_of[tid] = 0;
+      if (session >= 0) length = atomicMin(&p.held_after[session], INT_MIN + tid);
     }
     __syncthreads();
+    if (session >= 0 && length >= 0) closed_of[atomicExch(&p.held_after[session], 0) & (kScanThreads - 1)] = min(length >> p.shift, p.columns);
+    __syncthreads();
+    if (length < 0) {  // listed before, or a length below 0
+      atomicExch(&p.held_after[session], 0);
+      __threadfence();
+    }
     for (int i = wave; i < here; i += kWaves) {
       const int32_t* own = p.pages + (int64_t)session_of[i] * p.pages_stride;
       int n = 0;

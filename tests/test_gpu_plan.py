@@ -177,6 +177,23 @@ def test_sessions_that_end_twice_are_released_once():
     assert int(both.dev.free_count) == 200 and sorted(free) == list(range(200)) and not both.dev.held.any()
 
 
+@pytest.mark.parametrize("sessions,listed", [(3, 50), (70, 140), (40, 1024), (900, 3000), (1500, 5000)])
+def test_sessions_that_are_listed_twice_are_released_in_the_first_places(sessions, listed):
+    """In any order, within a wave, a workgroup's turn and beyond: the stack is the oracle's, entry by entry; numbers that are no session and lengths below 0 among them."""
+    both = Both(sessions, sessions, 6, 6 * sessions, 16)
+    both.hold(both.rng.integers(0, 6 * 16, sessions))
+    for _ in range(3):
+        ids = both.rng.integers(-1, sessions + 1, listed)
+        both.host.held[::7] = -5
+        both.dev.held[::7] = -5
+        qqq.qqq_kv8_release(both.dev, 16, _dev(ids.astype(np.int32)))
+        both.host.release(ids)
+        both.check()
+        both.host.held[::7] = 0
+        both.dev.held[::7] = 0
+        both.step(both.rng.integers(0, 40, sessions), max_new=40)
+
+
 @pytest.mark.parametrize("B,columns", [(8, 40), (200, 300)])
 def test_captured_steps(B, columns):
     """A step is captured once and replayed: each replay carries on from what the one before left, beside eager work of the same tensors' copies."""
