@@ -21,7 +21,8 @@ extern "C" {
  * What a program keeps of its sessions on the GPU, so that a step's tables can be made there (and a captured step replayed) without the host.
  *   pages [sessions, pages_stride] int32: the first held / page_tokens of a row's `columns` entries are the session's closed pages in order
  *   held [sessions] int32: tokens in the cache
- *   free_pages [pool] int32, free_count [1] int32: the pages that no session has, a stack; the last of the first free_count entries is taken first
+ *   free_pages [pool] int32, free_count [1] int32: the pages that no session has, a stack; the last of the first free_count entries is taken first.  They need not be all
+ *   of the cache's pages, nor the lowest: any numbers from 0 on
  *   held_after, free_count_after: where a call writes what holds after it; the same pointers, or others (then held and free_count stay as they are, and of
  *   held_after only the step's sessions are written)
  * All 4-byte aligned.  page_tokens 16, 32 or 64, as in qqq_kv8_cache.  The struct is a host struct, read before the call returns.
@@ -60,7 +61,7 @@ int qqq_kv8_plan(const qqq_kv8_sessions* sessions, const qqq_kv8_batch* batch, c
 
 /*
  * Sessions ids[0 .. count-1] (NULL: 0 .. count-1) end: their pages go to the stack in that order, a session's in their own, and they hold nothing.  In place only: held_after is
- * held and free_count_after is free_count.  Entries that are no page (-1) are dropped, and so is what the stack has no room for; a session that does not exist
+ * held and free_count_after is free_count.  Entries that are no page (below 0) are dropped, and so is what the stack has no room for; a session that does not exist
  * is skipped, one that is there twice is released once, in the first of its places.
  */
 int qqq_kv8_release(const qqq_kv8_sessions* sessions, const int32_t* ids, int64_t count, void* stream);

@@ -47,7 +47,7 @@ class Sessions:
             if not 0 <= s < len(self.held):
                 continue
             for page in self.pages[s, :min(max(int(self.held[s]), 0) // self.P, self.pages.shape[1])]:
-                if 0 <= page < len(self.free) and count < len(self.free):
+                if page >= 0 and count < len(self.free):
                     self.free[count] = page
                     count += 1
             self.held[s] = 0

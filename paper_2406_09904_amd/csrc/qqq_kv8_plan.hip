@@ -232,7 +232,7 @@ __global__ __launch_bounds__(kScanThreads) void kv8_release_kernel(const PlanArg
   __shared__ int session_of[kScanThreads], closed_of[kScanThreads], pages_of[kScanThreads];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   constexpr int kWaves = kScanThreads / 64;
-  auto is_page = [&](int page) { return (uint32_t)page < (uint32_t)p.pool; };
+  auto is_page = [&](int page) { return page >= 0; };  // (any of the cache: the stack may hold a part of its pages)
   int count = min(max(*p.free_count, 0), p.pool);
   for (int64_t first = 0; first < p.sequences; first += kScanThreads) {
     const int here = (int)min((int64_t)kScanThreads, p.sequences - first);

@@ -194,6 +194,22 @@ def test_sessions_that_are_listed_twice_are_released_in_the_first_places(session
         both.step(both.rng.integers(0, 40, sessions), max_new=40)
 
 
+@pytest.mark.parametrize("lowest", [1, 37, 10 ** 6])
+def test_pages_of_a_part_of_the_cache(lowest):
+    """The stack holds pages from some number on, others have the rest: their numbers may pass its size, and every one comes back."""
+    both = Both(lowest, 9, 5, 40, 16)
+    both.host.free += lowest
+    both.dev.free.copy_(_dev(both.host.free))
+    for turn in range(4):
+        both.step(both.rng.integers(0, 80, 9), max_new=80)
+        ends = both.rng.permutation(9)[:6]
+        qqq.qqq_kv8_release(both.dev, 16, _dev(ends.astype(np.int32)))
+        both.host.release(ends)
+        both.check()
+    qqq.qqq_kv8_release(both.dev, 16)
+    assert int(both.dev.free_count) == 40 and sorted(both.dev.free.tolist()) == list(range(lowest, lowest + 40)) and not both.dev.held.any()
+
+
 @pytest.mark.parametrize("B,columns", [(8, 40), (200, 300)])
 def test_captured_steps(B, columns):
     """A step is captured once and replayed: each replay carries on from what the one before left, beside eager work of the same tensors' copies."""
