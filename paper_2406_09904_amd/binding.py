@@ -76,21 +76,22 @@ def _load_native(library):
     it they are marshalled here."""
     global _native_linear, _native_rmsnorm, _native_gated, _native_append, _native_read, _native_attention, _native_plan, _native_w8a8, _native_logprobs
     path = _call_path()
+    addresses = lambda names: [ctypes.cast(getattr(library, n), ctypes.c_void_p).value for n in names]  # noqa: E731
     try:
         spec = importlib.util.spec_from_file_location("_qqq_call", path)
         module = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(module)
-    except ImportError as e:
+        # (an AttributeError or TypeError: one that was built from other sources than these)
+        module.bind(*addresses(("qqq_linear_w4a8_perchannel", "qqq_linear_w4a8_pergroup")))
+        module.bind_layer(*addresses(LAYER_SYMBOLS))
+        module.bind_serve(*addresses(("qqq_kv8_plan_workspace_bytes", "qqq_kv8_plan", "qqq_packed_w8_bytes", "qqq_gemm_w8a8_workspace_bytes", "qqq_gemm_w8a8",
+                                      "qqq_logprobs_workspace_bytes", "qqq_logprobs")))
+        calls = (module.linear, module.rmsnorm, module.gated, module.append, module.read, module.attention, module.plan, module.w8a8, module.logprobs)
+    except (ImportError, AttributeError, TypeError) as e:
         warnings.warn("linear calls are marshalled in Python, a microsecond slower each: build.py has not built %s for this torch and interpreter (%s)"
                       % (os.path.basename(path), e), RuntimeWarning, stacklevel=3)
         return
-    module.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (library.qqq_linear_w4a8_perchannel, library.qqq_linear_w4a8_pergroup)))
-    module.bind_layer(*(ctypes.cast(getattr(library, n), ctypes.c_void_p).value for n in LAYER_SYMBOLS))
-    _native_linear, _native_rmsnorm, _native_gated = module.linear, module.rmsnorm, module.gated
-    module.bind_serve(*(ctypes.cast(getattr(library, n), ctypes.c_void_p).value for n in (
-        "qqq_kv8_plan_workspace_bytes", "qqq_kv8_plan", "qqq_packed_w8_bytes", "qqq_gemm_w8a8_workspace_bytes", "qqq_gemm_w8a8", "qqq_logprobs_workspace_bytes", "qqq_logprobs")))
-    _native_append, _native_read, _native_attention = module.append, module.read, module.attention
-    _native_plan, _native_w8a8, _native_logprobs = module.plan, module.w8a8, module.logprobs
+    (_native_linear, _native_rmsnorm, _native_gated, _native_append, _native_read, _native_attention, _native_plan, _native_w8a8, _native_logprobs) = calls
 
 
 def lib():

@@ -45,6 +45,29 @@ def test_library_without_a_fitting_extension(monkeypatch, tmp_path, kind):
     assert module.qqq_packed_w4_bytes(4096, 4096) == 4096 * 4096 // 2
 
 
+@pytest.mark.parametrize("older", ["without the serving calls", "with fewer of them", "without one call"])
+def test_library_with_an_extension_of_other_sources(monkeypatch, tmp_path, older):
+    """One left from before a change, whose name is the same: as if it were not there, in every call and not only the first."""
+    path = tmp_path / "_qqq_call.py"
+    text = "def call(*args):\n    return 1\nbind = bind_layer = linear = rmsnorm = gated = append = read = attention = plan = w8a8 = call\n"
+    if older == "with fewer of them":
+        text += "def bind_serve(a, b):\n    pass\nlogprobs = call\n"
+    elif older == "without one call":
+        text += "bind_serve = call\n"
+    path.write_text(text)
+    spec = importlib.util.spec_from_file_location("paper_2406_09904_amd.binding_with_older", binding.__file__)
+    module = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(module)
+    monkeypatch.setattr(torch.cuda, "is_available", lambda: True)
+    monkeypatch.setattr(module, "_call_path", lambda: str(path))
+    with pytest.warns(RuntimeWarning, match="marshalled in Python"):
+        module.lib()
+    assert module.lib() is module._lib
+    for name in ("linear", "rmsnorm", "gated", "append", "read", "attention", "plan", "w8a8", "logprobs"):
+        assert getattr(module, "_native_" + name) is module._no_native, name
+    assert module.qqq_packed_w4_bytes(4096, 4096) == 4096 * 4096 // 2
+
+
 def test_extension_is_the_present_torchs():
     """The file's name carries the torch and the interpreter that it was built against."""
     from paper_2406_09904_amd import build
