@@ -811,9 +811,14 @@ Split split_of(int64_t M, int64_t V, int type) {
 
 template <bool F32>
 int launch_typed(LogprobArgs& p, int64_t M, const Split& s, hipStream_t st) {
+  const char* way = "logprobs in parts";
   if (s.parts == 1) {
     const bool past = M * p.V * (F32 ? 4 : 2) > kLastCacheBytes;
-#define QQQ_LP(T, U, PAST, TRACK) hipLaunchKernelGGL((logprobs_kernel<F32, T, U, PAST, TRACK>), dim3((unsigned)M), dim3(T), 0, st, p)
+#define QQQ_LP(T, U, PAST, TRACK)                                                                                              \
+  do {                                                                                                                       \
+    hipLaunchKernelGGL((logprobs_kernel<F32, T, U, PAST, TRACK>), dim3((unsigned)M), dim3(T), 0, st, p);                     \
+    way = "logprobs in turns threads=" #T " past=" #PAST " tracked=" #TRACK;                                                 \
+  } while (0)
     // Threads a row, us (256 / 512 / 1024): a row a CU or less 400 KB 35.9 / 20.9 / 17.5 (100 rows, top 20); many rows 40 KB 62 / 87 / 180
     // (8000 rows, top 5), 256 KB 248 / 203 / 190 (4096 rows, top 20), 166 / 161 / 167 (top 1); 777 rows of 131 KB, sums only, 24.8 / 26.6 / 31.0
     const int64_t bytes = (int64_t)p.V * (F32 ? 4 : 2);
@@ -822,7 +827,11 @@ int launch_typed(LogprobArgs& p, int64_t M, const Split& s, hipStream_t st) {
     const int64_t row_blocks = p.V / (F32 ? 4 : 8), a_thread = std::max<int64_t>((row_blocks + 511) / 512, 1);
     // Twice as many of up to 64 KB: 400 of 64 KB, the largest 20 10.2, in turns 11.6; more of them, or longer ones, are sooner in turns (777 of 64 KB 16.6 and 16.4, 400 of 131 KB 22.0 and 17.2)
     if (a_thread <= (M <= num_cus() ? 32 : M <= 2 * num_cus() ? 8 : 0)) {
-#define QQQ_LP_SHORT(T, U) hipLaunchKernelGGL((logprobs_short_kernel<F32, T, U>), dim3((unsigned)M), dim3(T), 0, st, p)
+#define QQQ_LP_SHORT(T, U)                                                                                                   \
+  do {                                                                                                                       \
+    hipLaunchKernelGGL((logprobs_short_kernel<F32, T, U>), dim3((unsigned)M), dim3(T), 0, st, p);                            \
+    way = "logprobs in registers threads=" #T " blocks=" #U;                                                                 \
+  } while (0)
       if (a_thread <= 1) QQQ_LP_SHORT(512, 1);
       else if (a_thread <= 2) QQQ_LP_SHORT(512, 2);
       else if (a_thread <= 4) QQQ_LP_SHORT(512, 4);
@@ -831,17 +840,21 @@ int launch_typed(LogprobArgs& p, int64_t M, const Split& s, hipStream_t st) {
       else if (a_thread <= 16) QQQ_LP_SHORT(1024, 8);
       else QQQ_LP_SHORT(1024, 16);
 #undef QQQ_LP_SHORT
-    } else if (M <= num_cus()) QQQ_LP(1024, 4, false, false);
-    // (TRACK, us without / with: 4096 rows of 256 KB, top 4 167 / 165, 8 172 / 166, 20 195 / 171, 64 276 / 183; of 128 KB, top 8 90 / 91, 20 99 / 93; 2100 rows of 80 KB, top 20
-    // 40 / 43, 64 49 / 48)
-    else if (bytes > 64 << 10 && p.top * bytes >= 1800 << 10)
+    } else if (M <= num_cus()) {
+      QQQ_LP(1024, 4, false, false);
+    } else if (bytes > 64 << 10 && p.top * bytes >= 1800 << 10) {
+      // (TRACK, us without / with: 4096 rows of 256 KB, top 4 167 / 165, 8 172 / 166, 20 195 / 171, 64 276 / 183; of 128 KB, top 8 90 / 91, 20 99 / 93; 2100 rows of 80 KB, top 20
+      // 40 / 43, 64 49 / 48)
       if (past) QQQ_LP(512, 2, true, true);
       else QQQ_LP(512, 2, false, true);
-    else if (bytes > 64 << 10 && (p.top > 0 || M >= 8 * num_cus()))
+    } else if (bytes > 64 << 10 && (p.top > 0 || M >= 8 * num_cus())) {
       if (past) QQQ_LP(512, 2, true, false);
       else QQQ_LP(512, 2, false, false);
-    else if (past) QQQ_LP(256, 2, true, false);
-    else QQQ_LP(256, 2, false, false);
+    } else if (past) {
+      QQQ_LP(256, 2, true, false);
+    } else {
+      QQQ_LP(256, 2, false, false);
+    }
 #undef QQQ_LP
   } else {
     p.splits = s.parts;
@@ -852,7 +865,8 @@ int launch_typed(LogprobArgs& p, int64_t M, const Split& s, hipStream_t st) {
   }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return set_error(QQQ_ERR_HIP, "logprobs launch: %s", hipGetErrorString(e));
-  route_note("logprobs parts=%d", s.parts);
+  if (s.parts > 1) route_note("%s=%d", way, s.parts);
+  else route_note("%s", way);
   return QQQ_OK;
 }
 

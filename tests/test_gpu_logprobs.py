@@ -207,6 +207,54 @@ def test_rows_that_are_past_the_last_cache():
             assert torch.equal(out.lse, out.lse[:56].repeat((M + 55) // 56)[:M])
 
 
+# (rows, values, how many of the largest) for each kernel, of fp16; fp32's rows are half as long
+KERNELS = [(3, 3000, 5, "in registers threads=512 blocks=1"), (3, 7001, 5, "in registers threads=512 blocks=2"), (400, 16001, 5, "in registers threads=512 blocks=4"),
+           (3, 32003, 5, "in registers threads=512 blocks=8"), (3, 48001, 20, "in registers threads=512 blocks=16"), (3, 48001, 64, "in registers threads=1024 blocks=8"),
+           (80, 128003, 7, "in registers threads=1024 blocks=16"), (80, 140003, 7, "in turns threads=1024 past=false tracked=false"),
+           (530, 30011, 5, "in turns threads=256 past=false tracked=false"), (9000, 20001, 5, "in turns threads=256 past=true tracked=false"),
+           (530, 40013, 5, "in turns threads=512 past=false tracked=false"), (2100, 80001, 5, "in turns threads=512 past=true tracked=false"),
+           (600, 60001, 64, "in turns threads=512 past=false tracked=true"), (2100, 80001, 20, "in turns threads=512 past=true tracked=true"), (2, 100001, 5, "in parts")]
+
+
+@pytest.mark.parametrize("dtype", [np.float16, np.float32])
+@pytest.mark.parametrize("M,V,top,kernel", KERNELS)
+def test_every_kernel(M, V, top, kernel, dtype):
+    """By the kernels' names, so that a limit that moves is seen: ordinary rows, masked ones, equal, rising and falling ones and what is no number."""
+    V = V if dtype == np.float16 else (V + 1) // 2
+    rng = np.random.default_rng(V + top)
+    some = _logits(rng, 11, V, dtype)
+    some[1, rng.random(V) < 0.99] = -np.inf
+    some[2, :] = -np.inf
+    some[3, rng.random(V) < 0.999] = np.finfo(dtype).min
+    some[4, :] = 1.25
+    some[5] = np.sort(rng.uniform(-8, 8, V))
+    some[6] = np.sort(rng.uniform(-8, 8, V))[::-1]
+    some[7, V // 2] = np.nan
+    some[8, [V - 1, 3]] = np.inf
+    some[9, V // 3:] = 2.0
+    tokens = rng.integers(0, V, 11).astype(np.int32)
+    want = ref.logprobs(some, tokens, top)
+    log_v = np.log(V)
+    r = (V / 256 * (1 + 6 / 16) + 100 + 3 * log_v) * U
+    for begin in range(0, 11, M):              # (few rows at a time where that is what is tested)
+        rows = np.arange(begin, min(begin + M, 11))
+        of = torch.from_numpy(rows[np.arange(M) % len(rows)]).cuda()
+        dev = torch.from_numpy(some).cuda()[of]
+        out = qqq.qqq_logprobs(dev, torch.from_numpy(tokens).cuda()[of], top)
+        assert qqq.last_route().startswith("logprobs " + kernel), qqq.last_route()
+        for at in {0, (M - 1) // len(rows) * len(rows)}:
+            n = min(len(rows), M - at)
+            x, got, w = some[rows[:n]], [o[at:at + n] for o in out], [o[rows[:n]] for o in want]
+            with np.errstate(invalid="ignore"):
+                largest = np.abs(np.where(np.isfinite(x), x.astype(np.float64), -1e300).max(1))
+                largest = np.where(largest == 1e300, 0, largest)
+                _close(got[2], w[2], r + 2 * U * (np.abs(w[2]) + largest + log_v), "lse")
+                _close(got[0], w[0], r + 2 * U * (2 * np.abs(w[0]) + 2 * log_v), "logprob")
+                _close(got[1], w[1], r * (1 + 2 * log_v) + 4 * U * log_v, "entropy")
+                assert np.array_equal(got[3].cpu().numpy(), w[3]), "top tokens"
+                _close(got[4], w[4], r + 2 * U * (2 * np.abs(w[4]) + 2 * log_v), "top logprobs")
+
+
 def test_no_token_and_a_short_vocabulary():
     x = _logits(np.random.default_rng(1), 6, 5, np.float16)
     out = _check(x, 9, np.array([-1, 0, 4, 5, -2 ** 31, 2 ** 31 - 1], np.int32))

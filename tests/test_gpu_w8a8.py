@@ -76,6 +76,28 @@ def test_parts_of_k(shape, k_splits):
         _check(M, N, K, seed=k_splits)
 
 
+TILES = {1: "w8a8 few rows ", 2: "w8a8 tile=256x256 ", 3: "w8a8 tile=192x256 ", 4: "w8a8 tile=128x256 ", 5: "w8a8 tile=128x128 ", 6: "w8a8 tile=64x128 "}
+
+
+@pytest.mark.parametrize("shape", range(1, 7))
+@pytest.mark.parametrize("k_splits", [0, 2, 7, 100])
+def test_the_kernel_that_is_asked_for_runs(shape, k_splits):
+    for M, N, K in ((1, 48, 1024), (270, 520, 384), (4097, 130, 256)):
+        qqq.set_w8a8_tuning(shape, k_splits)
+        _check(M, N, K, seed=shape, dtypes=(torch.float16,))
+        route = qqq.last_route()
+        if shape > 1 or M <= 4096:             # (the few-rows kernel is considered up to there)
+            assert route.startswith(TILES[shape]), route
+        assert ("ksplit=%d" % min(max(k_splits, 1), K // 128)) in route and route.endswith(" + sum") == (k_splits > 0), route
+
+
+# (one row of short K over many channels is near the cost model's border: 3.7 us by the few-rows kernel, 4.6 by the smallest tile)
+@pytest.mark.parametrize("M,N,K,shapes", [(1, 32000, 512, (1, 6)), (1, 32000, 4096, (1,)), (48, 5001, 1024, (1,)), (64, 130, 4096, (1,)), (3000, 9000, 512, (2,))])
+def test_the_kernel_that_is_chosen(M, N, K, shapes):
+    _check(M, N, K)
+    assert any(qqq.last_route().startswith(TILES[s]) for s in shapes), qqq.last_route()
+
+
 @pytest.mark.parametrize("M", [3, 100, 300])
 @pytest.mark.parametrize("N,ldy,offset", [(64, 64, 0), (64, 67, 0), (64, 72, 3), (96, 104, 8), (333, 333, 1), (336, 344, 0)])
 def test_output_rows_apart_and_unaligned(M, N, ldy, offset):
