@@ -15,9 +15,9 @@
 // Many rows: a workgroup a row, read in turns.  Up to as many as CUs, of up to 256 KB: the same with the row in registers, its largest known before the first exponential.  Few long
 // rows: each is split, the parts leave their sums and their groups' maxima in the workspace, and a second kernel joins them and looks again at the groups that pass.
 //
-// What bounds it: many rows the bytes (4096 rows of 256 KB, log probabilities and the likeliest token, 164 us, 6.4 TB/s; 777 of 131 KB 23 us, 4.4 TB/s, three rows a CU); few the launch, one
-// CU's exponentials (16 cycles for 64 of them, 1.6 us for 32000 values) and the chain of steps from the maxima to the ranks (one row of 64 KB, the largest 20, 6.8 us in a graph, 4.2 of them for
-// the sums; 48 of 200 KB, the largest 5, 8.5).
+// What bounds it: many rows the bytes (4096 rows of 256 KB, log probabilities and the likeliest token, 164 us, 6.4 TB/s; 777 of 131 KB 23 us, 4.4 TB/s, three rows a CU); few the launch and a
+// chain of steps that wait for each other (one row of 64 KB in a graph: sums 4.2 us, with the likeliest 5.5, with the largest 20 6.7; one CU's 32000 exponentials, 16 cycles for 64 on each of four
+// SIMDs, are under 0.9 of them; 48 of 200 KB, the largest 5, 8.5).
 #include <float.h>
 
 #include <algorithm>
